@@ -459,6 +459,104 @@ skip_status_t skip_bipartite_xattn_proj(const skip_problem_t* p, const void* Qh,
                                         void* stream);
 
 /*
+ * Passages held in 4 bits.  A passage's keys and values are written into a store
+ * once, when it is encoded, and attended to from there by every question that
+ * retrieves it, at 4.25 bits a value instead of 16 or 32.
+ *
+ * A block of 32 values x (32 features of one token's key of one head; 32 tokens of
+ * one feature of one head's values, counted from the passage's start) is held as
+ * signed codes of {0, 0.5, 1, 1.5, 2, 3, 4, 6}, rounded to nearest with ties to
+ * the even code, times one power of two: 2^(s - 127) with s the least in [1, 254]
+ * for which max|x| <= 7 * 2^(s - 127).
+ *   heads_kv  key/value heads H_kv, a divisor of H (query head h reads key head
+ *             h / (H / H_kv)); at most 32 query heads a key head
+ *   n_blocks  records of 32 tokens the store holds for every head
+ *   data      [n_blocks][H_kv][34 * d_h] bytes, 16-byte aligned.  A record holds
+ *             keys [2][d_h/32][16][16 bytes] (token 16 a + c and features 32 b .. at
+ *             [a][b][c]), values [d_h][16 bytes] (32 tokens), the keys' scales
+ *             [chunk % 2][16][2][chunk / 2] (chunk b and token of the keys' c, a) and
+ *             the values' [feature % 32][feature / 32]; the lower of two codes in
+ *             the low half of a byte
+ * A passage of L tokens takes ceil(L / 32) records in a row from its first,
+ * passage_blocks[j]; several entries of a batch may name one stored passage.  A
+ * record outside [0, n_blocks) is neither written nor read (results are then
+ * unspecified).  d_h is the problem's.
+ */
+typedef struct skip_kv_store {
+  int32_t heads_kv;
+  int32_t reserved;        /* must be 0 */
+  int64_t n_blocks;
+  void* data;
+} skip_kv_store_t;
+
+/* Bytes of a store's data: n_blocks * heads_kv * 34 * d_h (d_h 64 or 128). */
+skip_status_t skip_store_bytes(int32_t heads_kv, int32_t d_h, int64_t n_blocks, size_t* bytes);
+
+/*
+ * Writes the problem's passages into the store.
+ *   Kh, Vh          [total_tokens][H_kv][d_h] keys and values, element type dtype
+ *   passage_offsets [total_passages+1] token offsets
+ *   passage_blocks  [total_passages] int32 first record of each passage; records
+ *                   of different passages must not overlap
+ *   keys_out        out [total_passages][H * d_h] float: the passages' mean keys
+ *                   (float64 sums of Kh as given; a key head's mean once for each
+ *                   query head that reads it), the passage_keys of the graph; or
+ *                   NULL
+ * The tokens that pad a passage's last record are written as zeros; no other byte
+ * of the store is touched.  Of the problem dtype, H, d, d_h, total_passages,
+ * total_tokens and L_max are used.  Nothing is launched without passages.
+ */
+skip_status_t skip_quantize_passages(const skip_problem_t* p, const skip_kv_store_t* store,
+                                     const void* Kh, const void* Vh,
+                                     const int32_t* passage_offsets,
+                                     const int32_t* passage_blocks, float* keys_out,
+                                     void* stream);
+
+/*
+ * Reads passages back: the values that the store holds (exact in either element
+ * type), for the calls that take Kh and Vh.  Kh, Vh out [total_tokens][H_kv][d_h];
+ * other arguments as above.
+ */
+skip_status_t skip_dequantize_passages(const skip_problem_t* p, const skip_kv_store_t* store,
+                                       const int32_t* passage_offsets,
+                                       const int32_t* passage_blocks, void* Kh, void* Vh,
+                                       void* stream);
+
+/* Workspace of skip_bipartite_xattn_quant (host-only). */
+skip_status_t skip_workspace_bytes_quant(const skip_problem_t* p, const skip_kv_store_t* store,
+                                         size_t* bytes);
+
+/*
+ * Stage 2 over the store: skip_bipartite_xattn with the keys and values that the
+ * store holds.  bf16 rows (SKIP_ERR_UNSUPPORTED otherwise); O bf16, or float with
+ * o_f32.  Logits and sums are float32 and the held values enter exactly; softmax
+ * weights enter the product with V to about 2^-16 relative for bf16 output and
+ * 2^-24 for float output.
+ *   rows            kept_idx NULL: queries [total_kept][H][d_h]; else V [B][N][d],
+ *                   row r of question b being V[b][kept_idx[r]]
+ *   edge_rows       [total_kept][d] bf16 rows to cut the graph on, or NULL: `rows`
+ *   passage_offsets [total_passages+1]: the batch's passages, by their lengths
+ *   passage_blocks  [total_passages] first record of each
+ *   passage_keys    [total_passages][d] float: required unless the graph is given
+ *   passage_keep    NULL or a gate's mask as in skip_bipartite_xattn_masked (not
+ *                   with a given graph)
+ *   edge_rowptr, edge_col  a given graph, or both NULL
+ * Other arguments, results and limits as in skip_bipartite_xattn.
+ */
+skip_status_t skip_bipartite_xattn_quant(const skip_problem_t* p, const skip_kv_store_t* store,
+                                         const void* rows, const int32_t* kept_offsets,
+                                         const int32_t* kept_idx, const void* edge_rows,
+                                         const int32_t* passage_offsets,
+                                         const int32_t* passage_blocks,
+                                         const int32_t* query_passages,
+                                         const float* passage_keys,
+                                         const uint8_t* passage_keep,
+                                         const int32_t* edge_rowptr, const int32_t* edge_col,
+                                         void* O, float* lse, int32_t* edge_rowptr_out,
+                                         int32_t* edge_col_out, void* workspace,
+                                         size_t workspace_bytes, void* stream);
+
+/*
  * Both stages fused (Alg. 1: scoring, TopK, graph, fuse): the kept visual
  * tokens are the attention queries (Qh = the kept rows of V viewed as
  * [H][d_h], which requires H * d_h == d) and are read straight from V, never

@@ -24,7 +24,8 @@ LIB = os.path.join(LIBDIR, "libskip.so")
 BUILD = os.path.join(ROOT, "_build")
 ARCH = "gfx950"
 
-SOURCES = ["skip_api.hip", "prune.hip", "graph.hip", "attn.hip", "mlp.hip", "gate.hip", "regions.hip", "proj.hip"]
+SOURCES = ["skip_api.hip", "prune.hip", "graph.hip", "attn.hip", "mlp.hip", "gate.hip", "regions.hip", "proj.hip",
+           "store.hip", "attn_store.hip"]
 
 # Per-source flags.  attn.hip: no NaN ever arises in the attention (finite
 # inputs; masked logits are -inf and meet only max, exp2 and a finite

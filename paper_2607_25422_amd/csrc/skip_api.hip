@@ -504,6 +504,166 @@ skip_status_t skip_skv_gate(const skip_problem_t* p, const skip_skv_gate_t* gate
   return SKIP_OK;
 }
 
+static_assert(sizeof(skip_kv_store_t) == 24 && offsetof(skip_kv_store_t, data) == 16,
+              "skip_kv_store_t layout is part of the ABI");
+
+// The problem's passages and the store that holds them (no dtype, no graph).
+static skip_status_t check_store(const skip_problem_t* p, const skip_kv_store_t* st) {
+  if (!p || !st || st->reserved != 0) return SKIP_ERR_INVALID_ARG;
+  if (p->dtype != SKIP_F32 && p->dtype != SKIP_BF16) return SKIP_ERR_INVALID_ARG;
+  if (st->heads_kv < 1 || st->n_blocks < 0) return SKIP_ERR_INVALID_ARG;
+  if (p->H < 1 || p->d_h < 1 || (int64_t)p->H * p->d_h != p->d) return SKIP_ERR_INVALID_ARG;
+  if (p->H % st->heads_kv != 0) return SKIP_ERR_INVALID_ARG;
+  if (p->total_passages < 0 || p->total_tokens < p->total_passages) return SKIP_ERR_INVALID_ARG;
+  if (p->total_passages > 0 && (p->L_max < 1 || p->L_max > p->total_tokens))
+    return SKIP_ERR_INVALID_ARG;
+  if (st->n_blocks > 0 && !st->data) return SKIP_ERR_INVALID_ARG;
+  if (!al16(st->data)) return SKIP_ERR_INVALID_ARG;
+  if (p->d_h != 64 && p->d_h != 128) return SKIP_ERR_UNSUPPORTED;
+  if (p->d > kMaxD) return SKIP_ERR_UNSUPPORTED;
+  // more records than the batch can need leave the store (each passage alone: at
+  // least its own)
+  if (p->total_passages > 0 && (int64_t)(p->L_max + 31) / 32 > st->n_blocks)
+    return SKIP_ERR_INVALID_ARG;
+  return SKIP_OK;
+}
+
+skip_status_t skip_store_bytes(int32_t heads_kv, int32_t d_h, int64_t n_blocks, size_t* bytes) {
+  if (!bytes || heads_kv < 1 || n_blocks < 0 || d_h < 1) return SKIP_ERR_INVALID_ARG;
+  if (d_h != 64 && d_h != 128) return SKIP_ERR_UNSUPPORTED;
+  const int64_t rec = (int64_t)heads_kv * 34 * d_h;
+  if (n_blocks > INT64_MAX / rec) return SKIP_ERR_INVALID_ARG;
+  *bytes = (size_t)(n_blocks * rec);
+  return SKIP_OK;
+}
+
+skip_status_t skip_quantize_passages(const skip_problem_t* p, const skip_kv_store_t* store,
+                                     const void* Kh, const void* Vh,
+                                     const int32_t* passage_offsets,
+                                     const int32_t* passage_blocks, float* keys_out,
+                                     void* stream) {
+  skip_status_t st = check_store(p, store);
+  if (st != SKIP_OK) return st;
+  if (p->total_passages == 0) return SKIP_OK;
+  if (!Kh || !Vh || !passage_offsets || !passage_blocks) return SKIP_ERR_INVALID_ARG;
+  if (!al16(Kh) || !al16(Vh) || !al16(keys_out)) return SKIP_ERR_INVALID_ARG;
+  SKIP_TRY(launch_store_write(*p, *store, Kh, Vh, passage_offsets, passage_blocks, keys_out,
+                              static_cast<hipStream_t>(stream)));
+  return SKIP_OK;
+}
+
+skip_status_t skip_dequantize_passages(const skip_problem_t* p, const skip_kv_store_t* store,
+                                       const int32_t* passage_offsets,
+                                       const int32_t* passage_blocks, void* Kh, void* Vh,
+                                       void* stream) {
+  skip_status_t st = check_store(p, store);
+  if (st != SKIP_OK) return st;
+  if (p->total_passages == 0) return SKIP_OK;
+  if (!Kh || !Vh || !passage_offsets || !passage_blocks) return SKIP_ERR_INVALID_ARG;
+  if (!al16(Kh) || !al16(Vh)) return SKIP_ERR_INVALID_ARG;
+  SKIP_TRY(launch_store_read(*p, *store, passage_offsets, passage_blocks, Kh, Vh,
+                             static_cast<hipStream_t>(stream)));
+  return SKIP_OK;
+}
+
+// Workspace of the attention over the store: the graph's parts, then the partials
+// of split items.
+struct QuantWorkspace {
+  EdgePartials ep;
+  uint64_t* rowmask;
+  void* part;
+  size_t bytes;
+};
+static QuantWorkspace carve_quant(const skip_problem_t& p, int heads_kv, void* base) {
+  QuantWorkspace w{};
+  char* c = static_cast<char*>(base);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char* r = c + off;
+    off += align_up(bytes);
+    return r;
+  };
+  const size_t S = (size_t)edge_slices(p);
+  w.ep.part = reinterpret_cast<double*>(take((size_t)p.B * S * p.k_max * p.P_max * sizeof(double)));
+  w.ep.qn2 = reinterpret_cast<double*>(take((size_t)p.B * S * p.k_max * sizeof(double)));
+  w.ep.kn2 = reinterpret_cast<double*>(take((size_t)p.B * S * p.P_max * sizeof(double)));
+  w.rowmask = reinterpret_cast<uint64_t*>(take((size_t)p.total_kept * sizeof(uint64_t)));
+  w.part = take(quant_attn_scratch(p, heads_kv));
+  w.bytes = off;
+  return w;
+}
+
+// Problem and store of the attention over the store.
+static skip_status_t check_quant(const skip_problem_t* p, const skip_kv_store_t* store) {
+  skip_status_t st = check(p, kGraph);
+  if (st != SKIP_OK) return st;
+  st = check_store(p, store);
+  if (st != SKIP_OK) return st;
+  if (p->dtype != SKIP_BF16 || !quant_group_ok(p->H / store->heads_kv)) return SKIP_ERR_UNSUPPORTED;
+  return SKIP_OK;
+}
+
+skip_status_t skip_workspace_bytes_quant(const skip_problem_t* p, const skip_kv_store_t* store,
+                                         size_t* bytes) {
+  if (!bytes) return SKIP_ERR_INVALID_ARG;
+  skip_status_t st = check_quant(p, store);
+  if (st != SKIP_OK) return st;
+  *bytes = carve_quant(*p, store->heads_kv, nullptr).bytes;
+  return SKIP_OK;
+}
+
+skip_status_t skip_bipartite_xattn_quant(const skip_problem_t* p, const skip_kv_store_t* store,
+                                         const void* rows, const int32_t* kept_offsets,
+                                         const int32_t* kept_idx, const void* edge_rows,
+                                         const int32_t* passage_offsets,
+                                         const int32_t* passage_blocks,
+                                         const int32_t* query_passages,
+                                         const float* passage_keys,
+                                         const uint8_t* passage_keep,
+                                         const int32_t* edge_rowptr, const int32_t* edge_col,
+                                         void* O, float* lse, int32_t* edge_rowptr_out,
+                                         int32_t* edge_col_out, void* workspace,
+                                         size_t workspace_bytes, void* stream) {
+  skip_status_t st = check_quant(p, store);
+  if (st != SKIP_OK) return st;
+  if (!kept_offsets || !query_passages || !passage_offsets || !workspace)
+    return SKIP_ERR_INVALID_ARG;
+  if (p->total_kept > 0 && (!rows || !O)) return SKIP_ERR_INVALID_ARG;
+  if (p->total_passages > 0 && !passage_blocks) return SKIP_ERR_INVALID_ARG;
+  if (kept_idx && (p->N < 1 || p->k_max > p->N)) return SKIP_ERR_INVALID_ARG;
+  if (!al16(rows) || !al16(edge_rows) || !al16(O) || !al16(passage_keys) || !al16(workspace))
+    return SKIP_ERR_INVALID_ARG;
+  const bool given = edge_rowptr || edge_col;
+  if (given && (!edge_rowptr || (!edge_col && p->total_edges > 0))) return SKIP_ERR_INVALID_ARG;
+  if (given && (edge_rowptr_out || edge_rows || passage_keep)) return SKIP_ERR_INVALID_ARG;
+  if (!given && p->total_passages > 0 && !passage_keys) return SKIP_ERR_INVALID_ARG;
+  if ((edge_rowptr_out == nullptr) != (edge_col_out == nullptr)) return SKIP_ERR_INVALID_ARG;
+  if (kept_idx && (int64_t)p->B * p->N > INT32_MAX) return SKIP_ERR_UNSUPPORTED;
+  const QuantWorkspace w = carve_quant(*p, store->heads_kv, workspace);
+  if (workspace_bytes < w.bytes) return SKIP_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (p->total_kept == 0) {
+    // no kept rows: only the (empty) graph needs its closing offset
+    if (edge_rowptr_out)
+      SKIP_TRY(launch_edge_select(*p, w.ep, kept_offsets, query_passages, w.rowmask,
+                                  edge_rowptr_out, edge_col_out, s, passage_keep));
+    return SKIP_OK;
+  }
+  const QuerySource q{rows, kept_idx, p->N};
+  if (given) {
+    SKIP_TRY(launch_csr_to_mask(*p, kept_offsets, query_passages, edge_rowptr, edge_col,
+                                w.rowmask, s));
+  } else {
+    const QuerySource e = edge_rows ? QuerySource{edge_rows, nullptr, 0} : q;
+    SKIP_TRY(launch_edge_dot(*p, e, kept_offsets, query_passages, nullptr, passage_keys, w.ep, s));
+    SKIP_TRY(launch_edge_select(*p, w.ep, kept_offsets, query_passages, w.rowmask,
+                                edge_rowptr_out, edge_col_out, s, passage_keep));
+  }
+  SKIP_TRY(launch_attention_quant(*p, *store, q, kept_offsets, passage_offsets, passage_blocks,
+                                  query_passages, w.rowmask, O, lse, w.part, s));
+  return SKIP_OK;
+}
+
 // Arguments of the fused route other than the workspace (host-side only).
 static skip_status_t check_fused_args(const skip_problem_t* p, const void* V, const void* Qtok,
                                       const int32_t* q_offsets, const void* w_bias,

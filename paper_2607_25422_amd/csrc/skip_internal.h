@@ -162,4 +162,20 @@ hipError_t launch_attention(const skip_problem_t& p, QuerySource q,
                             const uint64_t* rowmask, const int32_t* plan, void* O, float* lse,
                             hipStream_t s);
 
+// Passages held in 4 bits --------------------------------------------------
+// keys_out: mean keys [total_passages][H * d_h], or NULL
+hipError_t launch_store_write(const skip_problem_t& p, const skip_kv_store_t& st, const void* Kh,
+                              const void* Vh, const int32_t* passage_offsets,
+                              const int32_t* passage_blocks, float* keys_out, hipStream_t s);
+hipError_t launch_store_read(const skip_problem_t& p, const skip_kv_store_t& st,
+                             const int32_t* passage_offsets, const int32_t* passage_blocks,
+                             void* Kh, void* Vh, hipStream_t s);
+bool quant_group_ok(int group);       // query heads of a key head that the attention takes
+size_t quant_attn_scratch(const skip_problem_t& p, int heads_kv);   // partials of split items
+hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t& st,
+                                  QuerySource q, const int32_t* kept_offsets,
+                                  const int32_t* passage_offsets, const int32_t* passage_blocks,
+                                  const int32_t* query_passages, const uint64_t* rowmask,
+                                  void* O, float* lse, void* scratch, hipStream_t s);
+
 }  // namespace skip

@@ -367,7 +367,7 @@ def prepare(case, seed):
             s["p"] = B.make_problem(c["dtype"], B=1, passage_offsets=po,
                                     query_passages=[0, len(Ls)], **common)
             s["po"], s["pb"] = dev(po), dev(first)
-            s["cache"] = B.KvCache(s["data"], hk, n_blocks)
+            s["store"] = B.KvStore(s["data"], hk, n_blocks)
             s["out"] = torch.empty_like(s["Kh"]), torch.empty_like(s["Vh"])
         return s
     _store(s.pop("Kh"), s.pop("Vh"), s["plan"], s["data"])          # filled before
@@ -397,8 +397,8 @@ def prepare(case, seed):
                                 total_edges=0 if s["col"] is None else s["col"].numel(), **common)
         s["ko"], s["po"], s["qp"] = dev(ko), dev(po), dev(qp)
         s["pb"] = dev([first[i] for i in ids])
-        s["cache"] = B.KvCache(s["data"], hk, n_blocks)
-        s["ws"] = torch.empty(B.workspace_bytes_quant(s["p"], s["cache"]), dtype=torch.uint8,
+        s["store"] = B.KvStore(s["data"], hk, n_blocks)
+        s["ws"] = torch.empty(B.workspace_bytes_quant(s["p"], s["store"]), dtype=torch.uint8,
                               device=DEV)
     return s
 
@@ -414,8 +414,8 @@ def run(state):
 def _run_quant(s):
     if own:
         B = s["B"]
-        B.quantize_passages(s["p"], s["cache"], s["Kh"], s["Vh"], s["po"], s["pb"])
-        return B.dequantize_passages(s["p"], s["cache"], s["po"], s["pb"], out=s["out"])
+        B.quantize_passages(s["p"], s["store"], s["Kh"], s["Vh"], s["po"], s["pb"])
+        return B.dequantize_passages(s["p"], s["store"], s["po"], s["pb"], out=s["out"])
     _store(s["Kh"], s["Vh"], s["plan"], s["data"])
     K, V = _read(s["data"], s["plan"], s["c"]["d_h"])
     return K.to(s["Kh"].dtype), V.to(s["Kh"].dtype)
@@ -449,7 +449,7 @@ def _run_attn(s):
     c = s["c"]
     if own:
         return s["B"].bipartite_xattn_quant(
-            s["p"], s["cache"], s["Q"], s["ko"], s["po"], s["pb"], s["qp"], kept_idx=s["idx"],
+            s["p"], s["store"], s["Q"], s["ko"], s["po"], s["pb"], s["qp"], kept_idx=s["idx"],
             passage_keys=s["keys"], edges=None if s["col"] is None else (s["rowptr"], s["col"]),
             out=(s["O"], s["lse"]), workspace=s["ws"])
     H, hk, D = c["heads"], c["heads_kv"], c["d_h"]
