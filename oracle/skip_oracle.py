@@ -431,6 +431,53 @@ def bsca_attention(Qh: np.ndarray, Kh: np.ndarray, Vh: np.ndarray,
 # --------------------------------------------------------------------------
 # Whole route for a batch of questions (Alg. 1: scoring, TopK, graph, fuse)
 # --------------------------------------------------------------------------
+# Passages held in 4 bits
+
+HELD_VALUES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def held_block(x):
+    """What a block of values is held as: signed values of HELD_VALUES times one
+    power of two, the least 2^e with e in [-126, 127] and max|x| <= 7 * 2^e; every
+    value at its nearest, a tie at the value of even position.  Returns (codes
+    with the sign in bit 3, e + 127, the values)."""
+    x = np.asarray(x, dtype=np.float64)
+    a = float(np.max(np.abs(x)))
+    e = -126
+    while a > 7.0 * 2.0 ** e and e < 127:
+        e += 1
+    codes = []
+    for v in x:
+        y = abs(float(v)) / 2.0 ** e
+        best = 0
+        for c in range(1, 8):
+            d, d0 = abs(HELD_VALUES[c] - y), abs(HELD_VALUES[best] - y)
+            if d < d0 or (d == d0 and c % 2 == 0):
+                best = c
+        codes.append(best | (8 if math.copysign(1.0, float(v)) < 0 else 0))
+    vals = [(-1.0 if c & 8 else 1.0) * HELD_VALUES[c & 7] * 2.0 ** e for c in codes]
+    return codes, e + 127, np.asarray(vals)
+
+
+def held_passage(K, V):
+    """Keys and values [L, heads, d_h] of one passage as held in 4 bits (blocks of
+    32 features of a token's key, of 32 tokens of a value feature; tokens past
+    the passage count as zeros)."""
+    K = np.asarray(K, dtype=np.float64)
+    V = np.asarray(V, dtype=np.float64)
+    L, H, D = K.shape
+    Ko, Vo = np.zeros_like(K), np.zeros_like(V)
+    for h in range(H):
+        for t in range(L):
+            for c in range(0, D, 32):
+                Ko[t, h, c:c + 32] = held_block(K[t, h, c:c + 32])[2]
+        for t in range(0, L, 32):
+            for f in range(D):
+                Vo[t:t + 32, h, f] = held_block(V[t:t + 32, h, f])[2]
+    return Ko, Vo
+
+
+# --------------------------------------------------------------------------
 
 @dataclass
 class RouteResult:

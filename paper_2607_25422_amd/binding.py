@@ -35,7 +35,9 @@ ENTRY_POINTS = ("skip_abi_version", "skip_status_string", "skip_workspace_bytes"
                 "skip_workspace_bytes_project", "skip_gather_project",
                 "skip_bipartite_xattn_proj", "skip_pack_projection",
                 "skip_gather_project_packed", "skip_route_fused_noalloc",
-                "skip_workspace_bytes_project_keys", "skip_project_passage_keys")
+                "skip_workspace_bytes_project_keys", "skip_project_passage_keys",
+                "skip_store_bytes", "skip_quantize_passages", "skip_dequantize_passages",
+                "skip_workspace_bytes_quant", "skip_bipartite_xattn_quant")
 FUSED_STAGES = ("pool", "score", "edge_cos", "edge_select", "attention")
 
 
@@ -74,6 +76,14 @@ class SkipSkvGate(ctypes.Structure):
         ("hidden", ctypes.c_int32), ("reserved", ctypes.c_int32),
         ("W", ctypes.c_void_p), ("b1", ctypes.c_void_p), ("w2", ctypes.c_void_p),
         ("b2", ctypes.c_double), ("tau", ctypes.c_double), ("rho", ctypes.c_double),
+    ]
+
+
+class SkipKvStore(ctypes.Structure):
+    """skip_kv_store_t: passages held in 4 bits (device data)."""
+    _fields_ = [
+        ("heads_kv", ctypes.c_int32), ("reserved", ctypes.c_int32), ("n_blocks", ctypes.c_int64),
+        ("data", ctypes.c_void_p),
     ]
 
 
@@ -150,6 +160,20 @@ def _load() -> ctypes.CDLL:
     lib.skip_bipartite_xattn_proj.restype = ctypes.c_int
     lib.skip_bipartite_xattn_proj.argtypes = [P, vp, vp, i32p, vp, vp, i32p, i32p, vp, vp, vp,
                                               vp, i32p, i32p, vp, ctypes.c_size_t, vp]
+    S = ctypes.POINTER(SkipKvStore)
+    lib.skip_store_bytes.restype = ctypes.c_int
+    lib.skip_store_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int64,
+                                     ctypes.POINTER(ctypes.c_size_t)]
+    lib.skip_quantize_passages.restype = ctypes.c_int
+    lib.skip_quantize_passages.argtypes = [P, S, vp, vp, i32p, i32p, vp, vp]
+    lib.skip_dequantize_passages.restype = ctypes.c_int
+    lib.skip_dequantize_passages.argtypes = [P, S, i32p, i32p, vp, vp, vp]
+    lib.skip_workspace_bytes_quant.restype = ctypes.c_int
+    lib.skip_workspace_bytes_quant.argtypes = [P, S, ctypes.POINTER(ctypes.c_size_t)]
+    lib.skip_bipartite_xattn_quant.restype = ctypes.c_int
+    lib.skip_bipartite_xattn_quant.argtypes = [P, S, vp, i32p, i32p, vp, i32p, i32p, i32p, vp, vp,
+                                               i32p, i32p, vp, vp, i32p, i32p, vp,
+                                               ctypes.c_size_t, vp]
     lib.skip_route_fused_noalloc.restype = ctypes.c_int
     lib.skip_route_fused_noalloc.argtypes = [P, vp, vp, i32p, vp, i32p, vp, vp, i32p, i32p, vp,
                                              i32p, vp, vp, vp]
@@ -560,6 +584,84 @@ def skip_bipartite_xattn_proj(p: SkipProblem, Qh, edge_rows, kept_offsets, Kh, V
     _check(st, "skip_bipartite_xattn_proj")
 
 
+def store_bytes(heads_kv: int, d_h: int, n_blocks: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(LIB.skip_store_bytes(int(heads_kv), int(d_h), int(n_blocks), ctypes.byref(n)),
+           "skip_store_bytes")
+    return int(n.value)
+
+
+def _store_struct(p: SkipProblem, store: "KvStore") -> SkipKvStore:
+    need = store_bytes(store.heads_kv, p.d_h, store.n_blocks) if p.d_h in (64, 128) else None
+    return SkipKvStore(int(store.heads_kv), 0, int(store.n_blocks),
+                       _ptr(store.data, "store.data", torch.uint8, need))
+
+
+def workspace_bytes_quant(p: SkipProblem, store: "KvStore") -> int:
+    n = ctypes.c_size_t(0)
+    st = _store_struct(p, store)
+    _check(LIB.skip_workspace_bytes_quant(ctypes.byref(p), ctypes.byref(st), ctypes.byref(n)),
+           "skip_workspace_bytes_quant")
+    return int(n.value)
+
+
+def skip_quantize_passages(p: SkipProblem, store: "KvStore", Kh, Vh, passage_offsets,
+                           passage_blocks, keys_out=None, stream=None):
+    et = _elem_dtype(p)
+    n = p.total_tokens * store.heads_kv * p.d_h
+    s = _store_struct(p, store)
+    st = LIB.skip_quantize_passages(
+        ctypes.byref(p), ctypes.byref(s), _ptr(Kh, "Kh", et, n), _ptr(Vh, "Vh", et, n),
+        _ptr(passage_offsets, "passage_offsets", torch.int32, p.total_passages + 1),
+        _ptr(passage_blocks, "passage_blocks", torch.int32, p.total_passages),
+        _ptr(keys_out, "keys_out", torch.float32, p.total_passages * p.d), _stream(stream))
+    _check(st, "skip_quantize_passages")
+
+
+def skip_dequantize_passages(p: SkipProblem, store: "KvStore", passage_offsets, passage_blocks,
+                             Kh, Vh, stream=None):
+    et = _elem_dtype(p)
+    n = p.total_tokens * store.heads_kv * p.d_h
+    s = _store_struct(p, store)
+    st = LIB.skip_dequantize_passages(
+        ctypes.byref(p), ctypes.byref(s),
+        _ptr(passage_offsets, "passage_offsets", torch.int32, p.total_passages + 1),
+        _ptr(passage_blocks, "passage_blocks", torch.int32, p.total_passages),
+        _ptr(Kh, "Kh", et, n), _ptr(Vh, "Vh", et, n), _stream(stream))
+    _check(st, "skip_dequantize_passages")
+
+
+def skip_bipartite_xattn_quant(p: SkipProblem, store: "KvStore", rows, kept_offsets,
+                               passage_offsets, passage_blocks, query_passages, O, lse=None,
+                               kept_idx=None, edge_rows=None, passage_keys=None,
+                               passage_keep=None, edge_rowptr=None, edge_col=None,
+                               edge_rowptr_out=None, edge_col_out=None, workspace=None,
+                               stream=None):
+    et = _elem_dtype(p)
+    s = _store_struct(p, store)
+    if workspace is None:
+        workspace = _fresh_workspace(workspace_bytes_quant(p, store), kept_offsets.device, stream)
+    n_rows = p.B * p.N if kept_idx is not None else p.total_kept
+    st = LIB.skip_bipartite_xattn_quant(
+        ctypes.byref(p), ctypes.byref(s), _ptr(rows, "rows", et, n_rows * p.d),
+        _ptr(kept_offsets, "kept_offsets", torch.int32, p.B + 1),
+        _ptr(kept_idx, "kept_idx", torch.int32, p.total_kept),
+        _ptr(edge_rows, "edge_rows", et, p.total_kept * p.d),
+        _ptr(passage_offsets, "passage_offsets", torch.int32, p.total_passages + 1),
+        _ptr(passage_blocks, "passage_blocks", torch.int32, p.total_passages),
+        _ptr(query_passages, "query_passages", torch.int32, p.B + 1),
+        _ptr(passage_keys, "passage_keys", torch.float32, p.total_passages * p.d),
+        _ptr(passage_keep, "passage_keep", torch.uint8, p.total_passages),
+        _ptr(edge_rowptr, "edge_rowptr", torch.int32, p.total_kept + 1),
+        _ptr(edge_col, "edge_col", torch.int32, p.total_edges),
+        _ptr(O, "O", _out_dtype(p), p.total_kept * p.d),
+        _ptr(lse, "lse", torch.float32, p.total_kept * p.H),
+        _ptr(edge_rowptr_out, "edge_rowptr_out", torch.int32, p.total_kept + 1),
+        _ptr(edge_col_out, "edge_col_out", torch.int32, p.total_kept * p.P_max),
+        workspace.data_ptr(), workspace.numel(), _stream(stream))
+    _check(st, "skip_bipartite_xattn_quant")
+
+
 def skip_route_fused(p: SkipProblem, V, Qtok, q_offsets, w_bias, kept_offsets, Kh, Vh,
                      passage_offsets, query_passages, kept_idx, O, lse=None,
                      passage_keys=None, workspace=None, stream=None, stage_events=None):
@@ -908,3 +1010,77 @@ def route_fused(db: DeviceBatch, passage_keys=None, out=None, stage_events=None)
                      db.passage_offsets, db.query_passages, kept_idx, O, lse, passage_keys,
                      db.workspace, stage_events=stage_events)
     return kept_idx[:p.total_kept], O[:p.total_kept], lse[:p.total_kept]
+
+
+# ---------------------------------------------------------------------------
+# Passages held in 4 bits
+
+@dataclass
+class KvStore:
+    """A store of passages in 4 bits: ``data`` uint8 of ``store_bytes`` bytes
+    (any shape), records of 32 tokens for each of ``heads_kv`` heads."""
+    data: torch.Tensor
+    heads_kv: int
+    n_blocks: int
+
+
+def passage_blocks(passage_offsets, first: int = 0):
+    """Records of passages placed one after the other from record ``first``:
+    (first record of each [passages] numpy int32, the record after the last)."""
+    n = (np.diff(_host_i32(passage_offsets)) + 31) // 32
+    ends = first + np.cumsum(n)
+    return (ends - n).astype(np.int32), int(ends[-1]) if n.size else first
+
+
+def new_kv_store(heads_kv: int, d_h: int, n_blocks: int, device="cuda") -> KvStore:
+    data = torch.empty(store_bytes(heads_kv, d_h, n_blocks), dtype=torch.uint8, device=device)
+    return KvStore(data, int(heads_kv), int(n_blocks))
+
+
+def quantize_passages(p: SkipProblem, store: KvStore, Kh, Vh, passage_offsets, passage_blocks,
+                      want_keys=False, stream=None):
+    """Writes the problem's passages into the store.  Returns their mean keys
+    [total_passages, H * d_h] float32 with ``want_keys``, else None."""
+    keys = None
+    if want_keys:
+        keys = torch.empty((max(p.total_passages, 1), p.d), dtype=torch.float32,
+                           device=store.data.device)
+        s = _torch_stream(stream)
+        if s != torch.cuda.current_stream():
+            keys.record_stream(s)
+    skip_quantize_passages(p, store, Kh, Vh, passage_offsets, passage_blocks, keys, stream)
+    return None if keys is None else keys[:p.total_passages]
+
+
+def dequantize_passages(p: SkipProblem, store: KvStore, passage_offsets, passage_blocks,
+                        out=None) -> Tuple:
+    """The keys and values that the store holds, [total_tokens, heads_kv, d_h]
+    each, in the problem's element type.  ``out`` = two preallocated tensors."""
+    if out is None:
+        shape = (p.total_tokens, store.heads_kv, p.d_h)
+        out = tuple(torch.empty(shape, dtype=_elem_dtype(p), device=store.data.device)
+                    for _ in range(2))
+    skip_dequantize_passages(p, store, passage_offsets, passage_blocks, out[0], out[1])
+    return out
+
+
+def bipartite_xattn_quant(p: SkipProblem, store: KvStore, rows, kept_offsets, passage_offsets,
+                          passage_blocks, query_passages, kept_idx=None, edge_rows=None,
+                          passage_keys=None, passage_keep=None, edges=None, out=None,
+                          workspace=None) -> Tuple:
+    """Stage 2 over a store.  ``rows``: the queries [total_kept, H, d_h], or V
+    with ``kept_idx``.  The graph is built from ``passage_keys``, or ``edges`` =
+    (rowptr, col) with p.total_edges columns.  Returns (O, lse); ``out`` = the two
+    preallocated."""
+    if out is None:
+        dev = kept_offsets.device
+        out = (torch.empty((max(p.total_kept, 1), p.H, p.d_h), dtype=_out_dtype(p), device=dev),
+               torch.empty((max(p.total_kept, 1), p.H), dtype=torch.float32, device=dev))
+    O, lse = out
+    skip_bipartite_xattn_quant(
+        p, store, rows if p.total_kept else None, kept_offsets, passage_offsets, passage_blocks,
+        query_passages, O if p.total_kept else None, lse if p.total_kept else None,
+        kept_idx=kept_idx, edge_rows=edge_rows, passage_keys=passage_keys,
+        passage_keep=passage_keep, edge_rowptr=None if edges is None else edges[0],
+        edge_col=None if edges is None else edges[1], workspace=workspace)
+    return O[:p.total_kept], lse[:p.total_kept]

@@ -521,8 +521,7 @@ static skip_status_t check_store(const skip_problem_t* p, const skip_kv_store_t*
   if (!al16(st->data)) return SKIP_ERR_INVALID_ARG;
   if (p->d_h != 64 && p->d_h != 128) return SKIP_ERR_UNSUPPORTED;
   if (p->d > kMaxD) return SKIP_ERR_UNSUPPORTED;
-  // more records than the batch can need leave the store (each passage alone: at
-  // least its own)
+  // the longest passage has to fit
   if (p->total_passages > 0 && (int64_t)(p->L_max + 31) / 32 > st->n_blocks)
     return SKIP_ERR_INVALID_ARG;
   return SKIP_OK;
