@@ -557,6 +557,58 @@ skip_status_t skip_bipartite_xattn_quant(const skip_problem_t* p, const skip_kv_
                                          size_t workspace_bytes, void* stream);
 
 /*
+ * A layer on the rows (the output projection of the attention with the kept
+ * tokens' skip connection; a perceptron's layers; the visual projector):
+ *   Y[r] = act(W x_r + b) + R[r],
+ * bf16 rows, weights and residual, float32 sums, bias, activation and residual
+ * in float32, one rounding at the end.
+ *   SKIP_ACT_GELU  x / 2 (1 + erf(x / sqrt(2)));  SKIP_ACT_SILU  x / (1 + exp(-x))
+ */
+typedef enum skip_activation {
+  SKIP_ACT_NONE = 0,
+  SKIP_ACT_RELU = 1,
+  SKIP_ACT_GELU = 2,
+  SKIP_ACT_SILU = 3
+} skip_activation_t;
+
+/*
+ * The weights, packed once for the matrix cores into a caller buffer of
+ * skip_packed_bytes_dense bytes (an opaque layout of this ABI version, for the d
+ * of the problem and the d_out it was packed for; the caller owns it).
+ *   W      [d_out][d] bf16, 16-byte aligned, as `packed`
+ *   d_out  a multiple of 8, at most 65536;  d a multiple of 32, at most 65536
+ * Of the problem dtype (bf16, else SKIP_ERR_UNSUPPORTED) and d are used.  A short
+ * buffer: SKIP_ERR_WORKSPACE.
+ */
+skip_status_t skip_packed_bytes_dense(const skip_problem_t* p, int32_t d_out, size_t* bytes);
+skip_status_t skip_pack_dense(const skip_problem_t* p, const void* W, int32_t d_out, void* packed,
+                              size_t packed_bytes, void* stream);
+
+/*
+ * The layer on total_kept rows.
+ *   rows          rows_idx NULL: [total_kept][d]; else [B][N][d], row r of question
+ *                 b being rows[b][rows_idx[r]] (rows_idx: a kept_idx)
+ *   bias          [d_out] float, 16-byte aligned, or NULL
+ *   activation    skip_activation_t
+ *   residual      NULL, or residual_idx NULL: [total_kept][d_out] bf16; else
+ *                 [B][N][d_out] bf16, read through residual_idx in the same way
+ *   kept_offsets  [B+1], needed where an index is given
+ *   Y             out [total_kept][d_out], bf16 (out_f32 = 0) or float (1); it may
+ *                 be the residual itself where that is bf16 rows as given and Y is
+ *                 bf16, and overlaps no other argument
+ *   workspace     skip_workspace_bytes_dense bytes (0 for most sizes: it may then be
+ *                 NULL), 16-byte aligned
+ * Of the problem dtype, B, N, d, k_max and total_kept are used.
+ */
+skip_status_t skip_workspace_bytes_dense(const skip_problem_t* p, int32_t d_out, size_t* bytes);
+skip_status_t skip_gather_dense(const skip_problem_t* p, const void* rows,
+                                const int32_t* kept_offsets, const int32_t* rows_idx,
+                                const void* packed, int32_t d_out, const float* bias,
+                                int32_t activation, const void* residual,
+                                const int32_t* residual_idx, void* Y, int32_t out_f32,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Both stages fused (Alg. 1: scoring, TopK, graph, fuse): the kept visual
  * tokens are the attention queries (Qh = the kept rows of V viewed as
  * [H][d_h], which requires H * d_h == d) and are read straight from V, never

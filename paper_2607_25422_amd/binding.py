@@ -37,7 +37,9 @@ ENTRY_POINTS = ("skip_abi_version", "skip_status_string", "skip_workspace_bytes"
                 "skip_gather_project_packed", "skip_route_fused_noalloc",
                 "skip_workspace_bytes_project_keys", "skip_project_passage_keys",
                 "skip_store_bytes", "skip_quantize_passages", "skip_dequantize_passages",
-                "skip_workspace_bytes_quant", "skip_bipartite_xattn_quant")
+                "skip_workspace_bytes_quant", "skip_bipartite_xattn_quant",
+                "skip_packed_bytes_dense", "skip_pack_dense", "skip_workspace_bytes_dense",
+                "skip_gather_dense")
 FUSED_STAGES = ("pool", "score", "edge_cos", "edge_select", "attention")
 
 
@@ -90,6 +92,7 @@ class SkipKvStore(ctypes.Structure):
 # skip_edge_rule_t and skip_edge_metric_t, by the names the oracle uses
 EDGE_RULES = {"question": 0, "row": 1, "fraction": 2}
 EDGE_METRICS = {"cosine": 0, "dot": 1}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}     # skip_activation_t
 
 
 def _load() -> ctypes.CDLL:
@@ -174,6 +177,14 @@ def _load() -> ctypes.CDLL:
     lib.skip_bipartite_xattn_quant.argtypes = [P, S, vp, i32p, i32p, vp, i32p, i32p, i32p, vp, vp,
                                                i32p, i32p, vp, vp, i32p, i32p, vp,
                                                ctypes.c_size_t, vp]
+    for name in ("skip_packed_bytes_dense", "skip_workspace_bytes_dense"):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [P, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.skip_pack_dense.restype = ctypes.c_int
+    lib.skip_pack_dense.argtypes = [P, vp, ctypes.c_int32, vp, ctypes.c_size_t, vp]
+    lib.skip_gather_dense.restype = ctypes.c_int
+    lib.skip_gather_dense.argtypes = [P, vp, i32p, i32p, vp, ctypes.c_int32, vp, ctypes.c_int32,
+                                      vp, i32p, vp, ctypes.c_int32, vp, ctypes.c_size_t, vp]
     lib.skip_route_fused_noalloc.restype = ctypes.c_int
     lib.skip_route_fused_noalloc.argtypes = [P, vp, vp, i32p, vp, i32p, vp, vp, i32p, i32p, vp,
                                              i32p, vp, vp, vp]
@@ -662,6 +673,51 @@ def skip_bipartite_xattn_quant(p: SkipProblem, store: "KvStore", rows, kept_offs
     _check(st, "skip_bipartite_xattn_quant")
 
 
+def packed_bytes_dense(p: SkipProblem, d_out: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(LIB.skip_packed_bytes_dense(ctypes.byref(p), int(d_out), ctypes.byref(n)),
+           "skip_packed_bytes_dense")
+    return int(n.value)
+
+
+def workspace_bytes_dense(p: SkipProblem, d_out: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(LIB.skip_workspace_bytes_dense(ctypes.byref(p), int(d_out), ctypes.byref(n)),
+           "skip_workspace_bytes_dense")
+    return int(n.value)
+
+
+def skip_pack_dense(p: SkipProblem, W, packed, stream=None):
+    d_out = int(W.shape[0])
+    st = LIB.skip_pack_dense(ctypes.byref(p), _ptr(W, "W", _elem_dtype(p), d_out * p.d), d_out,
+                             _ptr(packed, "packed", torch.uint8), packed.numel(), _stream(stream))
+    _check(st, "skip_pack_dense")
+
+
+def skip_gather_dense(p: SkipProblem, rows, kept_offsets, rows_idx, packed, d_out, Y, bias=None,
+                      activation="none", residual=None, residual_idx=None, out_f32=False,
+                      workspace=None, stream=None):
+    et = _elem_dtype(p)
+    d_out = int(d_out)
+    need = workspace_bytes_dense(p, d_out)
+    if workspace is None and need:
+        workspace = _fresh_workspace(need, packed.device, stream)
+    _ptr(packed, "packed", torch.uint8, packed_bytes_dense(p, d_out))
+    n_rows = p.B * p.N if rows_idx is not None else p.total_kept
+    n_res = p.B * p.N if residual_idx is not None else p.total_kept
+    st = LIB.skip_gather_dense(
+        ctypes.byref(p), _ptr(rows, "rows", et, n_rows * p.d),
+        _ptr(kept_offsets, "kept_offsets", torch.int32, p.B + 1),
+        _ptr(rows_idx, "rows_idx", torch.int32, p.total_kept),
+        _ptr(packed, "packed", torch.uint8), d_out, _ptr(bias, "bias", torch.float32, d_out),
+        ACTIVATIONS[activation], _ptr(residual, "residual", et, n_res * d_out),
+        _ptr(residual_idx, "residual_idx", torch.int32, p.total_kept),
+        _ptr(Y, "Y", torch.float32 if out_f32 else et, p.total_kept * d_out),
+        1 if out_f32 else 0, None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel(), _stream(stream))
+    _check(st, "skip_gather_dense")
+
+
 def skip_route_fused(p: SkipProblem, V, Qtok, q_offsets, w_bias, kept_offsets, Kh, Vh,
                      passage_offsets, query_passages, kept_idx, O, lse=None,
                      passage_keys=None, workspace=None, stream=None, stage_events=None):
@@ -1084,3 +1140,30 @@ def bipartite_xattn_quant(p: SkipProblem, store: KvStore, rows, kept_offsets, pa
         passage_keep=passage_keep, edge_rowptr=None if edges is None else edges[0],
         edge_col=None if edges is None else edges[1], workspace=workspace)
     return O[:p.total_kept], lse[:p.total_kept]
+
+
+# ---------------------------------------------------------------------------
+# The layer after the attention
+
+def pack_dense(p: SkipProblem, W: torch.Tensor) -> torch.Tensor:
+    """W [d_out, d] bf16 packed for ``gather_dense`` (a uint8 tensor owned by the
+    caller)."""
+    packed = torch.empty(packed_bytes_dense(p, int(W.shape[0])), dtype=torch.uint8,
+                         device=W.device)
+    skip_pack_dense(p, W, packed)
+    return packed
+
+
+def gather_dense(p: SkipProblem, rows, packed, d_out: int, kept_offsets=None, rows_idx=None,
+                 bias=None, activation="none", residual=None, residual_idx=None, out_f32=False,
+                 out=None, workspace=None) -> torch.Tensor:
+    """act(W x_r + b) + residual_r of the problem's rows [total_kept, d] (with
+    ``rows_idx``: of [B, N, d] through the kept indices; the same for
+    ``residual``).  Returns Y [total_kept, d_out], bf16 or float32 (``out``: its
+    type; a preallocated Y)."""
+    if out is None:
+        out = torch.empty((p.total_kept, int(d_out)), device=packed.device,
+                          dtype=torch.float32 if out_f32 else _elem_dtype(p))
+    skip_gather_dense(p, rows, kept_offsets, rows_idx, packed, d_out, out, bias, activation,
+                      residual, residual_idx, out.dtype == torch.float32, workspace)
+    return out

@@ -25,7 +25,7 @@ BUILD = os.path.join(ROOT, "_build")
 ARCH = "gfx950"
 
 SOURCES = ["skip_api.hip", "prune.hip", "graph.hip", "attn.hip", "mlp.hip", "gate.hip", "regions.hip", "proj.hip",
-           "store.hip", "attn_store.hip"]
+           "store.hip", "attn_store.hip", "dense.hip"]
 
 # Per-source flags.  attn.hip: no NaN ever arises in the attention (finite
 # inputs; masked logits are -inf and meet only max, exp2 and a finite

@@ -663,6 +663,72 @@ skip_status_t skip_bipartite_xattn_quant(const skip_problem_t* p, const skip_kv_
   return SKIP_OK;
 }
 
+// Problem, weights and widths of the layer calls (d up to 65536, unlike the
+// route's).
+static skip_status_t check_dense(const skip_problem_t* p, int32_t d_out) {
+  if (!p || d_out <= 0 || p->d < 1) return SKIP_ERR_INVALID_ARG;
+  if (p->dtype != SKIP_F32 && p->dtype != SKIP_BF16) return SKIP_ERR_INVALID_ARG;
+  if (p->dtype != SKIP_BF16 || p->d % 32 != 0 || p->d > 65536 || d_out % 8 != 0 || d_out > 65536)
+    return SKIP_ERR_UNSUPPORTED;
+  return SKIP_OK;
+}
+
+skip_status_t skip_packed_bytes_dense(const skip_problem_t* p, int32_t d_out, size_t* bytes) {
+  if (!bytes) return SKIP_ERR_INVALID_ARG;
+  skip_status_t st = check_dense(p, d_out);
+  if (st != SKIP_OK) return st;
+  *bytes = dense_packed_bytes(p->d, d_out);
+  return SKIP_OK;
+}
+
+skip_status_t skip_pack_dense(const skip_problem_t* p, const void* W, int32_t d_out, void* packed,
+                              size_t packed_bytes, void* stream) {
+  skip_status_t st = check_dense(p, d_out);
+  if (st != SKIP_OK) return st;
+  if (!W || !packed || !al16(W) || !al16(packed)) return SKIP_ERR_INVALID_ARG;
+  if (packed_bytes < dense_packed_bytes(p->d, d_out)) return SKIP_ERR_WORKSPACE;
+  SKIP_TRY(launch_dense_pack(p->d, d_out, W, packed, static_cast<hipStream_t>(stream)));
+  return SKIP_OK;
+}
+
+skip_status_t skip_workspace_bytes_dense(const skip_problem_t* p, int32_t d_out, size_t* bytes) {
+  if (!bytes) return SKIP_ERR_INVALID_ARG;
+  skip_status_t st = check_dense(p, d_out);
+  if (st != SKIP_OK) return st;
+  if (p->total_kept < 0) return SKIP_ERR_INVALID_ARG;
+  *bytes = dense_scratch_bytes(p->total_kept, p->d, d_out);
+  return SKIP_OK;
+}
+
+skip_status_t skip_gather_dense(const skip_problem_t* p, const void* rows,
+                                const int32_t* kept_offsets, const int32_t* rows_idx,
+                                const void* packed, int32_t d_out, const float* bias,
+                                int32_t activation, const void* residual,
+                                const int32_t* residual_idx, void* Y, int32_t out_f32,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  skip_status_t st = check_dense(p, d_out);
+  if (st != SKIP_OK) return st;
+  if (!packed || (out_f32 != 0 && out_f32 != 1) || p->B < 1 || p->total_kept < 0)
+    return SKIP_ERR_INVALID_ARG;
+  if (activation < SKIP_ACT_NONE || activation > SKIP_ACT_SILU) return SKIP_ERR_INVALID_ARG;
+  if (p->total_kept > 0 && (!rows || !Y)) return SKIP_ERR_INVALID_ARG;
+  if (residual_idx && !residual) return SKIP_ERR_INVALID_ARG;
+  if (!al16(rows) || !al16(packed) || !al16(bias) || !al16(residual) || !al16(Y) ||
+      !al16(workspace))
+    return SKIP_ERR_INVALID_ARG;
+  if (rows_idx || residual_idx) {
+    if (!kept_offsets || p->N < 1 || p->k_max < 0 || p->k_max > p->N) return SKIP_ERR_INVALID_ARG;
+    if ((int64_t)p->B * p->N > INT32_MAX) return SKIP_ERR_UNSUPPORTED;
+  }
+  const size_t need = dense_scratch_bytes(p->total_kept, p->d, d_out);
+  if (need > 0 && !workspace) return SKIP_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return SKIP_ERR_WORKSPACE;
+  SKIP_TRY(launch_dense(*p, rows, kept_offsets, rows_idx, packed, d_out, bias, activation,
+                        residual, residual_idx, Y, out_f32, workspace,
+                        static_cast<hipStream_t>(stream)));
+  return SKIP_OK;
+}
+
 // Arguments of the fused route other than the workspace (host-side only).
 static skip_status_t check_fused_args(const skip_problem_t* p, const void* V, const void* Qtok,
                                       const int32_t* q_offsets, const void* w_bias,

@@ -162,6 +162,15 @@ hipError_t launch_attention(const skip_problem_t& p, QuerySource q,
                             const uint64_t* rowmask, const int32_t* plan, void* O, float* lse,
                             hipStream_t s);
 
+// Layer after the attention -------------------------------------------------
+size_t dense_packed_bytes(int d, int d_out);
+size_t dense_scratch_bytes(int M, int d, int d_out);    // parts of a shared contraction
+hipError_t launch_dense_pack(int d, int d_out, const void* W, void* packed, hipStream_t s);
+hipError_t launch_dense(const skip_problem_t& p, const void* rows, const int32_t* kept_offsets,
+                        const int32_t* rows_idx, const void* packed, int d_out, const float* bias,
+                        int act, const void* residual, const int32_t* residual_idx, void* Y,
+                        int out_f32, void* scratch, hipStream_t s);
+
 // Passages held in 4 bits --------------------------------------------------
 // keys_out: mean keys [total_passages][H * d_h], or NULL
 hipError_t launch_store_write(const skip_problem_t& p, const skip_kv_store_t& st, const void* Kh,
