@@ -19,8 +19,7 @@
 // long as both operands agree, so the softmax weights stay in the lanes that
 // computed them, too: lane l (n = l % 32, hh = l / 32) holds row n's logits of
 // tokens 32 hh + 16 t + i in element i of product t.  The online softmax is in
-// base 2 and float32; a weight enters the second product as a sum of bf16 pieces
-// (two for bf16 output, 2^-16 relative; three for float output, 2^-24).
+// base 2 and float32.
 //
 // A unit's (O, max, sum) is merged into the item's, float32 in LDS, in the order
 // of the list, so that the result does not depend on which wave was faster: a
@@ -49,21 +48,6 @@ __device__ __forceinline__ float other_half(float x) {
   return __uint_as_float(__lane_id() < 32 ? r[1] : r[0]);
 }
 
-// Position of the n-th (from 0) set bit of x; n < popcount(x).
-__device__ __forceinline__ int nth_set(uint64_t x, int n) {
-  int pos = 0;
-#pragma unroll
-  for (int w = 32; w >= 1; w >>= 1) {
-    const int c = __popcll(x & ((1ull << w) - 1ull));
-    if (n >= c) {
-      n -= c;
-      x >>= w;
-      pos += w;
-    }
-  }
-  return pos;
-}
-
 // Eight 4-bit values (a dword) as bf16, exactly, times 2^(byte B of scales - 127).
 template <int B>
 __device__ __forceinline__ float scale_of(uint32_t scales) {
@@ -77,16 +61,37 @@ __device__ __forceinline__ u32x4 expand8(uint32_t codes, float scale) {
       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
 }
 
-// One addition to an LDS counter for the whole wave; returns the value before it,
-// uniform.  The wave barriers keep the branch on lane 0 to itself: without them
-// the compiler joins it with the next one like it across a loop's back edge, and
-// the other lanes run ahead.
-__device__ __forceinline__ int wave_fetch_add(int* counter) {
+// The same as half floats (exact where half_scales holds for the scale).
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ u32x4 expand8_half(uint32_t codes, float scale) {
+  return u32x4{
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3))};
+}
+__device__ __forceinline__ f32x16_t mfma32_half(const u32x4& a, const u32x4& b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a),
+                                                __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+// Whether N scale bytes are all from 112 to 139, 2^-15 to 2^12: held values of 2^-16
+// to 24576, which are half floats (normal and below).
+template <int N>
+__device__ __forceinline__ bool half_scales(uint32_t scales) {
+  bool ok = true;
+#pragma unroll
+  for (int b = 0; b < N; ++b) ok &= ((scales >> (8 * b)) & 0xffu) - 112u <= 27u;
+  return ok;
+}
+
+// Adds one to an LDS counter for the whole wave.  The wave barriers keep the branch
+// on lane 0 to itself: without them the compiler may join it with another one like
+// it across a loop's back edge, and the other lanes run ahead.
+__device__ __forceinline__ void wave_add_one(int* counter) {
   __builtin_amdgcn_wave_barrier();
-  int x = 0;
-  if (__lane_id() == 0) x = atomicAdd(counter, 1);
+  if (__lane_id() == 0) atomicAdd(counter, 1);
   __builtin_amdgcn_wave_barrier();
-  return __builtin_amdgcn_readfirstlane(x);
 }
 
 template <int N, int I = 0, class F>
@@ -150,19 +155,181 @@ __device__ __forceinline__ bool quant_item(const QuantAttnArgs& a, int L, QuantI
   return x.nk > 0;
 }
 
-template <int D, int ROWS, int PIECES>
+// A tile of 64 tokens: two records of a passage, as a lane holds them.
+template <int D>
+struct QuantTile {
+  static constexpr int C = D / 32, KH = D / 64;   // feature chunks of a record; pairs of them
+  static constexpr int FB = D / 32;               // 32-feature blocks of O
+  u32x4 k[2][KH], v[FB];
+  uint32_t ks, vs;                                // scales, a byte each
+  // lane l: n = l % 32, hh = l / 32.  Keys: row n of the two products is token 32
+  // kb + 16 h + ki, in features 64 kh + 32 hh ..; values: feature 32 fb + n, tokens
+  // 32 hh ..
+  __device__ __forceinline__ void load_k(const uint8_t* rec, int ki, int hh) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int kh = 0; kh < KH; ++kh)
+        k[h][kh] = *reinterpret_cast<const u32x4*>(rec + ((h * C + 2 * kh + hh) * 16 + ki) * 16);
+    const uint8_t* sp = rec + 32 * D + (hh * 16 + ki) * C;
+    ks = C == 4 ? *reinterpret_cast<const uint32_t*>(sp) : *reinterpret_cast<const uint16_t*>(sp);
+  }
+  __device__ __forceinline__ void load_v(const uint8_t* rec, int n) {
+#pragma unroll
+    for (int fb = 0; fb < FB; ++fb)
+      v[fb] = *reinterpret_cast<const u32x4*>(rec + 16 * D + (32 * fb + n) * 16);
+    const uint8_t* sp = rec + 33 * D + n * C;
+    vs = C == 4 ? *reinterpret_cast<const uint32_t*>(sp) : *reinterpret_cast<const uint16_t*>(sp);
+  }
+  // S^T: element i of s[h] is token 32 hh + 16 h + i, column n
+  __device__ __forceinline__ void logits(const u32x4 (&q)[4 * KH], f32x16_t (&s)[2]) const {
+    unrolled<2>([&](auto h_) {
+      constexpr int h = decltype(h_)::value;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[h][i] = 0.f;
+      unrolled<KH>([&](auto kh_) {
+        constexpr int kh = decltype(kh_)::value;
+        const float scl = scale_of<h * KH + kh>(ks);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          s[h] = mfma32_bf16(expand8(k[h][kh][c], scl), q[4 * kh + c], s[h]);
+      });
+    });
+  }
+  // Weights 2^(sc s - ref), O^T += V^T . P^T; returns the lane's sum of them.  A
+  // weight enters as a sum of PIECES bf16 values, all but the last truncated (the
+  // rest is exact), or as one half float (PIECES 0).
+  template <int PIECES>
+  __device__ __forceinline__ float weigh(const f32x16_t (&s)[2], float sc, float ref,
+                                            f32x16_t (&acc)[FB]) const {
+    constexpr int NP = PIECES ? PIECES : 1;
+    float ls = 0.f;
+    unrolled<4>([&](auto q_) {
+      constexpr int q = decltype(q_)::value, h = q >> 1, i0 = 8 * (q & 1);
+      u32x4 pc[NP];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float p0 = __builtin_amdgcn_exp2f(fmaf(s[h][i0 + 2 * e], sc, -ref));
+        float p1 = __builtin_amdgcn_exp2f(fmaf(s[h][i0 + 2 * e + 1], sc, -ref));
+        ls += p0 + p1;
+#pragma unroll
+        for (int c = 0; c + 1 < NP; ++c) {
+          const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+          pc[c][e] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+          p0 -= __uint_as_float(b0 & 0xffff0000u);
+          p1 -= __uint_as_float(b1 & 0xffff0000u);
+        }
+        pc[NP - 1][e] = PIECES ? pack2_bf16(p0, p1)
+                               : __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)p0, (_Float16)p1});
+      }
+      unrolled<FB>([&](auto fb_) {
+        constexpr int fb = decltype(fb_)::value;
+        if constexpr (PIECES == 0) {
+          acc[fb] = mfma32_half(expand8_half(v[fb][q], scale_of<fb>(vs)), pc[0], acc[fb]);
+        } else {
+          const u32x4 va = expand8(v[fb][q], scale_of<fb>(vs));
+#pragma unroll
+          for (int c = 0; c < PIECES; ++c) acc[fb] = mfma32_bf16(va, pc[c], acc[fb]);
+        }
+      });
+    });
+    return ls;
+  }
+};
+
+// How softmax weights enter the second product.  Float output: three bf16 pieces.
+// bf16 output: one half float (11 bits: 2^-12 relative, an eighth of the output's
+// own rounding; weights are at most 2^kQLazy) as long as the held values are half
+// floats, which saves a third of the matrix products and a seventh of the vector
+// instructions; a wave that meets a tile whose values are not goes over its tiles
+// again with two bf16 pieces.  (A branch within the loop would hold the registers
+// of both forms.)
+template <bool OUT_F32> constexpr int kQForm = OUT_F32 ? 3 : 0;
+
+// Logits of the tokens from `rem` on (of the lane's 32) as -inf.
+__device__ __forceinline__ void mask_tail(f32x16_t (&s)[2], int rem) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (16 * h + i >= rem) s[h][i] = -INFINITY;
+}
+__device__ __forceinline__ float lane_max(const f32x16_t (&s)[2]) {
+  float lm = s[0][0];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) lm = fmaxf(lm, s[h][i]);
+  return lm;
+}
+
+// The reference maximum of the softmax moves when a logit exceeds it by more than
+// kQLazy (weights stay <= 2^kQLazy), so most tiles need no exchange or rescale.
+// lm: the lane's largest logit; `first`: nothing is summed yet.
+template <int FB>
+__device__ __forceinline__ void move_max(float lm, float sc, bool first, float& m_run,
+                                         float& l_run, f32x16_t (&acc)[FB]) {
+  if (!__any(lm * sc > m_run + kQLazy)) return;
+  const float mx = fmaxf(lm, other_half(lm)) * sc;
+  const bool up = mx > m_run + kQLazy;
+  if (!first) {
+    const float alpha = !up ? 1.f : m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mx);
+    l_run *= alpha;
+#pragma unroll
+    for (int fb = 0; fb < FB; ++fb) acc[fb] *= alpha;
+  }
+  m_run = up ? mx : m_run;
+}
+
+// The store as one (question, key head) sees it.
+template <int D>
+struct QuantHead {
+  const uint8_t* base;
+  size_t stride;
+  long long n_blocks;
+  __device__ __forceinline__ QuantHead(const QuantAttnArgs& a, int hk)
+      : base(a.store + (size_t)hk * kStoreRecord<D>),
+        stride((size_t)a.heads_kv * kStoreRecord<D>), n_blocks(a.n_blocks) {}
+  // records of a tile's two blocks, i and i + 1 of a passage (past its last
+  // block: that one, masked); all of it uniform
+  __device__ __forceinline__ void records(int first, int last, int i, const uint8_t*& r0,
+                                          const uint8_t*& r1) const {
+    auto at = [&](int c) -> const uint8_t* {
+      long long blk = (long long)first + min(c, last);
+      blk = blk < 0 ? 0 : (blk >= n_blocks ? n_blocks - 1 : blk);
+      return base + (size_t)blk * stride;
+    };
+    r0 = at(i);
+    r1 = at(i + 1);
+  }
+};
+
+// Result of a virtual row (four features): O, and the LSE with the first.
+template <int D>
+__device__ __forceinline__ void quant_store(const QuantAttnArgs& a, const QuantItem& it, int i,
+                                            int head, int q, float4 o, float m, float l) {
+  const float inv = (l > 0.f) ? 1.f / l : 0.f;
+  const size_t at = (size_t)(it.k0 + it.i0 + i) * a.H + head;
+  if (a.o_f32)
+    *reinterpret_cast<float4*>(static_cast<float*>(a.O) + at * D + q * 4) =
+        make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  else
+    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + at * D + q * 4) =
+        make_uint2(pack2_bf16(o.x * inv, o.y * inv), pack2_bf16(o.z * inv, o.w * inv));
+  if (a.lse && q == 0) a.lse[at] = (l > 0.f) ? (m + log2f(l)) * kQLn2 : -INFINITY;
+}
+
+template <int D, int ROWS, bool OUT_F32>
 __global__ void __launch_bounds__(kQThreads, 2)
 attn_quant_kernel(QuantAttnArgs a) {
-  constexpr int C = D / 32, KH = D / 64;    // feature chunks of a record; pairs of them
-  constexpr int FB = D / 32;                // 32-feature blocks of O
-  constexpr int REC = kStoreRecord<D>;
+  constexpr int KH = QuantTile<D>::KH, FB = QuantTile<D>::FB;
   constexpr int NC4 = D / 4;                // 4-float chunks of an accumulator row
   constexpr int MW = (ROWS + 63) / 64;      // words of a row mask
   __shared__ __attribute__((aligned(16))) float Oacc[ROWS * D];
   __shared__ float m_acc[ROWS], l_acc[ROWS];
-  __shared__ uint64_t rmask[MW][kQMaxP];    // virtual rows adjacent to each passage
-  __shared__ int p_len[kQMaxP], p_blk[kQMaxP], p_cnt[kQMaxP], u_first[kQMaxP];
-  __shared__ int u_total, seg_tiles, next_unit, merged;
+  __shared__ uint8_t rowlist[kQMaxP][ROWS]; // virtual rows adjacent to each passage, ascending
+  __shared__ int p_cnt[kQMaxP];
+  __shared__ int merged;                    // units merged so far
 
   QuantItem it;
   if (!quant_item(a, blockIdx.x, it)) return;
@@ -170,294 +337,433 @@ attn_quant_kernel(QuantAttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, hh = lane >> 5;
+  const uint32_t recip_G = (65536u + (uint32_t)G - 1) / (uint32_t)G;   // v / G for v < 192, G <= 32
+  auto over_G = [&](int v) -> int { return (int)(((uint32_t)v * recip_G) >> 16); };
 
-  // accumulators, passages, adjacent rows of each
+  // lane j: passage j (every wave the same)
+  int my_len = 0, my_blk = 0;
+  if (lane < P) {
+    int ts, te;
+    range_of(a.passage_offsets, it.p0 + lane, a.total_tokens, ts, te);
+    my_len = te - ts;
+    my_blk = a.passage_blocks[it.p0 + lane];
+  }
+  uint64_t mk[MW];
+#pragma unroll
+  for (int w = 0; w < MW; ++w) {
+    const int v = 64 * w + lane;
+    mk[w] = v < nv ? a.rowmask[it.k0 + it.i0 + over_G(v)] : 0ull;
+  }
   for (int i = tid; i < nv * NC4; i += kQThreads)
     reinterpret_cast<float4*>(Oacc)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = tid; i < nv; i += kQThreads) {
     m_acc[i] = -INFINITY;
     l_acc[i] = 0.f;
   }
-  if (tid < P) {
-    int ts, te;
-    range_of(a.passage_offsets, it.p0 + tid, a.total_tokens, ts, te);
-    p_len[tid] = te - ts;
-    p_blk[tid] = a.passage_blocks[it.p0 + tid];
-  }
-  if (wave < MW) {
-    const uint64_t mk = tid < nv ? a.rowmask[it.k0 + it.i0 + tid / G] : 0ull;
-    for (int j = 0; j < P; ++j) {
-      const uint64_t bal = __ballot((mk >> j) & 1ull);
-      if (lane == 0) rmask[wave][j] = bal;
+  if (tid == 0) merged = 0;
+  // adjacent rows of each passage, every wave its share of the passages
+  const uint64_t below = (1ull << lane) - 1ull;
+  for (int j = wave; j < P; j += kQWaves) {
+    int cnt = 0;
+#pragma unroll
+    for (int w = 0; w < MW; ++w) {
+      const bool on = (mk[w] >> j) & 1ull;
+      const uint64_t bal = __ballot(on);
+      if (on) rowlist[j][cnt + __popcll(bal & below)] = (uint8_t)(64 * w + lane);
+      cnt += __popcll(bal);
     }
+    if (lane == 0) p_cnt[j] = cnt;
   }
+
+  // The list of units: 32-row blocks of every adjacent passage, each over `segs`
+  // equal runs of its tiles (more than one where whole passages would leave waves
+  // without a unit).  Every wave forms it (prefix sums of three-bit counts by
+  // ballots); wave w takes every eighth unit.
   __syncthreads();
-  // the list of units: 32-row blocks of every adjacent passage, each over
-  // segments of seg_tiles tiles
-  if (wave == 0) {
-    int cnt = 0, tiles = 0;
-    if (lane < P) {
+  const int my_cnt = lane < P ? p_cnt[lane] : 0;
+  const int my_nblk = my_len > 0 ? (my_cnt + 31) / 32 : 0;
+  static_assert(ROWS <= 7 * 32, "blocks of a passage in three bits");
+  int blocks = 0, my_first = 0;
 #pragma unroll
-      for (int w = 0; w < MW; ++w) cnt += __popcll(rmask[w][lane]);
-      tiles = (p_len[lane] + 63) / 64;
-    }
-    const int nblk = tiles > 0 ? (cnt + 31) / 32 : 0;
-    int work = nblk * tiles;
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) work += __shfl_xor(work, s, kWave);
-    // about four units a wave, two tiles at least
-    const int st = max(2, work / (4 * kQWaves * a.splits));
-    const int units = nblk * ((tiles + st - 1) / st);
-    int x = units;
-#pragma unroll
-    for (int s = 1; s < kWave; s <<= 1) {
-      const int y = __shfl_up(x, s, kWave);
-      if (lane >= s) x += y;
-    }
-    if (lane < P) {
-      p_cnt[lane] = cnt;
-      u_first[lane] = x - units;
-    }
-    if (lane == kWave - 1) {
-      const int first = (int)((long long)x * it.split / a.splits);
-      u_total = (int)((long long)x * (it.split + 1) / a.splits);
-      next_unit = first;
-      merged = first;
-      seg_tiles = st;
-    }
+  for (int bit = 0; bit < 3; ++bit) {
+    const uint64_t bal = __ballot((my_nblk >> bit) & 1);
+    blocks += __popcll(bal) << bit;
+    my_first += __popcll(bal & below) << bit;
   }
-  __syncthreads();
-  const int U = u_total, st = seg_tiles, u_begin = merged;
-  const int my_first = lane < P ? u_first[lane] : 0x7fffffff;
-  __syncthreads();                           // every wave has read `merged`
+  const int segs = blocks >= 2 * kQWaves || blocks == 0
+      ? 1 : min((2 * kQWaves + blocks - 1) / blocks, 8);
+  my_first *= segs;
+  const int u_end = blocks * segs;
 
   const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;   // folded into the queries
   // (not zero: masked logits stay -inf)
   const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);
   const int ki = 4 * (n >> 3) + (n & 3), kb = (n >> 2) & 1;       // the lane's key row
 
-  for (;;) {
-    const int u = wave_fetch_add(&next_unit);
-    if (u >= U) break;
-    // passage of the unit (the last one that starts at or before it; empty
-    // passages start where the next does)
+  struct Unit {
+    int blk0, last_blk;             // first record of the passage, its last block
+    int t0, t1;                     // tokens
+    int before;                     // units to be merged before this one
+    int row;                        // this lane's row (-1: none, not merged)
+    int src;                        // the kept row, or its visual token
+  };
+  auto unit = [&](int u, Unit& x) {
+    // passage of the unit: the last that starts at or before it (passages
+    // without units start where the next one does)
     const int j = __popcll(__ballot(my_first <= u)) - 1;
-    const int cnt = __builtin_amdgcn_readfirstlane(p_cnt[j]);
-    const int len = __builtin_amdgcn_readfirstlane(p_len[j]);
-    const int blk0 = __builtin_amdgcn_readfirstlane(p_blk[j]);
-    const int uf = __builtin_amdgcn_readfirstlane(u_first[j]);
+    const int cnt = __builtin_amdgcn_readlane(my_cnt, j);
+    const int len = __builtin_amdgcn_readlane(my_len, j);
+    const int uf = __builtin_amdgcn_readlane(my_first, j);
+    x.blk0 = __builtin_amdgcn_readlane(my_blk, j);
+    x.last_blk = (len - 1) >> 5;
     const int nblk = (cnt + 31) / 32;
-    const int seg = (u - uf) / nblk, rb = (u - uf) % nblk;
-    const int t0 = seg * st * 64, t1 = min(len, t0 + st * 64);
-    const int last_blk = (len - 1) >> 5;
+    const int seg = (u - uf) / nblk, m = 32 * ((u - uf) - seg * nblk) + n;
+    const int run = ((len + 63) / 64 + segs - 1) / segs * 64;    // tokens of a segment
+    x.t0 = min(seg * run, len);
+    x.t1 = min(x.t0 + run, len);
+    x.before = uf + seg * nblk;
+    x.row = m < cnt && x.t0 < x.t1 ? rowlist[j][m] : -1;         // (no tokens: nothing to merge)
+    x.src = it.k0 + it.i0 + over_G(max(x.row, 0));
+    if (a.kept_idx) x.src = a.kept_idx[x.src];
+  };
+  u32x4 qf[4 * KH];                          // features 64 kh + 32 hh .. + 31
+  auto load_q = [&](const Unit& x) {
+    const int v = max(x.row, 0);
+    const size_t r = a.kept_idx ? (size_t)it.b * a.N + clampi(x.src, 0, a.N - 1) : (size_t)x.src;
+    const bf16_t* src = a.q + (r * a.H + (size_t)(it.hk * G + (v - over_G(v) * G))) * D + 32 * hh;
+#pragma unroll
+    for (int kh = 0; kh < KH; ++kh)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        qf[4 * kh + s] = *reinterpret_cast<const u32x4*>(src + 64 * kh + 8 * s);
+  };
+  const QuantHead<D> head(a, it.hk);
+  QuantTile<D> x;
+  const uint8_t *r0, *r1;                    // the tile's records
+  auto load_k = [&](const Unit& w, int t) {
+    head.records(w.blk0, w.last_blk, t >> 5, r0, r1);
+    x.load_k(kb ? r1 : r0, ki, hh);
+  };
+  auto load_v = [&]() { x.load_v(hh ? r1 : r0, n); };
 
-    // this lane's row (past the block's rows: a placeholder that is not merged)
-    int row = -1;
-    {
-      int m = 32 * rb + n;
-      if (m < cnt) {
+  int u = wave;
+  Unit cur, nxt;
+  if (u < u_end) {
+    // (in this order, as in the loop: the counted waits there go by it)
+    unit(u, cur);
+    load_q(cur);
+    asm volatile("" ::: "memory");
+    load_k(cur, cur.t0);
+    asm volatile("" ::: "memory");
+    load_v();
+    asm volatile("" ::: "memory");
+  }
+  for (; u < u_end; u += kQWaves) {
+    // the next unit's first tile is loaded during this one's last, its queries
+    // during the merge
+    nxt = cur;
+    if (u + kQWaves < u_end) unit(u + kQWaves, nxt);
+    // (the queries are waited for here, not in the loop, where the wait would
+    // reach the tile's loads, too)
 #pragma unroll
-        for (int w = 0; w < MW; ++w) {
-          const uint64_t bits = rmask[w][j];
-          const int c = __popcll(bits);
-          if (row < 0 && m < c) row = 64 * w + nth_set(bits, m);
-          m -= c;
-        }
-      }
+    for (int i = 0; i < 4 * KH; ++i) {
+      qf[i] ^= neg;
+      asm volatile("" : "+v"(qf[i]));
     }
-    u32x4 qf[4 * KH];                        // features 64 kh + 32 hh .. + 31
-    {
-      const int v = max(row, 0);
-      const int kr = it.k0 + it.i0 + v / G;
-      const size_t r = a.kept_idx
-          ? (size_t)it.b * a.N + clampi(a.kept_idx[kr], 0, a.N - 1) : (size_t)kr;
-      const bf16_t* src = a.q + (r * a.H + (size_t)(it.hk * G + v % G)) * D + 32 * hh;
-#pragma unroll
-      for (int kh = 0; kh < KH; ++kh)
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-          qf[4 * kh + s] = *reinterpret_cast<const u32x4*>(src + 64 * kh + 8 * s) ^ neg;
-    }
-
-    // record of the passage's block i (past its last block: that one, masked)
-    auto record = [&](int i) -> const uint8_t* {
-      long long blk = (long long)blk0 + min(i, last_blk);
-      blk = blk < 0 ? 0 : (blk >= a.n_blocks ? a.n_blocks - 1 : blk);
-      return a.store + ((size_t)blk * a.heads_kv + it.hk) * REC;
-    };
-    u32x4 kx[2][KH], vx[FB];
-    uint32_t ks = 0, vs = 0;
-    auto load_k = [&](int t) {
-      const uint8_t* rec = record((t >> 5) + kb);
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int kh = 0; kh < KH; ++kh)
-          kx[h][kh] = *reinterpret_cast<const u32x4*>(rec + ((h * C + 2 * kh + hh) * 16 + ki) * 16);
-      const uint8_t* sp = rec + 32 * D + (hh * 16 + ki) * C;
-      ks = C == 4 ? *reinterpret_cast<const uint32_t*>(sp) : *reinterpret_cast<const uint16_t*>(sp);
-    };
-    auto load_v = [&](int t) {
-      const uint8_t* rec = record((t >> 5) + hh);
+    f32x16_t acc[FB];
+    float m_run, l_run;
+    auto start = [&]() {
+      m_run = -INFINITY;
+      l_run = 0.f;
 #pragma unroll
       for (int fb = 0; fb < FB; ++fb)
-        vx[fb] = *reinterpret_cast<const u32x4*>(rec + 16 * D + (32 * fb + n) * 16);
-      const uint8_t* sp = rec + 33 * D + n * C;
-      vs = C == 4 ? *reinterpret_cast<const uint32_t*>(sp) : *reinterpret_cast<const uint16_t*>(sp);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[fb][i] = 0.f;
     };
-
-    f32x16_t acc[FB];
-#pragma unroll
-    for (int fb = 0; fb < FB; ++fb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[fb][i] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
-
-    load_k(t0);
-    load_v(t0);
-    for (int t = t0; t < t1; t += 64) {
+    // (a segment's first tile has a token in every column: m_run is finite then)
+    auto attend = [&](int t, f32x16_t (&s)[2]) {
+      if (t + 64 > cur.t1) mask_tail(s, cur.t1 - t - 32 * hh);
+      move_max(lane_max(s), sc, t == cur.t0, m_run, l_run, acc);
+    };
+    start();
+    bool again = false;
+    int t = cur.t0;
+    do {                                     // (once for an empty segment, too: masked)
       f32x16_t s[2];
-      unrolled<2>([&](auto h_) {
-        constexpr int h = decltype(h_)::value;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[h][i] = 0.f;
-        unrolled<KH>([&](auto kh_) {
-          constexpr int kh = decltype(kh_)::value;
-          const float scl = scale_of<h * KH + kh>(ks);
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            s[h] = mfma32_bf16(expand8(kx[h][kh][q], scl), qf[4 * kh + q], s[h]);
-        });
-      });
-      // the next tile's keys land during the softmax and the second product
-      // (past the segment: the last tile again, unused)
-      const int tn = min(t + 64, (t1 - 1) & ~63);
-      load_k(tn);
-      if (t + 64 > t1) {
-        const int rem = t1 - t - 32 * hh;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (16 * h + i >= rem) s[h][i] = -INFINITY;
+      x.logits(qf, s);
+      // the next keys land during the softmax and the second product
+      const bool last = t + 64 >= cur.t1;
+      const int tn = last ? nxt.t0 : t + 64;
+      load_k(last ? nxt : cur, tn);
+      attend(t, s);
+      if (!OUT_F32 && !__all(half_scales<FB>(x.vs))) {
+        again = true;
+        break;
       }
-      float lm = s[0][0];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) lm = fmaxf(lm, s[h][i]);
-      // the reference maximum moves when a logit exceeds it by more than kQLazy
-      // (weights stay <= 2^kQLazy), so most tiles need no exchange or rescale
-      if (__any(lm * sc > m_run + kQLazy)) {
-        const float mx = fmaxf(lm, other_half(lm)) * sc;
-        if (mx > m_run + kQLazy) {
-          const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - mx);
-          m_run = mx;
-          l_run *= alpha;
-#pragma unroll
-          for (int fb = 0; fb < FB; ++fb) acc[fb] *= alpha;
-        }
-      }
-      // (a segment's first tile has a token in every column, so m_run is finite)
-      float ls = 0.f;
-      unrolled<4>([&](auto q_) {
-        constexpr int q = decltype(q_)::value, h = q >> 1, i0 = 8 * (q & 1);
-        u32x4 pc[PIECES];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float p0 = __builtin_amdgcn_exp2f(fmaf(s[h][i0 + 2 * e], sc, -m_run));
-          float p1 = __builtin_amdgcn_exp2f(fmaf(s[h][i0 + 2 * e + 1], sc, -m_run));
-          ls += p0 + p1;
-          // all pieces but the last are truncated, the rest is exact
-#pragma unroll
-          for (int c = 0; c + 1 < PIECES; ++c) {
-            const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
-            pc[c][e] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
-            p0 -= __uint_as_float(b0 & 0xffff0000u);
-            p1 -= __uint_as_float(b1 & 0xffff0000u);
-          }
-          pc[PIECES - 1][e] = pack2_bf16(p0, p1);
-        }
-        unrolled<FB>([&](auto fb_) {
-          constexpr int fb = decltype(fb_)::value;
-          const u32x4 va = expand8(vx[fb][q], scale_of<fb>(vs));
-#pragma unroll
-          for (int c = 0; c < PIECES; ++c) acc[fb] = mfma32_bf16(va, pc[c], acc[fb]);
-        });
-      });
-      l_run += ls;
-      load_v(tn);
+      l_run += x.template weigh<kQForm<OUT_F32>>(s, sc, m_run, acc);
+      asm volatile("" ::: "memory");
+      load_v();
+      t += 64;
+    } while (t < cur.t1);
+    if (!OUT_F32 && again) {
+      start();
+      t = cur.t0;
+      do {
+        f32x16_t s[2];
+        load_k(cur, t);
+        load_v();
+        x.logits(qf, s);
+        attend(t, s);
+        l_run += x.template weigh<2>(s, sc, m_run, acc);
+        t += 64;
+      } while (t < cur.t1);
+      load_k(nxt, nxt.t0);
+      asm volatile("" ::: "memory");
+      load_v();
     }
+    load_q(nxt);
+    asm volatile("" ::: "memory");
 
     // merge in the order of the list: every unit of earlier passages and
     // segments first (the others of this one have other rows)
-    const int before = max(uf + seg * nblk, u_begin);
-    while (__hip_atomic_load(&merged, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) < before)
+    while (__hip_atomic_load(&merged, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) < cur.before)
       __builtin_amdgcn_s_sleep(1);
     asm volatile("" ::: "memory");
     const float l_tot = l_run + other_half(l_run);
+    const int row = cur.row;
     if (row >= 0) {
       const float mo = m_acc[row], lo = l_acc[row];
       const float mn = fmaxf(mo, m_run);
       const float fa = __builtin_amdgcn_exp2f(mo - mn);     // 0 while the row is empty
       const float fc = __builtin_amdgcn_exp2f(m_run - mn);
       float4* orow = reinterpret_cast<float4*>(Oacc + row * D);
+      // (a half of the row at a time in registers)
 #pragma unroll
-      for (int fb = 0; fb < FB; ++fb)
+      for (int f0 = 0; f0 < FB; f0 += 2) {
+        float4 ov[2][4];                     // features 32 fb + 8 c + 4 hh .. + 3
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          // features 32 fb + 8 c + 4 hh .. + 3
-          float4& o = orow[(8 * fb + 2 * c + hh) ^ (row & (NC4 - 1))];
-          o = make_float4(fmaf(o.x, fa, acc[fb][4 * c] * fc), fmaf(o.y, fa, acc[fb][4 * c + 1] * fc),
-                          fmaf(o.z, fa, acc[fb][4 * c + 2] * fc),
-                          fmaf(o.w, fa, acc[fb][4 * c + 3] * fc));
-        }
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            ov[f][c] = orow[(8 * (f0 + f) + 2 * c + hh) ^ (row & (NC4 - 1))];
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const float4 o = ov[f][c];
+            const f32x16_t& x = acc[f0 + f];
+            orow[(8 * (f0 + f) + 2 * c + hh) ^ (row & (NC4 - 1))] =
+                make_float4(fmaf(o.x, fa, x[4 * c] * fc), fmaf(o.y, fa, x[4 * c + 1] * fc),
+                            fmaf(o.z, fa, x[4 * c + 2] * fc), fmaf(o.w, fa, x[4 * c + 3] * fc));
+          }
+      }
       if (hh == 0) {
         m_acc[row] = mn;
         l_acc[row] = fmaf(lo, fa, l_tot * fc);
       }
     }
     wait_lgkm0();
-    wave_fetch_add(&merged);
+    wave_add_one(&merged);
+    cur = nxt;
   }
   __syncthreads();
 
-  if (a.splits > 1) {
-    // this split's partial: rows of D values, then maxima and sums
-    float* po = a.part + ((size_t)((it.b * a.heads_kv + it.hk) * a.chunks + it.chunk) * a.splits +
-                          it.split) * part_floats(a.rows_chunk * G, D);
-    for (int e = tid; e < nv * NC4; e += kQThreads) {
-      const int ri = e / NC4, q = e % NC4;
-      reinterpret_cast<float4*>(po)[e] =
-          reinterpret_cast<const float4*>(Oacc + ri * D)[q ^ (ri & (NC4 - 1))];
-    }
-    float* pm = po + (size_t)(a.rows_chunk * G) * D;
-    for (int i = tid; i < nv; i += kQThreads) {
-      pm[i] = m_acc[i];
-      pm[a.rows_chunk * G + i] = l_acc[i];
-    }
-    return;
-  }
   // O = acc / sum for every row, and the LSE (0 and -inf without neighbours)
   for (int e = tid; e < nv * NC4; e += kQThreads) {
-    const int ri = e / NC4, q = e % NC4;
-    const float4 v = reinterpret_cast<const float4*>(Oacc + ri * D)[q ^ (ri & (NC4 - 1))];
-    const float l = l_acc[ri];
-    const float inv = (l > 0.f) ? 1.f / l : 0.f;
-    const size_t off = ((size_t)(it.k0 + it.i0 + ri / G) * a.H + it.hk * G + ri % G) * D + q * 4;
-    if (a.o_f32)
-      *reinterpret_cast<float4*>(static_cast<float*>(a.O) + off) =
-          make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-    else
-      *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + off) =
-          make_uint2(pack2_bf16(v.x * inv, v.y * inv), pack2_bf16(v.z * inv, v.w * inv));
+    const int ri = e / NC4, q = e % NC4, i = over_G(ri);
+    quant_store<D>(a, it, i, it.hk * G + (ri - i * G), q,
+                   reinterpret_cast<const float4*>(Oacc + ri * D)[q ^ (ri & (NC4 - 1))],
+                   m_acc[ri], l_acc[ri]);
   }
-  if (a.lse)
-    for (int i = tid; i < nv; i += kQThreads) {
-      const float l = l_acc[i];
-      a.lse[(size_t)(it.k0 + it.i0 + i / G) * a.H + it.hk * G + i % G] =
-          (l > 0.f) ? (m_acc[i] + log2f(l)) * kQLn2 : -INFINITY;
+}
+
+// Row-tile form: up to 32 virtual rows a workgroup.  Its waves take the 64-token
+// tiles of the passages adjacent to any of the rows in turn, each with its own
+// (O, max, sum) in registers from its first tile to its last, so that the loop
+// has no LDS, no barrier and one stream of loads a tile ahead; a logit of a row that is not
+// adjacent to the tile's passage is -inf (its weight of 0 meets held values, which
+// are finite).  The waves' partials are merged in wave order through LDS at the end.
+constexpr int kQTileRows = 32;
+
+template <int D, bool OUT_F32>
+__global__ void __launch_bounds__(kQThreads, 2)
+attn_quant_tile_kernel(QuantAttnArgs a) {
+  constexpr int KH = QuantTile<D>::KH, FB = QuantTile<D>::FB, NC4 = D / 4;
+  constexpr int OS = D + 4;                 // floats per row of a wave's partial (bank spread)
+  __shared__ __attribute__((aligned(16))) float po[kQWaves][kQTileRows][OS];
+  __shared__ float pm[kQWaves][kQTileRows], pl[kQWaves][kQTileRows];
+  QuantItem it;
+  if (!quant_item(a, blockIdx.x, it)) return;
+  const int G = a.G, nv = it.nk * G, P = it.P;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int ki = 4 * (n >> 3) + (n & 3), kb = (n >> 2) & 1;       // the lane's key row
+
+  // this lane's row (past the item's rows: its last one, adjacent to nothing)
+  const int v = min(n, nv - 1), i = v / G, hq = it.hk * G + (v - i * G);
+  uint64_t mk = a.rowmask[it.k0 + it.i0 + i];
+  // lane j: passage j
+  int my_len = 0, my_blk = 0;
+  if (lane < P) {
+    int ts, te;
+    range_of(a.passage_offsets, it.p0 + lane, a.total_tokens, ts, te);
+    my_len = te - ts;
+    my_blk = a.passage_blocks[it.p0 + lane];
+  }
+  u32x4 qf[4 * KH];
+  {
+    const int kr = it.k0 + it.i0 + i;
+    const size_t r = a.kept_idx
+        ? (size_t)it.b * a.N + clampi(a.kept_idx[kr], 0, a.N - 1) : (size_t)kr;
+    const bf16_t* src = a.q + (r * a.H + hq) * D + 32 * hh;
+#pragma unroll
+    for (int kh = 0; kh < KH; ++kh)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        qf[4 * kh + s] = *reinterpret_cast<const u32x4*>(src + 64 * kh + 8 * s);
+  }
+  if (n >= nv) mk = 0ull;
+  uint64_t U = mk;                           // passages adjacent to some row
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) U |= (uint64_t)__shfl_xor((unsigned long long)U, s, kWave);
+  // tiles of the adjacent passages, one after the other
+  const int my_tiles = lane < P && ((U >> lane) & 1ull) ? (my_len + 63) / 64 : 0;
+  int my_end = my_tiles;
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) {
+    const int y = __shfl_up(my_end, s, kWave);
+    if (lane >= s) my_end += y;
+  }
+  const int my_first = my_end - my_tiles;
+  const int tiles = __builtin_amdgcn_readlane(my_end, kWave - 1);
+  const int x0 = (int)((long long)tiles * it.split / a.splits);
+  const int x1 = (int)((long long)tiles * (it.split + 1) / a.splits);
+
+  const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;   // folded into the queries
+  // (not zero: masked logits stay -inf)
+  const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);
+  const QuantHead<D> head(a, it.hk);
+  struct Place {
+    int j, t, len, blk0;
+  };
+  auto place = [&](int c, Place& w) {
+    w.j = __popcll(__ballot(my_first <= c)) - 1;         // as for the units above
+    w.len = __builtin_amdgcn_readlane(my_len, w.j);
+    w.blk0 = __builtin_amdgcn_readlane(my_blk, w.j);
+    w.t = (c - __builtin_amdgcn_readlane(my_first, w.j)) * 64;
+  };
+  auto load = [&](const Place& w, QuantTile<D>& x) {
+    const uint8_t *r0, *r1;                  // the tile's records
+    head.records(w.blk0, (w.len - 1) >> 5, w.t >> 5, r0, r1);
+    x.load_k(kb ? r1 : r0, ki, hh);
+    x.load_v(hh ? r1 : r0, n);
+    asm volatile("" ::: "memory");           // (tiles in order: the counted waits go by it)
+  };
+  f32x16_t acc[FB];
+  float m_run, l_run;
+  auto start = [&]() {
+    m_run = -INFINITY;
+    l_run = 0.f;
+#pragma unroll
+    for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[fb][e] = 0.f;
+  };
+  // one tile's logits into weights; returns the reference of their exponents
+  // (a row that is not adjacent: every weight 2^-inf = 0)
+  auto attend = [&](const Place& w, f32x16_t (&s)[2]) -> float {
+    if (w.t + 64 > w.len) mask_tail(s, w.len - w.t - 32 * hh);
+    const bool adj = (mk >> w.j) & 1ull;
+    move_max(adj ? lane_max(s) : -INFINITY, sc, false, m_run, l_run, acc);
+    return adj ? m_run : INFINITY;
+  };
+#pragma unroll
+  for (int e = 0; e < 4 * KH; ++e) {
+    qf[e] ^= neg;
+    asm volatile("" : "+v"(qf[e]));         // (waited for here, not in the loop)
+  }
+  start();
+  // two tiles in turn: one's loads are in flight while the other is computed
+  Place pa, pb;
+  QuantTile<D> xa, xb;
+  bool again = false;
+  auto compute = [&](const Place& w, const QuantTile<D>& x) {
+    f32x16_t s[2];
+    x.logits(qf, s);
+    const float ref = attend(w, s);
+    if (!OUT_F32 && !__all(half_scales<FB>(x.vs))) again = true;
+    else l_run += x.template weigh<kQForm<OUT_F32>>(s, sc, ref, acc);
+  };
+  int c = x0 + wave;
+  if (c < x1) {
+    place(c, pa);
+    load(pa, xa);
+    for (;;) {
+      c += kQWaves;
+      place(min(c, x1 - 1), pb);             // (past the last tile: one that is not used)
+      load(pb, xb);
+      compute(pa, xa);
+      if (c >= x1) break;
+      c += kQWaves;
+      place(min(c, x1 - 1), pa);
+      load(pa, xa);
+      compute(pb, xb);
+      if (c >= x1) break;
     }
+  }
+  if (!OUT_F32 && again) {
+    start();
+    for (c = x0 + wave; c < x1; c += kQWaves) {
+      place(c, pa);
+      load(pa, xa);
+      f32x16_t s[2];
+      xa.logits(qf, s);
+      const float ref = attend(pa, s);
+      l_run += xa.template weigh<2>(s, sc, ref, acc);
+    }
+  }
+
+  const float l_tot = l_run + other_half(l_run);
+  if (hh == 0) {
+    pm[wave][n] = m_run;
+    pl[wave][n] = l_tot;
+  }
+#pragma unroll
+  for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)              // features 32 fb + 8 q + 4 hh .. + 3
+      *reinterpret_cast<float4*>(&po[wave][n][32 * fb + 8 * q + 4 * hh]) =
+          make_float4(acc[fb][4 * q], acc[fb][4 * q + 1], acc[fb][4 * q + 2], acc[fb][4 * q + 3]);
+  __syncthreads();
+  float* part = a.part + ((size_t)((it.b * a.heads_kv + it.hk) * a.chunks + it.chunk) * a.splits +
+                          it.split) * part_floats(a.rows_chunk * G, D);
+  for (int e = tid; e < nv * NC4; e += kQThreads) {
+    const int ri = e / NC4, q = e % NC4;
+    float M = pm[0][ri];
+#pragma unroll
+    for (int w = 1; w < kQWaves; ++w) M = fmaxf(M, pm[w][ri]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kQWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(pm[w][ri] - ref);
+      const float4 y = *reinterpret_cast<const float4*>(&po[w][ri][4 * q]);
+      l = fmaf(pl[w][ri], f, l);
+      o = make_float4(fmaf(y.x, f, o.x), fmaf(y.y, f, o.y), fmaf(y.z, f, o.z), fmaf(y.w, f, o.w));
+    }
+    if (a.splits > 1) {
+      reinterpret_cast<float4*>(part)[e] = o;
+      if (q == 0) {
+        part[(size_t)a.rows_chunk * G * D + ri] = M;
+        part[(size_t)a.rows_chunk * G * (D + 1) + ri] = l;
+      }
+    } else {
+      const int ii = ri / G;
+      quant_store<D>(a, it, ii, it.hk * G + (ri - ii * G), q, o, M, l);
+    }
+  }
 }
 
 // The splits' partials of each item, added in their order.
@@ -477,49 +783,60 @@ attn_quant_merge_kernel(QuantAttnArgs a) {
   const float* pl = pm + rows;
   for (int e = threadIdx.x; e < nv * NC4; e += 256) {
     const int ri = e / NC4, q = e % NC4;
-    float M = -INFINITY;
-    for (int s = 0; s < S; ++s) M = fmaxf(M, pm[s * step + ri]);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float l = 0.f;
+    // (eight parts in flight; the maximum moves from batch to batch)
+    constexpr int U = 8;
+    float M = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < S; ++s) {
-      const float f = __builtin_amdgcn_exp2f(pm[s * step + ri] - ref);
-      l = fmaf(pl[s * step + ri], f, l);
-      const float4 x = reinterpret_cast<const float4*>(po + s * step)[e];
-      o.x = fmaf(x.x, f, o.x);
-      o.y = fmaf(x.y, f, o.y);
-      o.z = fmaf(x.z, f, o.z);
-      o.w = fmaf(x.w, f, o.w);
+    for (int s0 = 0; s0 < S; s0 += U) {
+      float m[U], ls[U];
+      float4 x[U];
+#pragma unroll
+      for (int c = 0; c < U; ++c) {
+        const size_t s = (size_t)min(s0 + c, S - 1) * step;
+        m[c] = pm[s + ri];
+        ls[c] = pl[s + ri];
+        x[c] = reinterpret_cast<const float4*>(po + s)[e];
+      }
+      float mx = M;
+#pragma unroll
+      for (int c = 0; c < U; ++c) mx = fmaxf(mx, m[c]);
+      if (mx == -INFINITY) continue;                       // no part with a unit of this row yet
+      const float f0 = __builtin_amdgcn_exp2f(M - mx);
+      M = mx;
+      l *= f0;
+      o = make_float4(o.x * f0, o.y * f0, o.z * f0, o.w * f0);
+#pragma unroll
+      for (int c = 0; c < U; ++c) {
+        const float f = s0 + c < S ? __builtin_amdgcn_exp2f(m[c] - mx) : 0.f;
+        l = fmaf(ls[c], f, l);
+        o = make_float4(fmaf(x[c].x, f, o.x), fmaf(x[c].y, f, o.y), fmaf(x[c].z, f, o.z),
+                        fmaf(x[c].w, f, o.w));
+      }
     }
-    const float inv = (l > 0.f) ? 1.f / l : 0.f;
-    const size_t at = (size_t)(it.k0 + it.i0 + ri / G) * a.H + it.hk * G + ri % G;
-    if (a.o_f32)
-      *reinterpret_cast<float4*>(static_cast<float*>(a.O) + at * D + q * 4) =
-          make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    else
-      *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + at * D + q * 4) =
-          make_uint2(pack2_bf16(o.x * inv, o.y * inv), pack2_bf16(o.z * inv, o.w * inv));
-    if (a.lse && q == 0) a.lse[at] = (l > 0.f) ? (M + log2f(l)) * kQLn2 : -INFINITY;
+    quant_store<D>(a, it, ri / G, it.hk * G + ri % G, q, o, M, l);
   }
 }
 
 // How a problem is cut: virtual rows of an item, chunks of a question, splits of
 // an item's list.
 struct QuantShape {
+  bool tile;
   int rows, chunks, rows_chunk, splits;
 };
 static QuantShape quant_shape(const skip_problem_t& p, int heads_kv) {
   const int G = p.H / heads_kv;
   const long long groups = (long long)p.B * heads_kv;
   QuantShape s;
-  for (int rows : {192, 64, 32}) {
+  auto cut = [&](int rows) {
     s.rows = rows;
     s.rows_chunk = std::max(1, rows / G);
     s.chunks = (p.k_max + s.rows_chunk - 1) / s.rows_chunk;
-    if (groups * s.chunks >= 512) break;
-  }
+    return groups * s.chunks;
+  };
   s.splits = 1;
-  const long long wgs = groups * s.chunks;
+  s.tile = cut(192) < 256;
+  if (!s.tile) return s;
+  const long long wgs = cut(kQTileRows);
   if (wgs > 0 && wgs < 256) {
     // at least eight tiles of 64 tokens a split
     const long long tiles = (long long)p.P_max * ((p.L_max + 63) / 64);
@@ -574,22 +891,20 @@ hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t
   const long long wgs = 8 * (((long long)a.groups + 7) / 8) * a.chunks * a.splits;
   if (wgs > (1 << 22)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)wgs);
-#define SKIP_ATTN_QUANT(DD, RR, PP)                                                        \
-  hipLaunchKernelGGL((attn_quant_kernel<DD, RR, PP>), grid, dim3(kQThreads), 0, s, a)
-#define SKIP_ATTN_QUANT_ROWS(DD, PP)                                                       \
+#define SKIP_ATTN_QUANT(DD, FF)                                                            \
   do {                                                                                     \
-    if (sh.rows == 192) SKIP_ATTN_QUANT(DD, 192, PP);                                      \
-    else if (sh.rows == 64) SKIP_ATTN_QUANT(DD, 64, PP);                                   \
-    else SKIP_ATTN_QUANT(DD, 32, PP);                                                      \
+    if (sh.tile)                                                                           \
+      hipLaunchKernelGGL((attn_quant_tile_kernel<DD, FF>), grid, dim3(kQThreads), 0, s, a); \
+    else                                                                                   \
+      hipLaunchKernelGGL((attn_quant_kernel<DD, 192, FF>), grid, dim3(kQThreads), 0, s, a); \
   } while (0)
   if (p.d_h == 64) {
-    if (p.o_f32) SKIP_ATTN_QUANT_ROWS(64, 3);
-    else SKIP_ATTN_QUANT_ROWS(64, 2);
+    if (p.o_f32) SKIP_ATTN_QUANT(64, true);
+    else SKIP_ATTN_QUANT(64, false);
   } else {
-    if (p.o_f32) SKIP_ATTN_QUANT_ROWS(128, 3);
-    else SKIP_ATTN_QUANT_ROWS(128, 2);
+    if (p.o_f32) SKIP_ATTN_QUANT(128, true);
+    else SKIP_ATTN_QUANT(128, false);
   }
-#undef SKIP_ATTN_QUANT_ROWS
 #undef SKIP_ATTN_QUANT
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;

@@ -54,9 +54,14 @@ class Held:
         return B.quantize_passages(self.p, self.store, self.K.cuda(), self.V.cuda(), self.po,
                                    self.pb, want_keys)
 
-    def held(self):
+    def held1(self):
+        """As held, of the passages that were written."""
+        return self.held(cum(self.Ls))
+
+    def held(self, off=None):
         Ko, Vo = [], []
-        for a, b in zip(self.off[:-1], self.off[1:]):
+        off = self.off if off is None else off
+        for a, b in zip(off[:-1], off[1:]):
             k, v = orc.held_passage(self.K[a:b].double().numpy(), self.V[a:b].double().numpy())
             Ko.append(k)
             Vo.append(v)
@@ -169,14 +174,16 @@ def random_graph(ks, Ps, seed):
     return out
 
 
-def reference(Q, K, V, nb, ks, Ps, off, scale, G, o_f32=False):
+def reference(Q, K, V, nb, ks, Ps, off, scale, G, o_f32=False, piece=None):
     """O, LSE in float64 and a bound of the kernel's error before the output's own
     rounding: the logits' products are exact and summed in float32 (at most D
     roundings of 2^-24 of the sum of magnitudes, the scale's and the exponent's
-    rounding a few more of the logit), the pieces of a weight miss it by at most
-    2^-16 (three pieces, for float output: 2^-24), the float32 sums of n weights by
-    n 2^-24; twice for numerator and denominator."""
-    piece = 2.0 ** -24 if o_f32 else 2.0 ** -16
+    rounding a few more of the logit), a weight enters as a half float, half a step
+    of 2^-10 off (three bf16 pieces for float output: 2^-24; two where a held value
+    is no half float: 2^-16; a weight below 2^-14 is off by at most 2^-25 of the
+    largest), the float32 sums of n weights by n 2^-24; twice for numerator and
+    denominator."""
+    piece = piece or (2.0 ** -24 if o_f32 else 2.0 ** -11)
     O = np.zeros(Q.shape)
     lse = np.full(Q.shape[:2], -np.inf)
     bound = np.zeros(Q.shape[:2])
@@ -250,6 +257,45 @@ def test_attention_shapes(B, D, H, Hkv, ks, Ps, Ls, o_f32):
     torch.cuda.synchronize()
     ref = reference(Q.double().numpy(), *x.held(), nb, ks, Ps, x.off, scale, H // Hkv, o_f32)
     check(O, lse, ref, o_f32, "shapes")
+
+
+def wide_values(x):
+    """Features from 2^-40 to 2^40: no half floats."""
+    return x * torch.exp2(torch.arange(x.shape[-1]).remainder(9).sub(4).float() * 10)
+
+
+def one_wide(x):
+    """Half floats but for one feature of the later tokens."""
+    x = x.clone()
+    x[100:, -1, 5] *= 2.0 ** 30
+    return x
+
+
+@pytest.mark.parametrize("make", [wide_values, one_wide])
+@pytest.mark.parametrize("nq", [1, 70])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_values_that_are_no_half_floats(B, D, nq, make):
+    """Both forms (few rows; past 256 items of 192 rows), elementwise against each
+    feature's own size."""
+    H, ks, Ps = 4, [9] * nq, [3] * nq
+    x = Held(B, [90, 64, 33], H, H, D, 25)
+    x.V = make(x.V.float()).to(x.dt)
+    x.write(B)
+    x.off, x.po = cum([90, 64, 33] * nq), dev(cum([90, 64, 33] * nq))
+    x.pb = dev(np.tile(x.blocks, nq))
+    say(f"store attention wide values D={D} nq={nq} {make.__name__}")
+    Q = rows_of(9, H, D, 26)
+    nb = random_graph([9], [3], 27)
+    O, lse = attend(B, x, Q.repeat(nq, 1, 1), nb * nq, ks, Ps, 0.2)
+    torch.cuda.synchronize()
+    K, V = x.held1()
+    ref = reference(Q.double().numpy(), K, V, nb, [9], [3], cum([90, 64, 33]), 0.2, 1)
+    size = np.abs(V).max(0)[None]                     # of each head's feature
+    lim = ref[2] / np.maximum(np.abs(V).max(), 1e-300)
+    O = O.cpu().double().numpy().reshape(nq, 9, H, D)
+    assert (O == O[:1]).all()
+    err = np.abs(O[0] - ref[0])
+    assert (err <= np.abs(ref[0]) * 2.0 ** -8 + lim.max() * size).all()
 
 
 @pytest.mark.parametrize("scale", [-0.3, 0.0, 2.0])
