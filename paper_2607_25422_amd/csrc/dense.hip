@@ -10,8 +10,8 @@
 // zeros up to a multiple of 256.
 //
 //   dense_tile_kernel : 32 MB rows x 256 columns a workgroup
-//   dense_rows_kernel : few rows: 32 MB rows x 64 columns, the contraction split
-//                       over the workgroup's waves
+//   dense_rows_kernel : up to 32 rows x 64 columns, the contraction split over the
+//                       workgroup's waves
 //   dense_join_kernel : adds the parts of a contraction that several workgroups
 //                       shared, in their order, and finishes
 #include <algorithm>
@@ -23,7 +23,8 @@
 namespace skip {
 
 constexpr int kDnNT = 256;         // columns of a packed tile
-constexpr int kDnKS = 32;          // contraction per step
+constexpr int kDnKS = 32;          // contraction of a packed step
+constexpr int kDnStep = 64;        // contraction per step of dense_tile_kernel
 constexpr int kDnThreads = 256;    // dense_tile_kernel: four waves of 64 columns
 constexpr int kDnWaves = 8;        // dense_rows_kernel
 constexpr long long kDnCUs = 256;
@@ -65,35 +66,52 @@ __device__ __forceinline__ size_t dense_row(const DenseArgs& a, const int32_t* i
   return (size_t)lo * a.N + clampi(idx[r], 0, a.N - 1);
 }
 
-__device__ __forceinline__ float dense_act(float x, int act) {
-  switch (act) {
-    case SKIP_ACT_RELU: return fmaxf(x, 0.f);
-    // (erfc: 1 + erf would lose the tail below zero)
-    case SKIP_ACT_GELU: return 0.5f * x * erfcf(x * -0.70710678118654752f);
-    case SKIP_ACT_SILU: return x / (1.f + __expf(-x));
-  }
-  return x;
+// x / 2 erfc(-x / sqrt 2).  With z = |x| / sqrt 2, erfc(z) = exp(-z^2) P(1 / (1 + p z)),
+// P a polynomial fitted to exp(z^2) erfc(z) on 0 <= z <= 6 by weighted least squares
+// (2.6e-7 relative; beyond, erfc is below 2^-54); for x > 0 the rest of x.  Six times
+// fewer instructions than the library's erfc, which took 45 us of 111 on 4616 rows of
+// 4096 columns.
+__device__ __forceinline__ float gelu(float x) {
+  constexpr float p = 0.3625f;
+  const float ax = fabsf(x);
+  const float t = __builtin_amdgcn_rcpf(fmaf(ax, p * 0.70710678f, 1.f));
+  float h = -0.16227377519580077f;
+  h = fmaf(h, t, 0.5469444163308744f);
+  h = fmaf(h, t, -0.3379855943955391f);
+  h = fmaf(h, t, 0.42285832312829363f);
+  h = fmaf(h, t, 0.1080726978837203f);
+  h = fmaf(h, t, 0.21891024798015968f);
+  h = fmaf(h, t, 0.2034739364192221f);
+  // (-z^2 log2 e)
+  const float q = 0.5f * h * t * __builtin_amdgcn_exp2f(ax * ax * -0.72134752044448170f);
+  const float m = fminf(ax, 1e3f);  // (infinity times q = 0 is no number)
+  return x < 0.f ? -m * q : fmaf(-m, q, x);
+}
+// x / (1 + exp(-x))
+__device__ __forceinline__ float silu(float x) {
+  return x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.4426950408889634f));
 }
 
-// Eight sums of row r, columns j .. j + 7: bias, activation, residual, store.
-__device__ __forceinline__ void dense_finish8(const DenseArgs& a, int r, int j, float (&x)[8]) {
-  if (a.bias) {
-    const float4 b0 = reinterpret_cast<const float4*>(a.bias + j)[0];
-    const float4 b1 = reinterpret_cast<const float4*>(a.bias + j)[1];
-    x[0] += b0.x; x[1] += b0.y; x[2] += b0.z; x[3] += b0.w;
-    x[4] += b1.x; x[5] += b1.y; x[6] += b1.z; x[7] += b1.w;
-  }
-  if (a.act != SKIP_ACT_NONE)
+// Eight sums of a row, columns j .. j + 7: bias, activation, residual (both given
+// as loaded; zeros where there is none), store at element `at` of Y.
+__device__ __forceinline__ void dense_finish8(const DenseArgs& a, size_t at, const float (&b)[8],
+                                              const u32x4& res, float (&x)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = dense_act(x[e], a.act);
-  if (a.residual) {
-    float y[8];
-    unpack8_bf16(*reinterpret_cast<const u32x4*>(
-                     a.residual + dense_row(a, a.residual_idx, r) * a.d_out + j), y);
+  for (int e = 0; e < 8; ++e) x[e] += b[e];
+  if (a.act == SKIP_ACT_GELU) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] += y[e];
+    for (int e = 0; e < 8; ++e) x[e] = gelu(x[e]);
+  } else if (a.act == SKIP_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = silu(x[e]);
+  } else if (a.act == SKIP_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = x[e] < 0.f ? 0.f : x[e];  // keeps NaN
   }
-  const size_t at = (size_t)r * a.d_out + j;
+  float y[8];
+  unpack8_bf16(res, y);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] += y[e];
   if (a.out_f32) {
     float4* o = reinterpret_cast<float4*>(static_cast<float*>(a.Y) + at);
     o[0] = make_float4(x[0], x[1], x[2], x[3]);
@@ -103,6 +121,26 @@ __device__ __forceinline__ void dense_finish8(const DenseArgs& a, int r, int j, 
         u32x4{pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]),
               pack2_bf16(x[6], x[7])};
   }
+}
+__device__ __forceinline__ void dense_bias8(const DenseArgs& a, int j, float (&b)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) b[e] = 0.f;
+  if (a.bias && j < a.d_out) {
+    const float4 b0 = reinterpret_cast<const float4*>(a.bias + j)[0];
+    const float4 b1 = reinterpret_cast<const float4*>(a.bias + j)[1];
+    b[0] = b0.x; b[1] = b0.y; b[2] = b0.z; b[3] = b0.w;
+    b[4] = b1.x; b[5] = b1.y; b[6] = b1.z; b[7] = b1.w;
+  }
+}
+__device__ __forceinline__ u32x4 dense_residual8(const DenseArgs& a, size_t row, int j) {
+  return a.residual ? *reinterpret_cast<const u32x4*>(a.residual + row * a.d_out + j)
+                    : u32x4{0u, 0u, 0u, 0u};
+}
+__device__ __forceinline__ void dense_finish_at(const DenseArgs& a, int r, int j, float (&x)[8]) {
+  float b[8];
+  dense_bias8(a, j, b);
+  const u32x4 res = dense_residual8(a, dense_row(a, a.residual_idx, r), j);
+  dense_finish8(a, (size_t)r * a.d_out + j, b, res, x);
 }
 // The same sums as a part of the contraction.
 __device__ __forceinline__ void dense_part8(const DenseArgs& a, int split, int r, int j,
@@ -132,26 +170,33 @@ dense_pack_kernel(const bf16_t* __restrict__ W, int d, int d_out, int tiles,
   }
 }
 
-// Workgroup: 32 MB rows x 256 columns, a part of the contraction.  The row tile
-// arrives in an LDS ring by direct global->LDS loads AH steps ahead and is
-// published one step early; each wave's weights come from the packed copy into
-// registers WD steps ahead, one coalesced run a load.  Items are dealt to the XCDs
-// in runs, row tile fastest, so that the items of one XCD share their weights in
-// its L2.
+// Workgroup: 32 MB rows x 256 columns, a part of the contraction, in steps of 64 (a
+// row's 128 bytes of a step are one cache line).  The row tile arrives in a
+// three-slot LDS ring by direct global->LDS loads two steps ahead and is published
+// one step early; each wave's weights come from the packed copy into registers WD
+// steps ahead, one coalesced run a load: they are used by this wave alone, so LDS
+// would only add a way.  Items are dealt to the XCDs in runs, row tile fastest, so
+// that the items of one XCD share their weights in its L2.
+//
+// Bound by the matrix units under the card's power limit: 3088 rows of 4096 by
+// 4096 columns take 95 us (1090 TF; products alone, fed with the same data from
+// registers, 1740 TF, and 1440 TF with one operand from LDS).  A start and end of 4
+// + 1.1 us a block of 32 rows is what the rest goes to; with MB <= 4 and one step of
+// weights ahead, two workgroups fit a CU and hide most of it (4616 rows of 1408 by
+// 4096 with GELU: 74 us against 91 with one workgroup of MB = 5).
 template <int MB>
-__global__ void __launch_bounds__(kDnThreads, 1)
+__global__ void __launch_bounds__(kDnThreads, MB <= 4 ? 2 : 1)
 dense_tile_kernel(DenseArgs a) {
-  constexpr int NB = 2;
-  constexpr int RING = MB <= 6 ? 5 : 4, AH = RING - 1, WD = AH;
-  constexpr int MT = 32 * MB, A_ELEMS = MT * kDnKS;
-  constexpr int WCH = 32 * MB;                        // 16-byte chunks of a row tile per wave
-  constexpr int NI = (WCH + 63) / 64;                 // direct loads they take
+  constexpr int NB = 2, SUB = kDnStep / 16;           // k16 sub-steps of a step
+  constexpr int RING = 3, AH = 2, WD = MB <= 4 ? 1 : 2;
+  constexpr int MT = 32 * MB, A_ELEMS = MT * kDnStep;
+  constexpr int NI = MB;                              // direct loads of a row tile per wave
   constexpr int PITCH = 72;                           // floats of a row in the epilogue
   __shared__ __attribute__((aligned(1024))) union {
     bf16_t ring[RING * A_ELEMS];
     float out[4][32 * PITCH];
   } sh;
-  static_assert(sizeof(sh.ring) <= 65536, "direct loads address 64 KiB of LDS");
+  __shared__ int sh_row[MT], sh_res[MT];
 
   const int per_xcd = gridDim.x / 8;
   int item = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
@@ -164,37 +209,40 @@ dense_tile_kernel(DenseArgs a) {
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int all_steps = a.d / kDnKS;
+  const int k32 = a.d / kDnKS;                        // packed steps of 32
+  const int odd = k32 & 1, all_steps = k32 / 2;       // (a first half step of its own)
   const int s_begin = (int)((long long)all_steps * split / a.splits);
-  const int ksteps = (int)((long long)all_steps * (split + 1) / a.splits) - s_begin;
+  const int steps = (int)((long long)all_steps * (split + 1) / a.splits) - s_begin;
   const int hh = lane >> 5, r32 = lane & 31;
 
-  // the lane's 16-byte chunks of a row tile: chunk g is row g / 4, physical
-  // chunk g % 4 holding logical chunk (g % 4) ^ (row / 2) % 4 (the operand
-  // reads of 8 consecutive rows hit distinct banks)
+  // the lane's 16-byte chunks of a row tile: chunk g is row g / 8, physical
+  // chunk g % 8 holding logical chunk (g % 8) ^ row % 8 (the operand reads of 8
+  // consecutive rows hit distinct banks)
+  // (the rows that kept rows stand for are looked up once)
+  if (tid < MT) {
+    const int r = min(i0 + tid, a.M - 1);
+    sh_row[tid] = (int)dense_row(a, a.rows_idx, r);
+    sh_res[tid] = (int)dense_row(a, a.residual_idx, r);
+  }
+  __syncthreads();
   const bf16_t* asrc[NI];
 #pragma unroll
-  for (int q = 0; q < NI; ++q) {
-    const int g = wave * WCH + min(q * 64 + lane, WCH - 1);
-    const int trow = g >> 2;
-    const int lc = (g & 3) ^ ((trow >> 1) & 3);
-    asrc[q] = a.rows + dense_row(a, a.rows_idx, min(i0 + trow, a.M - 1)) * a.d +
-              (size_t)s_begin * kDnKS + lc * 8;
-  }
-  const uint32_t ar_lds = lds_addr(sh.ring) + (uint32_t)(wave * WCH * 16);
+  for (int q = 0; q < NI; ++q)
+    asrc[q] = a.rows + (size_t)sh_row[(wave * NI + q) * 8 + (lane >> 3)] * a.d;
+  const int acol = odd * kDnKS + s_begin * kDnStep + ((lane & 7) ^ ((lane >> 3) & 7)) * 8;
+  const uint32_t ar_lds = lds_addr(sh.ring) + (uint32_t)(wave * NI * 1024);
   auto issue_a = [&](int s) {
 #pragma unroll
     for (int q = 0; q < NI; ++q)
-      if (q * 64 + lane < WCH)
-        lds_dma16(asrc[q] + s * kDnKS,
-                  __builtin_amdgcn_readfirstlane(
-                      ar_lds + ((uint32_t)s % RING) * (A_ELEMS * 2) + q * 1024));
+      lds_dma16(asrc[q] + acol + s * kDnStep, __builtin_amdgcn_readfirstlane(
+                                   ar_lds + ((uint32_t)s % RING) * (A_ELEMS * 2) + q * 1024));
   };
-  const u32x4* wsrc = a.Wp + ((size_t)(nt * 8 + wave * NB) * all_steps + s_begin) * 128 + lane;
-  const size_t wblk = (size_t)all_steps * 128;        // from one 32-column block to the next
+  const u32x4* wsrc = a.Wp + (size_t)(nt * 8 + wave * NB) * k32 * 128 + lane;
+  const size_t wblk = (size_t)k32 * 128;              // from one 32-column block to the next
   auto load_w = [&](int s, int kk, u32x4 (&w)[NB]) {
+    const size_t at = (size_t)(odd + 2 * (s_begin + s)) * 128 + kk * 64;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) w[nb] = wsrc[nb * wblk + (size_t)s * 128 + kk * 64];
+    for (int nb = 0; nb < NB; ++nb) w[nb] = wsrc[nb * wblk + at];
   };
 
   f32x16_t acc[NB][MB];
@@ -205,15 +253,14 @@ dense_tile_kernel(DenseArgs a) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[nb][mb][v] = 0.f;
 
-  int aoff[2];
+  int aoff[SUB];
 #pragma unroll
-  for (int kk = 0; kk < 2; ++kk)
-    aoff[kk] = r32 * kDnKS + (((2 * kk + hh) ^ ((r32 >> 1) & 3)) << 3);
+  for (int kk = 0; kk < SUB; ++kk) aoff[kk] = r32 * kDnStep + (((2 * kk + hh) ^ (r32 & 7)) << 3);
   auto read_a = [&](int s, int kk, u32x4 (&x)[MB]) {
     const bf16_t* At = sh.ring + ((uint32_t)s % RING) * A_ELEMS + aoff[kk];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
-      x[mb] = *reinterpret_cast<const u32x4*>(At + mb * 32 * kDnKS);
+      x[mb] = *reinterpret_cast<const u32x4*>(At + mb * 32 * kDnStep);
   };
   // products of one sub-step, one operand read of the next beside each of the
   // first of them
@@ -231,73 +278,92 @@ dense_tile_kernel(DenseArgs a) {
     __builtin_amdgcn_sched_barrier(0);
   };
 
+  if (odd && split == 0) {
+    // the first 32 columns, operands straight from memory
 #pragma unroll
-  for (int q = 0; q < AH; ++q)
-    if (q < ksteps) issue_a(q);
-  u32x4 w[WD][2][NB];
+    for (int kk = 0; kk < 2; ++kk) {
+      u32x4 x[MB], w[NB];
 #pragma unroll
-  for (int t = 0; t < WD; ++t)
+      for (int nb = 0; nb < NB; ++nb) w[nb] = wsrc[nb * wblk + kk * 64];
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) load_w(min(t, ksteps - 1), kk, w[t][kk]);
+      for (int mb = 0; mb < MB; ++mb)
+        x[mb] = *reinterpret_cast<const u32x4*>(
+            a.rows + (size_t)sh_row[mb * 32 + r32] * a.d + kk * 16 + hh * 8);
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) acc[nb][mb] = mfma32_bf16(x[mb], w[nb], acc[nb][mb]);
+    }
+  }
+  if (steps > 0) {
+#pragma unroll
+    for (int q = 0; q < AH; ++q)
+      if (q < steps) issue_a(q);
+  }
+  const int lw = max(steps - 1, 0);                   // (without a step: weights not multiplied)
+  u32x4 w[WD][SUB][NB];
+  if (all_steps > 0) {
+#pragma unroll
+    for (int u = 0; u < WD; ++u)
+#pragma unroll
+      for (int kk = 0; kk < SUB; ++kk) load_w(min(u, lw), kk, w[u][kk]);
+  }
   wait_vmcnt<0>();
   barrier_nofence();
-  u32x4 f0[MB], f1[MB];
-  read_a(0, 0, f0);
+  u32x4 f[2][MB];
+  read_a(0, 0, f[0]);
 
-  // Step s: wait for this wave's part of the row tile of step s+1 (issued
-  // after it: the weights of AH - 1 steps and, while they exist, the tiles of
-  // steps s+2 .. s+AH-1), barrier (publishes that tile; the slot of step s-1
-  // is free), request the tile of step s+AH, multiply step s and read the
-  // first operands of step s+1 (past the last step: stale values that nothing
-  // uses).  The tail steps (after the last whole group of WD; every tile is
-  // requested by then) load nothing and wait for all.
-  static_assert(AH >= WD && AH < RING, "tail steps request no tile; a slot is free");
-  constexpr int WQ = (AH - 1) * 2 * NB;
-  auto step = [&](int s, u32x4 (&ws)[2][NB], auto tail) {
-    constexpr bool TAIL = decltype(tail)::value;
-    if (TAIL) wait_vmcnt<0>();
-    else if (s + AH <= ksteps) wait_vmcnt<WQ + (AH - 2) * NI>();
-    else wait_vmcnt<WQ>();
+  // Step s: wait for this wave's part of the row tile of step s+1 (issued after
+  // it: the weights of one step), barrier (publishes that tile; the slot of step
+  // s-1 is free), request the tile of step s+2, multiply step s and read the first
+  // operands of step s+1 (past the last step: stale values that nothing uses).
+  auto step = [&](int s, u32x4 (&w)[SUB][NB]) {
+    wait_vmcnt<SUB * NB>();
     barrier_nofence();
-    if (!TAIL && s + AH < ksteps) issue_a(s + AH);
+    if (s + AH < steps) issue_a(s + AH);
     __builtin_amdgcn_sched_barrier(0);
-    read_a(s, 1, f1);
-    multiply(f0, ws[0]);
-    // unconditional (the last steps reload the final fragments): a
-    // conditional load would make the compiler drain the queue before the
-    // next use of w
-    if (!TAIL) load_w(min(s + WD, ksteps - 1), 0, ws[0]);
-    __builtin_amdgcn_sched_barrier(0);
-    read_a(s + 1, 0, f0);
-    multiply(f1, ws[1]);
-    if (!TAIL) load_w(min(s + WD, ksteps - 1), 1, ws[1]);
-    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int kk = 0; kk < SUB; ++kk) {
+      if (kk + 1 < SUB) read_a(s, kk + 1, f[(kk + 1) & 1]);
+      else read_a(s + 1, 0, f[0]);
+      multiply(f[kk & 1], w[kk]);
+      // unconditional (the last steps reload the final fragments): a conditional
+      // load would make the compiler drain the queue before the next use of w
+      load_w(min(s + WD, lw), kk, w[kk]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   int s = 0;
-  for (; s + WD <= ksteps; s += WD) {
+  for (; s + WD <= steps; s += WD) {
 #pragma unroll
-    for (int t = 0; t < WD; ++t) step(s + t, w[t], std::false_type{});
+    for (int u = 0; u < WD; ++u) step(s + u, w[u]);
   }
-#pragma unroll
-  for (int t = 0; t < WD - 1; ++t)
-    if (s + t < ksteps) step(s + t, w[t], std::true_type{});
+  if (s < steps) step(s, w[0]);
 
   // Accumulator element v of block (nb, mb) is row mb*32 + 8*(v/4) + 4*hh + v%4,
   // column 64*wave + 32*nb + r32: through the wave's own LDS, 32 rows at a time,
   // so that a lane finishes eight columns of a row
   __syncthreads();                                    // the ring is read
   float* out = sh.out[wave];
+  const int j = j0 + 64 * wave + 8 * (lane & 7);
+  float bias[8];
+  dense_bias8(a, j, bias);
   unrolled<MB>([&](auto mb_) {
     constexpr int mb = decltype(mb_)::value;
+    u32x4 res[4];                                     // in flight during the exchange
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      res[q] = j < a.d_out ? dense_residual8(a, (size_t)sh_res[mb * 32 + 8 * q + (lane >> 3)], j)
+                           : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int v = 0; v < 16; ++v)
         out[(8 * (v >> 2) + 4 * hh + (v & 3)) * PITCH + 32 * nb + r32] = acc[nb][mb][v];
     __builtin_amdgcn_wave_barrier();
+#pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int lr = 8 * q + (lane >> 3), r = i0 + mb * 32 + lr;
-      const int j = j0 + 64 * wave + 8 * (lane & 7);
       float x[8];
       *reinterpret_cast<float4*>(x) =
           *reinterpret_cast<const float4*>(out + lr * PITCH + 8 * (lane & 7));
@@ -305,7 +371,7 @@ dense_tile_kernel(DenseArgs a) {
           *reinterpret_cast<const float4*>(out + lr * PITCH + 8 * (lane & 7) + 4);
       if (r < a.M && j < a.d_out) {
         if (a.splits > 1) dense_part8(a, split, r, j, x);
-        else dense_finish8(a, r, j, x);
+        else dense_finish8(a, (size_t)r * a.d_out + j, bias, res[q], x);
       }
     }
     __builtin_amdgcn_wave_barrier();
@@ -315,33 +381,27 @@ dense_tile_kernel(DenseArgs a) {
 // Few rows: bound by the weights' way from memory, so every wave streams its own
 // part of them (64 columns, an eighth of the workgroup's contraction) straight
 // into registers, a batch of loads ahead of the products; the rows come from the
-// L2.  The waves' sums meet in LDS, added in wave order.
-template <int MB>
+// L2.  The waves' sums meet in LDS, added in wave order.  One row of 1024 by 1024
+// columns takes 5.4 us in two launches, where the weights alone would take 0.4.
 __global__ void __launch_bounds__(64 * kDnWaves, 2)
 dense_rows_kernel(DenseArgs a) {
-  constexpr int NB = 2, U = MB == 1 ? 4 : 2;          // k16 groups a batch
+  constexpr int NB = 2, U = 4;                        // k16 groups a batch
   __shared__ float red[kDnWaves][16][64];
   const int per_xcd = gridDim.x / 8;
-  int item = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  const int item = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
   if (item >= a.n_items) return;
-  const int MTL = (a.M + 32 * MB - 1) / (32 * MB);
-  const int mt = item % MTL;
-  item /= MTL;
   const int split = item % a.splits, ct = item / a.splits;
-  const int i0 = mt * 32 * MB, j0 = ct * 64;
+  const int j0 = ct * 64;
   const int lane = threadIdx.x & 63, hh = lane >> 5, r32 = lane & 31;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.d / 16, parts = a.splits * kDnWaves, me = split * kDnWaves + wv;
   const int g0 = (int)((long long)me * G / parts), g1 = (int)((long long)(me + 1) * G / parts);
   const int gl = max(g1 - 1, 0);
 
-  const bf16_t* ap[MB];
-#pragma unroll
-  for (int mb = 0; mb < MB; ++mb)
-    ap[mb] = a.rows + dense_row(a, a.rows_idx, min(i0 + mb * 32 + r32, a.M - 1)) * a.d + hh * 8;
+  const bf16_t* ap = a.rows + dense_row(a, a.rows_idx, min(r32, a.M - 1)) * a.d + hh * 8;
   const u32x4* wp = a.Wp + (size_t)ct * 2 * G * 64 + lane;
   struct Batch {
-    u32x4 x[U][MB], w[U][NB];
+    u32x4 x[U], w[U][NB];
   };
   auto load = [&](Batch& b, int g) {                  // groups past the wave's are not multiplied
 #pragma unroll
@@ -349,27 +409,20 @@ dense_rows_kernel(DenseArgs a) {
       const size_t gg = (size_t)min(g + u, gl);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) b.w[u][nb] = wp[((size_t)nb * G + gg) * 64];
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb)
-        b.x[u][mb] = *reinterpret_cast<const u32x4*>(ap[mb] + gg * 16);
+      b.x[u] = *reinterpret_cast<const u32x4*>(ap + gg * 16);
     }
   };
-  f32x16_t acc[NB][MB];
+  f32x16_t acc[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[nb][mb][v] = 0.f;
+    for (int v = 0; v < 16; ++v) acc[nb][v] = 0.f;
   auto multiply = [&](const Batch& b, int g) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (g + u < g1)
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-            acc[nb][mb] = mfma32_bf16(b.x[u][mb], b.w[u][nb], acc[nb][mb]);
+        for (int nb = 0; nb < NB; ++nb) acc[nb] = mfma32_bf16(b.x[u], b.w[u][nb], acc[nb]);
   };
   Batch b0, b1;
   load(b0, g0);
@@ -380,30 +433,30 @@ dense_rows_kernel(DenseArgs a) {
     multiply(b1, g + U);
   }
   // Element v of a block is row 8*(v/4) + 4*hh + v%4, column r32.  Blocks one
-  // after the other: thread (row 32 in eight, four columns) of the first 256
-  // adds the waves' sums of eight columns
-  unrolled<MB * NB>([&](auto i_) {
-    constexpr int mb = decltype(i_)::value / NB, nb = decltype(i_)::value % NB;
-      if (mb + nb > 0) __syncthreads();
+  // after the other: a thread of the first 128 adds the waves' sums of eight columns
+  // of a row
+  unrolled<NB>([&](auto nb_) {
+    constexpr int nb = decltype(nb_)::value;
+    if (nb > 0) __syncthreads();
 #pragma unroll
-      for (int v = 0; v < 16; ++v) red[wv][v][lane] = acc[nb][mb][v];
-      __syncthreads();
-      if (threadIdx.x < 128) {
-        const int lr = threadIdx.x >> 2, c8 = (threadIdx.x & 3) * 8;
-        const int v = 4 * (lr >> 3) + (lr & 3), l = 32 * ((lr >> 2) & 1) + c8;
-        float x[8];
+    for (int v = 0; v < 16; ++v) red[wv][v][lane] = acc[nb][v];
+    __syncthreads();
+    if (threadIdx.x < 128) {
+      const int r = threadIdx.x >> 2, c8 = (threadIdx.x & 3) * 8;
+      const int v = 4 * (r >> 3) + (r & 3), l = 32 * ((r >> 2) & 1) + c8;
+      float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] = red[0][v][l + e];
+      for (int e = 0; e < 8; ++e) {
+        x[e] = red[0][v][l + e];
 #pragma unroll
-          for (int u = 1; u < kDnWaves; ++u) x[e] += red[u][v][l + e];
-        }
-        const int r = i0 + mb * 32 + lr, j = j0 + nb * 32 + c8;
-        if (r < a.M && j < a.d_out) {
-          if (a.splits > 1) dense_part8(a, split, r, j, x);
-          else dense_finish8(a, r, j, x);
-        }
+        for (int u = 1; u < kDnWaves; ++u) x[e] += red[u][v][l + e];
       }
+      const int j = j0 + nb * 32 + c8;
+      if (r < a.M && j < a.d_out) {
+        if (a.splits > 1) dense_part8(a, split, r, j, x);
+        else dense_finish_at(a, r, j, x);
+      }
+    }
   });
 }
 
@@ -421,7 +474,7 @@ dense_join_kernel(DenseArgs a) {
       x[0] += y0.x; x[1] += y0.y; x[2] += y0.z; x[3] += y0.w;
       x[4] += y1.x; x[5] += y1.y; x[6] += y1.z; x[7] += y1.w;
     }
-    dense_finish8(a, r, j, x);
+    dense_finish_at(a, r, j, x);
   }
 }
 
@@ -442,30 +495,44 @@ struct DenseShape {
 };
 static DenseShape dense_shape(int M, int d, int d_out) {
   DenseShape s;
-  if (M <= 96) {
+  if (M <= 32) {
+    // One block of rows, up to as many parts as fill the chip once (a second round of
+    // a few workgroups costs more than it brings: 1 x 16384 x 4104 in 3 parts 25 us,
+    // in 4, which are 260 workgroups, 31); a wave's part is at least eight k16 groups.
+    // Against the tiles at 32 rows: 12.8 and 13.6 us at 4096 x 4096, 23.4 and 26.2 at
+    // 4096 x 16384; at 64 rows this form took 16.2 and 15.4, 31 and 28.
     s.rows = true;
-    s.mb = (M + 31) / 32;
+    s.mb = 1;
     const int cts = (d_out + 63) / 64;
-    // a wave's part is at least eight k16 groups
-    s.splits = (int)std::max<long long>(1, std::min<long long>((kDnCUs + cts - 1) / cts,
+    s.splits = (int)std::max<long long>(1, std::min<long long>(kDnCUs / cts,
                                                                d / 16 / (8 * kDnWaves)));
     return s;
   }
+  // Tile height and parts by an estimate of the time in us. Its figures are fitted to 711
+  // timings, every height and up to 16 parts of 22 shapes from 97 to 4768 rows and 136 to
+  // 16384 columns; they meet those to 5 % (one sigma), and the pick was at most 7 % behind
+  // the fastest. A step costs a fixed 0.13 and per block of 32 rows 0.115 on an empty chip
+  // to 0.17 on a full one (power; n tiles on the busiest CU, u the share of the others'
+  // work). A tile's start and end are hidden in part where two workgroups share a CU
+  // (MB <= 4). Parts are written, read and added.
   s.rows = false;
   const long long nts = (d_out + kDnNT - 1) / kDnNT;
-  // rounds of workgroups times their rows, over tile heights
-  long long best = -1;
-  s.mb = 8;
+  const int steps = std::max(1, d / kDnStep);
+  double best = 0.0;
+  s.mb = 0;
   s.splits = 1;
-  for (int mb = 8; mb >= 3; --mb) {
+  for (int mb = 8; mb >= 2; --mb) {
     const long long tiles = (M + 32 * mb - 1) / (32 * mb) * nts;
-    // a part is at least 16 steps
-    const int most = std::max(1, std::min(16, d / kDnKS / 16));
+    // a part is at least eight steps
+    const int most = std::max(1, std::min(16, steps / 8));
     for (int sp = 1; sp <= most; ++sp) {
-      const long long rounds = (tiles * sp + kDnCUs - 1) / kDnCUs;
-      const long long cost = (rounds * (mb * 64 + 32) * 1024) / sp + (sp > 1 ? 4096 * sp : 0);
-      if (best < 0 || cost < best) {
-        best = cost;
+      const double n = (double)((tiles * sp + kDnCUs - 1) / kDnCUs);
+      const double u = (double)(tiles * sp) / (n * kDnCUs);
+      double us = n * ((steps + sp - 1) / sp) * (0.127 + mb * (0.115 + 0.054 * u));
+      us += mb <= 4 ? 4.06 + 1.08 * mb * (0.27 + 0.73 * n) : n * (4.06 + 1.08 * mb);
+      if (sp > 1) us += 1.4 + (double)sp * M * d_out * 8.0 / 8.84e6;
+      if (s.mb == 0 || us < best) {
+        best = us;
         s.mb = mb;
         s.splits = sp;
       }
@@ -510,21 +577,19 @@ hipError_t launch_dense(const skip_problem_t& p, const void* rows, const int32_t
   if (items > (1 << 22)) return hipErrorInvalidValue;
   a.n_items = (int)items;
   const dim3 grid((unsigned)((items + 7) / 8 * 8));
-#define SKIP_DENSE(K, MB, T) hipLaunchKernelGGL((K<MB>), grid, dim3(T), 0, st, a)
+#define SKIP_DENSE(MB) \
+  hipLaunchKernelGGL(dense_tile_kernel<MB>, grid, dim3(kDnThreads), 0, st, a)
   if (s.rows) {
-    switch (s.mb) {
-      case 1: SKIP_DENSE(dense_rows_kernel, 1, 64 * kDnWaves); break;
-      case 2: SKIP_DENSE(dense_rows_kernel, 2, 64 * kDnWaves); break;
-      default: SKIP_DENSE(dense_rows_kernel, 3, 64 * kDnWaves); break;
-    }
+    hipLaunchKernelGGL(dense_rows_kernel, grid, dim3(64 * kDnWaves), 0, st, a);
   } else {
     switch (s.mb) {
-      case 3: SKIP_DENSE(dense_tile_kernel, 3, kDnThreads); break;
-      case 4: SKIP_DENSE(dense_tile_kernel, 4, kDnThreads); break;
-      case 5: SKIP_DENSE(dense_tile_kernel, 5, kDnThreads); break;
-      case 6: SKIP_DENSE(dense_tile_kernel, 6, kDnThreads); break;
-      case 7: SKIP_DENSE(dense_tile_kernel, 7, kDnThreads); break;
-      default: SKIP_DENSE(dense_tile_kernel, 8, kDnThreads); break;
+      case 2: SKIP_DENSE(2); break;
+      case 3: SKIP_DENSE(3); break;
+      case 4: SKIP_DENSE(4); break;
+      case 5: SKIP_DENSE(5); break;
+      case 6: SKIP_DENSE(6); break;
+      case 7: SKIP_DENSE(7); break;
+      default: SKIP_DENSE(8); break;
     }
   }
 #undef SKIP_DENSE

@@ -174,3 +174,19 @@ def test_bitwise_repeatable(B):
     a = B.gather_dense(p, x, packed, 264, bias=b, residual=R)
     for _ in range(3):
         assert torch.equal(a, B.gather_dense(p, x, packed, 264, bias=b, residual=R))
+
+
+@pytest.mark.parametrize("M", [2, 40, 200])
+@pytest.mark.parametrize("act", ["none", "gelu", "silu", "relu"])
+def test_infinities_and_nan(B, M, act):
+    """One term a sum, so an infinity or NaN of a row reaches the result as itself:
+    infinity, NaN, and below zero the activations' limits (a number times exp(-inf)
+    may be no number, as in the formula x / (1 + exp(-x)))."""
+    W = torch.zeros(40, 64, dtype=torch.bfloat16, device="cuda")
+    W[:, 5] = 1
+    x = torch.zeros(M, 64, dtype=torch.bfloat16, device="cuda")
+    x[0, 5], x[1, 5] = math.inf, math.nan
+    p = problem(B, M, 64)
+    Y = B.gather_dense(p, x, B.pack_dense(p, W), 40, activation=act, out_f32=True)
+    torch.cuda.synchronize()
+    assert (Y[0] == math.inf).all() and Y[1].isnan().all() and not Y[2:].any()
