@@ -109,14 +109,17 @@ struct QuantAttnArgs {
   const int32_t* query_passages;
   const int32_t* passage_offsets;
   const int32_t* passage_blocks;
-  const uint64_t* rowmask;
+  const uint64_t* rowmask;          // neighbours of each kept row, or
+  const int32_t* edge_rowptr;       // a given graph
+  const int32_t* edge_col;
   const uint8_t* store;
   void* O;
   float* lse;
   float* part;                      // partials of split items
   long long n_blocks;
-  int N, H, heads_kv, G, groups, chunks, splits, rows_chunk;   // rows_chunk: kept rows an item
-  int total_kept, total_passages, total_tokens, k_max, P_max, o_f32;
+  int B, N, H, heads_kv, G, groups, chunks, splits, rows_chunk;   // rows_chunk: kept rows an item
+  int ranked;                       // question_of_rank
+  int total_kept, total_passages, total_tokens, total_edges, k_max, P_max, o_f32;
   float scale_log2;
 };
 
@@ -131,8 +134,31 @@ struct QuantItem {
   int k0, i0, nk;                   // the question's first kept row; the item's rows i0 .. + nk - 1
   int p0, P;
 };
+// Batches of at most 64 questions whose items differ start with the questions of
+// the longest items (rows x tokens of an item; ties: lower index), so that the last
+// round of workgroups is a short one: lane b ranks question b.  24 questions of
+// mixed sizes, 616 items on 256 CUs: the call 168 us in order, 164 by rank.
+__device__ __forceinline__ int question_of_rank(const QuantAttnArgs& a, int r) {
+  const int b = min((int)__lane_id(), a.B - 1);
+  int k0, k1, p0, p1;
+  range_of(a.kept_offsets, b, a.total_kept, k0, k1);
+  range_of(a.query_passages, b, a.total_passages, p0, p1);
+  const int kq = min(k1 - k0, a.k_max), nch = (kq + a.rows_chunk - 1) / a.rows_chunk;
+  const int rpc = nch > 0 ? (kq + nch - 1) / nch : 0;
+  const int tok = clampi(a.passage_offsets[p1], 0, a.total_tokens) -
+                  clampi(a.passage_offsets[p0], 0, a.total_tokens);
+  const float cost = (float)rpc * (float)tok;     // (an order only)
+  int rank = 0;
+  for (int c = 0; c < a.B; ++c) {
+    const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(cost), c));
+    rank += (other > cost || (other == cost && c < b)) ? 1 : 0;
+  }
+  const uint64_t at = __ballot(rank == r && (int)__lane_id() < a.B);
+  return __builtin_amdgcn_readfirstlane(at ? __builtin_ctzll(at) : 0);
+}
 // Chunks and splits of a (question, key head) follow one another on one XCD
 // (workgroup id L goes to XCD L % 8), whose L2 then holds its passages once.
+template <bool RANKED = false>
 __device__ __forceinline__ bool quant_item(const QuantAttnArgs& a, int L, QuantItem& x) {
   const int per = a.chunks * a.splits;
   const int grp = (L & 7) + 8 * ((L >> 3) / per);
@@ -142,6 +168,7 @@ __device__ __forceinline__ bool quant_item(const QuantAttnArgs& a, int L, QuantI
   x.split = sub % a.splits;
   x.b = grp / a.heads_kv;
   x.hk = grp % a.heads_kv;
+  if (RANKED && a.ranked) x.b = question_of_rank(a, x.b);
   int k1, p1;
   range_of(a.kept_offsets, x.b, a.total_kept, x.k0, k1);
   range_of(a.query_passages, x.b, a.total_passages, x.p0, p1);
@@ -153,6 +180,26 @@ __device__ __forceinline__ bool quant_item(const QuantAttnArgs& a, int L, QuantI
   x.i0 = x.chunk * rpc;
   x.nk = min(kq, x.i0 + rpc) - x.i0;
   return x.nk > 0;
+}
+
+// Passages adjacent to a kept row, a bit each (of a given graph here, which saves
+// the launch that would write them: 2 us of 10 for one row).
+__device__ __forceinline__ uint64_t row_neighbours(const QuantAttnArgs& a, int row, int P) {
+  const uint64_t all = P < 64 ? (1ull << P) - 1ull : ~0ull;
+  if (!a.edge_rowptr) return a.rowmask[row] & all;
+  int e0, e1;
+  range_of(a.edge_rowptr, row, a.total_edges, e0, e1);
+  uint64_t m = 0;
+  constexpr int U = 8;                       // columns in flight
+  for (int e = e0; e < e1; e += U) {
+    int j[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) j[u] = a.edge_col[min(e + u, e1 - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (j[u] >= 0 && j[u] < P) m |= 1ull << j[u];
+  }
+  return m;
 }
 
 // A tile of 64 tokens: two records of a passage, as a lane holds them.
@@ -232,6 +279,8 @@ struct QuantTile {
           for (int c = 0; c < PIECES; ++c) acc[fb] = mfma32_bf16(va, pc[c], acc[fb]);
         }
       });
+      // (the pieces of one product at a time in registers)
+      if (PIECES > 1) __builtin_amdgcn_sched_barrier(0);
     });
     return ls;
   }
@@ -327,12 +376,13 @@ attn_quant_kernel(QuantAttnArgs a) {
   constexpr int MW = (ROWS + 63) / 64;      // words of a row mask
   __shared__ __attribute__((aligned(16))) float Oacc[ROWS * D];
   __shared__ float m_acc[ROWS], l_acc[ROWS];
+  __shared__ uint64_t neighbours[ROWS];     // of the item's kept rows
   __shared__ uint8_t rowlist[kQMaxP][ROWS]; // virtual rows adjacent to each passage, ascending
   __shared__ int p_cnt[kQMaxP];
   __shared__ int merged;                    // units merged so far
 
   QuantItem it;
-  if (!quant_item(a, blockIdx.x, it)) return;
+  if (!quant_item<true>(a, blockIdx.x, it)) return;
   const int G = a.G, nv = it.nk * G, P = it.P;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -348,12 +398,7 @@ attn_quant_kernel(QuantAttnArgs a) {
     my_len = te - ts;
     my_blk = a.passage_blocks[it.p0 + lane];
   }
-  uint64_t mk[MW];
-#pragma unroll
-  for (int w = 0; w < MW; ++w) {
-    const int v = 64 * w + lane;
-    mk[w] = v < nv ? a.rowmask[it.k0 + it.i0 + over_G(v)] : 0ull;
-  }
+  if (tid < it.nk) neighbours[tid] = row_neighbours(a, it.k0 + it.i0 + tid, P);
   for (int i = tid; i < nv * NC4; i += kQThreads)
     reinterpret_cast<float4*>(Oacc)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = tid; i < nv; i += kQThreads) {
@@ -361,7 +406,14 @@ attn_quant_kernel(QuantAttnArgs a) {
     l_acc[i] = 0.f;
   }
   if (tid == 0) merged = 0;
+  __syncthreads();
   // adjacent rows of each passage, every wave its share of the passages
+  uint64_t mk[MW];
+#pragma unroll
+  for (int w = 0; w < MW; ++w) {
+    const int v = 64 * w + lane;
+    mk[w] = v < nv ? neighbours[over_G(v)] : 0ull;
+  }
   const uint64_t below = (1ull << lane) - 1ull;
   for (int j = wave; j < P; j += kQWaves) {
     int cnt = 0;
@@ -602,7 +654,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
 
   // this lane's row (past the item's rows: its last one, adjacent to nothing)
   const int v = min(n, nv - 1), i = v / G, hq = it.hk * G + (v - i * G);
-  uint64_t mk = a.rowmask[it.k0 + it.i0 + i];
+  uint64_t mk = row_neighbours(a, it.k0 + it.i0 + i, P);
   // lane j: passage j
   int my_len = 0, my_blk = 0;
   if (lane < P) {
@@ -857,8 +909,8 @@ size_t quant_attn_scratch(const skip_problem_t& p, int heads_kv) {
 hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t& st,
                                   QuerySource q, const int32_t* kept_offsets,
                                   const int32_t* passage_offsets, const int32_t* passage_blocks,
-                                  const int32_t* query_passages, const uint64_t* rowmask,
-                                  void* O, float* lse, void* scratch, hipStream_t s) {
+                                  const int32_t* query_passages, QuantGraph graph, void* O,
+                                  float* lse, void* scratch, hipStream_t s) {
   const QuantShape sh = quant_shape(p, st.heads_kv);
   QuantAttnArgs a;
   a.q = static_cast<const bf16_t*>(q.base);
@@ -867,12 +919,16 @@ hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t
   a.query_passages = query_passages;
   a.passage_offsets = passage_offsets;
   a.passage_blocks = passage_blocks;
-  a.rowmask = rowmask;
+  a.rowmask = graph.rowmask;
+  a.edge_rowptr = graph.rowptr;
+  a.edge_col = graph.col;
+  a.total_edges = p.total_edges;
   a.store = static_cast<const uint8_t*>(st.data);
   a.O = O;
   a.lse = lse;
   a.part = static_cast<float*>(scratch);
   a.n_blocks = st.n_blocks;
+  a.B = p.B;
   a.N = q.N;
   a.H = p.H;
   a.heads_kv = st.heads_kv;
@@ -881,6 +937,10 @@ hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t
   a.chunks = sh.chunks;
   a.splits = sh.splits;
   a.rows_chunk = sh.rows_chunk;
+  // (questions of one size: total_kept and total_passages are B times the largest)
+  a.ranked = !sh.tile && p.B > 1 && p.B <= 64 &&
+             ((int64_t)p.total_kept < (int64_t)p.B * p.k_max ||
+              (int64_t)p.total_tokens < (int64_t)p.B * p.P_max * p.L_max);
   a.total_kept = p.total_kept;
   a.total_passages = p.total_passages;
   a.total_tokens = p.total_tokens;

@@ -649,17 +649,15 @@ skip_status_t skip_bipartite_xattn_quant(const skip_problem_t* p, const skip_kv_
     return SKIP_OK;
   }
   const QuerySource q{rows, kept_idx, p->N};
-  if (given) {
-    SKIP_TRY(launch_csr_to_mask(*p, kept_offsets, query_passages, edge_rowptr, edge_col,
-                                w.rowmask, s));
-  } else {
+  if (!given) {
     const QuerySource e = edge_rows ? QuerySource{edge_rows, nullptr, 0} : q;
     SKIP_TRY(launch_edge_dot(*p, e, kept_offsets, query_passages, nullptr, passage_keys, w.ep, s));
     SKIP_TRY(launch_edge_select(*p, w.ep, kept_offsets, query_passages, w.rowmask,
                                 edge_rowptr_out, edge_col_out, s, passage_keep));
   }
   SKIP_TRY(launch_attention_quant(*p, *store, q, kept_offsets, passage_offsets, passage_blocks,
-                                  query_passages, w.rowmask, O, lse, w.part, s));
+                                  query_passages, QuantGraph{w.rowmask, edge_rowptr, edge_col}, O,
+                                  lse, w.part, s));
   return SKIP_OK;
 }
 

@@ -180,11 +180,15 @@ hipError_t launch_store_read(const skip_problem_t& p, const skip_kv_store_t& st,
                              const int32_t* passage_offsets, const int32_t* passage_blocks,
                              void* Kh, void* Vh, hipStream_t s);
 bool quant_group_ok(int group);       // query heads of a key head that the attention takes
+struct QuantGraph {
+  const uint64_t* rowmask;            // neighbour masks of the kept rows, or
+  const int32_t *rowptr, *col;        // a given graph (rowptr not NULL)
+};
 size_t quant_attn_scratch(const skip_problem_t& p, int heads_kv);   // partials of split items
 hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t& st,
                                   QuerySource q, const int32_t* kept_offsets,
                                   const int32_t* passage_offsets, const int32_t* passage_blocks,
-                                  const int32_t* query_passages, const uint64_t* rowmask,
-                                  void* O, float* lse, void* scratch, hipStream_t s);
+                                  const int32_t* query_passages, QuantGraph graph, void* O,
+                                  float* lse, void* scratch, hipStream_t s);
 
 }  // namespace skip
