@@ -320,16 +320,30 @@ def _ptr(t: Optional[torch.Tensor], name: str, dtype=None, numel=None) -> Option
         raise ValueError(f"{name} must be contiguous")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if numel is not None and t.numel() < numel:
-        raise ValueError(f"{name} needs {numel} elements, has {t.numel()}")
-    if t.numel() and t.data_ptr() % 16:
+    n = t.numel()
+    if numel is not None and n < numel:
+        raise ValueError(f"{name} needs {numel} elements, has {n}")
+    if not n:
+        return None
+    ptr = t.data_ptr()
+    if ptr % 16:
         raise ValueError(f"{name} must be 16-byte aligned")
-    return t.data_ptr() if t.numel() else None
+    return ptr
+
+
+def _on_current_device(*tensors) -> None:
+    """Refuses tensors of another device than the current one, on whose stream the
+    kernels run."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != dev:
+            raise ValueError(f"a tensor is on device {t.get_device()}, the current one is {dev}")
 
 
 def _stream(stream) -> int:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # (with its index given, torch does not look the device up: 2.9 us otherwise)
+        stream = torch.cuda.current_stream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -603,7 +617,7 @@ def store_bytes(heads_kv: int, d_h: int, n_blocks: int) -> int:
 
 
 def _store_struct(p: SkipProblem, store: "KvStore") -> SkipKvStore:
-    need = store_bytes(store.heads_kv, p.d_h, store.n_blocks) if p.d_h in (64, 128) else None
+    need = store.n_blocks * store.heads_kv * 34 * p.d_h     # store_bytes
     return SkipKvStore(int(store.heads_kv), 0, int(store.n_blocks),
                        _ptr(store.data, "store.data", torch.uint8, need))
 
@@ -621,6 +635,7 @@ def skip_quantize_passages(p: SkipProblem, store: "KvStore", Kh, Vh, passage_off
     et = _elem_dtype(p)
     n = p.total_tokens * store.heads_kv * p.d_h
     s = _store_struct(p, store)
+    _on_current_device(store.data, Kh, Vh, passage_offsets, passage_blocks, keys_out)
     st = LIB.skip_quantize_passages(
         ctypes.byref(p), ctypes.byref(s), _ptr(Kh, "Kh", et, n), _ptr(Vh, "Vh", et, n),
         _ptr(passage_offsets, "passage_offsets", torch.int32, p.total_passages + 1),
@@ -634,6 +649,7 @@ def skip_dequantize_passages(p: SkipProblem, store: "KvStore", passage_offsets, 
     et = _elem_dtype(p)
     n = p.total_tokens * store.heads_kv * p.d_h
     s = _store_struct(p, store)
+    _on_current_device(store.data, Kh, Vh, passage_offsets, passage_blocks)
     st = LIB.skip_dequantize_passages(
         ctypes.byref(p), ctypes.byref(s),
         _ptr(passage_offsets, "passage_offsets", torch.int32, p.total_passages + 1),
@@ -650,6 +666,9 @@ def skip_bipartite_xattn_quant(p: SkipProblem, store: "KvStore", rows, kept_offs
                                stream=None):
     et = _elem_dtype(p)
     s = _store_struct(p, store)
+    _on_current_device(store.data, rows, kept_offsets, passage_offsets, passage_blocks,
+                       query_passages, O, lse, kept_idx, edge_rows, passage_keys, passage_keep,
+                       edge_rowptr, edge_col, edge_rowptr_out, edge_col_out, workspace)
     if workspace is None:
         workspace = _fresh_workspace(workspace_bytes_quant(p, store), kept_offsets.device, stream)
     n_rows = p.B * p.N if kept_idx is not None else p.total_kept
@@ -689,6 +708,7 @@ def workspace_bytes_dense(p: SkipProblem, d_out: int) -> int:
 
 def skip_pack_dense(p: SkipProblem, W, packed, stream=None):
     d_out = int(W.shape[0])
+    _on_current_device(W, packed)
     st = LIB.skip_pack_dense(ctypes.byref(p), _ptr(W, "W", _elem_dtype(p), d_out * p.d), d_out,
                              _ptr(packed, "packed", torch.uint8), packed.numel(), _stream(stream))
     _check(st, "skip_pack_dense")
@@ -699,17 +719,20 @@ def skip_gather_dense(p: SkipProblem, rows, kept_offsets, rows_idx, packed, d_ou
                       workspace=None, stream=None):
     et = _elem_dtype(p)
     d_out = int(d_out)
-    need = workspace_bytes_dense(p, d_out)
-    if workspace is None and need:
-        workspace = _fresh_workspace(need, packed.device, stream)
-    _ptr(packed, "packed", torch.uint8, packed_bytes_dense(p, d_out))
+    _on_current_device(rows, kept_offsets, rows_idx, packed, Y, bias, residual, residual_idx,
+                       workspace)
+    if workspace is None:
+        need = workspace_bytes_dense(p, d_out)
+        if need:
+            workspace = _fresh_workspace(need, packed.device, stream)
     n_rows = p.B * p.N if rows_idx is not None else p.total_kept
     n_res = p.B * p.N if residual_idx is not None else p.total_kept
     st = LIB.skip_gather_dense(
         ctypes.byref(p), _ptr(rows, "rows", et, n_rows * p.d),
         _ptr(kept_offsets, "kept_offsets", torch.int32, p.B + 1),
         _ptr(rows_idx, "rows_idx", torch.int32, p.total_kept),
-        _ptr(packed, "packed", torch.uint8), d_out, _ptr(bias, "bias", torch.float32, d_out),
+        _ptr(packed, "packed", torch.uint8, (d_out + 255) // 256 * 512 * p.d), d_out,
+        _ptr(bias, "bias", torch.float32, d_out),
         ACTIVATIONS[activation], _ptr(residual, "residual", et, n_res * d_out),
         _ptr(residual_idx, "residual_idx", torch.int32, p.total_kept),
         _ptr(Y, "Y", torch.float32 if out_f32 else et, p.total_kept * d_out),
