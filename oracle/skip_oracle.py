@@ -438,17 +438,17 @@ HELD_VALUES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
 
 def held_block(x):
     """What a block of values is held as: signed values of HELD_VALUES times one
-    power of two, the least 2^e with e in [-126, 127] and max|x| <= 7 * 2^e; every
-    value at its nearest, a tie at the value of even position.  Returns (codes
+    power of two, the least 2^e with e in [-126, 125] and max|x| <= 7 * 2^e (125 if
+    none); every value at its nearest, a tie at the value of even position.  Returns (codes
     with the sign in bit 3, e + 127, the values)."""
     x = np.asarray(x, dtype=np.float64)
     a = float(np.max(np.abs(x)))
     e = -126
-    while a > 7.0 * 2.0 ** e and e < 127:
+    while a > 7.0 * 2.0 ** e and e < 125:
         e += 1
     codes = []
     for v in x:
-        y = abs(float(v)) / 2.0 ** e
+        y = min(abs(float(v)) / 2.0 ** e, 7.0)      # (more only where e is the largest)
         best = 0
         for c in range(1, 8):
             d, d0 = abs(HELD_VALUES[c] - y), abs(HELD_VALUES[best] - y)

@@ -287,7 +287,7 @@ struct QuantTile {
 };
 
 // How softmax weights enter the second product.  Float output: three bf16 pieces.
-// bf16 output: one half float (11 bits: 2^-12 relative, an eighth of the output's
+// bf16 output: one half float (11 bits: 2^-11 relative, an eighth of the output's
 // own rounding; weights are at most 2^kQLazy) as long as the held values are half
 // floats, which saves a third of the matrix products and a seventh of the vector
 // instructions; a wave that meets a tile whose values are not goes over its tiles
@@ -357,7 +357,7 @@ struct QuantHead {
 template <int D>
 __device__ __forceinline__ void quant_store(const QuantAttnArgs& a, const QuantItem& it, int i,
                                             int head, int q, float4 o, float m, float l) {
-  const float inv = (l > 0.f) ? 1.f / l : 0.f;
+  const float inv = (l == 0.f) ? 0.f : 1.f / l;            // (keeps NaN)
   const size_t at = (size_t)(it.k0 + it.i0 + i) * a.H + head;
   if (a.o_f32)
     *reinterpret_cast<float4*>(static_cast<float*>(a.O) + at * D + q * 4) =
@@ -365,7 +365,7 @@ __device__ __forceinline__ void quant_store(const QuantAttnArgs& a, const QuantI
   else
     *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + at * D + q * 4) =
         make_uint2(pack2_bf16(o.x * inv, o.y * inv), pack2_bf16(o.z * inv, o.w * inv));
-  if (a.lse && q == 0) a.lse[at] = (l > 0.f) ? (m + log2f(l)) * kQLn2 : -INFINITY;
+  if (a.lse && q == 0) a.lse[at] = (l == 0.f) ? -INFINITY : (m + log2f(l)) * kQLn2;
 }
 
 template <int D, int ROWS, bool OUT_F32>
@@ -712,6 +712,20 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
     x.load_v(hh ? r1 : r0, n);
     asm volatile("" ::: "memory");           // (tiles in order: the counted waits go by it)
   };
+#pragma unroll
+  for (int e = 0; e < 4 * KH; ++e) {
+    qf[e] ^= neg;
+    asm volatile("" : "+v"(qf[e]));         // (waited for here, not in the loop)
+  }
+  // whether some query element is 2^100 or more: with all of them below, products
+  // with keys below 8 (scale bytes below 128) stay finite
+  uint32_t qm = 0u;
+#pragma unroll
+  for (int e = 0; e < 4 * KH; ++e)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      qm = max(qm, max((qf[e][c] & 0x7fffu) << 16, qf[e][c] & 0x7fff0000u));
+  const bool large = __any(qm >= (227u << 23));
   f32x16_t acc[FB];
   float m_run, l_run;
   auto start = [&]() {
@@ -723,18 +737,20 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
       for (int e = 0; e < 16; ++e) acc[fb][e] = 0.f;
   };
   // one tile's logits into weights; returns the reference of their exponents
-  // (a row that is not adjacent: every weight 2^-inf = 0)
-  auto attend = [&](const Place& w, f32x16_t (&s)[2]) -> float {
+  // (a row that is not adjacent: every weight 2^-inf = 0; its logits are set to
+  // -inf only where they may be no numbers or +inf, which spares 32 selects a tile)
+  auto attend = [&](const Place& w, uint32_t ks, f32x16_t (&s)[2]) -> float {
     if (w.t + 64 > w.len) mask_tail(s, w.len - w.t - 32 * hh);
     const bool adj = (mk >> w.j) & 1ull;
+    if (large || __any((ks & 0x80808080u) != 0u)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[h][e] = adj ? s[h][e] : -INFINITY;
+    }
     move_max(adj ? lane_max(s) : -INFINITY, sc, false, m_run, l_run, acc);
     return adj ? m_run : INFINITY;
   };
-#pragma unroll
-  for (int e = 0; e < 4 * KH; ++e) {
-    qf[e] ^= neg;
-    asm volatile("" : "+v"(qf[e]));         // (waited for here, not in the loop)
-  }
   start();
   // two tiles in turn: one's loads are in flight while the other is computed
   Place pa, pb;
@@ -743,12 +759,33 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   auto compute = [&](const Place& w, const QuantTile<D>& x) {
     f32x16_t s[2];
     x.logits(qf, s);
-    const float ref = attend(w, s);
+    const float ref = attend(w, x.ks, s);
     if (!OUT_F32 && !__all(half_scales<FB>(x.vs))) again = true;
     else l_run += x.template weigh<kQForm<OUT_F32>>(s, sc, ref, acc);
   };
   int c = x0 + wave;
-  if (c < x1) {
+  if constexpr (OUT_F32 && D == 128) {
+    // (two tiles and three pieces of the weights exceed the registers: the next
+    // keys land during the softmax instead, as in the form above)
+    if (c < x1) {
+      place(c, pa);
+      load(pa, xa);
+    }
+    for (; c < x1; c += kQWaves) {
+      f32x16_t s[2];
+      xa.logits(qf, s);
+      const uint32_t ks = xa.ks;
+      place(min(c + kQWaves, x1 - 1), pb);
+      const uint8_t *r0, *r1;
+      head.records(pb.blk0, (pb.len - 1) >> 5, pb.t >> 5, r0, r1);
+      xa.load_k(kb ? r1 : r0, ki, hh);
+      const float ref = attend(pa, ks, s);
+      l_run += xa.template weigh<3>(s, sc, ref, acc);
+      asm volatile("" ::: "memory");
+      xa.load_v(hh ? r1 : r0, n);
+      pa = pb;
+    }
+  } else if (c < x1) {
     place(c, pa);
     load(pa, xa);
     for (;;) {
@@ -771,7 +808,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
       load(pa, xa);
       f32x16_t s[2];
       xa.logits(qf, s);
-      const float ref = attend(pa, s);
+      const float ref = attend(pa, xa.ks, s);
       l_run += xa.template weigh<2>(s, sc, ref, acc);
     }
   }

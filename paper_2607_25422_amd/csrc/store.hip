@@ -3,7 +3,8 @@
 //
 // A block of 32 values x is held as codes of {0, .5, 1, 1.5, 2, 3, 4, 6} with a
 // sign and one power of two 2^(s - 127), the least with max|x| <= 7 * 2^(s - 127)
-// (from there on 6 would be more than half a step away): 4.25 bits a value.  A
+// (from there on 6 would be more than half a step away), s from 1 to 252: 4.25 bits a
+// value, all of them finite (the largest is 6 * 2^125; infinities are held as it).  A
 // key block is 32 features of one token, a value block 32 tokens of one feature,
 // so that a lane of the attention's matrix products holds one block's values and
 // one scale.  Store record (32 tokens, one head, d_h = D), 34 D bytes:
@@ -53,7 +54,7 @@ __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
 // Scale byte of a block whose largest magnitude has these bits (sign cleared).
 __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
   const int s = (int)(amax >> 23) - 2 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return (uint32_t)clampi(s, 1, 254);
+  return (uint32_t)clampi(s, 1, 252);
 }
 // Eight values as codes (round to nearest even), the first in the low nibble.
 __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float scale) {

@@ -50,3 +50,10 @@ def test_passage_blocks():
     assert Vo[32:, 0, 7].tolist() == orc.held_block(V[32:, 0, 7])[2].tolist()
     assert Vo[:32, 0, 7].tolist() == orc.held_block(V[:32, 0, 7])[2].tolist()
     assert math.isfinite(float(Ko.sum() + Vo.sum()))
+
+
+def test_the_largest_values_are_held_as_finite_ones():
+    top = 6.0 * 2.0 ** 125
+    x = [math.inf, -math.inf, 3.4e38, -1.8 * 2.0 ** 127, 2.0 ** 127, 0.0]
+    _, s, v = orc.held_block(x)
+    assert s == 252 and v.tolist() == [top, -top, top, -top, 2.0 ** 127, 0.0]
