@@ -212,21 +212,34 @@ struct QuantTile {
   // lane l: n = l % 32, hh = l / 32.  Keys: row n of the two products is token 32
   // kb + 16 h + ki, in features 64 kh + 32 hh ..; values: feature 32 fb + n, tokens
   // 32 hh ..
-  __device__ __forceinline__ void load_k(const uint8_t* rec, int ki, int hh) {
+  // A lane's offsets in a tile whose second record is `step` bytes behind its first
+  // (0: the same, masked): of its key row and its values, and of their scales.
+  struct Offsets {
+    uint32_t k, ks, v, vs;
+  };
+  static __device__ __forceinline__ Offsets offsets(int n, int hh, uint32_t step) {
+    const int ki = 4 * (n >> 3) + (n & 3);        // the lane's key row, of record kb
+    const uint32_t kr = ((n >> 2) & 1) ? step : 0u, vr = hh ? step : 0u;
+    return {kr + (hh * 16 + ki) * 16, kr + 32 * D + (hh * 16 + ki) * C, vr + n * 16,
+            vr + 33 * D + n * C};
+  }
+  static __device__ __forceinline__ uint32_t scales(const uint8_t* r, uint32_t off) {
+    return C == 4 ? *reinterpret_cast<const uint32_t*>(r + off)
+                  : *reinterpret_cast<const uint16_t*>(r + off);
+  }
+  __device__ __forceinline__ void load_k(const uint8_t* r, const Offsets& o) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int kh = 0; kh < KH; ++kh)
-        k[h][kh] = *reinterpret_cast<const u32x4*>(rec + ((h * C + 2 * kh + hh) * 16 + ki) * 16);
-    const uint8_t* sp = rec + 32 * D + (hh * 16 + ki) * C;
-    ks = C == 4 ? *reinterpret_cast<const uint32_t*>(sp) : *reinterpret_cast<const uint16_t*>(sp);
+        k[h][kh] = *reinterpret_cast<const u32x4*>(r + o.k + (h * C + 2 * kh) * 256);
+    ks = scales(r, o.ks);
   }
-  __device__ __forceinline__ void load_v(const uint8_t* rec, int n) {
+  __device__ __forceinline__ void load_v(const uint8_t* r, const Offsets& o) {
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb)
-      v[fb] = *reinterpret_cast<const u32x4*>(rec + 16 * D + (32 * fb + n) * 16);
-    const uint8_t* sp = rec + 33 * D + n * C;
-    vs = C == 4 ? *reinterpret_cast<const uint32_t*>(sp) : *reinterpret_cast<const uint16_t*>(sp);
+      v[fb] = *reinterpret_cast<const u32x4*>(r + o.v + 16 * D + 512 * fb);
+    vs = scales(r, o.vs);
   }
   // S^T: element i of s[h] is token 32 hh + 16 h + i, column n
   __device__ __forceinline__ void logits(const u32x4 (&q)[4 * KH], f32x16_t (&s)[2]) const {
@@ -296,12 +309,17 @@ struct QuantTile {
 template <bool OUT_F32> constexpr int kQForm = OUT_F32 ? 3 : 0;
 
 // Logits of the tokens from `rem` on (of the lane's 32) as -inf.
-__device__ __forceinline__ void mask_tail(f32x16_t (&s)[2], int rem) {
+// (The asm holds the values in their branch: as selects in every tile the compiler
+// made them an eighth of the vector instructions.)
+__device__ __forceinline__ void mask_from(f32x16_t (&s)[2], int rem) {
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (16 * h + i >= rem) s[h][i] = -INFINITY;
+    for (int i = 0; i < 16; ++i) {
+      float x = 16 * h + i >= rem ? -INFINITY : s[h][i];
+      asm volatile("" : "+v"(x));
+      s[h][i] = x;
+    }
 }
 __device__ __forceinline__ float lane_max(const f32x16_t (&s)[2]) {
   float lm = s[0][0];
@@ -330,26 +348,25 @@ __device__ __forceinline__ void move_max(float lm, float sc, bool first, float& 
   m_run = up ? mx : m_run;
 }
 
-// The store as one (question, key head) sees it.
-template <int D>
-struct QuantHead {
-  const uint8_t* base;
-  size_t stride;
-  long long n_blocks;
-  __device__ __forceinline__ QuantHead(const QuantAttnArgs& a, int hk)
-      : base(a.store + (size_t)hk * kStoreRecord<D>),
-        stride((size_t)a.heads_kv * kStoreRecord<D>), n_blocks(a.n_blocks) {}
-  // records of a tile's two blocks, i and i + 1 of a passage (past its last
-  // block: that one, masked); all of it uniform
-  __device__ __forceinline__ void records(int first, int last, int i, const uint8_t*& r0,
-                                          const uint8_t*& r1) const {
-    auto at = [&](int c) -> const uint8_t* {
-      long long blk = (long long)first + min(c, last);
-      blk = blk < 0 ? 0 : (blk >= n_blocks ? n_blocks - 1 : blk);
-      return base + (size_t)blk * stride;
-    };
-    r0 = at(i);
-    r1 = at(i + 1);
+// A stored passage of one key head: its first record, the bytes to the next, its last
+// record.  One that is not wholly inside the store is read at record 0 alone.
+struct QuantRun {
+  const uint8_t* first;
+  uint32_t step;
+  int last;
+  template <int D>
+  __device__ __forceinline__ void set(const QuantAttnArgs& a, int hk, int blk, int len) {
+    last = max(len - 1, 0) >> 5;
+    const bool inside = blk >= 0 && (long long)blk + last < a.n_blocks;
+    const uint32_t stride = (uint32_t)a.heads_kv * kStoreRecord<D>;
+    step = inside ? stride : 0u;
+    first = a.store + (size_t)hk * kStoreRecord<D> + (size_t)(uint32_t)(inside ? blk : 0) * stride;
+  }
+  // the record of token t (a multiple of 64), and how far behind it the next one
+  __device__ __forceinline__ const uint8_t* tile(int t, uint32_t& next) const {
+    const int i = min(t >> 5, last);
+    next = i < last ? step : 0u;
+    return first + (size_t)(uint32_t)i * step;
   }
 };
 
@@ -450,10 +467,9 @@ attn_quant_kernel(QuantAttnArgs a) {
   const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;   // folded into the queries
   // (not zero: masked logits stay -inf)
   const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);
-  const int ki = 4 * (n >> 3) + (n & 3), kb = (n >> 2) & 1;       // the lane's key row
 
   struct Unit {
-    int blk0, last_blk;             // first record of the passage, its last block
+    QuantRun run;
     int t0, t1;                     // tokens
     int before;                     // units to be merged before this one
     int row;                        // this lane's row (-1: none, not merged)
@@ -466,10 +482,9 @@ attn_quant_kernel(QuantAttnArgs a) {
     const int cnt = __builtin_amdgcn_readlane(my_cnt, j);
     const int len = __builtin_amdgcn_readlane(my_len, j);
     const int uf = __builtin_amdgcn_readlane(my_first, j);
-    x.blk0 = __builtin_amdgcn_readlane(my_blk, j);
-    x.last_blk = (len - 1) >> 5;
+    x.run.template set<D>(a, it.hk, __builtin_amdgcn_readlane(my_blk, j), len);
     const int nblk = (cnt + 31) / 32;
-    const int seg = (u - uf) / nblk, m = 32 * ((u - uf) - seg * nblk) + n;
+    const int seg = segs == 1 ? 0 : (u - uf) / nblk, m = 32 * ((u - uf) - seg * nblk) + n;
     const int run = ((len + 63) / 64 + segs - 1) / segs * 64;    // tokens of a segment
     x.t0 = min(seg * run, len);
     x.t1 = min(x.t0 + run, len);
@@ -489,14 +504,7 @@ attn_quant_kernel(QuantAttnArgs a) {
       for (int s = 0; s < 4; ++s)
         qf[4 * kh + s] = *reinterpret_cast<const u32x4*>(src + 64 * kh + 8 * s);
   };
-  const QuantHead<D> head(a, it.hk);
   QuantTile<D> x;
-  const uint8_t *r0, *r1;                    // the tile's records
-  auto load_k = [&](const Unit& w, int t) {
-    head.records(w.blk0, w.last_blk, t >> 5, r0, r1);
-    x.load_k(kb ? r1 : r0, ki, hh);
-  };
-  auto load_v = [&]() { x.load_v(hh ? r1 : r0, n); };
 
   int u = wave;
   Unit cur, nxt;
@@ -505,9 +513,12 @@ attn_quant_kernel(QuantAttnArgs a) {
     unit(u, cur);
     load_q(cur);
     asm volatile("" ::: "memory");
-    load_k(cur, cur.t0);
+    uint32_t next;
+    const uint8_t* r = cur.run.tile(cur.t0, next);
+    const auto o = x.offsets(n, hh, next);
+    x.load_k(r, o);
     asm volatile("" ::: "memory");
-    load_v();
+    x.load_v(r, o);
     asm volatile("" ::: "memory");
   }
   for (; u < u_end; u += kQWaves) {
@@ -534,47 +545,66 @@ attn_quant_kernel(QuantAttnArgs a) {
     };
     // (a segment's first tile has a token in every column: m_run is finite then)
     auto attend = [&](int t, f32x16_t (&s)[2]) {
-      if (t + 64 > cur.t1) mask_tail(s, cur.t1 - t - 32 * hh);
+      if (t + 64 > cur.t1) mask_from(s, cur.t1 - t - 32 * hh);
       move_max(lane_max(s), sc, t == cur.t0, m_run, l_run, acc);
     };
     start();
     bool again = false;
     int t = cur.t0;
-    do {                                     // (once for an empty segment, too: masked)
+    // one tile; the next one's keys (`r`) land during the softmax and the second
+    // product, its values during the next logits, and with a unit's last tile the
+    // next unit's queries
+    auto step = [&](auto last, const uint8_t* r, uint32_t next) {
       f32x16_t s[2];
       x.logits(qf, s);
-      // the next keys land during the softmax and the second product
-      const bool last = t + 64 >= cur.t1;
-      const int tn = last ? nxt.t0 : t + 64;
-      load_k(last ? nxt : cur, tn);
-      attend(t, s);
-      if (!OUT_F32 && !__all(half_scales<FB>(x.vs))) {
-        again = true;
-        break;
+      const auto o = x.offsets(n, hh, next);
+      x.load_k(r, o);
+      if constexpr (decltype(last)::value) {
+        asm volatile("" ::: "memory");
+        load_q(nxt);
+        asm volatile("" ::: "memory");
       }
-      l_run += x.template weigh<kQForm<OUT_F32>>(s, sc, m_run, acc);
+      attend(t, s);
+      if (!OUT_F32 && !__all(half_scales<FB>(x.vs))) again = true;
+      else l_run += x.template weigh<kQForm<OUT_F32>>(s, sc, m_run, acc);
       asm volatile("" ::: "memory");
-      load_v();
+      x.load_v(r, o);
       t += 64;
-    } while (t < cur.t1);
+    };
+    uint32_t next;
+    while (t + 64 < cur.t1 && !again) {
+      const uint8_t* r = cur.run.tile(t + 64, next);
+      step(std::false_type{}, r, next);
+    }
+    if (!again) {                            // (for an empty segment, too: masked)
+      const uint8_t* r = nxt.run.tile(nxt.t0, next);
+      step(std::true_type{}, r, next);
+    }
     if (!OUT_F32 && again) {
+      load_q(cur);
       start();
       t = cur.t0;
+#pragma unroll
+      for (int i = 0; i < 4 * KH; ++i) qf[i] ^= neg;
       do {
         f32x16_t s[2];
-        load_k(cur, t);
-        load_v();
+        const uint8_t* r = cur.run.tile(t, next);
+        const auto o = x.offsets(n, hh, next);
+        x.load_k(r, o);
+        x.load_v(r, o);
         x.logits(qf, s);
         attend(t, s);
         l_run += x.template weigh<2>(s, sc, m_run, acc);
         t += 64;
       } while (t < cur.t1);
-      load_k(nxt, nxt.t0);
+      const uint8_t* r = nxt.run.tile(nxt.t0, next);
+      const auto o = x.offsets(n, hh, next);
+      x.load_k(r, o);
+      load_q(nxt);
       asm volatile("" ::: "memory");
-      load_v();
+      x.load_v(r, o);
+      asm volatile("" ::: "memory");
     }
-    load_q(nxt);
-    asm volatile("" ::: "memory");
 
     // merge in the order of the list: every unit of earlier passages and
     // segments first (the others of this one have other rows)
@@ -650,7 +680,6 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, hh = lane >> 5;
-  const int ki = 4 * (n >> 3) + (n & 3), kb = (n >> 2) & 1;       // the lane's key row
 
   // this lane's row (past the item's rows: its last one, adjacent to nothing)
   const int v = min(n, nv - 1), i = v / G, hq = it.hk * G + (v - i * G);
@@ -695,21 +724,22 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;   // folded into the queries
   // (not zero: masked logits stay -inf)
   const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);
-  const QuantHead<D> head(a, it.hk);
   struct Place {
-    int j, t, len, blk0;
+    int j, t, len;
+    QuantRun run;
   };
   auto place = [&](int c, Place& w) {
     w.j = __popcll(__ballot(my_first <= c)) - 1;         // as for the units above
     w.len = __builtin_amdgcn_readlane(my_len, w.j);
-    w.blk0 = __builtin_amdgcn_readlane(my_blk, w.j);
+    w.run.template set<D>(a, it.hk, __builtin_amdgcn_readlane(my_blk, w.j), w.len);
     w.t = (c - __builtin_amdgcn_readlane(my_first, w.j)) * 64;
   };
   auto load = [&](const Place& w, QuantTile<D>& x) {
-    const uint8_t *r0, *r1;                  // the tile's records
-    head.records(w.blk0, (w.len - 1) >> 5, w.t >> 5, r0, r1);
-    x.load_k(kb ? r1 : r0, ki, hh);
-    x.load_v(hh ? r1 : r0, n);
+    uint32_t next;
+    const uint8_t* r = w.run.tile(w.t, next);
+    const auto o = x.offsets(n, hh, next);
+    x.load_k(r, o);
+    x.load_v(r, o);
     asm volatile("" ::: "memory");           // (tiles in order: the counted waits go by it)
   };
 #pragma unroll
@@ -740,14 +770,9 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   // (a row that is not adjacent: every weight 2^-inf = 0; its logits are set to
   // -inf only where they may be no numbers or +inf, which spares 32 selects a tile)
   auto attend = [&](const Place& w, uint32_t ks, f32x16_t (&s)[2]) -> float {
-    if (w.t + 64 > w.len) mask_tail(s, w.len - w.t - 32 * hh);
+    if (w.t + 64 > w.len) mask_from(s, w.len - w.t - 32 * hh);
     const bool adj = (mk >> w.j) & 1ull;
-    if (large || __any((ks & 0x80808080u) != 0u)) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[h][e] = adj ? s[h][e] : -INFINITY;
-    }
+    if (large || __any((ks & 0x80808080u) != 0u)) mask_from(s, adj ? 32 : 0);
     move_max(adj ? lane_max(s) : -INFINITY, sc, false, m_run, l_run, acc);
     return adj ? m_run : INFINITY;
   };
@@ -776,13 +801,14 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
       xa.logits(qf, s);
       const uint32_t ks = xa.ks;
       place(min(c + kQWaves, x1 - 1), pb);
-      const uint8_t *r0, *r1;
-      head.records(pb.blk0, (pb.len - 1) >> 5, pb.t >> 5, r0, r1);
-      xa.load_k(kb ? r1 : r0, ki, hh);
+      uint32_t next;
+      const uint8_t* r = pb.run.tile(pb.t, next);
+      const auto o = xa.offsets(n, hh, next);
+      xa.load_k(r, o);
       const float ref = attend(pa, ks, s);
       l_run += xa.template weigh<3>(s, sc, ref, acc);
       asm volatile("" ::: "memory");
-      xa.load_v(hh ? r1 : r0, n);
+      xa.load_v(r, o);
       pa = pb;
     }
   } else if (c < x1) {

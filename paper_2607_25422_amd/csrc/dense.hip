@@ -522,7 +522,7 @@ static DenseShape dense_shape(int M, int d, int d_out) {
   s.mb = 0;
   s.splits = 1;
   for (int mb = 8; mb >= 2; --mb) {
-    const long long tiles = (M + 32 * mb - 1) / (32 * mb) * nts;
+    const long long tiles = ((long long)M + 32 * mb - 1) / (32 * mb) * nts;
     // a part is at least eight steps
     const int most = std::max(1, std::min(16, steps / 8));
     for (int sp = 1; sp <= most; ++sp) {
@@ -572,7 +572,7 @@ hipError_t launch_dense(const skip_problem_t& p, const void* rows, const int32_t
   const DenseShape s = dense_shape(a.M, a.d, d_out);
   a.splits = s.splits;
   const int width = s.rows ? 64 : kDnNT;
-  const long long items = (long long)((a.M + 32 * s.mb - 1) / (32 * s.mb)) *
+  const long long items = ((long long)a.M + 32 * s.mb - 1) / (32 * s.mb) *
                           ((d_out + width - 1) / width) * s.splits;
   if (items > (1 << 22)) return hipErrorInvalidValue;
   a.n_items = (int)items;
