@@ -391,7 +391,8 @@ attn_quant_kernel(QuantAttnArgs a) {
   constexpr int KH = QuantTile<D>::KH, FB = QuantTile<D>::FB;
   constexpr int NC4 = D / 4;                // 4-float chunks of an accumulator row
   constexpr int MW = (ROWS + 63) / 64;      // words of a row mask
-  __shared__ __attribute__((aligned(16))) float Oacc[ROWS * D];
+  constexpr int OS = D + 4;                 // floats of an accumulator row (bank spread)
+  __shared__ __attribute__((aligned(16))) float Oacc[ROWS * OS];
   __shared__ float m_acc[ROWS], l_acc[ROWS];
   __shared__ uint64_t neighbours[ROWS];     // of the item's kept rows
   __shared__ uint8_t rowlist[kQMaxP][ROWS]; // virtual rows adjacent to each passage, ascending
@@ -416,7 +417,7 @@ attn_quant_kernel(QuantAttnArgs a) {
     my_blk = a.passage_blocks[it.p0 + lane];
   }
   if (tid < it.nk) neighbours[tid] = row_neighbours(a, it.k0 + it.i0 + tid, P);
-  for (int i = tid; i < nv * NC4; i += kQThreads)
+  for (int i = tid; i < nv * (OS / 4); i += kQThreads)
     reinterpret_cast<float4*>(Oacc)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = tid; i < nv; i += kQThreads) {
     m_acc[i] = -INFINITY;
@@ -504,6 +505,14 @@ attn_quant_kernel(QuantAttnArgs a) {
       for (int s = 0; s < 4; ++s)
         qf[4 * kh + s] = *reinterpret_cast<const u32x4*>(src + 64 * kh + 8 * s);
   };
+  auto negate_q = [&]() {
+    if (neg)
+#pragma unroll
+      for (int i = 0; i < 4 * KH; ++i) {
+        qf[i] ^= neg;
+        asm volatile("" : "+v"(qf[i]));      // (a branch)
+      }
+  };
   QuantTile<D> x;
 
   int u = wave;
@@ -529,10 +538,8 @@ attn_quant_kernel(QuantAttnArgs a) {
     // (the queries are waited for here, not in the loop, where the wait would
     // reach the tile's loads, too)
 #pragma unroll
-    for (int i = 0; i < 4 * KH; ++i) {
-      qf[i] ^= neg;
-      asm volatile("" : "+v"(qf[i]));
-    }
+    for (int i = 0; i < 4 * KH; ++i) asm volatile("" : "+v"(qf[i]));
+    negate_q();
     f32x16_t acc[FB];
     float m_run, l_run;
     auto start = [&]() {
@@ -584,8 +591,7 @@ attn_quant_kernel(QuantAttnArgs a) {
       load_q(cur);
       start();
       t = cur.t0;
-#pragma unroll
-      for (int i = 0; i < 4 * KH; ++i) qf[i] ^= neg;
+      negate_q();
       do {
         f32x16_t s[2];
         const uint8_t* r = cur.run.tile(t, next);
@@ -614,11 +620,19 @@ attn_quant_kernel(QuantAttnArgs a) {
     const float l_tot = l_run + other_half(l_run);
     const int row = cur.row;
     if (row >= 0) {
+      // (the row's reference moves as move_max's does, so that most merges add only)
       const float mo = m_acc[row], lo = l_acc[row];
-      const float mn = fmaxf(mo, m_run);
-      const float fa = __builtin_amdgcn_exp2f(mo - mn);     // 0 while the row is empty
+      const bool up = m_run > mo + kQLazy;
+      const float mn = up ? m_run : mo;
+      const float fa = up && mo != -INFINITY ? __builtin_amdgcn_exp2f(mo - mn) : 1.f;
       const float fc = __builtin_amdgcn_exp2f(m_run - mn);
-      float4* orow = reinterpret_cast<float4*>(Oacc + row * D);
+      float4* orow = reinterpret_cast<float4*>(Oacc + row * OS) + hh;
+      if (__any(fa != 1.f))
+#pragma unroll
+        for (int c = 0; c < NC4 / 2; ++c) {
+          const float4 o = orow[2 * c];
+          orow[2 * c] = make_float4(o.x * fa, o.y * fa, o.z * fa, o.w * fa);
+        }
       // (a half of the row at a time in registers)
 #pragma unroll
       for (int f0 = 0; f0 < FB; f0 += 2) {
@@ -626,22 +640,21 @@ attn_quant_kernel(QuantAttnArgs a) {
 #pragma unroll
         for (int f = 0; f < 2; ++f)
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            ov[f][c] = orow[(8 * (f0 + f) + 2 * c + hh) ^ (row & (NC4 - 1))];
+          for (int c = 0; c < 4; ++c) ov[f][c] = orow[8 * (f0 + f) + 2 * c];
 #pragma unroll
         for (int f = 0; f < 2; ++f)
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const float4 o = ov[f][c];
             const f32x16_t& x = acc[f0 + f];
-            orow[(8 * (f0 + f) + 2 * c + hh) ^ (row & (NC4 - 1))] =
-                make_float4(fmaf(o.x, fa, x[4 * c] * fc), fmaf(o.y, fa, x[4 * c + 1] * fc),
-                            fmaf(o.z, fa, x[4 * c + 2] * fc), fmaf(o.w, fa, x[4 * c + 3] * fc));
+            orow[8 * (f0 + f) + 2 * c] =
+                make_float4(fmaf(x[4 * c], fc, o.x), fmaf(x[4 * c + 1], fc, o.y),
+                            fmaf(x[4 * c + 2], fc, o.z), fmaf(x[4 * c + 3], fc, o.w));
           }
       }
       if (hh == 0) {
         m_acc[row] = mn;
-        l_acc[row] = fmaf(lo, fa, l_tot * fc);
+        l_acc[row] = fmaf(l_tot, fc, lo * fa);
       }
     }
     wait_lgkm0();
@@ -654,7 +667,7 @@ attn_quant_kernel(QuantAttnArgs a) {
   for (int e = tid; e < nv * NC4; e += kQThreads) {
     const int ri = e / NC4, q = e % NC4, i = over_G(ri);
     quant_store<D>(a, it, i, it.hk * G + (ri - i * G), q,
-                   reinterpret_cast<const float4*>(Oacc + ri * D)[q ^ (ri & (NC4 - 1))],
+                   reinterpret_cast<const float4*>(Oacc + ri * OS)[q],
                    m_acc[ri], l_acc[ri]);
   }
 }
@@ -953,9 +966,10 @@ static QuantShape quant_shape(const skip_problem_t& p, int heads_kv) {
   if (!s.tile) return s;
   const long long wgs = cut(kQTileRows);
   if (wgs > 0 && wgs < 256) {
-    // at least eight tiles of 64 tokens a split
+    // one workgroup a CU (a second round of short ones costs more than it brings),
+    // at least eight tiles of 64 tokens each
     const long long tiles = (long long)p.P_max * ((p.L_max + 63) / 64);
-    s.splits = (int)std::max<long long>(1, std::min<long long>((512 + wgs - 1) / wgs, tiles / 8));
+    s.splits = (int)std::max<long long>(1, std::min<long long>(256 / wgs, tiles / 8));
   }
   return s;
 }
