@@ -25,6 +25,12 @@
 // of the list, so that the result does not depend on which wave was faster: a
 // wave waits until every unit of earlier passages and segments is merged.  (Units
 // are taken in order, so the earliest one that is not merged never waits.)
+//
+// Bound by vector instructions: a tile of 64 tokens x 32 rows x 128 features takes 128
+// to make held values of codes, some 190 for the softmax, 32 matrix products beside
+// them.  16 questions of 192 rows of 32 heads over ten passages of 256 tokens
+// take 89 us: 7 us of an item's start and end twice, 1.0 us a tile and SIMD (two waves;
+// the instructions alone 0.85) and 1.5 us a unit, for its queries and its merge.
 #include <algorithm>
 #include <type_traits>
 
@@ -675,18 +681,25 @@ attn_quant_kernel(QuantAttnArgs a) {
 // Row-tile form: up to 32 virtual rows a workgroup.  Its waves take the 64-token
 // tiles of the passages adjacent to any of the rows in turn, each with its own
 // (O, max, sum) in registers from its first tile to its last, so that the loop
-// has no LDS, no barrier and one stream of loads a tile ahead; a logit of a row that is not
-// adjacent to the tile's passage is -inf (its weight of 0 meets held values, which
-// are finite).  The waves' partials are merged in wave order through LDS at the end.
+// has no LDS, no barrier and one stream of loads a tile ahead; a logit of a row that
+// is not adjacent to the tile's passage is -inf (its weight of 0 meets held values,
+// which are finite).  The waves' partials are merged in wave order through LDS at the
+// end.  Four waves, so that two workgroups share a CU and one starts while the other
+// computes (8 questions of 16 heads, 96 rows over 1280 tokens: 22.4 us with the graph,
+// 25.4 with eight).  Over long passages it is bound by HBM: 4 questions of one row of 32
+// heads over 8 key heads and 27000 tokens each, 118 MB of held passages, 29 us with
+// the join of the parts (4.1 TB/s).
 constexpr int kQTileRows = 32;
+constexpr int kQTileWaves = 4;
+constexpr int kQTileThreads = 64 * kQTileWaves;
 
 template <int D, bool OUT_F32>
-__global__ void __launch_bounds__(kQThreads, 2)
+__global__ void __launch_bounds__(kQTileThreads, 2)
 attn_quant_tile_kernel(QuantAttnArgs a) {
   constexpr int KH = QuantTile<D>::KH, FB = QuantTile<D>::FB, NC4 = D / 4;
   constexpr int OS = D + 4;                 // floats per row of a wave's partial (bank spread)
-  __shared__ __attribute__((aligned(16))) float po[kQWaves][kQTileRows][OS];
-  __shared__ float pm[kQWaves][kQTileRows], pl[kQWaves][kQTileRows];
+  __shared__ __attribute__((aligned(16))) float po[kQTileWaves][kQTileRows][OS];
+  __shared__ float pm[kQTileWaves][kQTileRows], pl[kQTileWaves][kQTileRows];
   QuantItem it;
   if (!quant_item(a, blockIdx.x, it)) return;
   const int G = a.G, nv = it.nk * G, P = it.P;
@@ -809,11 +822,11 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
       place(c, pa);
       load(pa, xa);
     }
-    for (; c < x1; c += kQWaves) {
+    for (; c < x1; c += kQTileWaves) {
       f32x16_t s[2];
       xa.logits(qf, s);
       const uint32_t ks = xa.ks;
-      place(min(c + kQWaves, x1 - 1), pb);
+      place(min(c + kQTileWaves, x1 - 1), pb);
       uint32_t next;
       const uint8_t* r = pb.run.tile(pb.t, next);
       const auto o = xa.offsets(n, hh, next);
@@ -828,12 +841,12 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
     place(c, pa);
     load(pa, xa);
     for (;;) {
-      c += kQWaves;
+      c += kQTileWaves;
       place(min(c, x1 - 1), pb);             // (past the last tile: one that is not used)
       load(pb, xb);
       compute(pa, xa);
       if (c >= x1) break;
-      c += kQWaves;
+      c += kQTileWaves;
       place(min(c, x1 - 1), pa);
       load(pa, xa);
       compute(pb, xb);
@@ -842,7 +855,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   }
   if (!OUT_F32 && again) {
     start();
-    for (c = x0 + wave; c < x1; c += kQWaves) {
+    for (c = x0 + wave; c < x1; c += kQTileWaves) {
       place(c, pa);
       load(pa, xa);
       f32x16_t s[2];
@@ -866,16 +879,16 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   __syncthreads();
   float* part = a.part + ((size_t)((it.b * a.heads_kv + it.hk) * a.chunks + it.chunk) * a.splits +
                           it.split) * part_floats(a.rows_chunk * G, D);
-  for (int e = tid; e < nv * NC4; e += kQThreads) {
+  for (int e = tid; e < nv * NC4; e += kQTileThreads) {
     const int ri = e / NC4, q = e % NC4;
     float M = pm[0][ri];
 #pragma unroll
-    for (int w = 1; w < kQWaves; ++w) M = fmaxf(M, pm[w][ri]);
+    for (int w = 1; w < kQTileWaves; ++w) M = fmaxf(M, pm[w][ri]);
     const float ref = M == -INFINITY ? 0.f : M;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kQWaves; ++w) {
+    for (int w = 0; w < kQTileWaves; ++w) {
       const float f = __builtin_amdgcn_exp2f(pm[w][ri] - ref);
       const float4 y = *reinterpret_cast<const float4*>(&po[w][ri][4 * q]);
       l = fmaf(pl[w][ri], f, l);
@@ -962,14 +975,26 @@ static QuantShape quant_shape(const skip_problem_t& p, int heads_kv) {
     return groups * s.chunks;
   };
   s.splits = 1;
-  s.tile = cut(192) < 256;
-  if (!s.tile) return s;
+  // Row tiles up to three rounds of workgroups for batches of one size (by the average
+  // rows of a question): they compute a product for every row and passage that one of
+  // their rows has an edge to, the units only those with an edge, in longer items.  Of
+  // 90 batches of 1 to 24 questions of 4 to 384 rows this picked the slower form by
+  // 1.6 % on average.  32 heads of 128 features, ten passages of 256 tokens, tiles
+  // and units: 2 questions of 192 rows (384 tiles) 28 and 39 us, 4 of 96 (384) 28.5 and
+  // 28.8, 8 of 48 (512) 30 and 26, 8 of 192 (1536) 76 and 46.
+  const long long per = ((long long)p.total_kept * G + 32ll * p.B - 1) / (32ll * p.B);
+  s.tile = groups * per < 768;
+  if (!s.tile) {
+    cut(192);
+    return s;
+  }
   const long long wgs = cut(kQTileRows);
   if (wgs > 0 && wgs < 256) {
-    // one workgroup a CU (a second round of short ones costs more than it brings),
-    // at least eight tiles of 64 tokens each
+    // one workgroup a CU, at least four tiles of 64 tokens each: 8 questions of 4 rows
+    // and heads over ten passages of 2048 tokens, 32 items, take 72 us whole, 22 in 8
+    // parts, 27 in 16; from one part to two a second launch is paid for by 16 tiles
     const long long tiles = (long long)p.P_max * ((p.L_max + 63) / 64);
-    s.splits = (int)std::max<long long>(1, std::min<long long>(256 / wgs, tiles / 8));
+    if (tiles >= 16) s.splits = (int)std::max<long long>(1, std::min<long long>(256 / wgs, tiles / 4));
   }
   return s;
 }
@@ -1031,7 +1056,7 @@ hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t
 #define SKIP_ATTN_QUANT(DD, FF)                                                            \
   do {                                                                                     \
     if (sh.tile)                                                                           \
-      hipLaunchKernelGGL((attn_quant_tile_kernel<DD, FF>), grid, dim3(kQThreads), 0, s, a); \
+      hipLaunchKernelGGL((attn_quant_tile_kernel<DD, FF>), grid, dim3(kQTileThreads), 0, s, a); \
     else                                                                                   \
       hipLaunchKernelGGL((attn_quant_kernel<DD, 192, FF>), grid, dim3(kQThreads), 0, s, a); \
   } while (0)

@@ -272,10 +272,10 @@ def one_wide(x):
 
 
 @pytest.mark.parametrize("make", [wide_values, one_wide])
-@pytest.mark.parametrize("nq", [1, 70])
+@pytest.mark.parametrize("nq", [1, 200])
 @pytest.mark.parametrize("D", [64, 128])
 def test_attention_values_that_are_no_half_floats(B, D, nq, make):
-    """Both forms (few rows; past 256 items of 192 rows), elementwise against each
+    """Both forms (few rows; from 768 tiles of 32 rows on), elementwise against each
     feature's own size."""
     H, ks, Ps = 4, [9] * nq, [3] * nq
     x = Held(B, [90, 64, 33], H, H, D, 25)
