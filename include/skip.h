@@ -468,7 +468,7 @@ skip_status_t skip_bipartite_xattn_proj(const skip_problem_t* p, const void* Qh,
  * signed codes of {0, 0.5, 1, 1.5, 2, 3, 4, 6}, rounded to nearest with ties to
  * the even code, times one power of two: 2^(s - 127) with s the least in [1, 252]
  * for which max|x| <= 7 * 2^(s - 127), or 252.  Held values are finite: an infinity
- * is held as 6 * 2^125, a NaN as some value of the block.
+ * is held as 6 * 2^125, a NaN as some value, the rest of their block by their scale.
  *   heads_kv  key/value heads H_kv, a divisor of H (query head h reads key head
  *             h / (H / H_kv)); at most 32 query heads a key head
  *   n_blocks  records of 32 tokens the store holds for every head
@@ -531,10 +531,9 @@ skip_status_t skip_workspace_bytes_quant(const skip_problem_t* p, const skip_kv_
  * Stage 2 over the store: skip_bipartite_xattn with the keys and values that the
  * store holds.  bf16 rows (SKIP_ERR_UNSUPPORTED otherwise); O bf16, or float with
  * o_f32.  Logits and sums are float32 and the held values enter exactly.  Softmax
- * weights (relative to the largest of a row so far times at most 2^8) enter the
- * product with V for float output to 2^-24 relative; for bf16 output as half floats,
- * 2^-11 relative down to 2^-14 and 2^-25 absolute below, or where a tile's held
- * values are no half floats to 2^-16 relative.
+ * weights enter the product with V for float output to 2^-24 relative; for bf16
+ * output as half floats, to 2^-11 relative or 2^-32 of the row's largest, or where a
+ * tile's held values are no half floats to 2^-16 relative.
  *   rows            kept_idx NULL: queries [total_kept][H][d_h]; else V [B][N][d],
  *                   row r of question b being V[b][kept_idx[r]]
  *   edge_rows       [total_kept][d] bf16 rows to cut the graph on, or NULL: `rows`

@@ -719,6 +719,8 @@ def skip_gather_dense(p: SkipProblem, rows, kept_offsets, rows_idx, packed, d_ou
                       workspace=None, stream=None):
     et = _elem_dtype(p)
     d_out = int(d_out)
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}, got {activation!r}")
     _on_current_device(rows, kept_offsets, rows_idx, packed, Y, bias, residual, residual_idx,
                        workspace)
     if workspace is None:

@@ -42,7 +42,11 @@ namespace skip {
 
 constexpr float kQLog2e = 1.4426950408889634f;
 constexpr float kQLn2 = 0.6931471805599453f;
-constexpr float kQLazy = 8.f;              // log2 slack of the softmax reference maximum
+// Weights are 2^(logit - reference), in units of log2: a reference is set 7 below the
+// largest logit so far and kept until one exceeds it by 15, so that the largest weight
+// is from 2^7 to 2^15 and a half float (normal from 2^-14, steps of 2^-24 below)
+// is off by at most 2^-32 of it where small.
+constexpr float kQHead = 7.f, kQLazy = 15.f;
 constexpr int kQWaves = 8;
 constexpr int kQThreads = 64 * kQWaves;
 constexpr int kQMaxP = 64;                 // passages of a question
@@ -307,7 +311,7 @@ struct QuantTile {
 
 // How softmax weights enter the second product.  Float output: three bf16 pieces.
 // bf16 output: one half float (11 bits: 2^-11 relative, an eighth of the output's
-// own rounding; weights are at most 2^kQLazy) as long as the held values are half
+// own rounding) as long as the held values are half
 // floats, which saves a third of the matrix products and a seventh of the vector
 // instructions; a wave that meets a tile whose values are not goes over its tiles
 // again with two bf16 pieces.  (A branch within the loop would hold the registers
@@ -337,7 +341,7 @@ __device__ __forceinline__ float lane_max(const f32x16_t (&s)[2]) {
 }
 
 // The reference maximum of the softmax moves when a logit exceeds it by more than
-// kQLazy (weights stay <= 2^kQLazy), so most tiles need no exchange or rescale.
+// kQLazy, so most tiles need no exchange or rescale.
 // lm: the lane's largest logit; `first`: nothing is summed yet.
 template <int FB>
 __device__ __forceinline__ void move_max(float lm, float sc, bool first, float& m_run,
@@ -345,13 +349,14 @@ __device__ __forceinline__ void move_max(float lm, float sc, bool first, float& 
   if (!__any(lm * sc > m_run + kQLazy)) return;
   const float mx = fmaxf(lm, other_half(lm)) * sc;
   const bool up = mx > m_run + kQLazy;
+  const float to = mx - kQHead;
   if (!first) {
-    const float alpha = !up ? 1.f : m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mx);
+    const float alpha = !up ? 1.f : m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - to);
     l_run *= alpha;
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb) acc[fb] *= alpha;
   }
-  m_run = up ? mx : m_run;
+  m_run = up ? to : m_run;
 }
 
 // A stored passage of one key head: its first record, the bytes to the next, its last
@@ -626,7 +631,7 @@ attn_quant_kernel(QuantAttnArgs a) {
     const float l_tot = l_run + other_half(l_run);
     const int row = cur.row;
     if (row >= 0) {
-      // (the row's reference moves as move_max's does, so that most merges add only)
+      // (the row's reference moves as a unit's does, so that most merges add only)
       const float mo = m_acc[row], lo = l_acc[row];
       const bool up = m_run > mo + kQLazy;
       const float mn = up ? m_run : mo;

@@ -374,3 +374,37 @@ def test_tensors_of_another_device_are_refused(B, monkeypatch):
                  lambda: B.gather_dense(p, Q, packed, 8, workspace=ws)):
         with pytest.raises(ValueError, match="device"):
             call()
+
+
+@pytest.mark.parametrize("nq", [1, 200])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("e", [15.0, 24.0, 29.5])
+def test_many_small_weights(B, nq, D, e):
+    """A token of weight 1 and value 0, 4000 of weight 2^-e and value 1 (all held as
+    they are): no weight is lost, each off by 2^-11 of itself or 2^-32 of the largest
+    (and its exponent by the float32 logit, 2^-22 e), the result by its own half step."""
+    L, H = 4001, 4
+    x = Held(B, [L], H, H, D, 55)
+    x.K, x.V = torch.zeros_like(x.K), torch.ones_like(x.V)
+    x.K[1:, :, 3] = -6.0
+    x.V[0] = 0.0
+    x.write(B)
+    x.off, x.po, x.pb = cum([L] * nq), dev(cum([L] * nq)), dev(np.tile(x.blocks, nq))
+    Q = torch.zeros(2, H, D).bfloat16()
+    Q[:, :, 3] = 1.0
+    O, lse = attend(B, x, Q.repeat(nq, 1, 1), [[0]] * (2 * nq), [2] * nq, [1] * nq,
+                    e * math.log(2) / 6)
+    torch.cuda.synchronize()
+    s = 4000 * 2.0 ** -e
+    want = s / (1 + s)
+    err = (O.double() - want).abs().max().item()
+    say(f"small weights e={e} D={D}: relative error {err / want:.2e}")
+    assert err <= want * (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -22 * e) + 4000 * 2.0 ** -32
+    assert (lse.double() - math.log1p(s)).abs().max().item() <= 2.0 ** -20
+
+
+def test_unknown_activation_is_refused(B):
+    p = B.make_problem("bf16", B=1, d=64, kept_offsets=[0, 1])
+    W = torch.zeros(8, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="activation"):
+        B.gather_dense(p, W[:1], B.pack_dense(p, W), 8, activation="tanh")
