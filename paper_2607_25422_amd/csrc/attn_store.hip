@@ -42,11 +42,6 @@ namespace skip {
 
 constexpr float kQLog2e = 1.4426950408889634f;
 constexpr float kQLn2 = 0.6931471805599453f;
-// Weights are 2^(logit - reference), in units of log2: a reference is set 7 below the
-// largest logit so far and kept until one exceeds it by 15, so that the largest weight
-// is from 2^7 to 2^15 and a half float (normal from 2^-14, steps of 2^-24 below)
-// is off by at most 2^-32 of it where small.
-constexpr float kQHead = 7.f, kQLazy = 15.f;
 constexpr int kQWaves = 8;
 constexpr int kQThreads = 64 * kQWaves;
 constexpr int kQMaxP = 64;                 // passages of a question
@@ -310,13 +305,21 @@ struct QuantTile {
 };
 
 // How softmax weights enter the second product.  Float output: three bf16 pieces.
-// bf16 output: one half float (11 bits: 2^-11 relative, an eighth of the output's
-// own rounding) as long as the held values are half
-// floats, which saves a third of the matrix products and a seventh of the vector
-// instructions; a wave that meets a tile whose values are not goes over its tiles
-// again with two bf16 pieces.  (A branch within the loop would hold the registers
-// of both forms.)
+// bf16 output: one half float (2^-11 relative, an eighth of the output's own rounding)
+// as long as the held values are half floats, which saves a third of the matrix
+// products and a seventh of the vector instructions; a wave that meets a tile whose
+// values are not goes over its tiles again with two bf16 pieces.  (A branch within the
+// loop would hold the registers of both forms.)
+//
+// Weights are 2^(logit - reference), in units of log2; a reference is set `below` under
+// the largest logit so far and kept until one exceeds it by `slack`.  Half floats: the
+// largest weight is from 2^7 to 2^15, and small ones (normal from 2^-14, steps of 2^-24
+// below) are off by at most 2^-32 of it.  bf16 pieces: from 2^-24 to 2^-16, and with
+// the same slack of 2^8 when a unit is merged, so that the sum over many tokens of the
+// largest held values (2^127) stays finite.
 template <bool OUT_F32> constexpr int kQForm = OUT_F32 ? 3 : 0;
+template <int PIECES> constexpr float kQBelow = PIECES ? -24.f : 7.f;
+template <int PIECES> constexpr float kQSlack = PIECES ? -16.f : 15.f;
 
 // Logits of the tokens from `rem` on (of the lane's 32) as -inf.
 // (The asm holds the values in their branch: as selects in every tile the compiler
@@ -340,16 +343,16 @@ __device__ __forceinline__ float lane_max(const f32x16_t (&s)[2]) {
   return lm;
 }
 
-// The reference maximum of the softmax moves when a logit exceeds it by more than
-// kQLazy, so most tiles need no exchange or rescale.
-// lm: the lane's largest logit; `first`: nothing is summed yet.
-template <int FB>
-__device__ __forceinline__ void move_max(float lm, float sc, bool first, float& m_run,
+// The reference for the next weights (rarely moved: most tiles need no exchange or
+// rescale).  lm: the lane's largest logit; `first`: nothing is summed yet.
+template <int PIECES, int FB>
+__device__ __forceinline__ void move_ref(float lm, float sc, bool first, float& m_run,
                                          float& l_run, f32x16_t (&acc)[FB]) {
-  if (!__any(lm * sc > m_run + kQLazy)) return;
+  constexpr float slack = kQSlack<PIECES>;
+  if (!__any(lm * sc > m_run + slack)) return;
   const float mx = fmaxf(lm, other_half(lm)) * sc;
-  const bool up = mx > m_run + kQLazy;
-  const float to = mx - kQHead;
+  const bool up = mx > m_run + slack;
+  const float to = mx - kQBelow<PIECES>;
   if (!first) {
     const float alpha = !up ? 1.f : m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - to);
     l_run *= alpha;
@@ -562,9 +565,9 @@ attn_quant_kernel(QuantAttnArgs a) {
         for (int i = 0; i < 16; ++i) acc[fb][i] = 0.f;
     };
     // (a segment's first tile has a token in every column: m_run is finite then)
-    auto attend = [&](int t, f32x16_t (&s)[2]) {
+    auto attend = [&](auto form, int t, f32x16_t (&s)[2]) {
       if (t + 64 > cur.t1) mask_from(s, cur.t1 - t - 32 * hh);
-      move_max(lane_max(s), sc, t == cur.t0, m_run, l_run, acc);
+      move_ref<decltype(form)::value>(lane_max(s), sc, t == cur.t0, m_run, l_run, acc);
     };
     start();
     bool again = false;
@@ -582,7 +585,7 @@ attn_quant_kernel(QuantAttnArgs a) {
         load_q(nxt);
         asm volatile("" ::: "memory");
       }
-      attend(t, s);
+      attend(std::integral_constant<int, kQForm<OUT_F32>>{}, t, s);
       if (!OUT_F32 && !__all(half_scales<FB>(x.vs))) again = true;
       else l_run += x.template weigh<kQForm<OUT_F32>>(s, sc, m_run, acc);
       asm volatile("" ::: "memory");
@@ -610,7 +613,7 @@ attn_quant_kernel(QuantAttnArgs a) {
         x.load_k(r, o);
         x.load_v(r, o);
         x.logits(qf, s);
-        attend(t, s);
+        attend(std::integral_constant<int, 2>{}, t, s);
         l_run += x.template weigh<2>(s, sc, m_run, acc);
         t += 64;
       } while (t < cur.t1);
@@ -633,7 +636,7 @@ attn_quant_kernel(QuantAttnArgs a) {
     if (row >= 0) {
       // (the row's reference moves as a unit's does, so that most merges add only)
       const float mo = m_acc[row], lo = l_acc[row];
-      const bool up = m_run > mo + kQLazy;
+      const bool up = m_run > mo + (OUT_F32 || again ? 8.f : kQSlack<0>);
       const float mn = up ? m_run : mo;
       const float fa = up && mo != -INFINITY ? __builtin_amdgcn_exp2f(mo - mn) : 1.f;
       const float fc = __builtin_amdgcn_exp2f(m_run - mn);
@@ -800,11 +803,11 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   // one tile's logits into weights; returns the reference of their exponents
   // (a row that is not adjacent: every weight 2^-inf = 0; its logits are set to
   // -inf only where they may be no numbers or +inf, which spares 32 selects a tile)
-  auto attend = [&](const Place& w, uint32_t ks, f32x16_t (&s)[2]) -> float {
+  auto attend = [&](auto form, const Place& w, uint32_t ks, f32x16_t (&s)[2]) -> float {
     if (w.t + 64 > w.len) mask_from(s, w.len - w.t - 32 * hh);
     const bool adj = (mk >> w.j) & 1ull;
     if (large || __any((ks & 0x80808080u) != 0u)) mask_from(s, adj ? 32 : 0);
-    move_max(adj ? lane_max(s) : -INFINITY, sc, false, m_run, l_run, acc);
+    move_ref<decltype(form)::value>(adj ? lane_max(s) : -INFINITY, sc, false, m_run, l_run, acc);
     return adj ? m_run : INFINITY;
   };
   start();
@@ -815,7 +818,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   auto compute = [&](const Place& w, const QuantTile<D>& x) {
     f32x16_t s[2];
     x.logits(qf, s);
-    const float ref = attend(w, x.ks, s);
+    const float ref = attend(std::integral_constant<int, kQForm<OUT_F32>>{}, w, x.ks, s);
     if (!OUT_F32 && !__all(half_scales<FB>(x.vs))) again = true;
     else l_run += x.template weigh<kQForm<OUT_F32>>(s, sc, ref, acc);
   };
@@ -836,7 +839,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
       const uint8_t* r = pb.run.tile(pb.t, next);
       const auto o = xa.offsets(n, hh, next);
       xa.load_k(r, o);
-      const float ref = attend(pa, ks, s);
+      const float ref = attend(std::integral_constant<int, 3>{}, pa, ks, s);
       l_run += xa.template weigh<3>(s, sc, ref, acc);
       asm volatile("" ::: "memory");
       xa.load_v(r, o);
@@ -865,7 +868,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
       load(pa, xa);
       f32x16_t s[2];
       xa.logits(qf, s);
-      const float ref = attend(pa, xa.ks, s);
+      const float ref = attend(std::integral_constant<int, 2>{}, pa, xa.ks, s);
       l_run += xa.template weigh<2>(s, sc, ref, acc);
     }
   }

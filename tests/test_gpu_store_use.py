@@ -408,3 +408,23 @@ def test_unknown_activation_is_refused(B):
     W = torch.zeros(8, 64, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(ValueError, match="activation"):
         B.gather_dense(p, W[:1], B.pack_dense(p, W), 8, activation="tanh")
+
+
+@pytest.mark.parametrize("nq", [1, 200])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("o_f32", [False, True])
+def test_the_largest_values_do_not_overflow(B, nq, D, o_f32):
+    """Values near the largest held ones: the result is one of their averages."""
+    H, Ls = 4, [300, 40]
+    x = Held(B, Ls, H, H, D, 56, make=None)
+    x.V = (x.V.float() * 2.0 ** 124).clamp(-2.0 ** 127, 2.0 ** 127).to(x.dt)
+    x.write(B)
+    x.off, x.po, x.pb = cum(Ls * nq), dev(cum(Ls * nq)), dev(np.tile(x.blocks, nq))
+    Q = rows_of(5, H, D, 57)
+    nb = [[0, 1], [1], [], [0], [0, 1]]
+    O, lse = attend(B, x, Q.repeat(nq, 1, 1), nb * nq, [5] * nq, [2] * nq, 0.05, o_f32)
+    torch.cuda.synchronize()
+    O, lse = O.view(nq, 5, H, D), lse.view(nq, 5, H)
+    assert (O == O[:1]).all() and (lse == lse[:1]).all()
+    ref = reference(Q.double().numpy(), *x.held(cum(Ls)), nb, [5], [2], cum(Ls), 0.05, 1, o_f32)
+    check(O[0], lse[0], ref, o_f32, "largest values")
