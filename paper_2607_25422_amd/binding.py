@@ -336,7 +336,7 @@ def _on_current_device(*tensors) -> None:
     kernels run."""
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != dev:
+        if t is not None and t.get_device() != dev and t.is_cuda:
             raise ValueError(f"a tensor is on device {t.get_device()}, the current one is {dev}")
 
 

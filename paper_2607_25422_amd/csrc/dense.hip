@@ -511,10 +511,12 @@ static DenseShape dense_shape(int M, int d, int d_out) {
   // Tile height and parts by an estimate of the time in us.  Its figures are fitted to
   // 711 timings, heights from 96 on and up to 16 parts of 22 shapes of 97 to 4768 rows and
   // 136 to 16384 columns, weights warm; its picks were at most 7 % behind the fastest
-  // there and 4 % in 336 more of 6 shapes whose weights came from HBM.  A step
+  // there, 4 % in 336 more of 6 shapes whose weights came from HBM, and in 714 of 16
+  // shapes with and without GELU and residual 2 % on average, 14 % at most.  A step
   // costs a fixed 0.13 and per block of 32 rows 0.115 on an empty chip to 0.17 on a full
   // one (power; n tiles on the busiest CU, u the share of the others' work).  A tile's
-  // start and end are hidden in part where two workgroups share a CU (MB <= 4).  Parts
+  // start and end are hidden in part where two workgroups share a CU (MB <= 4);
+  // above, 1.7 a block stands for 1.08 and an activation's or a residual's share.  Parts
   // are written, read and added.  Every row tile reads the weights, through the L2s at
   // 41 TB/s.
   s.rows = false;
@@ -531,7 +533,7 @@ static DenseShape dense_shape(int M, int d, int d_out) {
       const double n = (double)((tiles * sp + kDnCUs - 1) / kDnCUs);
       const double u = (double)(tiles * sp) / (n * kDnCUs);
       double us = n * ((steps + sp - 1) / sp) * (0.127 + mb * (0.115 + 0.054 * u));
-      us += mb <= 4 ? 4.06 + 1.08 * mb * (0.27 + 0.73 * n) : n * (4.06 + 1.08 * mb);
+      us += mb <= 4 ? 4.06 + 1.08 * mb * (0.27 + 0.73 * n) : n * (4.06 + 1.7 * mb);
       if (sp > 1) us += 1.4 + (double)sp * M * d_out * 8.0 / 8.84e6;
       us += (double)((M + 32ll * mb - 1) / (32 * mb)) * d * d_out * 2.0 / 41e6;
       if (s.mb == 0 || us < best) {
