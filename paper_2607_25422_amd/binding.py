@@ -1152,7 +1152,7 @@ def bipartite_xattn_quant(p: SkipProblem, store: KvStore, rows, kept_offsets, pa
     """Stage 2 over a store.  ``rows``: the queries [total_kept, H, d_h], or V
     with ``kept_idx``.  The graph is built from ``passage_keys``, or ``edges`` =
     (rowptr, col) with p.total_edges columns.  Returns (O, lse); ``out`` = the two
-    preallocated."""
+    preallocated (lse None: not written)."""
     if out is None:
         dev = kept_offsets.device
         out = (torch.empty((max(p.total_kept, 1), p.H, p.d_h), dtype=_out_dtype(p), device=dev),
@@ -1164,7 +1164,7 @@ def bipartite_xattn_quant(p: SkipProblem, store: KvStore, rows, kept_offsets, pa
         kept_idx=kept_idx, edge_rows=edge_rows, passage_keys=passage_keys,
         passage_keep=passage_keep, edge_rowptr=None if edges is None else edges[0],
         edge_col=None if edges is None else edges[1], workspace=workspace)
-    return O[:p.total_kept], lse[:p.total_kept]
+    return O[:p.total_kept], None if lse is None else lse[:p.total_kept]
 
 
 # ---------------------------------------------------------------------------

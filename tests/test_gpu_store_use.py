@@ -428,3 +428,14 @@ def test_the_largest_values_do_not_overflow(B, nq, D, o_f32):
     assert (O == O[:1]).all() and (lse == lse[:1]).all()
     ref = reference(Q.double().numpy(), *x.held(cum(Ls)), nb, [5], [2], cum(Ls), 0.05, 1, o_f32)
     check(O[0], lse[0], ref, o_f32, "largest values")
+
+
+def test_outputs_given_without_lse(B):
+    x = Held(B, [40, 70], 2, 2, 64, 58)
+    x.write(B)
+    Q, nb = rows_of(6, 2, 64, 59), random_graph([6], [2], 60)
+    O = torch.full((9, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    got, none = attend(B, x, Q, nb, [6], [2], 0.2, out=(O, None))
+    want, _ = attend(B, x, Q, nb, [6], [2], 0.2)
+    torch.cuda.synchronize()
+    assert none is None and torch.equal(got, want) and (O[6:] == 7.0).all()
