@@ -188,24 +188,54 @@ __device__ __forceinline__ bool quant_item(const QuantAttnArgs& a, int L, QuantI
 }
 
 // Passages adjacent to a kept row, a bit each (of a given graph here, which saves
-// the launch that would write them: 2 us of 10 for one row).
-__device__ __forceinline__ uint64_t row_neighbours(const QuantAttnArgs& a, int row, int P) {
-  const uint64_t all = P < 64 ? (1ull << P) - 1ull : ~0ull;
-  if (!a.edge_rowptr) return a.rowmask[row] & all;
+// the launch that would write them: 2 us of 10 for one row).  In two steps, so that the
+// loads of the first are in flight with the caller's others.
+struct RowEdges {
+  uint64_t m;
   int e0, e1;
-  range_of(a.edge_rowptr, row, a.total_edges, e0, e1);
-  uint64_t m = 0;
-  constexpr int U = 8;                       // columns in flight
-  for (int e = e0; e < e1; e += U) {
-    int j[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) j[u] = a.edge_col[min(e + u, e1 - 1)];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (j[u] >= 0 && j[u] < P) m |= 1ull << j[u];
+  __device__ __forceinline__ void load(const QuantAttnArgs& a, int row) {
+    m = 0ull;
+    e0 = e1 = 0;
+    if (a.edge_rowptr) {
+      e0 = a.edge_rowptr[row];
+      e1 = a.edge_rowptr[row + 1];
+    } else {
+      m = a.rowmask[row];
+    }
   }
-  return m;
-}
+  __device__ __forceinline__ uint64_t passages(const QuantAttnArgs& a, int P) {
+    const uint64_t all = P < 64 ? (1ull << P) - 1ull : ~0ull;
+    if (!a.edge_rowptr) return m & all;
+    const int b = clampi(e0, 0, a.total_edges), c = clampi(e1, b, a.total_edges);
+    constexpr int U = 8;                     // columns in flight
+    for (int e = b; e < c; e += U) {
+      int j[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) j[u] = a.edge_col[min(e + u, c - 1)];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (j[u] >= 0 && j[u] < P) m |= 1ull << j[u];
+    }
+    return m;
+  }
+};
+// The question's passage of this lane (lane j: passage j), likewise.
+struct LanePassage {
+  int t0, t1, blk;
+  __device__ __forceinline__ void load(const QuantAttnArgs& a, const QuantItem& it) {
+    t0 = t1 = blk = 0;
+    const int j = (int)__lane_id();
+    if (j < it.P) {
+      t0 = a.passage_offsets[it.p0 + j];
+      t1 = a.passage_offsets[it.p0 + j + 1];
+      blk = a.passage_blocks[it.p0 + j];
+    }
+  }
+  __device__ __forceinline__ int tokens(const QuantAttnArgs& a) const {
+    const int b = clampi(t0, 0, a.total_tokens);
+    return clampi(t1, b, a.total_tokens) - b;
+  }
+};
 
 // A tile of 64 tokens: two records of a passage, as a lane holds them.
 template <int D>
@@ -422,15 +452,10 @@ attn_quant_kernel(QuantAttnArgs a) {
   const uint32_t recip_G = (65536u + (uint32_t)G - 1) / (uint32_t)G;   // v / G for v < 192, G <= 32
   auto over_G = [&](int v) -> int { return (int)(((uint32_t)v * recip_G) >> 16); };
 
-  // lane j: passage j (every wave the same)
-  int my_len = 0, my_blk = 0;
-  if (lane < P) {
-    int ts, te;
-    range_of(a.passage_offsets, it.p0 + lane, a.total_tokens, ts, te);
-    my_len = te - ts;
-    my_blk = a.passage_blocks[it.p0 + lane];
-  }
-  if (tid < it.nk) neighbours[tid] = row_neighbours(a, it.k0 + it.i0 + tid, P);
+  RowEdges edges;
+  if (tid < it.nk) edges.load(a, it.k0 + it.i0 + tid);
+  LanePassage passage;                      // (every wave the same)
+  passage.load(a, it);
   for (int i = tid; i < nv * (OS / 4); i += kQThreads)
     reinterpret_cast<float4*>(Oacc)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = tid; i < nv; i += kQThreads) {
@@ -438,6 +463,8 @@ attn_quant_kernel(QuantAttnArgs a) {
     l_acc[i] = 0.f;
   }
   if (tid == 0) merged = 0;
+  if (tid < it.nk) neighbours[tid] = edges.passages(a, P);
+  const int my_len = passage.tokens(a), my_blk = passage.blk;
   __syncthreads();
   // adjacent rows of each passage, every wave its share of the passages
   uint64_t mk[MW];
@@ -717,15 +744,10 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
 
   // this lane's row (past the item's rows: its last one, adjacent to nothing)
   const int v = min(n, nv - 1), i = v / G, hq = it.hk * G + (v - i * G);
-  uint64_t mk = row_neighbours(a, it.k0 + it.i0 + i, P);
-  // lane j: passage j
-  int my_len = 0, my_blk = 0;
-  if (lane < P) {
-    int ts, te;
-    range_of(a.passage_offsets, it.p0 + lane, a.total_tokens, ts, te);
-    my_len = te - ts;
-    my_blk = a.passage_blocks[it.p0 + lane];
-  }
+  RowEdges edges;
+  edges.load(a, it.k0 + it.i0 + i);
+  LanePassage passage;
+  passage.load(a, it);
   u32x4 qf[4 * KH];
   {
     const int kr = it.k0 + it.i0 + i;
@@ -738,7 +760,8 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
       for (int s = 0; s < 4; ++s)
         qf[4 * kh + s] = *reinterpret_cast<const u32x4*>(src + 64 * kh + 8 * s);
   }
-  if (n >= nv) mk = 0ull;
+  const uint64_t mk = n < nv ? edges.passages(a, P) : 0ull;
+  const int my_len = passage.tokens(a), my_blk = passage.blk;
   uint64_t U = mk;                           // passages adjacent to some row
 #pragma unroll
   for (int s = 1; s < 32; s <<= 1) U |= (uint64_t)__shfl_xor((unsigned long long)U, s, kWave);
