@@ -356,12 +356,20 @@ def _torch_stream(stream):
     return torch.cuda.ExternalStream(int(stream))
 
 
+def _record(t: torch.Tensor, stream) -> None:
+    """Records a call's stream on a tensor allocated for it, unless it is the
+    current one (None is)."""
+    if stream is None:
+        return
+    s = _torch_stream(stream)
+    if s != torch.cuda.current_stream():
+        t.record_stream(s)
+
+
 def _fresh_workspace(nbytes: int, device, stream=None) -> torch.Tensor:
     """A workspace allocated for one call on ``stream`` (see _ws)."""
     ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
-    s = _torch_stream(stream)
-    if s != torch.cuda.current_stream():
-        ws.record_stream(s)
+    _record(ws, stream)
     return ws
 
 
@@ -372,9 +380,7 @@ def _ws(p, workspace, stream=None):
     handing the memory to other work before they finish."""
     if workspace is None:
         workspace = new_workspace(p)
-        s = _torch_stream(stream)
-        if s != torch.cuda.current_stream():
-            workspace.record_stream(s)
+        _record(workspace, stream)
     return workspace, workspace.data_ptr(), workspace.numel()
 
 
@@ -1126,9 +1132,7 @@ def quantize_passages(p: SkipProblem, store: KvStore, Kh, Vh, passage_offsets, p
     if want_keys:
         keys = torch.empty((max(p.total_passages, 1), p.d), dtype=torch.float32,
                            device=store.data.device)
-        s = _torch_stream(stream)
-        if s != torch.cuda.current_stream():
-            keys.record_stream(s)
+        _record(keys, stream)
     skip_quantize_passages(p, store, Kh, Vh, passage_offsets, passage_blocks, keys, stream)
     return None if keys is None else keys[:p.total_passages]
 
