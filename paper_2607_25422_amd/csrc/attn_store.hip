@@ -341,15 +341,24 @@ struct QuantTile {
 // values are not goes over its tiles again with two bf16 pieces.  (A branch within the
 // loop would hold the registers of both forms.)
 //
-// Weights are 2^(logit - reference), in units of log2; a reference is set `below` under
-// the largest logit so far and kept until one exceeds it by `slack`.  Half floats: the
+// Weights are 2^(logit - reference), in units of log2.  Half floats: the reference is
+// set 7 under the largest logit so far and kept until one exceeds it by 15, so that the
 // largest weight is from 2^7 to 2^15, and small ones (normal from 2^-14, steps of 2^-24
-// below) are off by at most 2^-32 of it.  bf16 pieces: from 2^-24 to 2^-16, and with
-// the same slack of 2^8 when a unit is merged, so that the sum over many tokens of the
-// largest held values (2^127) stays finite.
+// below) are off by at most 2^-32 of it.  bf16 pieces: it is the largest logit, kept
+// until one exceeds it by 8.  A unit's reference may lag by that much, and the row's
+// that it is merged into by as much again: a weight is at most 2^16 of the row's, and
+// 2^31 of them with values below 2^67 sum to less than 2^114.  In a tile with larger
+// values the reference is 47 over the largest logit (weights of 2^-31 of the row's at
+// most, values below 2^127.6), so that those sums stay finite, too; it is not so
+// otherwise, since an exponent of that size is rounded in float32.
 template <bool OUT_F32> constexpr int kQForm = OUT_F32 ? 3 : 0;
-template <int PIECES> constexpr float kQBelow = PIECES ? -24.f : 7.f;
-template <int PIECES> constexpr float kQSlack = PIECES ? -16.f : 15.f;
+template <int PIECES> constexpr float kQBelow = PIECES ? 0.f : 7.f;
+template <int PIECES> constexpr float kQSlack = PIECES ? 8.f : 15.f;
+// Distance from the largest logit to the reference of a tile with these value scales
+// (of the lane): 47 where some are 2^65 or more (bytes from 192 on).
+__device__ __forceinline__ float over_largest(uint32_t vs) {
+  return __any((vs & (vs << 1) & 0x80808080u) != 0u) ? 47.f : 0.f;
+}
 
 // Logits of the tokens from `rem` on (of the lane's 32) as -inf.
 // (The asm holds the values in their branch: as selects in every tile the compiler
@@ -374,15 +383,16 @@ __device__ __forceinline__ float lane_max(const f32x16_t (&s)[2]) {
 }
 
 // The reference for the next weights (rarely moved: most tiles need no exchange or
-// rescale).  lm: the lane's largest logit; `first`: nothing is summed yet.
+// rescale).  lm: the lane's largest logit; over: over_largest of the tile; `first`:
+// nothing is summed yet.
 template <int PIECES, int FB>
-__device__ __forceinline__ void move_ref(float lm, float sc, bool first, float& m_run,
-                                         float& l_run, f32x16_t (&acc)[FB]) {
-  constexpr float slack = kQSlack<PIECES>;
+__device__ __forceinline__ void move_ref(float lm, float sc, float over, bool first,
+                                         float& m_run, float& l_run, f32x16_t (&acc)[FB]) {
+  const float slack = kQSlack<PIECES> - over;
   if (!__any(lm * sc > m_run + slack)) return;
   const float mx = fmaxf(lm, other_half(lm)) * sc;
   const bool up = mx > m_run + slack;
-  const float to = mx - kQBelow<PIECES>;
+  const float to = mx - (kQBelow<PIECES> - over);
   if (!first) {
     const float alpha = !up ? 1.f : m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - to);
     l_run *= alpha;
@@ -593,8 +603,9 @@ attn_quant_kernel(QuantAttnArgs a) {
     };
     // (a segment's first tile has a token in every column: m_run is finite then)
     auto attend = [&](auto form, int t, f32x16_t (&s)[2]) {
+      constexpr int F = decltype(form)::value;
       if (t + 64 > cur.t1) mask_from(s, cur.t1 - t - 32 * hh);
-      move_ref<decltype(form)::value>(lane_max(s), sc, t == cur.t0, m_run, l_run, acc);
+      move_ref<F>(lane_max(s), sc, F ? over_largest(x.vs) : 0.f, t == cur.t0, m_run, l_run, acc);
     };
     start();
     bool again = false;
@@ -663,7 +674,7 @@ attn_quant_kernel(QuantAttnArgs a) {
     if (row >= 0) {
       // (the row's reference moves as a unit's does, so that most merges add only)
       const float mo = m_acc[row], lo = l_acc[row];
-      const bool up = m_run > mo + (OUT_F32 || again ? 8.f : kQSlack<0>);
+      const bool up = m_run > mo + (OUT_F32 || again ? kQSlack<2> : kQSlack<0>);
       const float mn = up ? m_run : mo;
       const float fa = up && mo != -INFINITY ? __builtin_amdgcn_exp2f(mo - mn) : 1.f;
       const float fc = __builtin_amdgcn_exp2f(m_run - mn);
@@ -826,11 +837,14 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   // one tile's logits into weights; returns the reference of their exponents
   // (a row that is not adjacent: every weight 2^-inf = 0; its logits are set to
   // -inf only where they may be no numbers or +inf, which spares 32 selects a tile)
-  auto attend = [&](auto form, const Place& w, uint32_t ks, f32x16_t (&s)[2]) -> float {
+  auto attend = [&](auto form, const Place& w, uint32_t ks, uint32_t vs,
+                    f32x16_t (&s)[2]) -> float {
+    constexpr int F = decltype(form)::value;
     if (w.t + 64 > w.len) mask_from(s, w.len - w.t - 32 * hh);
     const bool adj = (mk >> w.j) & 1ull;
     if (large || __any((ks & 0x80808080u) != 0u)) mask_from(s, adj ? 32 : 0);
-    move_ref<decltype(form)::value>(adj ? lane_max(s) : -INFINITY, sc, false, m_run, l_run, acc);
+    move_ref<F>(adj ? lane_max(s) : -INFINITY, sc, F ? over_largest(vs) : 0.f, false, m_run, l_run,
+                acc);
     return adj ? m_run : INFINITY;
   };
   start();
@@ -841,7 +855,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   auto compute = [&](const Place& w, const QuantTile<D>& x) {
     f32x16_t s[2];
     x.logits(qf, s);
-    const float ref = attend(std::integral_constant<int, kQForm<OUT_F32>>{}, w, x.ks, s);
+    const float ref = attend(std::integral_constant<int, kQForm<OUT_F32>>{}, w, x.ks, x.vs, s);
     if (!OUT_F32 && !__all(half_scales<FB>(x.vs))) again = true;
     else l_run += x.template weigh<kQForm<OUT_F32>>(s, sc, ref, acc);
   };
@@ -862,7 +876,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
       const uint8_t* r = pb.run.tile(pb.t, next);
       const auto o = xa.offsets(n, hh, next);
       xa.load_k(r, o);
-      const float ref = attend(std::integral_constant<int, 3>{}, pa, ks, s);
+      const float ref = attend(std::integral_constant<int, 3>{}, pa, ks, xa.vs, s);
       l_run += xa.template weigh<3>(s, sc, ref, acc);
       asm volatile("" ::: "memory");
       xa.load_v(r, o);
@@ -891,7 +905,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
       load(pa, xa);
       f32x16_t s[2];
       xa.logits(qf, s);
-      const float ref = attend(std::integral_constant<int, 2>{}, pa, xa.ks, s);
+      const float ref = attend(std::integral_constant<int, 2>{}, pa, xa.ks, xa.vs, s);
       l_run += xa.template weigh<2>(s, sc, ref, acc);
     }
   }
