@@ -531,9 +531,8 @@ skip_status_t skip_workspace_bytes_quant(const skip_problem_t* p, const skip_kv_
  * Stage 2 over the store: skip_bipartite_xattn with the keys and values that the
  * store holds.  bf16 rows (SKIP_ERR_UNSUPPORTED otherwise); O bf16, or float with
  * o_f32.  Logits and sums are float32 and the held values enter exactly.  Softmax
- * weights enter the product with V for float output to 2^-24 relative; for bf16
- * output as half floats, to 2^-11 relative or 2^-32 of the row's largest, or where a
- * tile's held values are no half floats to 2^-16 relative.
+ * weights enter the product with V as pairs of bf16 values (to 2^-16 relative), for
+ * float output as three (2^-24).
  *   rows            kept_idx NULL: queries [total_kept][H][d_h]; else V [B][N][d],
  *                   row r of question b being V[b][kept_idx[r]]
  *   edge_rows       [total_kept][d] bf16 rows to cut the graph on, or NULL: `rows`

@@ -66,30 +66,6 @@ __device__ __forceinline__ u32x4 expand8(uint32_t codes, float scale) {
       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
 }
 
-// The same as half floats (exact where half_scales holds for the scale).
-typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ u32x4 expand8_half(uint32_t codes, float scale) {
-  return u32x4{
-      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0)),
-      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1)),
-      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2)),
-      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3))};
-}
-__device__ __forceinline__ f32x16_t mfma32_half(const u32x4& a, const u32x4& b, f32x16_t c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a),
-                                                __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-}
-// Whether N scale bytes are all from 112 to 139, 2^-15 to 2^12: held values of 2^-16
-// to 24576, which are half floats (normal and below).
-template <int N>
-__device__ __forceinline__ bool half_scales(uint32_t scales) {
-  bool ok = true;
-#pragma unroll
-  for (int b = 0; b < N; ++b) ok &= ((scales >> (8 * b)) & 0xffu) - 112u <= 27u;
-  return ok;
-}
-
 // Adds one to an LDS counter for the whole wave.  The wave barriers keep the branch
 // on lane 0 to itself: without them the compiler may join it with another one like
 // it across a loop's back edge, and the other lanes run ahead.
@@ -293,67 +269,56 @@ struct QuantTile {
   }
   // Weights 2^(sc s - ref), O^T += V^T . P^T; returns the lane's sum of them.  A
   // weight enters as a sum of PIECES bf16 values, all but the last truncated (the
-  // rest is exact), or as one half float (PIECES 0).
+  // rest is exact).
   template <int PIECES>
   __device__ __forceinline__ float weigh(const f32x16_t (&s)[2], float sc, float ref,
                                             f32x16_t (&acc)[FB]) const {
-    constexpr int NP = PIECES ? PIECES : 1;
     float ls = 0.f;
     unrolled<4>([&](auto q_) {
       constexpr int q = decltype(q_)::value, h = q >> 1, i0 = 8 * (q & 1);
-      u32x4 pc[NP];
+      u32x4 pc[PIECES];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float p0 = __builtin_amdgcn_exp2f(fmaf(s[h][i0 + 2 * e], sc, -ref));
         float p1 = __builtin_amdgcn_exp2f(fmaf(s[h][i0 + 2 * e + 1], sc, -ref));
         ls += p0 + p1;
 #pragma unroll
-        for (int c = 0; c + 1 < NP; ++c) {
+        for (int c = 0; c + 1 < PIECES; ++c) {
           const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
           pc[c][e] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
           p0 -= __uint_as_float(b0 & 0xffff0000u);
           p1 -= __uint_as_float(b1 & 0xffff0000u);
         }
-        pc[NP - 1][e] = PIECES ? pack2_bf16(p0, p1)
-                               : __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)p0, (_Float16)p1});
+        pc[PIECES - 1][e] = pack2_bf16(p0, p1);
       }
       unrolled<FB>([&](auto fb_) {
         constexpr int fb = decltype(fb_)::value;
-        if constexpr (PIECES == 0) {
-          acc[fb] = mfma32_half(expand8_half(v[fb][q], scale_of<fb>(vs)), pc[0], acc[fb]);
-        } else {
-          const u32x4 va = expand8(v[fb][q], scale_of<fb>(vs));
+        const u32x4 va = expand8(v[fb][q], scale_of<fb>(vs));
 #pragma unroll
-          for (int c = 0; c < PIECES; ++c) acc[fb] = mfma32_bf16(va, pc[c], acc[fb]);
-        }
+        for (int c = 0; c < PIECES; ++c) acc[fb] = mfma32_bf16(va, pc[c], acc[fb]);
       });
       // (the pieces of one product at a time in registers)
-      if (PIECES > 1) __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_sched_barrier(0);
     });
     return ls;
   }
 };
 
-// How softmax weights enter the second product.  Float output: three bf16 pieces.
-// bf16 output: one half float (2^-11 relative, an eighth of the output's own rounding)
-// as long as the held values are half floats, which saves a third of the matrix
-// products and a seventh of the vector instructions; a wave that meets a tile whose
-// values are not goes over its tiles again with two bf16 pieces.  (A branch within the
-// loop would hold the registers of both forms.)
+// bf16 pieces of a softmax weight in the second product: two for bf16 output (2^-16
+// relative, as in the attention over bf16 passages), three for float output (2^-24).
+// One half float a weight (2^-11) would spare bf16 output a third of the products and a
+// seventh of the vector instructions (the case above 99 us, 115 with two pieces), but
+// not an average that cancels: its own rounding is then far below a weight's.
 //
-// Weights are 2^(logit - reference), in units of log2.  Half floats: the reference is
-// set 7 under the largest logit so far and kept until one exceeds it by 15, so that the
-// largest weight is from 2^7 to 2^15, and small ones (normal from 2^-14, steps of 2^-24
-// below) are off by at most 2^-32 of it.  bf16 pieces: it is the largest logit, kept
-// until one exceeds it by 8.  A unit's reference may lag by that much, and the row's
-// that it is merged into by as much again: a weight is at most 2^16 of the row's, and
-// 2^31 of them with values below 2^67 sum to less than 2^114.  In a tile with larger
-// values the reference is 47 over the largest logit (weights of 2^-31 of the row's at
-// most, values below 2^127.6), so that those sums stay finite, too; it is not so
-// otherwise, since an exponent of that size is rounded in float32.
-template <bool OUT_F32> constexpr int kQForm = OUT_F32 ? 3 : 0;
-template <int PIECES> constexpr float kQBelow = PIECES ? 0.f : 7.f;
-template <int PIECES> constexpr float kQSlack = PIECES ? 8.f : 15.f;
+// Weights are 2^(logit - reference), in units of log2; the reference is the largest
+// logit so far, kept until one exceeds it by 8.  A unit's reference may lag by that much,
+// and the row's that it is merged into by as much again: a weight is at most 2^16 of the
+// row's, and 2^31 of them with values below 2^67 sum to less than 2^114.  In a tile with
+// larger values the reference is 47 over the largest logit (weights of 2^-31 of the
+// row's at most, values below 2^127.6), so that those sums stay finite, too; it is not
+// so otherwise, since an exponent of that size is rounded in float32.
+template <bool OUT_F32> constexpr int kQPieces = OUT_F32 ? 3 : 2;
+constexpr float kQSlack = 8.f;
 // Distance from the largest logit to the reference of a tile with these value scales
 // (of the lane): 47 where some are 2^65 or more (bytes from 192 on).
 __device__ __forceinline__ float over_largest(uint32_t vs) {
@@ -385,14 +350,14 @@ __device__ __forceinline__ float lane_max(const f32x16_t (&s)[2]) {
 // The reference for the next weights (rarely moved: most tiles need no exchange or
 // rescale).  lm: the lane's largest logit; over: over_largest of the tile; `first`:
 // nothing is summed yet.
-template <int PIECES, int FB>
+template <int FB>
 __device__ __forceinline__ void move_ref(float lm, float sc, float over, bool first,
                                          float& m_run, float& l_run, f32x16_t (&acc)[FB]) {
-  const float slack = kQSlack<PIECES> - over;
+  const float slack = kQSlack - over;
   if (!__any(lm * sc > m_run + slack)) return;
   const float mx = fmaxf(lm, other_half(lm)) * sc;
   const bool up = mx > m_run + slack;
-  const float to = mx - (kQBelow<PIECES> - over);
+  const float to = mx + over;
   if (!first) {
     const float alpha = !up ? 1.f : m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - to);
     l_run *= alpha;
@@ -592,27 +557,16 @@ attn_quant_kernel(QuantAttnArgs a) {
     for (int i = 0; i < 4 * KH; ++i) asm volatile("" : "+v"(qf[i]));
     negate_q();
     f32x16_t acc[FB];
-    float m_run, l_run;
-    auto start = [&]() {
-      m_run = -INFINITY;
-      l_run = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-      for (int fb = 0; fb < FB; ++fb)
+    for (int fb = 0; fb < FB; ++fb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[fb][i] = 0.f;
-    };
-    // (a segment's first tile has a token in every column: m_run is finite then)
-    auto attend = [&](auto form, int t, f32x16_t (&s)[2]) {
-      constexpr int F = decltype(form)::value;
-      if (t + 64 > cur.t1) mask_from(s, cur.t1 - t - 32 * hh);
-      move_ref<F>(lane_max(s), sc, F ? over_largest(x.vs) : 0.f, t == cur.t0, m_run, l_run, acc);
-    };
-    start();
-    bool again = false;
+      for (int i = 0; i < 16; ++i) acc[fb][i] = 0.f;
     int t = cur.t0;
     // one tile; the next one's keys (`r`) land during the softmax and the second
     // product, its values during the next logits, and with a unit's last tile the
     // next unit's queries
+    // (a segment's first tile has a token in every column: m_run is finite then)
     auto step = [&](auto last, const uint8_t* r, uint32_t next) {
       f32x16_t s[2];
       x.logits(qf, s);
@@ -623,45 +577,21 @@ attn_quant_kernel(QuantAttnArgs a) {
         load_q(nxt);
         asm volatile("" ::: "memory");
       }
-      attend(std::integral_constant<int, kQForm<OUT_F32>>{}, t, s);
-      if (!OUT_F32 && !__all(half_scales<FB>(x.vs))) again = true;
-      else l_run += x.template weigh<kQForm<OUT_F32>>(s, sc, m_run, acc);
+      if (t + 64 > cur.t1) mask_from(s, cur.t1 - t - 32 * hh);
+      move_ref(lane_max(s), sc, over_largest(x.vs), t == cur.t0, m_run, l_run, acc);
+      l_run += x.template weigh<kQPieces<OUT_F32>>(s, sc, m_run, acc);
       asm volatile("" ::: "memory");
       x.load_v(r, o);
       t += 64;
     };
     uint32_t next;
-    while (t + 64 < cur.t1 && !again) {
+    while (t + 64 < cur.t1) {
       const uint8_t* r = cur.run.tile(t + 64, next);
       step(std::false_type{}, r, next);
     }
-    if (!again) {                            // (for an empty segment, too: masked)
+    {                                        // (for an empty segment, too: masked)
       const uint8_t* r = nxt.run.tile(nxt.t0, next);
       step(std::true_type{}, r, next);
-    }
-    if (!OUT_F32 && again) {
-      load_q(cur);
-      start();
-      t = cur.t0;
-      negate_q();
-      do {
-        f32x16_t s[2];
-        const uint8_t* r = cur.run.tile(t, next);
-        const auto o = x.offsets(n, hh, next);
-        x.load_k(r, o);
-        x.load_v(r, o);
-        x.logits(qf, s);
-        attend(std::integral_constant<int, 2>{}, t, s);
-        l_run += x.template weigh<2>(s, sc, m_run, acc);
-        t += 64;
-      } while (t < cur.t1);
-      const uint8_t* r = nxt.run.tile(nxt.t0, next);
-      const auto o = x.offsets(n, hh, next);
-      x.load_k(r, o);
-      load_q(nxt);
-      asm volatile("" ::: "memory");
-      x.load_v(r, o);
-      asm volatile("" ::: "memory");
     }
 
     // merge in the order of the list: every unit of earlier passages and
@@ -674,7 +604,7 @@ attn_quant_kernel(QuantAttnArgs a) {
     if (row >= 0) {
       // (the row's reference moves as a unit's does, so that most merges add only)
       const float mo = m_acc[row], lo = l_acc[row];
-      const bool up = m_run > mo + (OUT_F32 || again ? kQSlack<2> : kQSlack<0>);
+      const bool up = m_run > mo + kQSlack;
       const float mn = up ? m_run : mo;
       const float fa = up && mo != -INFINITY ? __builtin_amdgcn_exp2f(mo - mn) : 1.f;
       const float fc = __builtin_amdgcn_exp2f(m_run - mn);
@@ -825,89 +755,44 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
       qm = max(qm, max((qf[e][c] & 0x7fffu) << 16, qf[e][c] & 0x7fff0000u));
   const bool large = __any(qm >= (227u << 23));
   f32x16_t acc[FB];
-  float m_run, l_run;
-  auto start = [&]() {
-    m_run = -INFINITY;
-    l_run = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-    for (int fb = 0; fb < FB; ++fb)
+  for (int fb = 0; fb < FB; ++fb)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[fb][e] = 0.f;
-  };
-  // one tile's logits into weights; returns the reference of their exponents
+    for (int e = 0; e < 16; ++e) acc[fb][e] = 0.f;
+  QuantTile<D> x;
+  // its logits into weights; returns the reference of their exponents
   // (a row that is not adjacent: every weight 2^-inf = 0; its logits are set to
   // -inf only where they may be no numbers or +inf, which spares 32 selects a tile)
-  auto attend = [&](auto form, const Place& w, uint32_t ks, uint32_t vs,
-                    f32x16_t (&s)[2]) -> float {
-    constexpr int F = decltype(form)::value;
+  auto attend = [&](const Place& w, uint32_t ks, f32x16_t (&s)[2]) -> float {
     if (w.t + 64 > w.len) mask_from(s, w.len - w.t - 32 * hh);
     const bool adj = (mk >> w.j) & 1ull;
     if (large || __any((ks & 0x80808080u) != 0u)) mask_from(s, adj ? 32 : 0);
-    move_ref<F>(adj ? lane_max(s) : -INFINITY, sc, F ? over_largest(vs) : 0.f, false, m_run, l_run,
-                acc);
+    move_ref(adj ? lane_max(s) : -INFINITY, sc, over_largest(x.vs), false, m_run, l_run, acc);
     return adj ? m_run : INFINITY;
   };
-  start();
-  // two tiles in turn: one's loads are in flight while the other is computed
-  Place pa, pb;
-  QuantTile<D> xa, xb;
-  bool again = false;
-  auto compute = [&](const Place& w, const QuantTile<D>& x) {
+  // one tile in registers; the next one's keys land during the softmax, its values
+  // during the next logits
+  Place w, nw;
+  int c = x0 + wave;
+  if (c < x1) {
+    place(c, w);
+    load(w, x);
+  }
+  for (; c < x1; c += kQTileWaves) {
     f32x16_t s[2];
     x.logits(qf, s);
-    const float ref = attend(std::integral_constant<int, kQForm<OUT_F32>>{}, w, x.ks, x.vs, s);
-    if (!OUT_F32 && !__all(half_scales<FB>(x.vs))) again = true;
-    else l_run += x.template weigh<kQForm<OUT_F32>>(s, sc, ref, acc);
-  };
-  int c = x0 + wave;
-  if constexpr (OUT_F32 && D == 128) {
-    // (two tiles and three pieces of the weights exceed the registers: the next
-    // keys land during the softmax instead, as in the form above)
-    if (c < x1) {
-      place(c, pa);
-      load(pa, xa);
-    }
-    for (; c < x1; c += kQTileWaves) {
-      f32x16_t s[2];
-      xa.logits(qf, s);
-      const uint32_t ks = xa.ks;
-      place(min(c + kQTileWaves, x1 - 1), pb);
-      uint32_t next;
-      const uint8_t* r = pb.run.tile(pb.t, next);
-      const auto o = xa.offsets(n, hh, next);
-      xa.load_k(r, o);
-      const float ref = attend(std::integral_constant<int, 3>{}, pa, ks, xa.vs, s);
-      l_run += xa.template weigh<3>(s, sc, ref, acc);
-      asm volatile("" ::: "memory");
-      xa.load_v(r, o);
-      pa = pb;
-    }
-  } else if (c < x1) {
-    place(c, pa);
-    load(pa, xa);
-    for (;;) {
-      c += kQTileWaves;
-      place(min(c, x1 - 1), pb);             // (past the last tile: one that is not used)
-      load(pb, xb);
-      compute(pa, xa);
-      if (c >= x1) break;
-      c += kQTileWaves;
-      place(min(c, x1 - 1), pa);
-      load(pa, xa);
-      compute(pb, xb);
-      if (c >= x1) break;
-    }
-  }
-  if (!OUT_F32 && again) {
-    start();
-    for (c = x0 + wave; c < x1; c += kQTileWaves) {
-      place(c, pa);
-      load(pa, xa);
-      f32x16_t s[2];
-      xa.logits(qf, s);
-      const float ref = attend(std::integral_constant<int, 2>{}, pa, xa.ks, xa.vs, s);
-      l_run += xa.template weigh<2>(s, sc, ref, acc);
-    }
+    const uint32_t ks = x.ks;
+    place(min(c + kQTileWaves, x1 - 1), nw);   // (past the last tile: one that is not used)
+    uint32_t next;
+    const uint8_t* r = nw.run.tile(nw.t, next);
+    const auto o = x.offsets(n, hh, next);
+    x.load_k(r, o);
+    const float ref = attend(w, ks, s);
+    l_run += x.template weigh<kQPieces<OUT_F32>>(s, sc, ref, acc);
+    asm volatile("" ::: "memory");
+    x.load_v(r, o);
+    w = nw;
   }
 
   const float l_tot = l_run + other_half(l_run);

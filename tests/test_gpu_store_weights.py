@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_store import Held, attend, check, cum, dev, reference, say
+from test_gpu_store import Held, attend, check, cum, dev, reference, rows_of, say
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +50,63 @@ def test_rising_logits_over_the_largest_values(B, nq, D, o_f32):
     ref = reference(Q.double().numpy(), x.K.double().numpy(), V, nb, [n], [2], cum(Ls),
                     math.log(2), 1, o_f32)
     check(O[0], lse[0], ref, o_f32, "rising logits")
+
+
+@pytest.mark.parametrize("nq", [1, 200])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("o_f32", [False, True])
+def test_weights_of_averages_that_cancel(B, nq, D, o_f32):
+    """Two tokens of values a and -b, their weights b to a as near as a query of three
+    bf16 features says it: the average is near 0, so that a bf16 output has steps far
+    below a weight's error of 2^-16 of itself (the bound of `reference`, which takes
+    the values' magnitude for the size of that error)."""
+    H = 4
+    pairs = [(3.0, 1.0), (3.0, 2.0), (6.0, 1.0), (6.0, 4.0), (6.0, 0.5), (1.5, 0.5)]
+    Ls, n = [2] * len(pairs), len(pairs)
+    x = Held(B, Ls, H, H, D, 61)
+    x.K, x.V = torch.zeros_like(x.K), torch.zeros_like(x.V)
+    x.K[0::2, :, :3] = 1.0
+    Q = torch.zeros(n, H, D)
+    for i, (a, b) in enumerate(pairs):
+        x.V[2 * i], x.V[2 * i + 1] = a, -b
+        z = math.log(b / a)
+        for f in range(3):
+            Q[i, :, f] = torch.tensor(z).bfloat16().float()
+            z -= float(Q[i, 0, f])
+    Q = Q.bfloat16()
+    x.write(B)
+    K, V = x.held1()
+    assert np.array_equal(K, x.K.double().numpy()) and np.array_equal(V, x.V.double().numpy())
+    batch(x, Ls, nq)
+    nb = [[i] for i in range(n)]
+    say(f"weights of averages that cancel nq={nq} D={D} f32={o_f32}")
+    O, lse = attend(B, x, Q.repeat(nq, 1, 1), nb * nq, [n] * nq, [n] * nq, 1.0, o_f32)
+    torch.cuda.synchronize()
+    O, lse = O.view(nq, n, H, D), lse.view(nq, n, H)
+    assert (O == O[:1]).all() and (lse == lse[:1]).all()
+    ref = reference(Q.double().numpy(), K, V, nb, [n], [n], cum(Ls), 1.0, 1, o_f32,
+                    piece=2.0 ** -24 if o_f32 else 2.0 ** -16)
+    check(O[0], lse[0], ref, o_f32, "cancelling")
+
+
+@pytest.mark.parametrize("nq", [1, 200])
+@pytest.mark.parametrize("D", [64, 128])
+def test_zero_features_leave_the_others_as_they_are(B, nq, D):
+    """Heads padded by features of zeros: the other features' bits and the LSE are
+    those without them."""
+    H, Ls, k = 4, [70, 33, 128], 9
+    nb = [[0, 2], [1], [], [0, 1, 2], [2], [0], [1, 2], [0, 1], [2]]
+    Q = rows_of(k, H, D, 63).repeat(nq, 1, 1)
+    got = []
+    for pad in (False, True):
+        x = Held(B, Ls, H, H, D, 64)
+        if pad:
+            x.V = x.V.clone()
+            x.V[:, :, D // 2:] = 0.0
+        x.write(B)
+        batch(x, Ls, nq)
+        got.append(attend(B, x, Q, nb * nq, [k] * nq, [3] * nq, 0.3))
+    torch.cuda.synchronize()
+    (O, lse), (P, plse) = got
+    assert torch.equal(O[:, :, :D // 2], P[:, :, :D // 2]) and torch.equal(lse, plse)
+    assert not P[:, :, D // 2:].any()
