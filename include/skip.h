@@ -523,7 +523,10 @@ skip_status_t skip_dequantize_passages(const skip_problem_t* p, const skip_kv_st
                                        const int32_t* passage_blocks, void* Kh, void* Vh,
                                        void* stream);
 
-/* Workspace of skip_bipartite_xattn_quant (host-only). */
+/* Workspace of skip_bipartite_xattn_quant (host-only).  Both calls refuse batches of
+ * more than 2^22 workgroups (SKIP_ERR_UNSUPPORTED): 8 ceil(B * H_kv / 8) of them for
+ * each chunk of a question's k_max rows (192 / (H / H_kv) rows or more; 32 in place of
+ * 192 in batches of fewer than 768 blocks of 32 rows and heads). */
 skip_status_t skip_workspace_bytes_quant(const skip_problem_t* p, const skip_kv_store_t* store,
                                          size_t* bytes);
 
@@ -599,7 +602,8 @@ skip_status_t skip_pack_dense(const skip_problem_t* p, const void* W, int32_t d_
  *                 bf16, and overlaps no other argument
  *   workspace     skip_workspace_bytes_dense bytes (0 for most sizes: it may then be
  *                 NULL), 16-byte aligned
- * Of the problem dtype, B, N, d, k_max and total_kept are used.
+ * Of the problem dtype, B, N, d, k_max and total_kept are used.  More than 2^22
+ * workgroups, each 64 to 256 rows by 256 columns, are SKIP_ERR_UNSUPPORTED.
  */
 skip_status_t skip_workspace_bytes_dense(const skip_problem_t* p, int32_t d_out, size_t* bytes);
 skip_status_t skip_gather_dense(const skip_problem_t* p, const void* rows,

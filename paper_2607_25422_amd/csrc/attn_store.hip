@@ -931,6 +931,15 @@ static QuantShape quant_shape(const skip_problem_t& p, int heads_kv) {
 
 bool quant_group_ok(int G) { return G >= 1 && G <= 32; }
 
+// Workgroups of the attention's launch (a question's and key head's follow one another on
+// one XCD), and whether one grid dimension holds them.
+static long long quant_workgroups(const skip_problem_t& p, int heads_kv, const QuantShape& s) {
+  return 8 * (((long long)p.B * heads_kv + 7) / 8) * s.chunks * s.splits;
+}
+bool quant_attn_fits(const skip_problem_t& p, int heads_kv) {
+  return quant_workgroups(p, heads_kv, quant_shape(p, heads_kv)) <= (1 << 22);
+}
+
 size_t quant_attn_scratch(const skip_problem_t& p, int heads_kv) {
   const QuantShape s = quant_shape(p, heads_kv);
   if (s.splits <= 1) return 0;
@@ -980,9 +989,7 @@ hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t
   a.P_max = p.P_max;
   a.o_f32 = p.o_f32;
   a.scale_log2 = p.sm_scale * kQLog2e;
-  const long long wgs = 8 * (((long long)a.groups + 7) / 8) * a.chunks * a.splits;
-  if (wgs > (1 << 22)) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)wgs);
+  const dim3 grid((unsigned)quant_workgroups(p, st.heads_kv, sh));
 #define SKIP_ATTN_QUANT(DD, FF)                                                            \
   do {                                                                                     \
     if (sh.tile)                                                                           \

@@ -546,6 +546,15 @@ static DenseShape dense_shape(int M, int d, int d_out) {
   return s;
 }
 
+// Workgroups of the layer's launch, and whether one grid dimension holds them.
+static long long dense_items(int M, int d_out, const DenseShape& s) {
+  const int width = s.rows ? 64 : kDnNT;
+  return ((long long)M + 32 * s.mb - 1) / (32 * s.mb) * ((d_out + width - 1) / width) * s.splits;
+}
+bool dense_fits(int M, int d, int d_out) {
+  return M <= 0 || dense_items(M, d_out, dense_shape(M, d, d_out)) <= (1 << 22);
+}
+
 size_t dense_scratch_bytes(int M, int d, int d_out) {
   if (M <= 0) return 0;
   const DenseShape s = dense_shape(M, d, d_out);
@@ -576,12 +585,8 @@ hipError_t launch_dense(const skip_problem_t& p, const void* rows, const int32_t
   if (a.M <= 0) return hipSuccess;
   const DenseShape s = dense_shape(a.M, a.d, d_out);
   a.splits = s.splits;
-  const int width = s.rows ? 64 : kDnNT;
-  const long long items = ((long long)a.M + 32 * s.mb - 1) / (32 * s.mb) *
-                          ((d_out + width - 1) / width) * s.splits;
-  if (items > (1 << 22)) return hipErrorInvalidValue;
-  a.n_items = (int)items;
-  const dim3 grid((unsigned)((items + 7) / 8 * 8));
+  a.n_items = (int)dense_items(a.M, d_out, s);
+  const dim3 grid((unsigned)((a.n_items + 7) / 8 * 8));
 #define SKIP_DENSE(MB) \
   hipLaunchKernelGGL(dense_tile_kernel<MB>, grid, dim3(kDnThreads), 0, st, a)
   if (s.rows) {

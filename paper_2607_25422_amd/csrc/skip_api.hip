@@ -599,6 +599,7 @@ static skip_status_t check_quant(const skip_problem_t* p, const skip_kv_store_t*
   st = check_store(p, store);
   if (st != SKIP_OK) return st;
   if (p->dtype != SKIP_BF16 || !quant_group_ok(p->H / store->heads_kv)) return SKIP_ERR_UNSUPPORTED;
+  if (!quant_attn_fits(*p, store->heads_kv)) return SKIP_ERR_UNSUPPORTED;
   return SKIP_OK;
 }
 
@@ -694,6 +695,7 @@ skip_status_t skip_workspace_bytes_dense(const skip_problem_t* p, int32_t d_out,
   skip_status_t st = check_dense(p, d_out);
   if (st != SKIP_OK) return st;
   if (p->total_kept < 0) return SKIP_ERR_INVALID_ARG;
+  if (!dense_fits(p->total_kept, p->d, d_out)) return SKIP_ERR_UNSUPPORTED;
   *bytes = dense_scratch_bytes(p->total_kept, p->d, d_out);
   return SKIP_OK;
 }
@@ -718,6 +720,7 @@ skip_status_t skip_gather_dense(const skip_problem_t* p, const void* rows,
     if (!kept_offsets || p->N < 1 || p->k_max < 0 || p->k_max > p->N) return SKIP_ERR_INVALID_ARG;
     if ((int64_t)p->B * p->N > INT32_MAX) return SKIP_ERR_UNSUPPORTED;
   }
+  if (!dense_fits(p->total_kept, p->d, d_out)) return SKIP_ERR_UNSUPPORTED;
   const size_t need = dense_scratch_bytes(p->total_kept, p->d, d_out);
   if (need > 0 && !workspace) return SKIP_ERR_INVALID_ARG;
   if (workspace_bytes < need) return SKIP_ERR_WORKSPACE;

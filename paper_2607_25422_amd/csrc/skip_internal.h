@@ -165,6 +165,7 @@ hipError_t launch_attention(const skip_problem_t& p, QuerySource q,
 // Layer after the attention -------------------------------------------------
 size_t dense_packed_bytes(int d, int d_out);
 size_t dense_scratch_bytes(int M, int d, int d_out);    // parts of a shared contraction
+bool dense_fits(int M, int d, int d_out);               // the launch's workgroups
 hipError_t launch_dense_pack(int d, int d_out, const void* W, void* packed, hipStream_t s);
 hipError_t launch_dense(const skip_problem_t& p, const void* rows, const int32_t* kept_offsets,
                         const int32_t* rows_idx, const void* packed, int d_out, const float* bias,
@@ -184,6 +185,7 @@ struct QuantGraph {
   const uint64_t* rowmask;            // neighbour masks of the kept rows, or
   const int32_t *rowptr, *col;        // a given graph (rowptr not NULL)
 };
+bool quant_attn_fits(const skip_problem_t& p, int heads_kv);        // the launch's workgroups
 size_t quant_attn_scratch(const skip_problem_t& p, int heads_kv);   // partials of split items
 hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t& st,
                                   QuerySource q, const int32_t* kept_offsets,
