@@ -481,7 +481,8 @@ skip_status_t skip_bipartite_xattn_proj(const skip_problem_t* p, const void* Qh,
  * A passage of L tokens takes ceil(L / 32) records in a row from its first,
  * passage_blocks[j]; several entries of a batch may name one stored passage.  A
  * record outside [0, n_blocks) is neither written nor read (results are then
- * unspecified).  d_h is the problem's.
+ * unspecified).  d_h is the problem's.  total_tokens is at most 2^31 - 128
+ * (SKIP_ERR_UNSUPPORTED past it).
  */
 typedef struct skip_kv_store {
   int32_t heads_kv;

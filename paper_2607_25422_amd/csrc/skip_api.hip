@@ -521,6 +521,8 @@ static skip_status_t check_store(const skip_problem_t* p, const skip_kv_store_t*
   if (!al16(st->data)) return SKIP_ERR_INVALID_ARG;
   if (p->d_h != 64 && p->d_h != 128) return SKIP_ERR_UNSUPPORTED;
   if (p->d > kMaxD) return SKIP_ERR_UNSUPPORTED;
+  // (a token's number plus a tile's stays below 2^31)
+  if (p->total_tokens > INT32_MAX - 127) return SKIP_ERR_UNSUPPORTED;
   // the longest passage has to fit
   if (p->total_passages > 0 && (int64_t)(p->L_max + 31) / 32 > st->n_blocks)
     return SKIP_ERR_INVALID_ARG;

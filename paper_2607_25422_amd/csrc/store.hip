@@ -77,6 +77,15 @@ __device__ __forceinline__ void values8(uint32_t codes, float scale, float (&x)[
   x[4] = c[0]; x[5] = c[1]; x[6] = d[0]; x[7] = d[1];
 }
 
+// First token of block i of the passage of tokens ts .. te - 1; false: the passage ends
+// before it.  (The blocks go by the longest passage, and ts + 32 i of another one may
+// pass 32 bits.)
+__host__ __device__ bool store_block(int ts, int te, int i, int& t0) {
+  if (i > (te - ts - 1) >> 5) return false;
+  t0 = ts + 32 * i;
+  return true;
+}
+
 // The work of a wave: record (passage j, block i of it, head h); false: none.
 struct StoreItem {
   int h, t0, te;        // head, first token and end of the passage (source rows)
@@ -89,9 +98,8 @@ __device__ __forceinline__ bool store_item(const StoreShape& a, long long item, 
   int ts, te;
   range_of(a.passage_offsets, j, a.total_tokens, ts, te);
   x.h = hg * kStoreWaves + (int)(threadIdx.x >> 6);
-  x.t0 = ts + 32 * i;
   x.te = te;
-  if (x.t0 >= te || x.h >= a.heads) return false;
+  if (!store_block(ts, te, i, x.t0) || x.h >= a.heads) return false;
   const long long blk = (long long)a.passage_blocks[j] + i;
   if (blk < 0 || blk >= a.n_blocks) return false;      // outside the store: not touched
   x.rec = (size_t)blk * a.heads + x.h;

@@ -64,3 +64,40 @@ def test_too_many_tiles_of_the_layer():
     a, b = call(1 << 23, 65536)                      # 8 388 608 x 65536: 2^23 tiles at least
     assert a == b() == B.SKIP_ERR_UNSUPPORTED
     assert call(1 << 20, 65536)[0] == B.SKIP_OK
+
+
+def test_token_numbers_near_the_end_of_32_bits():
+    """2^31 - 128 tokens are taken, more refused (by the same check as a passage that
+    does not fit its store, whose count of records must not wrap)."""
+    inv, uns = B.SKIP_ERR_INVALID_ARG, B.SKIP_ERR_UNSUPPORTED
+    top = (1 << 31) - 128
+    for n, n_blocks, want in ((top, top // 32, B.SKIP_OK), (top, top // 32 - 1, inv), (top, 1, inv),
+                              (top + 1, 1, uns), ((1 << 31) - 1, 1, uns),
+                              ((1 << 31) - 1, 1 << 26, uns)):
+        p = problem(H=1, L_max=n)
+        st = B.SkipKvStore(1, 0, n_blocks, FAKE)
+        size = ctypes.c_size_t(0)
+        assert B.LIB.skip_workspace_bytes_quant(ctypes.byref(p), ctypes.byref(st),
+                                                ctypes.byref(size)) == want, (n, n_blocks)
+        if want != B.SKIP_OK:
+            assert B.LIB.skip_quantize_passages(ctypes.byref(p), ctypes.byref(st), FAKE, FAKE,
+                                                FAKE, FAKE, None, None) == want
+            assert B.LIB.skip_dequantize_passages(ctypes.byref(p), ctypes.byref(st), FAKE, FAKE,
+                                                  FAKE, FAKE, None) == want
+
+
+def test_blocks_of_a_passage():
+    """The blocks that the store's kernels visit go by the batch's longest passage: those
+    past a shorter one's end are none of its, also where their token number would pass
+    32 bits."""
+    f = B.LIB["_ZN4skip11store_blockEiiiRi"]
+    f.restype, f.argtypes = ctypes.c_bool, [ctypes.c_int] * 3 + [ctypes.POINTER(ctypes.c_int)]
+    top = (1 << 31) - 128
+    cases = [(0, 0), (5, 5), (0, 1), (7, 39), (7, 40), (100, 197), (0, top), (top - 40, top),
+             (1 << 30, (1 << 30) + 33), (top, top)]
+    for ts, te in cases:
+        for i in {0, 1, 2, 3, 1 << 24, (1 << 25) + 2, (top - 1) // 32}:
+            t0 = ctypes.c_int(-1)
+            got = f(ts, te, i, ctypes.byref(t0))
+            assert got == (ts + 32 * i < te), (ts, te, i)
+            assert not got or t0.value == ts + 32 * i
