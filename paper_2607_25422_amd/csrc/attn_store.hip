@@ -481,9 +481,11 @@ attn_quant_kernel(QuantAttnArgs a) {
   my_first *= segs;
   const int u_end = blocks * segs;
 
-  const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;   // folded into the queries
-  // (not zero: masked logits stay -inf)
-  const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);
+  // a sign of the scale, and a scale of 0, are folded into the queries (masked logits
+  // stay -inf)
+  const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;
+  const bool flat = a.scale_log2 == 0.f;
+  const float sc = flat ? 1.f : fabsf(a.scale_log2);
 
   struct Unit {
     QuantRun run;
@@ -521,11 +523,11 @@ attn_quant_kernel(QuantAttnArgs a) {
       for (int s = 0; s < 4; ++s)
         qf[4 * kh + s] = *reinterpret_cast<const u32x4*>(src + 64 * kh + 8 * s);
   };
-  auto negate_q = [&]() {
-    if (neg)
+  auto sign_q = [&]() {
+    if (neg || flat)
 #pragma unroll
       for (int i = 0; i < 4 * KH; ++i) {
-        qf[i] ^= neg;
+        qf[i] = flat ? u32x4{0u, 0u, 0u, 0u} : qf[i] ^ neg;
         asm volatile("" : "+v"(qf[i]));      // (a branch)
       }
   };
@@ -555,7 +557,7 @@ attn_quant_kernel(QuantAttnArgs a) {
     // reach the tile's loads, too)
 #pragma unroll
     for (int i = 0; i < 4 * KH; ++i) asm volatile("" : "+v"(qf[i]));
-    negate_q();
+    sign_q();
     f32x16_t acc[FB];
     float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
@@ -719,9 +721,11 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   const int x0 = (int)((long long)tiles * it.split / a.splits);
   const int x1 = (int)((long long)tiles * (it.split + 1) / a.splits);
 
-  const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;   // folded into the queries
-  // (not zero: masked logits stay -inf)
-  const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);
+  // a sign of the scale, and a scale of 0, are folded into the queries (masked logits
+  // stay -inf)
+  const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;
+  const bool flat = a.scale_log2 == 0.f;
+  const float sc = flat ? 1.f : fabsf(a.scale_log2);
   struct Place {
     int j, t, len;
     QuantRun run;
@@ -742,7 +746,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
   };
 #pragma unroll
   for (int e = 0; e < 4 * KH; ++e) {
-    qf[e] ^= neg;
+    qf[e] = flat ? u32x4{0u, 0u, 0u, 0u} : qf[e] ^ neg;
     asm volatile("" : "+v"(qf[e]));         // (waited for here, not in the loop)
   }
   // whether some query element is 2^100 or more: with all of them below, products

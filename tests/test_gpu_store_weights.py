@@ -110,3 +110,25 @@ def test_zero_features_leave_the_others_as_they_are(B, nq, D):
     (O, lse), (P, plse) = got
     assert torch.equal(O[:, :, :D // 2], P[:, :, :D // 2]) and torch.equal(lse, plse)
     assert not P[:, :, D // 2:].any()
+
+
+@pytest.mark.parametrize("nq", [1, 200])
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -121, -2.0 ** -110])
+@pytest.mark.parametrize("o_f32", [False, True])
+def test_small_scales_of_large_products(B, nq, scale, o_f32):
+    """Queries and keys of 2^57: products of 2^120, which a scale brings down to 2^-1,
+    2^10 or 0."""
+    H, D, Ls, k = 4, 64, [70, 33], 5
+    x = Held(B, Ls, H, H, D, 65, make=None)
+    x.K = (x.K.float() * 2.0 ** 57).to(x.dt)
+    x.write(B)
+    Q = (rows_of(k, H, D, 66).float() * 2.0 ** 57).bfloat16()
+    batch(x, Ls, nq)
+    nb = [[0, 1], [1], [], [0], [0, 1]]
+    say(f"small scale {scale} nq={nq} f32={o_f32}")
+    O, lse = attend(B, x, Q.repeat(nq, 1, 1), nb * nq, [k] * nq, [2] * nq, scale, o_f32)
+    torch.cuda.synchronize()
+    O, lse = O.view(nq, k, H, D), lse.view(nq, k, H)
+    ref = reference(Q.double().numpy(), *x.held1(), nb, [k], [2], cum(Ls), scale, 1, o_f32)
+    check(O[0], lse[0], ref, o_f32, "small scale")
+    assert (O == O[:1]).all() and (lse == lse[:1]).all()
