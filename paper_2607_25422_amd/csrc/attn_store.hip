@@ -367,6 +367,10 @@ __device__ __forceinline__ void move_ref(float lm, float sc, float over, bool fi
   m_run = up ? to : m_run;
 }
 
+// The reference for weights: where no logit was above -inf so far (products past
+// float32), one that leaves them 0 and keeps NaN.
+__device__ __forceinline__ float finite_ref(float m_run) { return m_run == -INFINITY ? 0.f : m_run; }
+
 // A stored passage of one key head: its first record, the bytes to the next, its last
 // record.  One that is not wholly inside the store is read at record 0 alone.
 struct QuantRun {
@@ -568,7 +572,6 @@ attn_quant_kernel(QuantAttnArgs a) {
     // one tile; the next one's keys (`r`) land during the softmax and the second
     // product, its values during the next logits, and with a unit's last tile the
     // next unit's queries
-    // (a segment's first tile has a token in every column: m_run is finite then)
     auto step = [&](auto last, const uint8_t* r, uint32_t next) {
       f32x16_t s[2];
       x.logits(qf, s);
@@ -581,7 +584,7 @@ attn_quant_kernel(QuantAttnArgs a) {
       }
       if (t + 64 > cur.t1) mask_from(s, cur.t1 - t - 32 * hh);
       move_ref(lane_max(s), sc, over_largest(x.vs), t == cur.t0, m_run, l_run, acc);
-      l_run += x.template weigh<kQPieces<OUT_F32>>(s, sc, m_run, acc);
+      l_run += x.template weigh<kQPieces<OUT_F32>>(s, sc, finite_ref(m_run), acc);
       asm volatile("" ::: "memory");
       x.load_v(r, o);
       t += 64;
@@ -609,7 +612,7 @@ attn_quant_kernel(QuantAttnArgs a) {
       const bool up = m_run > mo + kQSlack;
       const float mn = up ? m_run : mo;
       const float fa = up && mo != -INFINITY ? __builtin_amdgcn_exp2f(mo - mn) : 1.f;
-      const float fc = __builtin_amdgcn_exp2f(m_run - mn);
+      const float fc = __builtin_amdgcn_exp2f(m_run - finite_ref(mn));   // (0 times 0, or NaN)
       float4* orow = reinterpret_cast<float4*>(Oacc + row * OS) + hh;
       if (__any(fa != 1.f))
 #pragma unroll
@@ -773,7 +776,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
     const bool adj = (mk >> w.j) & 1ull;
     if (large || __any((ks & 0x80808080u) != 0u)) mask_from(s, adj ? 32 : 0);
     move_ref(adj ? lane_max(s) : -INFINITY, sc, over_largest(x.vs), false, m_run, l_run, acc);
-    return adj ? m_run : INFINITY;
+    return adj ? finite_ref(m_run) : INFINITY;
   };
   // one tile in registers; the next one's keys land during the softmax, its values
   // during the next logits
@@ -818,7 +821,7 @@ attn_quant_tile_kernel(QuantAttnArgs a) {
     float M = pm[0][ri];
 #pragma unroll
     for (int w = 1; w < kQTileWaves; ++w) M = fmaxf(M, pm[w][ri]);
-    const float ref = M == -INFINITY ? 0.f : M;
+    const float ref = finite_ref(M);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
 #pragma unroll
@@ -875,14 +878,14 @@ attn_quant_merge_kernel(QuantAttnArgs a) {
       float mx = M;
 #pragma unroll
       for (int c = 0; c < U; ++c) mx = fmaxf(mx, m[c]);
-      if (mx == -INFINITY) continue;                       // no part with a unit of this row yet
-      const float f0 = __builtin_amdgcn_exp2f(M - mx);
+      // (no part with a tile of this row yet: every factor 0, which keeps NaN)
+      const float ref = finite_ref(mx), f0 = __builtin_amdgcn_exp2f(M - ref);
       M = mx;
       l *= f0;
       o = make_float4(o.x * f0, o.y * f0, o.z * f0, o.w * f0);
 #pragma unroll
       for (int c = 0; c < U; ++c) {
-        const float f = s0 + c < S ? __builtin_amdgcn_exp2f(m[c] - mx) : 0.f;
+        const float f = s0 + c < S ? __builtin_amdgcn_exp2f(m[c] - ref) : 0.f;
         l = fmaf(ls[c], f, l);
         o = make_float4(fmaf(x[c].x, f, o.x), fmaf(x[c].y, f, o.y), fmaf(x[c].z, f, o.z),
                         fmaf(x[c].w, f, o.w));

@@ -132,3 +132,61 @@ def test_small_scales_of_large_products(B, nq, scale, o_f32):
     ref = reference(Q.double().numpy(), *x.held1(), nb, [k], [2], cum(Ls), scale, 1, o_f32)
     check(O[0], lse[0], ref, o_f32, "small scale")
     assert (O == O[:1]).all() and (lse == lse[:1]).all()
+
+
+FORMS = pytest.mark.parametrize("nq,Hkv,Ls", [(1, 1, [40, 2000]),      # split and joined
+                                              (3, 4, [40, 90]),        # row tiles
+                                              (200, 4, [40, 90])])     # many items
+
+
+@FORMS
+@pytest.mark.parametrize("o_f32", [False, True])
+def test_logits_past_float32_weigh_nothing(B, nq, Hkv, Ls, o_f32):
+    """A passage whose every product is -2^160: -inf in float32, and of no weight beside
+    another passage, whichever comes first."""
+    H, D, k = 4, 64, 4
+    for order in (0, 1):
+        far = slice(0, Ls[0]) if order == 0 else slice(Ls[1], sum(Ls))
+        L = Ls if order == 0 else Ls[::-1]
+        x = Held(B, L, H, Hkv, D, 67)
+        x.K = x.K.clone()
+        x.K[:, :, :32] = 0.0
+        x.K[far, :, 3] = -2.0 ** 60
+        x.write(B)
+        Q = rows_of(k, H, D, 68)
+        Q[:, :, 3] = 2.0 ** 100
+        batch(x, L, nq)
+        near = 1 - order
+        nb = [[0, 1], [near], [0, 1], []]
+        say(f"past float32 nq={nq} Ls={L} f32={o_f32}")
+        O, lse = attend(B, x, Q.repeat(nq, 1, 1), nb * nq, [k] * nq, [2] * nq, 0.2, o_f32)
+        torch.cuda.synchronize()
+        O, lse = O.view(nq, k, H, D), lse.view(nq, k, H)
+        assert (O == O[:1]).all() and (lse == lse[:1]).all()
+        Q = Q.clone()
+        Q[:, :, 3] = 0.0                     # (its products with the other passage)
+        ref = reference(Q.double().numpy(), *x.held1(), [[near], [near], [near], []], [k], [2],
+                        cum(L), 0.2, H // Hkv, o_f32)
+        check(O[0], lse[0], ref, o_f32, "past float32")
+
+
+@FORMS
+@pytest.mark.parametrize("o_f32", [False, True])
+def test_a_row_that_is_no_number_stays_one(B, nq, Hkv, Ls, o_f32):
+    """NaN in, NaN out in every form, and nothing else changes."""
+    H, D, k = 4, 64, 5
+    x = Held(B, Ls, H, Hkv, D, 69)
+    x.write(B)
+    batch(x, Ls, nq)
+    Q = rows_of(k, H, D, 70)
+    nb = [[0, 1], [1], [0, 1], [0], []]
+    a = attend(B, x, Q.repeat(nq, 1, 1), nb * nq, [k] * nq, [2] * nq, 0.2, o_f32)
+    Q[2, 1, 7] = math.nan
+    b = attend(B, x, Q.repeat(nq, 1, 1), nb * nq, [k] * nq, [2] * nq, 0.2, o_f32)
+    torch.cuda.synchronize()
+    for s, t in ((a[0].view(nq, k, H, D).clone(), b[0].view(nq, k, H, D)),
+                 (a[1].view(nq, k, H, 1).clone(), b[1].view(nq, k, H, 1))):
+        assert t[:, 2, 1].isnan().all()
+        s[:, 2, 1] = 0
+        t[:, 2, 1] = 0
+        assert torch.equal(s, t)
