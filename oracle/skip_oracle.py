@@ -429,9 +429,8 @@ def bsca_attention(Qh: np.ndarray, Kh: np.ndarray, Vh: np.ndarray,
 
 
 # --------------------------------------------------------------------------
-# Whole route for a batch of questions (Alg. 1: scoring, TopK, graph, fuse)
-# --------------------------------------------------------------------------
 # Passages held in 4 bits
+# --------------------------------------------------------------------------
 
 HELD_VALUES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
 
@@ -477,6 +476,8 @@ def held_passage(K, V):
     return Ko, Vo
 
 
+# --------------------------------------------------------------------------
+# Whole route for a batch of questions (Alg. 1: scoring, TopK, graph, fuse)
 # --------------------------------------------------------------------------
 
 @dataclass
