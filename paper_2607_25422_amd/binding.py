@@ -714,6 +714,8 @@ def workspace_bytes_dense(p: SkipProblem, d_out: int) -> int:
 
 def skip_pack_dense(p: SkipProblem, W, packed, stream=None):
     d_out = int(W.shape[0])
+    if W.numel() != d_out * p.d:
+        raise ValueError(f"W must be [d_out, {p.d}], got {tuple(W.shape)}")
     _on_current_device(W, packed)
     st = LIB.skip_pack_dense(ctypes.byref(p), _ptr(W, "W", _elem_dtype(p), d_out * p.d), d_out,
                              _ptr(packed, "packed", torch.uint8), packed.numel(), _stream(stream))

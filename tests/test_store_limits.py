@@ -3,6 +3,7 @@ on the host, by the workspace queries too, before anything is enqueued."""
 import ctypes
 
 import pytest
+import torch
 
 from paper_2607_25422_amd import binding as B
 
@@ -101,3 +102,12 @@ def test_blocks_of_a_passage():
             got = f(ts, te, i, ctypes.byref(t0))
             assert got == (ts + 32 * i < te), (ts, te, i)
             assert not got or t0.value == ts + 32 * i
+
+
+@pytest.mark.parametrize("shape", [(8, 96), (8, 32), (64,), (8, 2, 64)])
+def test_weights_of_another_width_are_refused(shape):
+    """Wider rows would be packed as rows of the problem's width."""
+    p = B.make_problem("bf16", B=1, d=64, kept_offsets=[0, 1])
+    with pytest.raises(ValueError, match="W must be"):
+        B.skip_pack_dense(p, torch.zeros(shape, dtype=torch.bfloat16),
+                          torch.empty(1 << 16, dtype=torch.uint8))
