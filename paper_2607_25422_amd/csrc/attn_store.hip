@@ -32,7 +32,6 @@
 // take 89 us: 7 us of an item's start and end twice, 1.0 us a tile and SIMD (two waves;
 // the instructions alone 0.85) and 1.5 us a unit, for its queries and its merge.
 #include <algorithm>
-#include <type_traits>
 
 #include "skip_common.h"
 #include "skip_internal.h"
@@ -45,6 +44,7 @@ constexpr float kQLn2 = 0.6931471805599453f;
 constexpr int kQWaves = 8;
 constexpr int kQThreads = 64 * kQWaves;
 constexpr int kQMaxP = 64;                 // passages of a question
+constexpr int kQRows = 192;                // virtual rows of an item
 
 // Value of lane l ^ 32.
 __device__ __forceinline__ float other_half(float x) {
@@ -73,14 +73,6 @@ __device__ __forceinline__ void wave_add_one(int* counter) {
   __builtin_amdgcn_wave_barrier();
   if (__lane_id() == 0) atomicAdd(counter, 1);
   __builtin_amdgcn_wave_barrier();
-}
-
-template <int N, int I = 0, class F>
-__device__ __forceinline__ void unrolled(F&& f) {
-  if constexpr (I < N) {
-    f(std::integral_constant<int, I>{});
-    unrolled<N, I + 1>(f);
-  }
 }
 
 struct QuantAttnArgs {
@@ -408,12 +400,12 @@ __device__ __forceinline__ void quant_store(const QuantAttnArgs& a, const QuantI
   if (a.lse && q == 0) a.lse[at] = (l == 0.f) ? -INFINITY : (m + log2f(l)) * kQLn2;
 }
 
-template <int D, int ROWS, bool OUT_F32>
+template <int D, bool OUT_F32>
 __global__ void __launch_bounds__(kQThreads, 2)
 attn_quant_kernel(QuantAttnArgs a) {
   constexpr int KH = QuantTile<D>::KH, FB = QuantTile<D>::FB;
   constexpr int NC4 = D / 4;                // 4-float chunks of an accumulator row
-  constexpr int MW = (ROWS + 63) / 64;      // words of a row mask
+  constexpr int ROWS = kQRows, MW = (ROWS + 63) / 64;      // words of a row mask
   constexpr int OS = D + 4;                 // floats of an accumulator row (bank spread)
   __shared__ __attribute__((aligned(16))) float Oacc[ROWS * OS];
   __shared__ float m_acc[ROWS], l_acc[ROWS];
@@ -922,7 +914,7 @@ static QuantShape quant_shape(const skip_problem_t& p, int heads_kv) {
   const long long per = ((long long)p.total_kept * G + 32ll * p.B - 1) / (32ll * p.B);
   s.tile = groups * per < 768;
   if (!s.tile) {
-    cut(192);
+    cut(kQRows);
     return s;
   }
   const long long wgs = cut(kQTileRows);
@@ -1002,7 +994,7 @@ hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t
     if (sh.tile)                                                                           \
       hipLaunchKernelGGL((attn_quant_tile_kernel<DD, FF>), grid, dim3(kQTileThreads), 0, s, a); \
     else                                                                                   \
-      hipLaunchKernelGGL((attn_quant_kernel<DD, 192, FF>), grid, dim3(kQThreads), 0, s, a); \
+      hipLaunchKernelGGL((attn_quant_kernel<DD, FF>), grid, dim3(kQThreads), 0, s, a); \
   } while (0)
   if (p.d_h == 64) {
     if (p.o_f32) SKIP_ATTN_QUANT(64, true);

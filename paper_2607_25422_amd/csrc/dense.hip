@@ -15,7 +15,6 @@
 //   dense_join_kernel : adds the parts of a contraction that several workgroups
 //                       shared, in their order, and finishes
 #include <algorithm>
-#include <type_traits>
 
 #include "skip_common.h"
 #include "skip_internal.h"
@@ -44,15 +43,6 @@ struct DenseArgs {
   float* part;                     // [splits][M][d_out], where splits > 1
   int n_items;
 };
-
-// f(0), .., f(N-1) with compile-time indices.
-template <int N, int I = 0, class F>
-__device__ __forceinline__ void unrolled(F&& f) {
-  if constexpr (I < N) {
-    f(std::integral_constant<int, I>{});
-    unrolled<N, I + 1>(f);
-  }
-}
 
 // Row that a kept row r stands for: itself, or the row of [B][N] of its index.
 __device__ __forceinline__ size_t dense_row(const DenseArgs& a, const int32_t* idx, int r) {

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "skip.h"
 
 namespace skip {
@@ -16,6 +18,15 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+// f(0), .., f(N-1) with compile-time indices.
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void unrolled(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    unrolled<N, I + 1>(f);
+  }
+}
 
 // ---- matrix cores (bf16 operands as 16-byte words, float32 accumulators)
 // D (32 x 32) += A (32 x 16) . B (16 x 32): lane l holds A[l % 32][8(l / 32)
