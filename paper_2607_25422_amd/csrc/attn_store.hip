@@ -26,11 +26,13 @@
 // wave waits until every unit of earlier passages and segments is merged.  (Units
 // are taken in order, so the earliest one that is not merged never waits.)
 //
-// Bound by vector instructions: a tile of 64 tokens x 32 rows x 128 features takes 128
-// to make held values of codes, some 190 for the softmax, 32 matrix products beside
-// them.  16 questions of 192 rows of 32 heads over ten passages of 256 tokens
-// take 89 us: 7 us of an item's start and end twice, 1.0 us a tile and SIMD (two waves;
-// the instructions alone 0.85) and 1.5 us a unit, for its queries and its merge.
+// A tile of 64 tokens x 32 rows x 128 features takes 128 instructions to make held
+// values of codes, some 270 for the softmax and its weights' pieces, and 48 matrix
+// products beside them.  16 questions of 192 rows of 32 heads over ten passages of 256
+// tokens take 113 us, and no unit is full: vector instructions are active for 52 % of
+// the SIMDs' cycles, matrix products for 35 %, and a wave waits for 31 % of its own.  7 us
+// of an item's start and end go twice, uncovered (an item's LDS fills a CU), 1.3 a tile and
+// SIMD (two waves) and 1.5 a unit, for its queries and its merge.
 #include <algorithm>
 
 #include "skip_common.h"
@@ -110,7 +112,7 @@ struct QuantItem {
 // Batches of at most 64 questions whose items differ start with the questions of
 // the longest items (rows x tokens of an item; ties: lower index), so that the last
 // round of workgroups is a short one: lane b ranks question b.  24 questions of
-// mixed sizes, 616 items on 256 CUs: the call 168 us in order, 164 by rank.
+// mixed sizes, 616 items on 256 CUs: the call 172 us in order, 167 by rank.
 __device__ __forceinline__ int question_of_rank(const QuantAttnArgs& a, int r) {
   const int b = min((int)__lane_id(), a.B - 1);
   int k0, k1, p0, p1;
@@ -658,10 +660,11 @@ attn_quant_kernel(QuantAttnArgs a) {
 // is not adjacent to the tile's passage is -inf (its weight of 0 meets held values,
 // which are finite).  The waves' partials are merged in wave order through LDS at the
 // end.  Four waves, so that two workgroups share a CU and one starts while the other
-// computes (8 questions of 16 heads, 96 rows over 1280 tokens: 22.4 us with the graph,
-// 25.4 with eight).  Over long passages it is bound by HBM: 4 questions of one row of 32
-// heads over 8 key heads and 27000 tokens each, 118 MB of held passages, 29 us with
-// the join of the parts (4.1 TB/s).
+// computes (8 questions of 16 heads, 96 rows over 1280 tokens: 28.0 us with the graph,
+// 31.3 with eight).  Over long passages: 4 questions of one row of 32 heads over 8 key
+// heads and 27000 tokens each, 118 MB of held passages, 30.5 us and 4.3 for the join of
+// the parts (3.9 TB/s; matrix products are active for 25 % of the SIMDs' cycles, most of
+// them for rows that an item of four rows does not have).
 constexpr int kQTileRows = 32;
 constexpr int kQTileWaves = 4;
 constexpr int kQTileThreads = 64 * kQTileWaves;
@@ -908,9 +911,9 @@ static QuantShape quant_shape(const skip_problem_t& p, int heads_kv) {
   // rows of a question): they compute a product for every row and passage that one of
   // their rows has an edge to, the units only those with an edge, in longer items.  Of
   // 90 batches of 1 to 24 questions of 4 to 384 rows this picked the slower form by
-  // 1.6 % on average.  32 heads of 128 features, ten passages of 256 tokens, tiles
-  // and units: 2 questions of 192 rows (384 tiles) 28 and 39 us, 4 of 96 (384) 28.5 and
-  // 28.8, 8 of 48 (512) 30 and 26, 8 of 192 (1536) 76 and 46.
+  // 1.4 % on average.  32 heads of 128 features, ten passages of 256 tokens, tiles
+  // and units: 2 questions of 192 rows (384 tiles) 32 and 47 us, 4 of 96 (384) 33 and
+  // 32, 8 of 48 (512) 37 and 30, 8 of 96 (768) 54 and 40, 8 of 192 (1536) 99 and 57.
   const long long per = ((long long)p.total_kept * G + 32ll * p.B - 1) / (32ll * p.B);
   s.tile = groups * per < 768;
   if (!s.tile) {
@@ -920,8 +923,8 @@ static QuantShape quant_shape(const skip_problem_t& p, int heads_kv) {
   const long long wgs = cut(kQTileRows);
   if (wgs > 0 && wgs < 256) {
     // one workgroup a CU, at least four tiles of 64 tokens each: 8 questions of 4 rows
-    // and heads over ten passages of 2048 tokens, 32 items, take 72 us whole, 22 in 8
-    // parts, 27 in 16; from one part to two a second launch is paid for by 16 tiles
+    // and heads over ten passages of 2048 tokens, 32 items, take 108 us whole, 25 in 8
+    // parts, 26 in 16; from one part to two a second launch is paid for by 16 tiles
     const long long tiles = (long long)p.P_max * ((p.L_max + 63) / 64);
     if (tiles >= 16) s.splits = (int)std::max<long long>(1, std::min<long long>(256 / wgs, tiles / 4));
   }
@@ -977,7 +980,7 @@ hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t
   a.chunks = sh.chunks;
   a.splits = sh.splits;
   a.rows_chunk = sh.rows_chunk;
-  // (questions of one size: total_kept and total_passages are B times the largest)
+  // (questions of one size: total_kept and total_tokens are B times the largest)
   a.ranked = !sh.tile && p.B > 1 && p.B <= 64 &&
              ((int64_t)p.total_kept < (int64_t)p.B * p.k_max ||
               (int64_t)p.total_tokens < (int64_t)p.B * p.P_max * p.L_max);

@@ -171,12 +171,14 @@ dense_pack_kernel(const bf16_t* __restrict__ W, int d, int d_out, int tiles,
 // would only add a way.  Items are dealt to the XCDs in runs, row tile fastest, so
 // that the items of one XCD share their weights in its L2.
 //
-// Bound by the matrix units under the card's power limit: 3088 rows of 4096 by
-// 4096 columns take 95 us (1090 TF; products alone, fed with the same data from
-// registers, 1740 TF, and 1440 TF with one operand from LDS).  A start and end of 4
-// + 1.1 us a block of 32 rows is what the rest goes to; with MB <= 4 and one step of
-// weights ahead, two workgroups fit a CU and hide most of it (4616 rows of 1408 by
-// 4096: MB = 4 62 us, 5 to 8 66, 72, 78 and 92).
+// 3088 rows of 4096 by 4096 columns take 93 us in a graph of such calls, 98 to 101 with
+// a residual and inputs from HBM (1.04 PF; products alone, fed with the same data from
+// registers, 1.74 PF, and 1.44 with one operand from LDS, where the card's power limit
+// lowers the clock).  The matrix units are 43 % busy: 224 items leave 32 of 256 CUs idle,
+// one workgroup a CU is one wave a SIMD, its operand reads meet bank conflicts (4.3 cycles
+// each), and a start and end take 4 + 1.1 us a block of 32 rows; with MB <= 4 and one
+// step of weights ahead, two workgroups fit a CU and hide most of that (4616 rows of 1408
+// by 4096: MB = 4 62 us, 5 to 8 66, 72, 78 and 92).
 template <int MB>
 __global__ void __launch_bounds__(kDnThreads, MB <= 4 ? 2 : 1)
 dense_tile_kernel(DenseArgs a) {
@@ -375,7 +377,7 @@ dense_tile_kernel(DenseArgs a) {
 // part of them (64 columns, an eighth of the workgroup's contraction) straight
 // into registers, a batch of loads ahead of the products; the rows come from the
 // L2.  The waves' sums meet in LDS, added in wave order.  One row of 1024 by 1024
-// columns takes 5.4 us in two launches, where the weights alone would take 0.4.
+// columns takes 5.9 us, where the weights alone would take 0.3.
 __global__ void __launch_bounds__(64 * kDnWaves, 2)
 dense_rows_kernel(DenseArgs a) {
   constexpr int NB = 2, U = 4;                        // k16 groups a batch
