@@ -615,6 +615,142 @@ skip_status_t skip_gather_dense(const skip_problem_t* p, const void* rows,
                                 void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Paged cache of keys and values, for the answer that a decoder writes over the
+ * fused tokens (Alg. 1, decode step).  B sequences share a pool of pages; token t of
+ * sequence b lies in page page_table[b][t / page_tokens], at t % page_tokens, one
+ * copy for a key head (query head h reads key head h / (H / heads_kv)).
+ *   heads_kv     key/value heads, a divisor of H; at most 32 query heads a key head
+ *   page_tokens  32, 64, 128 or 256
+ *   pages_max    columns of page_table
+ *   n_pages      pages of the pool, 1 .. 2^31 - 1
+ *   k, v         [n_pages][heads_kv][page_tokens][d_h] bf16, 16-byte aligned
+ *   mean         [n_pages][heads_kv][d_h] bf16: each page's mean key, kept by
+ *                skip_cache_append and read by skip_cache_select; 16-byte aligned;
+ *                NULL where pages are not selected
+ *   page_table   [B][pages_max] int32, on the device; an entry outside
+ *                [0, n_pages) is a page that is neither written nor read (a row's
+ *                result is then that of its other tokens)
+ * The cache calls take the new tokens of each sequence as rows and of the problem
+ * dtype, B, H, d, d_h, total_kept, k_max, L_max, sm_scale and o_f32:
+ *   row_offsets  [B+1]: rows row_offsets[b] .. row_offsets[b+1] - 1 are the new
+ *                tokens of sequence b, at most k_max, the last of its lens[b] tokens in
+ *                order (no rows: the sequence is passed over).  Rows from
+ *                row_offsets[B] to total_kept are left as they were, so that a
+ *                captured call can serve fewer rows than it was made for
+ *   lens         [B] int32: tokens held with the new ones, at most L_max (clamped
+ *                to it); L_max at most pages_max * page_tokens
+ * Slots behind a sequence's last token, and tokens that a row does not see, may
+ * hold anything, infinities and NaN among it.  Errors as for all entry points; d_h
+ * 64 or 128, else SKIP_ERR_UNSUPPORTED.
+ */
+typedef struct skip_kv_cache {
+  int32_t heads_kv;
+  int32_t page_tokens;
+  int32_t pages_max;
+  int32_t reserved;        /* must be 0 */
+  int64_t n_pages;
+  void* k;
+  void* v;
+  void* mean;
+  const int32_t* page_table;
+} skip_kv_cache_t;
+
+/*
+ * Rotation of queries and keys by the position: for pair i of a row's first `dims`
+ * features and the angle a = position * freq[i] (in double),
+ *   (x, y) -> (x cos a - y sin a, y cos a + x sin a).
+ *   freq   [dims / 2] float, on the device
+ *   dims   a multiple of 16, 16 .. d_h
+ *   pairs  0: pair i is features i and i + dims / 2;  1: features 2 i and 2 i + 1
+ */
+typedef struct skip_rotation {
+  const float* freq;
+  int32_t dims;
+  int32_t pairs;
+} skip_rotation_t;
+
+/*
+ * Appends the new tokens: queries and keys rotated (float32, one rounding), keys
+ * and values written into their pages, the mean key of every page that new tokens
+ * go to brought up to date (the mean, summed in float32, of its keys as held, up to
+ * the sequence's last token: tokens that were cut off or are written again do not
+ * count).  A page that new tokens go to belongs to one sequence of the call.
+ *   rotation   NULL: queries and keys as given
+ *   q          [rows][H][d_h] element type dtype, or NULL (then q_out may be NULL)
+ *   k, v       [rows][heads_kv][d_h] element type dtype
+ *   *_stride   elements from a row to the next, a multiple of 8, at least
+ *              the row's (q, k and v may be columns of one projection's output)
+ *   positions  [total_kept] int32 positions to rotate by, or NULL: each token's
+ *              place in its sequence
+ *   q_out      out [total_kept][H][d_h] bf16, contiguous; apart from q
+ * Arrays are 16-byte aligned.
+ */
+skip_status_t skip_cache_append(const skip_problem_t* p, const skip_kv_cache_t* cache,
+                                const skip_rotation_t* rotation, const void* q, int64_t q_stride,
+                                const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                const int32_t* row_offsets, const int32_t* lens,
+                                const int32_t* positions, void* q_out, void* stream);
+
+/* Workspace of the cache's attention (n_sel 0), of skip_cache_select and of
+ * skip_cache_attn_pages (n_sel pages a row; the larger of the two) (host-only).
+ * `prefixes`: whether prefix_ids will be given. */
+skip_status_t skip_workspace_bytes_cache(const skip_problem_t* p, const skip_kv_cache_t* cache,
+                                         int32_t n_sel, int32_t prefixes, size_t* bytes);
+
+/*
+ * Causal attention of the new tokens over the cache: the row of token t attends to
+ * tokens 0 .. t of its sequence, its own among them,
+ *   O = softmax(sm_scale <q, K>) V,  LSE = log sum exp,
+ * O = 0 and LSE = -inf where it sees none.  bf16 rows (SKIP_ERR_UNSUPPORTED otherwise); O
+ * bf16, or float with o_f32.  Logits and sums are float32; softmax weights enter the
+ * product with V as pairs of bf16 values (2^-16 relative), for float output as three.
+ *   q            [total_kept][H][d_h] (as skip_cache_append writes them)
+ *   prefix_ids   [B] int32, or NULL (then prefix_lens is): consecutive sequences
+ *                with the same id >= 0 and the same prefix_lens hold the same keys
+ *                and values in their first prefix_lens tokens, which are read once for
+ *                all of them (through the table row of one of them).  A hint on
+ *                speed alone where that is so; results may differ in their last bits
+ *   prefix_lens  [B] int32
+ *   O, lse       out [total_kept][H][d_h], [total_kept][H] float or NULL
+ *   workspace    skip_workspace_bytes_cache bytes (0: it may be NULL)
+ * Calls of 2^31 blocks of 32 tokens and 16 rows and heads or more are refused
+ * (SKIP_ERR_UNSUPPORTED).
+ */
+skip_status_t skip_cache_attn(const skip_problem_t* p, const skip_kv_cache_t* cache, const void* q,
+                              const int32_t* row_offsets, const int32_t* lens,
+                              const int32_t* prefix_ids, const int32_t* prefix_lens, void* O,
+                              float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Pages worth reading, for every new token and key head: among the pages 0 ..
+ * t / page_tokens that token t sees, the n_sel with the largest
+ *   s_j = <sum of the queries of the key head's group, mean key of page j>
+ * (double sums of the bf16 values; ties: the lower page), the n_first first and the
+ * n_last last always among them (the last page, whose mean may take in tokens behind
+ * t, so needs no score).  Fewer pages: all of them.  A page without a physical one scores 0.
+ *   n_sel    1 .. 1024;  n_first >= 0, n_last >= 1, n_first + n_last <= n_sel
+ *   pages    out [total_kept][heads_kv][n_sel] int32 ascending, -1 behind the last
+ * cache->mean is required.  At most 65535 rows and 16384 pages a sequence
+ * (SKIP_ERR_UNSUPPORTED).
+ */
+skip_status_t skip_cache_select(const skip_problem_t* p, const skip_kv_cache_t* cache,
+                                const void* q, const int32_t* row_offsets, const int32_t* lens,
+                                int32_t n_sel, int32_t n_first, int32_t n_last, int32_t* pages,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * skip_cache_attn over listed pages: the row of token t and key head h attends to
+ * the tokens <= t of the pages that pages[row][h][0 .. n_sel - 1] names (places in
+ * the sequence's row of page_table, in any order; entries outside the pages that t
+ * sees are passed over; a page named twice counts twice).
+ */
+skip_status_t skip_cache_attn_pages(const skip_problem_t* p, const skip_kv_cache_t* cache,
+                                    const void* q, const int32_t* row_offsets,
+                                    const int32_t* lens, const int32_t* pages, int32_t n_sel,
+                                    void* O, float* lse, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
+/*
  * Both stages fused (Alg. 1: scoring, TopK, graph, fuse): the kept visual
  * tokens are the attention queries (Qh = the kept rows of V viewed as
  * [H][d_h], which requires H * d_h == d) and are read straight from V, never

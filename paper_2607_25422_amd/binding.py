@@ -39,7 +39,8 @@ ENTRY_POINTS = ("skip_abi_version", "skip_status_string", "skip_workspace_bytes"
                 "skip_store_bytes", "skip_quantize_passages", "skip_dequantize_passages",
                 "skip_workspace_bytes_quant", "skip_bipartite_xattn_quant",
                 "skip_packed_bytes_dense", "skip_pack_dense", "skip_workspace_bytes_dense",
-                "skip_gather_dense")
+                "skip_gather_dense", "skip_cache_append", "skip_workspace_bytes_cache",
+                "skip_cache_attn", "skip_cache_select", "skip_cache_attn_pages")
 FUSED_STAGES = ("pool", "score", "edge_cos", "edge_select", "attention")
 
 
@@ -89,10 +90,26 @@ class SkipKvStore(ctypes.Structure):
     ]
 
 
+class SkipKvCache(ctypes.Structure):
+    """skip_kv_cache_t: a paged cache of keys and values (device arrays)."""
+    _fields_ = [
+        ("heads_kv", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+        ("pages_max", ctypes.c_int32), ("reserved", ctypes.c_int32), ("n_pages", ctypes.c_int64),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("mean", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p),
+    ]
+
+
+class SkipRotation(ctypes.Structure):
+    """skip_rotation_t: rotation of queries and keys by the position."""
+    _fields_ = [("freq", ctypes.c_void_p), ("dims", ctypes.c_int32), ("pairs", ctypes.c_int32)]
+
+
 # skip_edge_rule_t and skip_edge_metric_t, by the names the oracle uses
 EDGE_RULES = {"question": 0, "row": 1, "fraction": 2}
 EDGE_METRICS = {"cosine": 0, "dot": 1}
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}     # skip_activation_t
+ROTATIONS = {"halves": 0, "pairs": 1}                          # skip_rotation_t.pairs
 
 
 def _load() -> ctypes.CDLL:
@@ -185,6 +202,21 @@ def _load() -> ctypes.CDLL:
     lib.skip_gather_dense.restype = ctypes.c_int
     lib.skip_gather_dense.argtypes = [P, vp, i32p, i32p, vp, ctypes.c_int32, vp, ctypes.c_int32,
                                       vp, i32p, vp, ctypes.c_int32, vp, ctypes.c_size_t, vp]
+    C, i64, size_t = ctypes.POINTER(SkipKvCache), ctypes.c_int64, ctypes.c_size_t
+    lib.skip_cache_append.restype = ctypes.c_int
+    lib.skip_cache_append.argtypes = [P, C, ctypes.POINTER(SkipRotation), vp, i64, vp, i64, vp, i64,
+                                      i32p, i32p, i32p, vp, vp]
+    lib.skip_workspace_bytes_cache.restype = ctypes.c_int
+    lib.skip_workspace_bytes_cache.argtypes = [P, C, ctypes.c_int32, ctypes.c_int32,
+                                               ctypes.POINTER(size_t)]
+    lib.skip_cache_attn.restype = ctypes.c_int
+    lib.skip_cache_attn.argtypes = [P, C, vp, i32p, i32p, i32p, i32p, vp, vp, vp, size_t, vp]
+    lib.skip_cache_select.restype = ctypes.c_int
+    lib.skip_cache_select.argtypes = [P, C, vp, i32p, i32p, ctypes.c_int32, ctypes.c_int32,
+                                      ctypes.c_int32, i32p, vp, size_t, vp]
+    lib.skip_cache_attn_pages.restype = ctypes.c_int
+    lib.skip_cache_attn_pages.argtypes = [P, C, vp, i32p, i32p, i32p, ctypes.c_int32, vp, vp, vp,
+                                          size_t, vp]
     lib.skip_route_fused_noalloc.restype = ctypes.c_int
     lib.skip_route_fused_noalloc.argtypes = [P, vp, vp, i32p, vp, i32p, vp, vp, i32p, i32p, vp,
                                              i32p, vp, vp, vp]
@@ -751,6 +783,128 @@ def skip_gather_dense(p: SkipProblem, rows, kept_offsets, rows_idx, packed, d_ou
     _check(st, "skip_gather_dense")
 
 
+def _cache_struct(p: SkipProblem, cache: "KvCache") -> SkipKvCache:
+    k, v = cache.k, cache.v
+    n_pages, heads_kv, page, d_h = k.shape
+    if v.shape != k.shape or d_h != p.d_h:
+        raise ValueError(f"cache.k and cache.v must be [pages, heads_kv, page_tokens, {p.d_h}]")
+    t = cache.page_table
+    if t.dim() != 2 or t.shape[0] < p.B:
+        raise ValueError(f"cache.page_table needs {p.B} rows, has {tuple(t.shape)}")
+    bf, n = torch.bfloat16, n_pages * heads_kv * d_h
+    return SkipKvCache(heads_kv, page, t.shape[1], 0, n_pages, _ptr(k, "cache.k", bf),
+                       _ptr(v, "cache.v", bf), _ptr(cache.mean, "cache.mean", bf, n),
+                       _ptr(t, "cache.page_table", torch.int32))
+
+
+def _row_strided(t: torch.Tensor, name: str, dtype, rows: int, heads: int, d_h: int):
+    """Pointer and row stride of [rows, heads, d_h] whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != d_h:
+        raise ValueError(f"{name} must be [{rows}, {heads}, {d_h}], is {tuple(t.shape)}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d_h):
+        raise ValueError(f"{name}: a row's heads must be contiguous")
+    ptr = t.data_ptr()
+    if ptr % 16:
+        raise ValueError(f"{name} must be 16-byte aligned")
+    return ptr, t.stride(0) if t.shape[0] > 1 else heads * d_h
+
+
+def workspace_bytes_cache(p: SkipProblem, cache: "KvCache", n_sel: int = 0,
+                          prefixes: bool = False) -> int:
+    return _cache_bytes(p, _cache_struct(p, cache), n_sel, prefixes)
+
+
+def _cache_bytes(p, c, n_sel, prefixes) -> int:
+    n = ctypes.c_size_t(0)
+    _check(LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), int(n_sel),
+                                          int(prefixes), ctypes.byref(n)),
+           "skip_workspace_bytes_cache")
+    return int(n.value)
+
+
+def skip_cache_append(p: SkipProblem, cache: "KvCache", rotation, q, k, v, row_offsets, lens,
+                      q_out, positions=None, stream=None):
+    et = _elem_dtype(p)
+    c = _cache_struct(p, cache)
+    _on_current_device(cache.k, cache.v, cache.mean, cache.page_table, q, k, v, row_offsets, lens,
+                       q_out, positions, None if rotation is None else rotation.freq)
+    rot = None
+    if rotation is not None:
+        f = rotation.freq
+        rot = ctypes.byref(SkipRotation(_ptr(f, "rotation.freq", torch.float32), 2 * f.numel(),
+                                        ROTATIONS[rotation.style]))
+    M = p.total_kept
+    qp = kp = vp_ = (None, 0)
+    if M:
+        if q is not None:
+            qp = _row_strided(q, "q", et, M, p.H, p.d_h)
+        kp = _row_strided(k, "k", et, M, c.heads_kv, p.d_h)
+        vp_ = _row_strided(v, "v", et, M, c.heads_kv, p.d_h)
+    st = LIB.skip_cache_append(
+        ctypes.byref(p), ctypes.byref(c), rot, *qp, *kp, *vp_,
+        _ptr(row_offsets, "row_offsets", torch.int32, p.B + 1),
+        _ptr(lens, "lens", torch.int32, p.B), _ptr(positions, "positions", torch.int32, M),
+        _ptr(q_out, "q_out", torch.bfloat16, M * p.d), _stream(stream))
+    _check(st, "skip_cache_append")
+
+
+def _cache_ws(p, c, workspace, n_sel, prefixes, device, stream):
+    if workspace is None:
+        workspace = _fresh_workspace(_cache_bytes(p, c, n_sel, prefixes), device, stream)
+    return workspace, _ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
+
+
+def skip_cache_attn(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, O, lse=None,
+                    prefix_ids=None, prefix_lens=None, workspace=None, stream=None):
+    c = _cache_struct(p, cache)
+    _on_current_device(cache.k, cache.v, cache.page_table, q, row_offsets, lens, O, lse, prefix_ids,
+                       prefix_lens, workspace)
+    M = p.total_kept
+    ws, wp, wn = _cache_ws(p, c, workspace, 0, prefix_ids is not None, cache.k.device, stream)
+    st = LIB.skip_cache_attn(
+        ctypes.byref(p), ctypes.byref(c), _ptr(q, "q", torch.bfloat16, M * p.d),
+        _ptr(row_offsets, "row_offsets", torch.int32, p.B + 1),
+        _ptr(lens, "lens", torch.int32, p.B), _ptr(prefix_ids, "prefix_ids", torch.int32, p.B),
+        _ptr(prefix_lens, "prefix_lens", torch.int32, p.B), _ptr(O, "O", _out_dtype(p), M * p.d),
+        _ptr(lse, "lse", torch.float32, M * p.H), wp, wn, _stream(stream))
+    _check(st, "skip_cache_attn")
+
+
+def skip_cache_select(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, n_sel, pages,
+                      n_first=1, n_last=1, workspace=None, stream=None):
+    c = _cache_struct(p, cache)
+    _on_current_device(cache.mean, cache.page_table, q, row_offsets, lens, pages, workspace)
+    M = p.total_kept
+    ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, cache.k.device, stream)
+    st = LIB.skip_cache_select(
+        ctypes.byref(p), ctypes.byref(c), _ptr(q, "q", torch.bfloat16, M * p.d),
+        _ptr(row_offsets, "row_offsets", torch.int32, p.B + 1),
+        _ptr(lens, "lens", torch.int32, p.B), int(n_sel), int(n_first), int(n_last),
+        _ptr(pages, "pages", torch.int32, M * c.heads_kv * int(n_sel)), wp, wn, _stream(stream))
+    _check(st, "skip_cache_select")
+
+
+def skip_cache_attn_pages(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, pages, n_sel, O,
+                          lse=None, workspace=None, stream=None):
+    c = _cache_struct(p, cache)
+    _on_current_device(cache.k, cache.v, cache.page_table, q, row_offsets, lens, pages, O, lse,
+                       workspace)
+    M = p.total_kept
+    ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, cache.k.device, stream)
+    st = LIB.skip_cache_attn_pages(
+        ctypes.byref(p), ctypes.byref(c), _ptr(q, "q", torch.bfloat16, M * p.d),
+        _ptr(row_offsets, "row_offsets", torch.int32, p.B + 1),
+        _ptr(lens, "lens", torch.int32, p.B),
+        _ptr(pages, "pages", torch.int32, M * c.heads_kv * int(n_sel)), int(n_sel),
+        _ptr(O, "O", _out_dtype(p), M * p.d), _ptr(lse, "lse", torch.float32, M * p.H), wp, wn,
+        _stream(stream))
+    _check(st, "skip_cache_attn_pages")
+
+
 def skip_route_fused(p: SkipProblem, V, Qtok, q_offsets, w_bias, kept_offsets, Kh, Vh,
                      passage_offsets, query_passages, kept_idx, O, lse=None,
                      passage_keys=None, workspace=None, stream=None, stage_events=None):
@@ -1197,4 +1351,92 @@ def gather_dense(p: SkipProblem, rows, packed, d_out: int, kept_offsets=None, ro
                           dtype=torch.float32 if out_f32 else _elem_dtype(p))
     skip_gather_dense(p, rows, kept_offsets, rows_idx, packed, d_out, out, bias, activation,
                       residual, residual_idx, out.dtype == torch.float32, workspace)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# The paged cache
+
+@dataclass
+class KvCache:
+    """A paged cache: ``k`` and ``v`` [pages, heads_kv, page_tokens, d_h] bf16, the
+    pages' mean keys ``mean`` [pages, heads_kv, d_h] bf16 (None where pages are not
+    selected) and ``page_table`` [B, pages_max] int32, the page of each
+    ``page_tokens`` tokens of a sequence (-1: none)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    mean: Optional[torch.Tensor]
+    page_table: torch.Tensor
+
+
+@dataclass
+class Rotation:
+    """Rotation by the position: ``freq`` [dims / 2] float32 on the device, pairs of
+    features i and i + dims / 2 ("halves") or 2 i and 2 i + 1 ("pairs")."""
+    freq: torch.Tensor
+    style: str = "halves"
+
+
+def new_kv_cache(n_pages: int, heads_kv: int, page_tokens: int, d_h: int, page_table,
+                 mean: bool = True, device="cuda") -> KvCache:
+    """An empty cache (its pages hold whatever the memory held)."""
+    k, v = (torch.empty((n_pages, heads_kv, page_tokens, d_h), dtype=torch.bfloat16,
+                        device=device) for _ in range(2))
+    m = torch.empty((n_pages, heads_kv, d_h), dtype=torch.bfloat16, device=device) if mean else None
+    return KvCache(k, v, m, page_table)
+
+
+def cache_append(p: SkipProblem, cache: KvCache, q, k, v, row_offsets, lens, rotation=None,
+                 positions=None, out=None, stream=None) -> Optional[torch.Tensor]:
+    """Appends the new tokens: ``q`` [total_kept, H, d_h] (or None), ``k`` and ``v``
+    [total_kept, heads_kv, d_h] in the problem's element type, rows at any stride
+    of a multiple of 8 elements.  Returns the rotated queries, bf16 (``out``: a
+    preallocated tensor)."""
+    if out is None and q is not None:
+        out = torch.empty((p.total_kept, p.H, p.d_h), dtype=torch.bfloat16, device=cache.k.device)
+        _record(out, stream)
+    skip_cache_append(p, cache, rotation, q, k, v, row_offsets, lens, out, positions, stream)
+    return out
+
+
+def _cache_out(p, out, device, stream):
+    if out is None:
+        out = (torch.empty((p.total_kept, p.H, p.d_h), dtype=_out_dtype(p), device=device),
+               torch.empty((p.total_kept, p.H), dtype=torch.float32, device=device))
+        for t in out:
+            _record(t, stream)
+    return out
+
+
+def cache_attn(p: SkipProblem, cache: KvCache, q, row_offsets, lens, prefix_ids=None,
+               prefix_lens=None, out=None, workspace=None, stream=None) -> Tuple:
+    """Causal attention of the new tokens over the cache.  Returns (O, lse);
+    ``out`` = the two preallocated (lse None: not written)."""
+    O, lse = out = _cache_out(p, out, cache.k.device, stream)
+    skip_cache_attn(p, cache, q, row_offsets, lens, O, lse, prefix_ids, prefix_lens, workspace,
+                    stream)
+    return out
+
+
+def cache_select(p: SkipProblem, cache: KvCache, q, row_offsets, lens, n_sel: int,
+                 n_first: int = 1, n_last: int = 1, out=None, workspace=None,
+                 stream=None) -> torch.Tensor:
+    """The pages of the largest scores for every new token and key head, [total_kept,
+    heads_kv, n_sel] int32 ascending, -1 behind the last."""
+    if out is None:
+        out = torch.empty((p.total_kept, cache.k.shape[1], n_sel), dtype=torch.int32,
+                          device=cache.k.device)
+        _record(out, stream)
+    skip_cache_select(p, cache, q, row_offsets, lens, n_sel, out, n_first, n_last, workspace,
+                      stream)
+    return out
+
+
+def cache_attn_pages(p: SkipProblem, cache: KvCache, q, row_offsets, lens, pages, out=None,
+                     workspace=None, stream=None) -> Tuple:
+    """Attention of the new tokens over ``pages`` [total_kept, heads_kv, n_sel] int32.
+    Returns (O, lse); ``out`` = the two preallocated (lse None: not written)."""
+    O, lse = out = _cache_out(p, out, cache.k.device, stream)
+    skip_cache_attn_pages(p, cache, q, row_offsets, lens, pages, pages.shape[-1], O, lse,
+                          workspace, stream)
     return out

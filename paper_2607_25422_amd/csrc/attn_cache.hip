@@ -1,0 +1,773 @@
+// Attention of new tokens over a paged cache.
+//
+// For the new token at position t of a sequence and query head h, with key head h / G,
+//   e_m = sm_scale <q_h, K_m>,  O = softmax(e) . V,  LSE = log sum exp e
+// over the sequence's tokens m <= t, or over those of them that lie in the pages
+// listed for the token and its key head.
+//
+// A (row, query head of the group) pair is one virtual row: virtual row v of a set of
+// rows is its row v / G and query head v % G, and all of them meet the same keys.  An
+// item is up to 16 R virtual rows of one key head and one range of tokens:
+//   - the tokens of a sequence behind its shared prefix, for its rows;
+//   - a prefix, for the rows of all sequences of a run that shares it;
+//   - the listed pages of one row.
+// Its tokens are taken in tiles of 32 (a page holds a multiple of that), and a
+// wave computes a tile alone, with no LDS and no barrier:
+//   S^T (32 tokens x 16 R rows) = K . Q^T,  O^T (D x 16 R) += V^T . P^T
+// (v_mfma_f32_16x16x32_bf16).  Lane l is n = l % 16, g = l / 16.  Which token a row
+// of the first product stands for is free: row r of product a is token
+// 8 (r / 4) + 4 a + r % 4, so that lane (n, g) holds the logits of tokens 8 g .. + 7 for
+// virtual row n, as the second product takes its weights.  Which feature a row of
+// the second product stands for is free as well: row n of product i is feature
+// (D / 16) n + i, so that a lane takes the same D / 16 features of eight tokens with
+// eight loads, and pairs of tokens are joined by byte permutes.  The softmax is
+// online, in base 2 and float32.
+//
+// Work is split evenly whatever the lengths are: all tiles of all items, in order,
+// are cut into equal runs, one a workgroup, whose four waves take every fourth tile.
+// An item that a run does not hold whole leaves partial results (O, reference, sum),
+// which a second kernel joins in the order of the tokens, so that the result does
+// not depend on which workgroup was faster.
+#include <algorithm>
+
+#include "skip_cache.h"
+#include "skip_common.h"
+#include "skip_internal.h"
+#include "skip_select.h"
+
+namespace skip {
+
+constexpr float kCLog2e = 1.4426950408889634f;
+constexpr float kCLn2 = 0.6931471805599453f;
+constexpr int kCWaves = 4;
+constexpr int kCThreads = 64 * kCWaves;
+constexpr int kCTile = 32;                 // tokens of a tile
+constexpr int kCLeast = 8;                 // tiles of a run, at least
+constexpr int kCMeta = 8;                  // ints a sequence in the workspace
+constexpr float kCOver = 8.f;
+
+// bf16 pieces of a softmax weight in the second product: two for bf16 output (2^-16
+// relative, as in the attention over passages), three for float output (2^-24).
+template <bool OUT_F32> constexpr int kCPieces = OUT_F32 ? 3 : 2;
+
+struct CacheAttnArgs {
+  CacheView cache;
+  const bf16_t* q;
+  const int32_t *row_offsets, *lens, *prefix_ids, *prefix_lens;
+  const int32_t* pages;             // listed pages [rows][heads_kv][n_sel], or NULL
+  void* O;
+  float* lse;
+  int32_t* meta;                    // [B][kCMeta] + the run's tiles, where results are joined
+  float* part;                      // [2 runs] results of parts of items
+  float* whole;                     // [2][rows H] results of whole items, with prefixes
+  int B, H, G, total_rows, k_max, L_max, n_sel, o_f32, runs, direct;
+  float scale_log2;
+};
+
+// Floats of a partial result: cols rows of D values, references, sums.
+template <int D>
+__device__ __host__ constexpr size_t part_floats(int cols) { return (size_t)cols * (D + 2); }
+
+// 64 sequences, one a lane, and the tiles of their items.
+struct SeqBlock {
+  CacheSeq s;
+  int P, first, run_rows;           // shared prefix; its run's first lane and rows
+  int up, us, incl;                 // tiles of the prefix's items (of the run's first
+                                    // lane) and of the sequence's own; running sums
+  template <int COLS>
+  __device__ __forceinline__ int row_tiles(const CacheAttnArgs& a, int rows) const {
+    return (rows * a.G + COLS - 1) / COLS;
+  }
+  __device__ __forceinline__ static int tiles(int lo, int hi) {
+    return max((hi + kCTile - 1) / kCTile - lo / kCTile, 1);
+  }
+  template <int COLS>
+  __device__ __forceinline__ void load(const CacheAttnArgs& a, int b0) {
+    const int lane = (int)__lane_id(), b = b0 + lane;
+    s = CacheSeq{0, 0, 0};
+    int id = -1, pl = 0;
+    if (b < a.B) {
+      s.load(a.row_offsets, a.lens, b, a.total_rows, a.k_max, a.L_max);
+      if (a.prefix_ids) {
+        id = a.prefix_ids[b];
+        pl = clampi(a.prefix_lens[b], 0, a.L_max);
+      }
+    }
+    P = 0;
+    first = lane;
+    run_rows = 0;
+    up = 0;
+    if (a.prefix_ids) {
+      const int id_b = __shfl_up(id, 1, kWave), pl_b = __shfl_up(pl, 1, kWave);
+      const bool member = lane > 0 && id >= 0 && pl > 0 && id == id_b && pl == pl_b;
+      const uint64_t starts = __ballot(!member);
+      const uint64_t upto = lane == 63 ? ~0ull : (2ull << lane) - 1ull;
+      first = 63 - __builtin_clzll(starts & upto);
+      const uint64_t after = starts & ~upto;
+      const int last = after ? __builtin_ctzll(after) - 1 : 63;    // of the run
+      if (last > first) {
+        P = pl;
+        const int end = s.r0 + s.n;
+        run_rows = __shfl(end, last, kWave) - __shfl(s.r0, first, kWave);
+        if (lane == first && run_rows > 0)
+          up = a.cache.heads_kv * row_tiles<COLS>(a, run_rows) * tiles(0, P);
+      }
+    }
+    us = s.n > 0 ? a.cache.heads_kv * row_tiles<COLS>(a, s.n) * tiles(min(P, s.len), s.len) : 0;
+    incl = (int)wave_incl_scan((uint32_t)(up + us));
+  }
+};
+
+// What a run's part of an item is: tiles t0 .. t1 - 1 of its nt.
+struct CacheItem {
+  int hk, b;                        // key head; the sequence whose pages are read
+  int r0, v0, nv;                   // first row; virtual rows v0 .. v0 + nv - 1
+  int lo, hi, nt, t0, t1;
+  int start;                        // tile 0 among all items' tiles
+  bool shared;                      // rows with a prefix: results are joined
+  int kind;                         // 0 a prefix, 1 a sequence's own, 2 listed pages
+};
+
+template <int D, int R, bool OUT_F32, bool LISTED>
+__global__ void __launch_bounds__(kCThreads, R > 2 ? 1 : 2)
+cache_attn_kernel(CacheAttnArgs a) {
+  constexpr int COLS = 16 * R, KC = D / 32, NB = D / 16, FPL = D / 16, PIECES = kCPieces<OUT_F32>;
+  constexpr int VW = FPL / 2;               // dwords of a lane's features of a token
+  constexpr int OS = D + 4;
+  __shared__ __attribute__((aligned(16))) float po[kCWaves][COLS][OS];
+  __shared__ float pm[kCWaves][COLS], pl[kCWaves][COLS];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  const int shift = a.cache.shift, hkv = a.cache.heads_kv;
+
+  // a sign of the scale, and a scale of 0, are folded into the queries
+  const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;
+  const bool flat = a.scale_log2 == 0.f;
+  const float sc = flat ? 1.f : fabsf(a.scale_log2);
+
+  // lane offsets (elements) into a tile's keys and values
+  const int koff = (8 * (n >> 2) + (n & 3)) * D + 8 * g;
+  const int voff = 8 * g * D + FPL * n;
+
+  SeqBlock sb;                               // (of the item's sequences)
+  int sb0 = 0;                               // their first
+
+  // One part of an item: every wave its tiles, then the waves' results together.
+  auto work = [&](const CacheItem& it) {
+    // this lane's columns: rows, how many tokens they see
+    int lim[R];
+    u32x4 qf[R][KC];
+    const int nblk = (it.nv + 15) / 16;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int v = it.v0 + min(16 * r + n, it.nv - 1);
+      const int ri = v / a.G, row = it.r0 + ri;
+      const bf16_t* src = a.q + ((size_t)row * a.H + it.hk * a.G + (v - ri * a.G)) * D + 8 * g;
+      if (r < nblk)
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          qf[r][c] = *reinterpret_cast<const u32x4*>(src + 32 * c);
+          if (neg || flat) qf[r][c] = flat ? u32x4{0u, 0u, 0u, 0u} : qf[r][c] ^ neg;
+        }
+      if constexpr (LISTED) {
+        lim[r] = it.hi;
+      } else if (it.kind == 0) {
+        // the row's sequence: the last of the block that starts at or before it (a
+        // sequence without rows starts where the next one does)
+        int l = 0;
+#pragma unroll
+        for (int st = 32; st >= 1; st >>= 1)
+          if (__shfl(sb.s.r0, l + st, kWave) <= row && sb0 + l + st < a.B) l += st;
+        const int sr0 = __shfl(sb.s.r0, l, kWave), sn = __shfl(sb.s.n, l, kWave);
+        const int sl = __shfl(sb.s.len, l, kWave);
+        lim[r] = row < sr0 + sn ? min(it.hi, sl - sn + (row - sr0) + 1) : 0;
+      } else {
+        const int sn = __builtin_amdgcn_readlane(sb.s.n, it.b - sb0);
+        lim[r] = min(it.hi, it.hi - sn + ri + 1);        // (hi is the sequence's length)
+      }
+    }
+    int least = lim[0], most = lim[0];
+#pragma unroll
+    for (int r = 1; r < R; ++r) {
+      least = min(least, lim[r]);
+      most = max(most, lim[r]);
+    }
+#pragma unroll
+    for (int st = 1; st < 16; st <<= 1) {
+      least = min(least, __shfl_xor(least, st, kWave));
+      most = max(most, __shfl_xor(most, st, kWave));
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    most = __builtin_amdgcn_readfirstlane(most);
+
+    f32x4_t acc[R][NB];
+    float m_run[R], l_run[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      m_run[r] = -INFINITY;
+      l_run[r] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) acc[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+
+    u32x4 kf[2][KC];
+    uint32_t vf[8][VW];
+    auto load_k = [&](const bf16_t* kp) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+          kf[h][c] = *reinterpret_cast<const u32x4*>(kp + koff + 4 * h * D + 32 * c);
+    };
+    auto load_v = [&](const bf16_t* vp) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        if constexpr (VW == 4) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(vp + voff + t * D);
+#pragma unroll
+          for (int w = 0; w < VW; ++w) vf[t][w] = x[w];
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(vp + voff + t * D);
+          vf[t][0] = x.x;
+          vf[t][1] = x.y;
+        }
+      }
+    };
+
+    // 64 of the wave's tiles at a time, one a lane: where the tile lies, and its
+    // first token
+    for (int u0 = it.t0 + wave; u0 < it.t1; u0 += 64 * kCWaves) {
+      const int u = u0 + kCWaves * lane;
+      int at = -1, tok = 0;
+      if (u < it.t1) {
+        if constexpr (LISTED) {
+          const int per = 1 << (shift - 5), e = u / per;
+          const int j = a.pages[((size_t)it.r0 * hkv + it.hk) * a.n_sel + e];
+          tok = (j << shift) + (u - e * per) * kCTile;
+          if (j >= 0 && j <= (it.hi - 1) >> shift && tok < it.hi) at = a.cache.page(it.b, j);
+        } else {
+          tok = (it.lo / kCTile + u) * kCTile;
+          if (tok < most) at = a.cache.page(it.b, tok >> shift);
+        }
+      }
+      uint64_t todo = __ballot(at >= 0);
+      if (!todo) continue;
+      auto where = [&](int l, int& t) -> size_t {
+        t = __builtin_amdgcn_readlane(tok, l);
+        return a.cache.base<D>(__builtin_amdgcn_readlane(at, l), it.hk) +
+               (size_t)(t & ((1 << shift) - 1)) * D;
+      };
+      int t;
+      size_t off = where(__builtin_ctzll(todo), t);
+      load_k(a.cache.k + off);
+      asm volatile("" ::: "memory");
+      load_v(a.cache.v + off);
+      asm volatile("" ::: "memory");
+      while (todo) {
+        todo &= todo - 1;
+        int t_next = t;
+        const size_t next = todo ? where(__builtin_ctzll(todo), t_next) : off;
+        // logits
+        f32x4_t s[R][2];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          if (r < nblk)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              s[r][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int c = 0; c < KC; ++c) s[r][h] = mfma16_bf16(kf[h][c], qf[r][c], s[r][h]);
+            }
+        // (the next tile's keys land during the softmax and the second product, its
+        // values during the next logits)
+        asm volatile("" ::: "memory");
+        load_k(a.cache.k + next);
+        asm volatile("" ::: "memory");
+        bool apart = false;                   // values that some rows must not meet
+        if (t < it.lo || t + kCTile > least) {
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (r < nblk)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int m = t + 8 * g + e;
+              float x = m >= it.lo && m < lim[r] ? s[r][e >> 2][e & 3] : -INFINITY;
+              asm volatile("" : "+v"(x));
+              s[r][e >> 2][e & 3] = x;
+            }
+          // values that no row sees are left out; of the others a weight of 0 must
+          // not meet an infinity or NaN
+          bool odd = false;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int m = t + 8 * g + e;
+            const bool in = m >= it.lo && m < most;
+#pragma unroll
+            for (int w = 0; w < VW; ++w) {
+              uint32_t x = in ? vf[e][w] : 0u;
+              asm volatile("" : "+v"(x));
+              vf[e][w] = x;
+              odd |= m >= least && ((x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u);
+            }
+          }
+          apart = __any(odd);
+        }
+        // weights 2^(sc s - reference); the reference is 8 over the largest logit that
+        // moved it, so that weights are at most 1 and it is rarely moved
+        u32x4 pc[R][PIECES];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (r >= nblk) continue;
+          float lm = s[r][0][0];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) lm = fmaxf(lm, s[r][e >> 2][e & 3]);
+          if (__any(lm * sc > m_run[r])) {
+            const float mx = over_groups(lm, [](float x, float y) { return fmaxf(x, y); }) * sc;
+            const bool up = mx > m_run[r];
+            const float to = up ? mx + kCOver : m_run[r];
+            const float alpha = !up ? 1.f : m_run[r] == -INFINITY ? 0.f
+                                            : __builtin_amdgcn_exp2f(m_run[r] - to);
+            l_run[r] *= alpha;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) acc[r][i] *= alpha;
+            m_run[r] = to;
+          }
+          const float ref = m_run[r] == -INFINITY ? 0.f : m_run[r];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            float p0 = __builtin_amdgcn_exp2f(fmaf(s[r][w >> 1][2 * (w & 1)], sc, -ref));
+            float p1 = __builtin_amdgcn_exp2f(fmaf(s[r][w >> 1][2 * (w & 1) + 1], sc, -ref));
+            l_run[r] += p0 + p1;
+#pragma unroll
+            for (int c = 0; c + 1 < PIECES; ++c) {
+              const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+              pc[r][c][w] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+              p0 -= __uint_as_float(b0 & 0xffff0000u);
+              p1 -= __uint_as_float(b1 & 0xffff0000u);
+            }
+            pc[r][PIECES - 1][w] = pack2_bf16(p0, p1);
+          }
+        }
+        if (__builtin_expect(!apart, 1)) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i) {
+            u32x4 va;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              va[w] = __builtin_amdgcn_perm(vf[2 * w + 1][i / 2], vf[2 * w][i / 2],
+                                            i & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+              if (r < nblk)
+#pragma unroll
+                for (int c = 0; c < PIECES; ++c) acc[r][i] = mfma16_bf16(va, pc[r][c], acc[r][i]);
+          }
+        } else {
+          // token by token, each added to the rows that see it alone
+#pragma clang loop unroll(disable)
+          for (int m = 0; m < kCTile; ++m) {
+            const int e = m & 7;
+            uint32_t x[VW];
+#pragma unroll
+            for (int w = 0; w < VW; ++w) {
+              x[w] = 0u;
+#pragma unroll
+              for (int f = 0; f < 8; ++f) x[w] = f == e && g == m >> 3 ? vf[f][w] : x[w];
+            }
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              const uint32_t half = i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xffffu;
+              u32x4 va;
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+                va[w] = w == e >> 1 ? (e & 1 ? half << 16 : half) : 0u;
+#pragma unroll
+              for (int r = 0; r < R; ++r) {
+                if (r >= nblk) continue;
+                f32x4_t one = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < PIECES; ++c) one = mfma16_bf16(va, pc[r][c], one);
+                const bool sees = t + m >= it.lo && t + m < lim[r];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  acc[r][i][k] += sees ? one[k] : 0.f;
+              }
+            }
+          }
+        }
+        asm volatile("" ::: "memory");
+        load_v(a.cache.v + next);
+        asm volatile("" ::: "memory");
+        t = t_next;
+        off = next;
+      }
+    }
+
+    // the waves' results together, and where they go
+    __syncthreads();                           // (the last item's are read)
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r >= nblk) continue;
+      const float l = over_groups(l_run[r], [](float x, float y) { return x + y; });
+      const int col = 16 * r + n;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float* dst = &po[wave][col][FPL * (4 * g + k)];
+#pragma unroll
+        for (int i = 0; i < NB; i += 4)
+          *reinterpret_cast<float4*>(dst + i) = make_float4(
+              acc[r][i][k], acc[r][i + 1][k], acc[r][i + 2][k], acc[r][i + 3][k]);
+      }
+      if (g == 0) {
+        pm[wave][col] = m_run[r];
+        pl[wave][col] = l;
+      }
+    }
+    __syncthreads();
+    constexpr int NC4 = D / 4;
+    const bool all = it.t0 == 0 && it.t1 == it.nt;
+    const int run = blockIdx.x;
+    for (int e = tid; e < it.nv * NC4; e += kCThreads) {
+      const int col = e / NC4, c4 = e % NC4;
+      float m = pm[0][col];
+#pragma unroll
+      for (int w = 1; w < kCWaves; ++w) m = fmaxf(m, pm[w][col]);
+      const float ref = m == -INFINITY ? 0.f : m;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      float l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kCWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(pm[w][col] - ref);
+        const float4 x = *reinterpret_cast<const float4*>(&po[w][col][4 * c4]);
+        o.x = fmaf(x.x, f, o.x);
+        o.y = fmaf(x.y, f, o.y);
+        o.z = fmaf(x.z, f, o.z);
+        o.w = fmaf(x.w, f, o.w);
+        l = fmaf(pl[w][col], f, l);
+      }
+      const int v = it.v0 + col, ri = v / a.G;
+      const size_t vr = (size_t)(it.r0 + ri) * a.H + it.hk * a.G + (v - ri * a.G);
+      if (all && !it.shared) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;            // (keeps NaN)
+        if (OUT_F32)
+          *reinterpret_cast<float4*>(static_cast<float*>(a.O) + vr * D + 4 * c4) =
+              make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        else
+          *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + vr * D + 4 * c4) =
+              make_uint2(pack2_bf16(o.x * inv, o.y * inv), pack2_bf16(o.z * inv, o.w * inv));
+        if (a.lse && c4 == 0) a.lse[vr] = l == 0.f ? -INFINITY : (m + log2f(l)) * kCLn2;
+      } else if (all) {
+        float* w = a.whole + ((size_t)it.kind * a.total_rows * a.H + vr) * (D + 4);
+        *reinterpret_cast<float4*>(w + 4 * c4) = o;
+        if (c4 == 0) {
+          w[D] = m;
+          w[D + 1] = l;
+        }
+      } else {
+        float* w = a.part + (size_t)(2 * run + (it.t0 == 0 ? 1 : 0)) * part_floats<D>(COLS);
+        *reinterpret_cast<float4*>(w + (size_t)col * D + 4 * c4) = o;
+        if (c4 == 0) {
+          w[(size_t)COLS * D + col] = m;
+          w[(size_t)COLS * D + COLS + col] = l;
+        }
+      }
+    }
+  };
+
+  if constexpr (LISTED) {
+    const int rows = clampi(a.row_offsets[a.B], 0, a.total_rows);
+    const int nt = a.n_sel << (shift - 5);
+    const int W = rows * hkv * nt, per = a.direct ? nt : max((W + a.runs - 1) / a.runs, kCLeast);
+    if (blockIdx.x == 0 && tid == 0) a.meta[(size_t)a.B * kCMeta] = per;
+    int u = blockIdx.x * per;
+    const int end = min(W - u, per) + u;
+    while (u < end) {
+      const int i = u / nt;
+      CacheItem it;
+      it.r0 = i / hkv;
+      it.hk = i - it.r0 * hkv;
+      it.nt = nt;
+      it.start = i * nt;
+      it.t0 = u - it.start;
+      it.t1 = min(nt, end - it.start);
+      u = it.start + it.t1;
+      CacheSeq s;
+      it.b = seq_of_row(a.row_offsets, a.lens, a.B, a.total_rows, a.k_max, a.L_max, it.r0, s);
+      if (it.b < 0) continue;
+      it.v0 = 0;
+      it.nv = a.G;
+      it.lo = 0;
+      it.hi = max(s.len - s.n + it.r0 - s.r0 + 1, 0);
+      it.shared = false;
+      it.kind = 2;
+      work(it);
+    }
+  } else {
+    auto item = [&](int L, int start, int x, int end) -> CacheItem {
+      // tile x (among all) of the sequence in lane L, whose tiles begin at `start`
+      const int up = __builtin_amdgcn_readlane(sb.up, L);
+      const int n_ = __builtin_amdgcn_readlane(sb.s.n, L), len = __builtin_amdgcn_readlane(sb.s.len, L);
+      const int P = __builtin_amdgcn_readlane(sb.P, L);
+      CacheItem it;
+      it.b = sb0 + L;
+      it.r0 = __builtin_amdgcn_readlane(sb.s.r0, L);
+      it.shared = P > 0;
+      const bool pre = x - start < up;
+      it.kind = pre ? 0 : 1;
+      const int rows = pre ? __builtin_amdgcn_readlane(sb.run_rows, L) : n_;
+      const int rt = sb.row_tiles<COLS>(a, rows);
+      it.lo = pre ? 0 : min(P, len);
+      it.hi = pre ? P : len;
+      it.nt = SeqBlock::tiles(it.lo, it.hi);
+      const int s0 = pre ? start : start + up;
+      const int i = (x - s0) / it.nt;
+      it.hk = i / rt;
+      it.v0 = (i - it.hk * rt) * COLS;
+      it.nv = min(COLS, rows * a.G - it.v0);
+      it.start = s0 + i * it.nt;
+      it.t0 = x - it.start;
+      it.t1 = min(it.nt, end - it.start);
+      return it;
+    };
+    if (a.direct) {
+      // short sequences: an item a workgroup, no parts
+      const int rt = (a.k_max * a.G + COLS - 1) / COLS;
+      const int b = blockIdx.x / (hkv * rt), i = blockIdx.x - b * hkv * rt;
+      sb0 = b & ~63;
+      sb.load<COLS>(a, sb0);
+      CacheItem it;
+      it.b = b;
+      it.hk = i / rt;
+      it.v0 = (i - it.hk * rt) * COLS;
+      it.r0 = __builtin_amdgcn_readlane(sb.s.r0, b - sb0);
+      it.nv = min(COLS, __builtin_amdgcn_readlane(sb.s.n, b - sb0) * a.G - it.v0);
+      if (it.nv <= 0) return;
+      it.lo = 0;
+      it.hi = __builtin_amdgcn_readlane(sb.s.len, b - sb0);
+      it.nt = SeqBlock::tiles(0, it.hi);
+      it.t0 = it.start = 0;
+      it.t1 = it.nt;
+      it.shared = false;
+      it.kind = 1;
+      work(it);
+      return;
+    }
+    // all tiles, and the places of the items for the join
+    int W = 0;
+    for (sb0 = 0; sb0 < a.B; sb0 += 64) {
+      sb.load<COLS>(a, sb0);
+      if (blockIdx.x == 0 && wave == 0) {
+        const int own = W + sb.incl - sb.us;            // of the sequence's own items
+        const int pre = __shfl(W + sb.incl - sb.us - sb.up, sb.first, kWave);
+        const int r_first = __shfl(sb.s.r0, sb.first, kWave);
+        if (sb0 + lane < a.B) {
+          int32_t* w = a.meta + (size_t)(sb0 + lane) * kCMeta;
+          reinterpret_cast<int4*>(w)[0] = make_int4(own, pre, sb.P, r_first);
+          reinterpret_cast<int4*>(w)[1] = make_int4(sb.run_rows, sb.s.r0, sb.s.n, sb.s.len);
+        }
+      }
+      W += __builtin_amdgcn_readlane(sb.incl, 63);
+    }
+    const int per = max((W + a.runs - 1) / a.runs, kCLeast);
+    if (blockIdx.x == 0 && tid == 0) a.meta[(size_t)a.B * kCMeta] = per;
+    int u = blockIdx.x * per;
+    if (u >= W) return;
+    const int end = min(W - u, per) + u;
+    int base = 0;
+    sb0 = 0;
+    if (a.B > 64) sb.load<COLS>(a, 0);
+    while (u < end) {
+      while (u >= base + __builtin_amdgcn_readlane(sb.incl, 63)) {
+        base += __builtin_amdgcn_readlane(sb.incl, 63);
+        sb0 += 64;
+        sb.load<COLS>(a, sb0);
+      }
+      const int L = __popcll(__ballot(base + sb.incl <= u));
+      const int start = base + __builtin_amdgcn_readlane(sb.incl - sb.up - sb.us, L);
+      const CacheItem it = item(L, start, u, end);
+      u = it.start + it.t1;
+      work(it);
+    }
+  }
+}
+
+// Joins the parts of each virtual row: of its prefix, then of its own tokens, in order.
+// D / 4 lanes a virtual row.
+template <int D, int COLS, bool OUT_F32, bool LISTED>
+__global__ void __launch_bounds__(256)
+cache_join_kernel(CacheAttnArgs a) {
+  constexpr int NC4 = D / 4, VR = 256 / NC4;       // lanes a virtual row, virtual rows
+  const int hkv = a.cache.heads_kv, shift = a.cache.shift;
+  const int per_row = (a.H + VR - 1) / VR;
+  const int row = blockIdx.x / per_row;
+  const int h = (blockIdx.x - row * per_row) * VR + threadIdx.x / NC4;
+  const int c4 = threadIdx.x % NC4;
+  CacheSeq s;
+  const int b = seq_of_row(a.row_offsets, a.lens, a.B, a.total_rows, a.k_max, a.L_max, row, s);
+  if (b < 0 || h >= a.H) return;
+  const int per = a.meta[(size_t)a.B * kCMeta];
+  const int hk = h / a.G;
+  const size_t vr = (size_t)row * a.H + h;
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float4 x, float xm, float xl) {
+    const float to = fmaxf(m, xm), ref = to == -INFINITY ? 0.f : to;
+    const float f = __builtin_amdgcn_exp2f(m - ref), fx = __builtin_amdgcn_exp2f(xm - ref);
+    o = make_float4(fmaf(x.x, fx, o.x * f), fmaf(x.y, fx, o.y * f), fmaf(x.z, fx, o.z * f),
+                    fmaf(x.w, fx, o.w * f));
+    l = fmaf(xl, fx, l * f);
+    m = to;
+  };
+  // results of tiles [start, start + nt) in column col
+  auto parts = [&](int kind, int start, int nt, int col) -> bool {
+    const int c0 = start / per, c1 = (start + nt - 1) / per;
+    if (c0 == c1) {
+      if (!a.whole) return false;
+      const float* w = a.whole + ((size_t)kind * a.total_rows * a.H + vr) * (D + 4);
+      add(*reinterpret_cast<const float4*>(w + 4 * c4), w[D], w[D + 1]);
+      return true;
+    }
+    constexpr int U = 4;                           // parts in flight
+    for (int c = c0; c <= c1; c += U) {
+      float4 x[U];
+      float xm[U], xl[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int k = min(c + i, c1);
+        const float* w = a.part + (size_t)(2 * k + (k == c0 && start >= k * per ? 1 : 0)) *
+                                      part_floats<D>(COLS);
+        x[i] = *reinterpret_cast<const float4*>(w + (size_t)col * D + 4 * c4);
+        xm[i] = w[(size_t)COLS * D + col];
+        xl[i] = w[(size_t)COLS * D + COLS + col];
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (c + i <= c1) add(x[i], xm[i], xl[i]);
+    }
+    return true;
+  };
+  if constexpr (LISTED) {
+    const int nt = a.n_sel << (shift - 5);
+    if (!parts(1, (row * hkv + hk) * nt, nt, h - hk * a.G)) return;
+  } else {
+    const int4 x = reinterpret_cast<const int4*>(a.meta + (size_t)b * kCMeta)[0];
+    const int4 y = reinterpret_cast<const int4*>(a.meta + (size_t)b * kCMeta)[1];
+    const int own = x.x, pre = x.y, P = x.z;
+    const int g = h - hk * a.G;
+    if (P > 0) {
+      const int v = (row - x.w) * a.G + g, rt = (y.x * a.G + COLS - 1) / COLS;
+      const int nt = SeqBlock::tiles(0, P);
+      parts(0, pre + (hk * rt + v / COLS) * nt, nt, v % COLS);
+    }
+    const int v = (row - s.r0) * a.G + g, rt = (s.n * a.G + COLS - 1) / COLS;
+    const int lo = min(P, s.len), nt = SeqBlock::tiles(lo, s.len);
+    const int start = own + (hk * rt + v / COLS) * nt;
+    if (P == 0 && start / per == (start + nt - 1) / per) return;     // (it is written)
+    parts(1, start, nt, v % COLS);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (OUT_F32)
+    *reinterpret_cast<float4*>(static_cast<float*>(a.O) + vr * D + 4 * c4) =
+        make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  else
+    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + vr * D + 4 * c4) =
+        make_uint2(pack2_bf16(o.x * inv, o.y * inv), pack2_bf16(o.z * inv, o.w * inv));
+  if (a.lse && c4 == 0) a.lse[vr] = l == 0.f ? -INFINITY : (m + log2f(l)) * kCLn2;
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+
+namespace {
+
+struct CachePlan {
+  int R, runs;
+  bool direct, prefixes;
+  size_t meta, part, whole;          // bytes
+};
+
+CachePlan cache_plan(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel, bool prefixes) {
+  CachePlan x{};
+  const int G = p.H / c.heads_kv;
+  if (n_sel > 0) {
+    const int nt = n_sel * (c.page_tokens / kCTile);
+    x.R = G <= 16 ? 1 : 2;
+    x.direct = nt <= 16 || (long long)p.total_kept * c.heads_kv >= 512;
+    x.runs = x.direct ? p.total_kept * c.heads_kv : 512;
+  } else {
+    // sequences of up to 512 tokens: an item a workgroup, prefixes with them
+    x.direct = p.L_max <= 512;
+    x.prefixes = prefixes && !x.direct;
+    const long long rows = (long long)(x.prefixes ? p.total_kept : p.k_max) * G;
+    x.R = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    const int cols = 16 * x.R;
+    x.runs = x.direct ? p.B * c.heads_kv * ((p.k_max * G + cols - 1) / cols)
+                      : x.R > 2 ? 256 : 512;
+  }
+  if (!x.direct) {
+    auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+    x.meta = up(((size_t)p.B * kCMeta + 1) * sizeof(int32_t));
+    x.part = up(2 * (size_t)x.runs * 16 * x.R * (p.d_h + 2) * sizeof(float));
+    if (x.prefixes) x.whole = 2 * (size_t)p.total_kept * p.H * (p.d_h + 4) * sizeof(float);
+  }
+  return x;
+}
+
+template <int D, int R, bool OUT_F32, bool LISTED>
+hipError_t launch_one(const CacheAttnArgs& a, hipStream_t s) {
+  cache_attn_kernel<D, R, OUT_F32, LISTED><<<dim3((unsigned)a.runs), kCThreads, 0, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.direct) return e;
+  constexpr int VR = 1024 / D;
+  const unsigned grid = (unsigned)a.total_rows * (unsigned)((a.H + VR - 1) / VR);
+  cache_join_kernel<D, 16 * R, OUT_F32, LISTED><<<dim3(grid), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <int D, bool LISTED>
+hipError_t launch_rows(const CacheAttnArgs& a, int R, hipStream_t s) {
+  if (R == 1)
+    return a.o_f32 ? launch_one<D, 1, true, LISTED>(a, s) : launch_one<D, 1, false, LISTED>(a, s);
+  if (R == 2)
+    return a.o_f32 ? launch_one<D, 2, true, LISTED>(a, s) : launch_one<D, 2, false, LISTED>(a, s);
+  if constexpr (!LISTED)
+    return a.o_f32 ? launch_one<D, 4, true, false>(a, s) : launch_one<D, 4, false, false>(a, s);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+bool cache_attn_fits(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel) {
+  const long long G = p.H / c.heads_kv, hkv = c.heads_kv, rows = p.total_kept;
+  const long long items = n_sel > 0 ? rows * hkv : (rows * G / 16 + 2ll * p.B) * hkv;
+  const long long tiles = n_sel > 0 ? (long long)n_sel * (c.page_tokens / kCTile)
+                                    : p.L_max / kCTile + 2;
+  return items <= INT32_MAX / tiles && rows * p.H < (1ll << 31) &&
+         (long long)p.B * hkv * ((p.k_max * G + 15) / 16) < (1ll << 31);
+}
+
+size_t cache_attn_scratch(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel,
+                          bool prefixes) {
+  const CachePlan x = cache_plan(p, c, n_sel, prefixes);
+  return x.meta + x.part + x.whole;
+}
+
+hipError_t launch_cache_attn(const skip_problem_t& p, const skip_kv_cache_t& c, const void* q,
+                             const int32_t* row_offsets, const int32_t* lens,
+                             const int32_t* prefix_ids, const int32_t* prefix_lens,
+                             const int32_t* pages, int n_sel, void* O, float* lse, void* scratch,
+                             hipStream_t s) {
+  const CachePlan x = cache_plan(p, c, n_sel, prefix_ids != nullptr);
+  char* w = static_cast<char*>(scratch);
+  CacheAttnArgs a{cache_view(c), static_cast<const bf16_t*>(q), row_offsets, lens,
+                  x.prefixes ? prefix_ids : nullptr, prefix_lens, pages, O, lse,
+                  reinterpret_cast<int32_t*>(w), reinterpret_cast<float*>(w + x.meta),
+                  x.whole ? reinterpret_cast<float*>(w + x.meta + x.part) : nullptr, p.B, p.H,
+                  p.H / c.heads_kv, p.total_kept, p.k_max, p.L_max, n_sel, p.o_f32, x.runs,
+                  x.direct, p.sm_scale * kCLog2e};
+  if (n_sel > 0)
+    return p.d_h == 64 ? launch_rows<64, true>(a, x.R, s) : launch_rows<128, true>(a, x.R, s);
+  return p.d_h == 64 ? launch_rows<64, false>(a, x.R, s) : launch_rows<128, false>(a, x.R, s);
+}
+
+}  // namespace skip

@@ -1,0 +1,350 @@
+// A paged cache of keys and values: new tokens rotated by their positions and
+// appended, and the pages that a score selects for each of them.
+#include <algorithm>
+
+#include "skip_cache.h"
+#include "skip_common.h"
+#include "skip_internal.h"
+#include "skip_select.h"
+
+namespace skip {
+
+// ---------------------------------------------------------------------------
+// Append.  For the new token at position t (or the position given for it),
+//   a_i = t f_i,  (x, y) -> (x cos a_i - y sin a_i, y cos a_i + x sin a_i)
+// on the feature pairs i of every query and key head, one rounding to bf16; keys and
+// values into the token's page; the mean of the page's keys up to the sequence's
+// last token.
+//
+// A workgroup takes one page that new tokens go to, of one key head: its keys,
+// values and the group's queries of those tokens, and the page's mean, for which it
+// reads the keys that were there (so that the mean is the keys', whatever was
+// appended, cut off or written again before).  Memory bounds it: a new token's rows
+// are read once and written once.
+constexpr int kAppThreads = 256;
+constexpr int kAppTokens = 32;             // tokens whose angles are in LDS at a time
+constexpr int kAppMaxHalf = 64;            // rotated pairs of a row
+
+struct AppendArgs {
+  CacheView cache;
+  const void *q, *k, *v;
+  long long qs, ks, vs;                    // elements from one row to the next
+  const float* freq;
+  const int32_t *row_offsets, *lens, *positions;
+  bf16_t* q_out;
+  int B, H, G, total_rows, k_max, L_max, half, pairs;
+};
+
+// Eight elements as floats.
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+  x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16_t* p, float (&x)[8]) {
+  unpack8_bf16(*reinterpret_cast<const u32x4*>(p), x);
+}
+__device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
+  return u32x4{pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]),
+               pack2_bf16(x[6], x[7])};
+}
+
+// Features 8 c .. + 7 of a row, rotated by the angles of its token (cosine and sine
+// of pair i at cs[i]).
+template <typename T>
+__device__ __forceinline__ u32x4 rotated8(const T* row, int c, int half, int pairs,
+                                          const float2* cs) {
+  float x[8];
+  load8(row + 8 * c, x);
+  if (8 * c < 2 * half) {
+    if (pairs) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 w = cs[4 * c + e];
+        const float a = x[2 * e], b = x[2 * e + 1];
+        x[2 * e] = a * w.x - b * w.y;
+        x[2 * e + 1] = b * w.x + a * w.y;
+      }
+    } else {
+      const bool low = 8 * c < half;
+      const int i = low ? 8 * c : 8 * c - half;
+      float y[8];
+      load8(row + (low ? i + half : i), y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float2 w = cs[i + e];
+        x[e] = x[e] * w.x + (low ? -y[e] : y[e]) * w.y;
+      }
+    }
+  }
+  return pack8(x);
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kAppThreads)
+cache_append_kernel(AppendArgs a) {
+  constexpr int C = D / 8;                         // 16-byte chunks of a row
+  constexpr int TL = kAppThreads / C;              // tokens side by side
+  __shared__ float2 cs[kAppTokens][kAppMaxHalf];
+  __shared__ float sums[TL][D];
+  const int tid = threadIdx.x, lane = tid & 63, hk = blockIdx.y;
+  const int shift = a.cache.shift, page = 1 << shift;
+
+  // the sequence and page of this slot (every wave the same): prefix sums of the
+  // pages that each sequence's new tokens go to
+  int b = -1, pg = 0, slot = blockIdx.x;
+  CacheSeq q{0, 0, 0};
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    int pages = 0;
+    CacheSeq s{0, 0, 0};
+    if (b0 + lane < a.B) {
+      s.load(a.row_offsets, a.lens, b0 + lane, a.total_rows, a.k_max, a.L_max);
+      if (s.n > 0 && s.len > 0)
+        pages = ((s.len - 1) >> shift) - (max(s.len - s.n, 0) >> shift) + 1;
+    }
+    const int incl = (int)wave_incl_scan((uint32_t)pages);
+    const int total = __builtin_amdgcn_readlane(incl, 63);
+    if (slot < total) {
+      const int l = __popcll(__ballot(incl <= slot));
+      b = b0 + l;
+      q = CacheSeq{__builtin_amdgcn_readlane(s.r0, l), __builtin_amdgcn_readlane(s.n, l),
+                   __builtin_amdgcn_readlane(s.len, l)};
+      pg = (max(q.len - q.n, 0) >> shift) +
+           slot - __builtin_amdgcn_readlane(incl - pages, l);
+      break;
+    }
+    slot -= total;
+  }
+  if (b < 0) return;
+  const int t0 = pg << shift, first = max(q.len - q.n, t0), end = min(q.len, t0 + page);
+  const int row0 = q.r0 + q.n - q.len;             // row of token 0
+  const int at = a.cache.page(b, pg);
+  const size_t base = a.cache.base<D>(max(at, 0), hk);
+  bf16_t* const kp = a.cache.k + base;
+  bf16_t* const vp = a.cache.v + base;
+  const int c = tid % C, tl = tid / C;
+
+  // keys that were there
+  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (a.cache.mean && at >= 0)
+    for (int t = t0 + tl; t < max(first, t0); t += TL) {
+      float x[8];
+      load8(kp + (size_t)(t - t0) * D + 8 * c, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += x[e];
+    }
+
+  for (int u = max(first, 0); u < end; u += kAppTokens) {
+    const int nt = min(end - u, kAppTokens);
+    for (int i = tid; i < nt * a.half; i += kAppThreads) {
+      const int j = i / a.half, f = i - j * a.half;
+      const int pos = a.positions ? a.positions[row0 + u + j] : u + j;
+      // the angle in revolutions, reduced in 64 bits: an angle of a far position has
+      // no bits left in 32
+      const double rev = (double)pos * (double)a.freq[f] * 0.15915494309189533577;
+      const float frac = (float)(rev - rint(rev));
+      cs[j][f] = make_float2(cospif(2.f * frac), sinpif(2.f * frac));
+    }
+    __syncthreads();
+    // (rows: the key, the value, then the group's queries, of every token)
+    for (int j = tl; j < nt; j += TL) {
+      const int t = u + j;
+      const size_t r = (size_t)(row0 + t);
+      const u32x4 kx = rotated8(static_cast<const T*>(a.k) + r * a.ks + (size_t)hk * D, c, a.half,
+                                a.pairs, cs[j]);
+      float vx[8];
+      load8(static_cast<const T*>(a.v) + r * a.vs + (size_t)hk * D + 8 * c, vx);
+      if (at >= 0) {
+        *reinterpret_cast<u32x4*>(kp + (size_t)(t - t0) * D + 8 * c) = kx;
+        *reinterpret_cast<u32x4*>(vp + (size_t)(t - t0) * D + 8 * c) = pack8(vx);
+      }
+      float x[8];
+      unpack8_bf16(kx, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += x[e];
+    }
+    if (a.q)
+      for (int i = tl; i < nt * a.G; i += TL) {
+        const int j = i / a.G, h = hk * a.G + (i - j * a.G);
+        const size_t r = (size_t)(row0 + u + j);
+        *reinterpret_cast<u32x4*>(a.q_out + (r * a.H + h) * D + 8 * c) =
+            rotated8(static_cast<const T*>(a.q) + r * a.qs + (size_t)h * D, c, a.half, a.pairs,
+                     cs[j]);
+      }
+    __syncthreads();
+  }
+  if (!a.cache.mean || at < 0) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[tl][8 * c + e] = sum[e];
+  __syncthreads();
+  if (tid < D / 2) {
+    float x = 0.f, y = 0.f;
+    for (int i = 0; i < TL; ++i) {
+      x += sums[i][2 * tid];
+      y += sums[i][2 * tid + 1];
+    }
+    const float inv = 1.f / (float)(end - t0);
+    reinterpret_cast<uint32_t*>(a.cache.mean + ((size_t)(uint32_t)at * a.cache.heads_kv + hk) *
+                                                   D)[tid] = pack2_bf16(x * inv, y * inv);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Selection.  For the new token at position t and key head h,
+//   s_j = sum over features of (sum over the head's group of q) * mean key of page j
+// for the pages j <= t / page, and the n_sel pages of the largest s_j (ties: the
+// lower page), the n_first first and n_last last among them whatever their scores.
+// In float64: the inputs are bf16, so products are exact and sums good to 2^-50.
+
+struct SelectArgs {
+  CacheView cache;
+  const bf16_t* q;
+  const int32_t *row_offsets, *lens;
+  double* scores;                         // [rows][heads_kv][P]
+  int32_t* pages;                         // [rows][heads_kv][n_sel]
+  int B, H, G, total_rows, k_max, L_max, P, n_sel, n_first, n_last;
+};
+
+constexpr int kScoreThreads = 256;
+constexpr int kScorePages = 256;          // pages of a workgroup
+
+// Scores of kScorePages pages: D / 8 lanes a page, 16 bytes each.
+template <int D>
+__global__ void __launch_bounds__(kScoreThreads)
+cache_score_kernel(SelectArgs a) {
+  constexpr int C = D / 8, PL = kScoreThreads / C;   // lanes a page, pages side by side
+  const int row = blockIdx.z, hk = blockIdx.y, j0 = blockIdx.x * kScorePages;
+  CacheSeq s;
+  const int b = seq_of_row(a.row_offsets, a.lens, a.B, a.total_rows, a.k_max, a.L_max, row, s);
+  if (b < 0) return;
+  const int t = s.len - s.n + row - s.r0;
+  const int vis = t < 0 ? 0 : (t >> a.cache.shift) + 1;
+  if (j0 >= vis) return;
+  const int c = threadIdx.x % C, pl = threadIdx.x / C;
+  double qs[8] = {};
+  for (int g = 0; g < a.G; ++g) {
+    double x[8];
+    unpack16_f64<bf16_t>(*reinterpret_cast<const u32x4*>(
+        a.q + ((size_t)row * a.H + hk * a.G + g) * D + 8 * c), x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) qs[e] += x[e];
+  }
+  double* out = a.scores + ((size_t)row * a.cache.heads_kv + hk) * a.P;
+  const int end = min(min(vis, a.P), j0 + kScorePages);
+  for (int j = j0 + pl; j < j0 + kScorePages; j += PL) {
+    if (j - pl >= end) break;                        // (lanes of a page together)
+    const int at = a.cache.page(b, min(j, end - 1));
+    double z = 0.0;
+    if (at >= 0) {
+      double x[8];
+      unpack16_f64<bf16_t>(*reinterpret_cast<const u32x4*>(
+          a.cache.mean + ((size_t)(uint32_t)at * a.cache.heads_kv + hk) * D + 8 * c), x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z = fma(qs[e], x[e], z);
+    }
+#pragma unroll
+    for (int m = 1; m < C; m <<= 1) z += __shfl_xor(z, m, kWave);
+    if (c == 0 && j < end) out[j] = z;
+  }
+}
+
+// The selection of one row and key head: the scores' keys in registers, a radix
+// select, and the chosen pages in ascending order, -1 behind them.
+template <int MAXPT, int THREADS>
+__global__ void __launch_bounds__(THREADS)
+cache_select_kernel(SelectArgs a) {
+  __shared__ SelectShared sh;
+  __shared__ uint32_t scan[THREADS / 64 + 1];
+  const int row = blockIdx.y, hk = blockIdx.x, tid = threadIdx.x;
+  CacheSeq s;
+  const int b = seq_of_row(a.row_offsets, a.lens, a.B, a.total_rows, a.k_max, a.L_max, row, s);
+  if (b < 0) return;
+  const int t = s.len - s.n + row - s.r0;
+  const int vis = t < 0 ? 0 : min((t >> a.cache.shift) + 1, a.P);
+  const double* z = a.scores + ((size_t)row * a.cache.heads_kv + hk) * a.P;
+  int32_t* out = a.pages + ((size_t)row * a.cache.heads_kv + hk) * a.n_sel;
+  const int C = (vis + THREADS - 1) / THREADS, e0 = tid * C, cnt = clampi(vis - e0, 0, C);
+  uint64_t keys[MAXPT];
+#pragma unroll
+  for (int i = 0; i < MAXPT; ++i) {
+    keys[i] = 0;
+    const int j = e0 + i;
+    if (i < cnt) keys[i] = j < a.n_first || j >= vis - a.n_last ? ~0ull : order_key(z[j]);
+  }
+  const int kk = min(a.n_sel, vis);
+  SelectMask<MAXPT> flags;
+  if constexpr (THREADS == 1024) flags = block_select_top_wide<MAXPT>(keys, cnt, vis, kk, &sh);
+  else flags = block_select_top<MAXPT>(keys, cnt, vis, kk, &sh);
+  uint32_t total;
+  uint32_t at = block_exclusive_scan((uint32_t)__popcll((uint64_t)flags), scan, &total);
+#pragma unroll
+  for (int i = 0; i < MAXPT; ++i)
+    if ((flags >> i) & 1) out[at++] = e0 + i;
+  for (int i = (int)total + tid; i < a.n_sel; i += THREADS) out[i] = -1;
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+
+CacheView cache_view(const skip_kv_cache_t& c) {
+  int shift = 5;
+  while ((1 << shift) < c.page_tokens) ++shift;
+  return CacheView{static_cast<bf16_t*>(c.k), static_cast<bf16_t*>(c.v),
+                   static_cast<bf16_t*>(c.mean), c.page_table, (long long)c.n_pages, c.heads_kv,
+                   c.pages_max, shift};
+}
+
+hipError_t launch_cache_append(const skip_problem_t& p, const skip_kv_cache_t& c,
+                               const skip_rotation_t* rot, const void* q, int64_t qs,
+                               const void* k, int64_t ks, const void* v, int64_t vs,
+                               const int32_t* row_offsets, const int32_t* lens,
+                               const int32_t* positions, void* q_out, hipStream_t s) {
+  AppendArgs a{cache_view(c), q, k, v, qs, ks, vs, rot ? rot->freq : nullptr, row_offsets, lens,
+               positions, static_cast<bf16_t*>(q_out), p.B, p.H, p.H / c.heads_kv, p.total_kept,
+               p.k_max, p.L_max, rot ? rot->dims / 2 : 0, rot ? rot->pairs : 0};
+  // n tokens of a sequence go to at most n pages, and to n / page + 2
+  const long long slots = std::min<long long>(p.total_kept,
+                                              p.total_kept / c.page_tokens + 2ll * p.B);
+  const dim3 grid((unsigned)slots, (unsigned)c.heads_kv);
+  if (p.dtype == SKIP_F32) {
+    if (p.d_h == 64) cache_append_kernel<float, 64><<<grid, kAppThreads, 0, s>>>(a);
+    else cache_append_kernel<float, 128><<<grid, kAppThreads, 0, s>>>(a);
+  } else {
+    if (p.d_h == 64) cache_append_kernel<bf16_t, 64><<<grid, kAppThreads, 0, s>>>(a);
+    else cache_append_kernel<bf16_t, 128><<<grid, kAppThreads, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+static int select_pages(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  return (p.L_max + c.page_tokens - 1) / c.page_tokens;
+}
+
+bool cache_select_fits(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  return select_pages(p, c) <= 16384 && p.total_kept <= 65535;
+}
+
+size_t cache_select_scratch(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  return (size_t)p.total_kept * c.heads_kv * select_pages(p, c) * sizeof(double);
+}
+
+hipError_t launch_cache_select(const skip_problem_t& p, const skip_kv_cache_t& c, const void* q,
+                               const int32_t* row_offsets, const int32_t* lens, int n_sel,
+                               int n_first, int n_last, int32_t* pages, void* scratch,
+                               hipStream_t s) {
+  SelectArgs a{cache_view(c), static_cast<const bf16_t*>(q), row_offsets, lens,
+               static_cast<double*>(scratch), pages, p.B, p.H, p.H / c.heads_kv, p.total_kept,
+               p.k_max, p.L_max, select_pages(p, c), n_sel, n_first, n_last};
+  if (a.P > 0) {
+    const dim3 grid((unsigned)((a.P + kScorePages - 1) / kScorePages), (unsigned)c.heads_kv,
+                    (unsigned)p.total_kept);
+    if (p.d_h == 64) cache_score_kernel<64><<<grid, kScoreThreads, 0, s>>>(a);
+    else cache_score_kernel<128><<<grid, kScoreThreads, 0, s>>>(a);
+  }
+  const dim3 grid((unsigned)c.heads_kv, (unsigned)p.total_kept);
+  if (a.P <= 1024) cache_select_kernel<4, 256><<<grid, 256, 0, s>>>(a);
+  else cache_select_kernel<16, 1024><<<grid, 1024, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace skip

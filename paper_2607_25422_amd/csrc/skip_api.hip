@@ -732,6 +732,139 @@ skip_status_t skip_gather_dense(const skip_problem_t* p, const void* rows,
   return SKIP_OK;
 }
 
+// Problem and cache of the paged cache's calls.
+static skip_status_t check_cache(const skip_problem_t* p, const skip_kv_cache_t* c,
+                                 const int32_t* row_offsets, const int32_t* lens) {
+  skip_status_t st = check_common(p);
+  if (st != SKIP_OK) return st;
+  if (!c || c->reserved != 0 || !row_offsets || !lens) return SKIP_ERR_INVALID_ARG;
+  if (p->H < 1 || p->d_h < 1 || (int64_t)p->H * p->d_h != p->d) return SKIP_ERR_INVALID_ARG;
+  if (p->d_h != 64 && p->d_h != 128) return SKIP_ERR_UNSUPPORTED;
+  if (c->heads_kv < 1 || p->H % c->heads_kv != 0) return SKIP_ERR_INVALID_ARG;
+  if (p->H / c->heads_kv > 32) return SKIP_ERR_UNSUPPORTED;
+  if (c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128 &&
+      c->page_tokens != 256)
+    return SKIP_ERR_UNSUPPORTED;
+  if (c->n_pages < 1 || c->n_pages > INT32_MAX || c->pages_max < 1) return SKIP_ERR_INVALID_ARG;
+  if (!c->k || !c->v || !c->page_table || !al16(c->k) || !al16(c->v) || !al16(c->mean))
+    return SKIP_ERR_INVALID_ARG;
+  if (p->L_max < 0 || (int64_t)p->L_max > (int64_t)c->pages_max * c->page_tokens)
+    return SKIP_ERR_INVALID_ARG;
+  if (p->L_max > (1 << 30)) return SKIP_ERR_UNSUPPORTED;
+  if (!std::isfinite(p->sm_scale)) return SKIP_ERR_INVALID_ARG;
+  return SKIP_OK;
+}
+static skip_status_t check_listed(int32_t n_sel) {
+  return n_sel < 1 ? SKIP_ERR_INVALID_ARG : n_sel > 1024 ? SKIP_ERR_UNSUPPORTED : SKIP_OK;
+}
+
+skip_status_t skip_cache_append(const skip_problem_t* p, const skip_kv_cache_t* cache,
+                                const skip_rotation_t* rotation, const void* q, int64_t q_stride,
+                                const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                const int32_t* row_offsets, const int32_t* lens,
+                                const int32_t* positions, void* q_out, void* stream) {
+  skip_status_t st = check_cache(p, cache, row_offsets, lens);
+  if (st != SKIP_OK) return st;
+  if (rotation) {
+    if (!rotation->freq || (rotation->pairs != 0 && rotation->pairs != 1))
+      return SKIP_ERR_INVALID_ARG;
+    if (rotation->dims < 16 || rotation->dims > p->d_h) return SKIP_ERR_INVALID_ARG;
+    if (rotation->dims % 16 != 0) return SKIP_ERR_UNSUPPORTED;
+  }
+  if (p->total_kept == 0) return SKIP_OK;
+  if (!k || !v || (q && !q_out)) return SKIP_ERR_INVALID_ARG;
+  if (!al16(q) || !al16(k) || !al16(v) || !al16(q_out)) return SKIP_ERR_INVALID_ARG;
+  const int64_t kv = (int64_t)cache->heads_kv * p->d_h;
+  if (k_stride < kv || v_stride < kv || k_stride % 8 != 0 || v_stride % 8 != 0)
+    return SKIP_ERR_INVALID_ARG;
+  if (q && (q_stride < p->d || q_stride % 8 != 0)) return SKIP_ERR_INVALID_ARG;
+  SKIP_TRY(launch_cache_append(*p, *cache, rotation, q, q_stride, k, k_stride, v, v_stride,
+                               row_offsets, lens, positions, q_out,
+                               static_cast<hipStream_t>(stream)));
+  return SKIP_OK;
+}
+
+skip_status_t skip_workspace_bytes_cache(const skip_problem_t* p, const skip_kv_cache_t* cache,
+                                         int32_t n_sel, int32_t prefixes, size_t* bytes) {
+  if (!bytes || n_sel < 0) return SKIP_ERR_INVALID_ARG;
+  const int32_t given = 0;
+  skip_status_t st = check_cache(p, cache, &given, &given);
+  if (st == SKIP_OK && n_sel > 0) st = check_listed(n_sel);
+  if (st != SKIP_OK) return st;
+  if (!cache_attn_fits(*p, *cache, n_sel)) return SKIP_ERR_UNSUPPORTED;
+  size_t need = cache_attn_scratch(*p, *cache, n_sel, prefixes != 0);
+  if (n_sel > 0) {
+    if (!cache_select_fits(*p, *cache)) return SKIP_ERR_UNSUPPORTED;
+    const size_t sel = cache_select_scratch(*p, *cache);
+    need = sel > need ? sel : need;
+  }
+  *bytes = need;
+  return SKIP_OK;
+}
+
+static skip_status_t cache_attn_impl(const skip_problem_t* p, const skip_kv_cache_t* cache,
+                                     const void* q, const int32_t* row_offsets,
+                                     const int32_t* lens, const int32_t* prefix_ids,
+                                     const int32_t* prefix_lens, const int32_t* pages,
+                                     int32_t n_sel, void* O, float* lse, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  if (p->dtype != SKIP_BF16) return SKIP_ERR_UNSUPPORTED;
+  if (p->total_kept == 0) return SKIP_OK;
+  if (!q || !O || !al16(q) || !al16(O) || !al16(workspace)) return SKIP_ERR_INVALID_ARG;
+  if (!cache_attn_fits(*p, *cache, n_sel)) return SKIP_ERR_UNSUPPORTED;
+  const size_t need = cache_attn_scratch(*p, *cache, n_sel, prefix_ids != nullptr);
+  if (need > 0 && !workspace) return SKIP_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return SKIP_ERR_WORKSPACE;
+  SKIP_TRY(launch_cache_attn(*p, *cache, q, row_offsets, lens, prefix_ids, prefix_lens, pages,
+                             n_sel, O, lse, workspace, static_cast<hipStream_t>(stream)));
+  return SKIP_OK;
+}
+
+skip_status_t skip_cache_attn(const skip_problem_t* p, const skip_kv_cache_t* cache, const void* q,
+                              const int32_t* row_offsets, const int32_t* lens,
+                              const int32_t* prefix_ids, const int32_t* prefix_lens, void* O,
+                              float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  skip_status_t st = check_cache(p, cache, row_offsets, lens);
+  if (st != SKIP_OK) return st;
+  if ((prefix_ids == nullptr) != (prefix_lens == nullptr)) return SKIP_ERR_INVALID_ARG;
+  return cache_attn_impl(p, cache, q, row_offsets, lens, prefix_ids, prefix_lens, nullptr, 0, O,
+                         lse, workspace, workspace_bytes, stream);
+}
+
+skip_status_t skip_cache_select(const skip_problem_t* p, const skip_kv_cache_t* cache,
+                                const void* q, const int32_t* row_offsets, const int32_t* lens,
+                                int32_t n_sel, int32_t n_first, int32_t n_last, int32_t* pages,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  skip_status_t st = check_cache(p, cache, row_offsets, lens);
+  if (st == SKIP_OK) st = check_listed(n_sel);
+  if (st != SKIP_OK) return st;
+  if (n_first < 0 || n_last < 1 || (int64_t)n_first + n_last > n_sel || !cache->mean)
+    return SKIP_ERR_INVALID_ARG;
+  if (p->dtype != SKIP_BF16) return SKIP_ERR_UNSUPPORTED;
+  if (p->total_kept == 0) return SKIP_OK;
+  if (!q || !pages || !al16(q) || !al16(workspace)) return SKIP_ERR_INVALID_ARG;
+  if (!cache_select_fits(*p, *cache)) return SKIP_ERR_UNSUPPORTED;
+  const size_t need = cache_select_scratch(*p, *cache);
+  if (need > 0 && !workspace) return SKIP_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return SKIP_ERR_WORKSPACE;
+  SKIP_TRY(launch_cache_select(*p, *cache, q, row_offsets, lens, n_sel, n_first, n_last, pages,
+                               workspace, static_cast<hipStream_t>(stream)));
+  return SKIP_OK;
+}
+
+skip_status_t skip_cache_attn_pages(const skip_problem_t* p, const skip_kv_cache_t* cache,
+                                    const void* q, const int32_t* row_offsets,
+                                    const int32_t* lens, const int32_t* pages, int32_t n_sel,
+                                    void* O, float* lse, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+  skip_status_t st = check_cache(p, cache, row_offsets, lens);
+  if (st == SKIP_OK) st = check_listed(n_sel);
+  if (st != SKIP_OK) return st;
+  if (p->total_kept > 0 && !pages) return SKIP_ERR_INVALID_ARG;
+  return cache_attn_impl(p, cache, q, row_offsets, lens, nullptr, nullptr, pages, n_sel, O, lse,
+                         workspace, workspace_bytes, stream);
+}
+
 // Arguments of the fused route other than the workspace (host-side only).
 static skip_status_t check_fused_args(const skip_problem_t* p, const void* V, const void* Qtok,
                                       const int32_t* q_offsets, const void* w_bias,

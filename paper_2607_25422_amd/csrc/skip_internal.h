@@ -193,4 +193,26 @@ hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t
                                   const int32_t* query_passages, QuantGraph graph, void* O,
                                   float* lse, void* scratch, hipStream_t s);
 
+// Paged cache -----------------------------------------------------------------
+hipError_t launch_cache_append(const skip_problem_t& p, const skip_kv_cache_t& c,
+                               const skip_rotation_t* rot, const void* q, int64_t q_stride,
+                               const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                               const int32_t* row_offsets, const int32_t* lens,
+                               const int32_t* positions, void* q_out, hipStream_t s);
+bool cache_select_fits(const skip_problem_t& p, const skip_kv_cache_t& c);
+size_t cache_select_scratch(const skip_problem_t& p, const skip_kv_cache_t& c);
+hipError_t launch_cache_select(const skip_problem_t& p, const skip_kv_cache_t& c, const void* q,
+                               const int32_t* row_offsets, const int32_t* lens, int n_sel,
+                               int n_first, int n_last, int32_t* pages, void* scratch,
+                               hipStream_t s);
+// n_sel 0: all tokens; else the listed pages
+bool cache_attn_fits(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel);
+size_t cache_attn_scratch(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel,
+                          bool prefixes);
+hipError_t launch_cache_attn(const skip_problem_t& p, const skip_kv_cache_t& c, const void* q,
+                             const int32_t* row_offsets, const int32_t* lens,
+                             const int32_t* prefix_ids, const int32_t* prefix_lens,
+                             const int32_t* pages, int n_sel, void* O, float* lse, void* scratch,
+                             hipStream_t s);
+
 }  // namespace skip
