@@ -640,7 +640,8 @@ skip_status_t skip_gather_dense(const skip_problem_t* p, const void* rows,
  *   lens         [B] int32: tokens held with the new ones, at most L_max (clamped
  *                to it); L_max at most pages_max * page_tokens
  * Slots behind a sequence's last token, and tokens that a row does not see, may
- * hold anything, infinities and NaN among it.  Errors as for all entry points; d_h
+ * hold anything, infinities and NaN among it; of a value that it sees and that is not
+ * finite, infinity or NaN comes out.  Errors as for all entry points; d_h
  * 64 or 128, else SKIP_ERR_UNSUPPORTED.
  */
 typedef struct skip_kv_cache {

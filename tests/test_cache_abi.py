@@ -1,0 +1,210 @@
+"""Refusals of the paged cache's calls, on the host (every call here fails its checks
+before anything is enqueued), and its oracle in closed forms."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import cache_oracle as co
+
+FAKE = 1 << 40   # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2607_25422_amd import binding
+    return binding
+
+
+def problem(b, dtype="bf16", L_max=200, **kw):
+    base = dict(B=2, d=1024, H=16, d_h=64, kept_offsets=[0, 3, 5], sm_scale=0.125)
+    base.update(kw)
+    p = b.make_problem(dtype, **base)
+    p.L_max = L_max
+    return p
+
+
+def cache(b, **kw):
+    a = dict(heads_kv=4, page_tokens=64, pages_max=8, reserved=0, n_pages=20, k=FAKE, v=FAKE,
+             mean=FAKE, page_table=FAKE)
+    a.update(kw)
+    return b.SkipKvCache(*a.values())
+
+
+BAD_CACHES = [dict(heads_kv=0), dict(heads_kv=5), dict(pages_max=0), dict(pages_max=3),
+              dict(reserved=1), dict(n_pages=0), dict(n_pages=1 << 31), dict(k=None), dict(v=None),
+              dict(page_table=None), dict(k=FAKE + 8), dict(v=FAKE + 2), dict(mean=FAKE + 4)]
+ODD_CACHES = [dict(page_tokens=16), dict(page_tokens=0), dict(page_tokens=96),
+              dict(page_tokens=512)]
+
+
+def call(b, fn, p, c, **kw):
+    ref = lambda x: None if x is None else ctypes.byref(x)
+    a = dict(rot=None, q=FAKE, qs=1024, k=FAKE, ks=256, v=FAKE, vs=256, ro=FAKE, lens=FAKE,
+             pos=None, qo=FAKE, ids=None, pls=None, pages=FAKE, n_sel=4, n_first=1, n_last=1,
+             O=FAKE, lse=None, ws=FAKE, nb=1 << 40)
+    a.update(kw)
+    g = lambda *names: [a[n] for n in names]
+    if fn == "append":
+        return b.LIB.skip_cache_append(ref(p), ref(c), ref(a["rot"]),
+                                       *g("q", "qs", "k", "ks", "v", "vs", "ro", "lens", "pos",
+                                          "qo"), None)
+    if fn == "attn":
+        return b.LIB.skip_cache_attn(ref(p), ref(c), *g("q", "ro", "lens", "ids", "pls", "O", "lse",
+                                                        "ws", "nb"), None)
+    if fn == "select":
+        return b.LIB.skip_cache_select(ref(p), ref(c), *g("q", "ro", "lens", "n_sel", "n_first",
+                                                          "n_last", "pages", "ws", "nb"), None)
+    return b.LIB.skip_cache_attn_pages(ref(p), ref(c), *g("q", "ro", "lens", "pages", "n_sel", "O",
+                                                          "lse", "ws", "nb"), None)
+
+
+ALL = ("append", "attn", "select", "pages")
+
+
+def test_structs(b):
+    assert ctypes.sizeof(b.SkipKvCache) == 56 and b.SkipKvCache.k.offset == 24
+    assert ctypes.sizeof(b.SkipRotation) == 16
+
+
+@pytest.mark.parametrize("fn", ALL)
+def test_cache_and_problem(b, fn):
+    inv, uns = b.SKIP_ERR_INVALID_ARG, b.SKIP_ERR_UNSUPPORTED
+    assert call(b, fn, None, cache(b)) == inv and call(b, fn, problem(b), None) == inv
+    for kw in BAD_CACHES:
+        assert call(b, fn, problem(b), cache(b, **kw)) == inv, kw
+    for kw in ODD_CACHES:
+        assert call(b, fn, problem(b), cache(b, **kw)) == uns, kw
+    for kw in (dict(ro=None), dict(lens=None), dict(q=FAKE + 8)):
+        assert call(b, fn, problem(b), cache(b), **kw) == inv, kw
+    assert call(b, fn, problem(b, d=512), cache(b)) == inv                 # H * d_h != d
+    assert call(b, fn, problem(b, H=32, d_h=32), cache(b)) == uns
+    assert call(b, fn, problem(b, H=64, d=4096), cache(b, heads_kv=1)) == uns   # 64 to a key head
+    assert call(b, fn, problem(b, L_max=513), cache(b)) == inv             # past the page table
+    assert call(b, fn, problem(b, L_max=-1), cache(b)) == inv
+    assert call(b, fn, problem(b, L_max=(1 << 30) + 1), cache(b, pages_max=1 << 30)) == uns
+    assert call(b, fn, problem(b, sm_scale=float("nan")), cache(b)) == inv
+    # no rows: nothing to do
+    none = problem(b, kept_offsets=[0, 0, 0])
+    assert call(b, fn, none, cache(b), q=None, k=None, v=None, qo=None, pages=None, O=None,
+                ws=None, nb=0) == b.SKIP_OK
+
+
+def test_append(b):
+    inv, uns = b.SKIP_ERR_INVALID_ARG, b.SKIP_ERR_UNSUPPORTED
+    p, c = problem(b), cache(b)
+    for kw in (dict(k=None), dict(v=None), dict(qo=None), dict(k=FAKE + 2), dict(v=FAKE + 8),
+               dict(qo=FAKE + 4), dict(ks=248), dict(vs=0), dict(qs=1016), dict(ks=260),
+               dict(vs=-256), dict(qs=1028)):
+        assert call(b, "append", p, c, **kw) == inv, kw
+    for rot, st in (((None, 64, 0), inv), ((FAKE, 64, 2), inv), ((FAKE, 8, 0), inv),
+                    ((FAKE, 80, 0), inv), ((FAKE, 24, 0), uns)):
+        assert call(b, "append", p, c, rot=b.SkipRotation(*rot)) == st, rot
+
+
+def test_attention(b):
+    inv, uns = b.SKIP_ERR_INVALID_ARG, b.SKIP_ERR_UNSUPPORTED
+    c = cache(b, pages_max=100)
+    p = problem(b, L_max=6000)
+    for fn in ("attn", "pages", "select"):
+        assert call(b, fn, problem(b, dtype="f32"), c) == uns
+        assert call(b, fn, p, c, q=None) == inv
+        assert call(b, fn, p, c, ws=FAKE + 8) == inv
+    for fn in ("attn", "pages"):
+        assert call(b, fn, p, c, O=None) == inv and call(b, fn, p, c, O=FAKE + 4) == inv
+    for kw in (dict(ids=FAKE), dict(pls=FAKE), dict(ws=None)):
+        assert call(b, "attn", p, c, **kw) == inv, kw
+    for fn, n_sel, pre in (("attn", 0, 0), ("attn", 0, 1), ("select", 90, 0), ("pages", 90, 0)):
+        need = ctypes.c_size_t(0)
+        assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), n_sel, pre,
+                                                ctypes.byref(need)) == b.SKIP_OK
+        assert need.value > 0
+        kw = dict(n_sel=max(n_sel, 1))
+        if pre:
+            kw.update(ids=FAKE, pls=FAKE)
+        if fn != "select":
+            assert call(b, fn, p, c, nb=need.value - 1, **kw) == b.SKIP_ERR_WORKSPACE
+        assert call(b, fn, p, c, nb=7, **kw) == b.SKIP_ERR_WORKSPACE
+    # sequences that a workgroup takes whole need none
+    assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(problem(b)), ctypes.byref(c), 0, 1,
+                                            ctypes.byref(need)) == b.SKIP_OK and need.value == 0
+    assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), 0, 0, None) == inv
+    assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), -1, 0,
+                                            ctypes.byref(need)) == inv
+    # 2^31 blocks of work
+    wide = problem(b, B=4096, kept_offsets=list(range(4097)), L_max=1 << 30)
+    assert call(b, "attn", wide, cache(b, pages_max=1 << 30)) == uns
+
+
+def test_selection(b):
+    inv, uns = b.SKIP_ERR_INVALID_ARG, b.SKIP_ERR_UNSUPPORTED
+    p, c = problem(b), cache(b)
+    for kw in (dict(n_sel=0), dict(n_sel=-1), dict(pages=None)):
+        assert call(b, "select", p, c, **kw) == inv and call(b, "pages", p, c, **kw) == inv, kw
+    for fn in ("select", "pages"):
+        assert call(b, fn, p, c, n_sel=1025) == uns
+    for kw in (dict(n_first=-1), dict(n_last=0), dict(n_first=4), dict(n_last=4),
+               dict(n_first=(1 << 31) - 1, n_last=(1 << 31) - 1)):
+        assert call(b, "select", p, c, **kw) == inv, kw
+    assert call(b, "select", p, cache(b, mean=None)) == inv
+    assert call(b, "select", problem(b, L_max=64 * 16384 + 1), cache(b, pages_max=20000)) == uns
+    assert call(b, "select", problem(b, B=1, kept_offsets=[0, 65536]), c) == uns
+
+
+def test_binding_checks(b):
+    """Shapes are compared before any pointer goes to the library."""
+    import torch
+    p = problem(b)
+    kv = torch.empty(20, 4, 64, 64, dtype=torch.bfloat16)
+    t = torch.zeros(2, 8, dtype=torch.int32)
+    with pytest.raises(ValueError, match="page_tokens"):
+        b.workspace_bytes_cache(p, b.KvCache(kv, kv[:3], None, t))
+    with pytest.raises(ValueError, match="rows"):
+        b.workspace_bytes_cache(p, b.KvCache(kv, kv, None, t[:1]))
+    with pytest.raises(ValueError, match="device"):
+        b.workspace_bytes_cache(p, b.KvCache(kv, kv, None, t))
+
+
+# ---------------------------------------------------------------------------
+# The oracle
+
+def test_oracle_rotation():
+    x = np.zeros((2, 1, 6))
+    x[:, 0] = [1, 2, 3, 4, 5, 6]
+    half_turn = co.rotate(x, [1, 0], [np.pi, np.pi], "halves")
+    assert np.allclose(half_turn[0, 0], [-1, -2, -3, -4, 5, 6]) and (half_turn[1] == x[1]).all()
+    quarter = co.rotate(x, [2, 0], [np.pi / 4, 0.0], "pairs")
+    assert np.allclose(quarter[0, 0], [-2, 1, 3, 4, 5, 6])
+    # a product of two rotated rows depends on the distance of their positions alone
+    rng = np.random.default_rng(1)
+    q, k = rng.standard_normal((2, 1, 1, 8))
+    for style in ("halves", "pairs"):
+        dots = [float((co.rotate(q, [a], [0.3, 0.01], style) *
+                       co.rotate(k, [a + 5], [0.3, 0.01], style)).sum()) for a in (0, 17, 90000)]
+        assert np.allclose(dots, dots[0])
+
+
+def test_oracle_attention():
+    rng = np.random.default_rng(2)
+    k, v = rng.standard_normal((2, 3, 1, 4, 8))
+    table, ro, lens = np.array([[2, 0], [1, -1]]), [0, 2, 3], [6, 1]
+    q = rng.standard_normal((3, 2, 8))
+    O, lse, _ = co.attention(q, k, v, table, ro, lens, 0.0)
+    toks = np.concatenate([v[2, 0], v[0, 0]])
+    assert np.allclose(O[0], toks[:5].mean(0)) and np.allclose(O[1], toks[:6].mean(0))
+    assert np.allclose(O[2], v[1, 0, 0]) and np.allclose(lse, np.log([[5], [6], [1]]))
+    listed = np.full((3, 1, 2), -1)
+    listed[1, 0] = [1, 1]
+    O, lse, _ = co.attention(q, k, v, table, ro, lens, 0.0, listed)
+    assert np.allclose(O[1], toks[4:6].mean(0)) and np.allclose(lse[1], np.log(4))
+    assert (O[0] == 0).all() and (lse[0] == -np.inf).all()
+
+
+def test_oracle_selection():
+    mean = np.array([3., 1., 2., 2., 5.])[:, None, None] * np.ones((5, 1, 4))
+    q = np.ones((1, 2, 4))
+    pick = lambda **kw: co.select(q, mean, np.array([[0, 1, 2, 3, 4]]), 4, [0, 1], [20],
+                                  **kw)[0, 0].tolist()
+    assert pick(n_sel=3, n_first=0, n_last=1) == [0, 2, 4]            # a tie: the lower page
+    assert pick(n_sel=3, n_first=2, n_last=1) == [0, 1, 4]
+    assert pick(n_sel=7, n_first=1, n_last=1) == [0, 1, 2, 3, 4, -1, -1]
