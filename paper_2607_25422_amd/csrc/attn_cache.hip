@@ -308,7 +308,7 @@ cache_attn_kernel(CacheAttnArgs a) {
               uint32_t x = in ? vf[e][w] : 0u;
               asm volatile("" : "+v"(x));
               vf[e][w] = x;
-              odd |= m >= least && ((x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u);
+              odd |= bf16_odd_pair(x) != 0u;
             }
           }
           apart = __any(odd);
@@ -349,52 +349,43 @@ cache_attn_kernel(CacheAttnArgs a) {
             pc[r][PIECES - 1][w] = pack2_bf16(p0, p1);
           }
         }
-        if (__builtin_expect(!apart, 1)) {
 #pragma unroll
-          for (int i = 0; i < NB; ++i) {
-            u32x4 va;
+        for (int i = 0; i < NB; ++i) {
+          u32x4 va;
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
-              va[w] = __builtin_amdgcn_perm(vf[2 * w + 1][i / 2], vf[2 * w][i / 2],
-                                            i & 1 ? 0x07060302u : 0x05040100u);
+          for (int w = 0; w < 4; ++w)
+            va[w] = __builtin_amdgcn_perm(vf[2 * w + 1][i / 2], vf[2 * w][i / 2],
+                                          i & 1 ? 0x07060302u : 0x05040100u);
+          if (apart) {
+            // these are left out, too, and make NaN of the rows that see them (as one
+            // product more finds them, of ones)
+            u32x4 ones;
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-              if (r < nblk)
-#pragma unroll
-                for (int c = 0; c < PIECES; ++c) acc[r][i] = mfma16_bf16(va, pc[r][c], acc[r][i]);
-          }
-        } else {
-          // token by token, each added to the rows that see it alone
-#pragma clang loop unroll(disable)
-          for (int m = 0; m < kCTile; ++m) {
-            const int e = m & 7;
-            uint32_t x[VW];
-#pragma unroll
-            for (int w = 0; w < VW; ++w) {
-              x[w] = 0u;
-#pragma unroll
-              for (int f = 0; f < 8; ++f) x[w] = f == e && g == m >> 3 ? vf[f][w] : x[w];
+            for (int w = 0; w < 4; ++w) {
+              const uint32_t bad = bf16_odd_pair(va[w]);
+              va[w] &= ~bad;
+              ones[w] = bad & 0x3f803f80u;
             }
 #pragma unroll
-            for (int i = 0; i < NB; ++i) {
-              const uint32_t half = i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xffffu;
-              u32x4 va;
+            for (int r = 0; r < R; ++r) {
+              if (r >= nblk) continue;
+              u32x4 sees;
 #pragma unroll
-              for (int w = 0; w < 4; ++w)
-                va[w] = w == e >> 1 ? (e & 1 ? half << 16 : half) : 0u;
-#pragma unroll
-              for (int r = 0; r < R; ++r) {
-                if (r >= nblk) continue;
-                f32x4_t one = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < PIECES; ++c) one = mfma16_bf16(va, pc[r][c], one);
-                const bool sees = t + m >= it.lo && t + m < lim[r];
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  acc[r][i][k] += sees ? one[k] : 0.f;
+              for (int w = 0; w < 4; ++w) {
+                const int m = t + 8 * g + 2 * w;
+                sees[w] = (m >= it.lo && m < lim[r] ? 0x3f80u : 0u) |
+                          (m + 1 >= it.lo && m + 1 < lim[r] ? 0x3f800000u : 0u);
               }
+              const f32x4_t found = mfma16_bf16(ones, sees, f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+              for (int k = 0; k < 4; ++k) acc[r][i][k] += found[k] > 0.f ? NAN : 0.f;
             }
           }
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (r < nblk)
+#pragma unroll
+              for (int c = 0; c < PIECES; ++c) acc[r][i] = mfma16_bf16(va, pc[r][c], acc[r][i]);
         }
         asm volatile("" ::: "memory");
         load_v(a.cache.v + next);
@@ -748,6 +739,7 @@ bool cache_attn_fits(const skip_problem_t& p, const skip_kv_cache_t& c, int n_se
 
 size_t cache_attn_scratch(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel,
                           bool prefixes) {
+  if (n_sel == 0 && cache_tall(p, c)) return cache_tall_scratch(p, c);
   const CachePlan x = cache_plan(p, c, n_sel, prefixes);
   return x.meta + x.part + x.whole;
 }
@@ -757,6 +749,8 @@ hipError_t launch_cache_attn(const skip_problem_t& p, const skip_kv_cache_t& c, 
                              const int32_t* prefix_ids, const int32_t* prefix_lens,
                              const int32_t* pages, int n_sel, void* O, float* lse, void* scratch,
                              hipStream_t s) {
+  if (n_sel == 0 && cache_tall(p, c))
+    return launch_cache_tall(p, c, q, row_offsets, lens, O, lse, scratch, s);
   const CachePlan x = cache_plan(p, c, n_sel, prefix_ids != nullptr);
   char* w = static_cast<char*>(scratch);
   CacheAttnArgs a{cache_view(c), static_cast<const bf16_t*>(q), row_offsets, lens,

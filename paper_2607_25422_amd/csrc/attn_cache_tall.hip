@@ -1,0 +1,454 @@
+// Attention of new tokens over a paged cache, for sequences with many of them (the
+// formulas and the virtual rows are at the top of attn_cache.hip).
+//
+// An item is 128 virtual rows of one sequence and key head, over the tokens that its
+// last row sees or an equal share of them.  A workgroup takes one: its four waves
+// hold 32 virtual rows each and share tiles of 64 tokens in LDS, which direct loads
+// fill a tile ahead.  Per tile and wave,
+//   S^T (64 tokens x 32 rows) = K . Q^T,  O^T (D x 32) += V^T . P^T
+// (v_mfma_f32_32x32x16_bf16).  Lane l is n = l % 32, hh = l / 32.  Element i of the
+// first product's half h is token 32 h + 8 (i / 4) + 4 hh + i % 4 of row n, and stays
+// where it is as a weight: contraction slot (hh, j) of the second product's step
+// (h, q) stands for token 32 h + 16 q + 8 (j / 4) + 4 hh + j % 4.  Its V^T operand comes
+// out of row-major V by transposing LDS reads (16 lanes take four tokens of 16
+// features each way).
+//
+// A row of LDS is a token's D values in chunks of 16 bytes, at places exchanged by the
+// token: chunk c of token r lies at c ^ (r % 16) (keys: eight lanes of a 16-byte read
+// are eight tokens) and at c ^ 2 (r % 8) (values: 16 lanes of a transposing read are
+// four tokens of 32 bytes).  The direct loads take chunks in that order.
+#include <algorithm>
+
+#include "skip_cache.h"
+#include "skip_common.h"
+#include "skip_internal.h"
+
+namespace skip {
+
+constexpr int kTWaves = 4;
+constexpr int kTThreads = 64 * kTWaves;
+constexpr int kTRows = 32 * kTWaves;       // virtual rows of an item
+constexpr int kTTile = 64;                 // tokens of a tile
+constexpr float kTLn2 = 0.6931471805599453f;
+constexpr float kTOver = 8.f;
+template <bool OUT_F32> constexpr int kTPieces = OUT_F32 ? 3 : 2;
+
+struct TallArgs {
+  CacheView cache;
+  const bf16_t* q;
+  const int32_t *row_offsets, *lens;
+  void* O;
+  float* lse;
+  float* part;                      // [items][splits] results of shares
+  int B, H, G, total_rows, k_max, L_max, row_tiles, splits, grouped;
+  float scale_log2;
+};
+
+// Which sequence, key head, 128 virtual rows and share a workgroup takes.  Workgroup
+// id L goes to XCD L % 8; where sequences and key heads make whole eights, the items of
+// one of them follow one another on one XCD, whose L2 then holds its keys and values.
+// Row tiles from the last, which see most tokens, to the first.
+struct TallItem {
+  int b, hk, rt, split;
+  CacheSeq s;
+  int v0, nv;
+};
+__device__ __forceinline__ bool tall_item(const TallArgs& a, int L, TallItem& x) {
+  const int per = a.row_tiles * a.splits, groups = a.B * a.cache.heads_kv;
+  const int grp = a.grouped ? (L & 7) + 8 * ((L >> 3) / per) : L / per;
+  const int sub = a.grouped ? (L >> 3) % per : L % per;
+  if (grp >= groups) return false;
+  x.b = grp / a.cache.heads_kv;
+  x.hk = grp - x.b * a.cache.heads_kv;
+  x.s.load(a.row_offsets, a.lens, x.b, a.total_rows, a.k_max, a.L_max);
+  const int rts = (x.s.n * a.G + kTRows - 1) / kTRows, i = sub / a.splits;
+  if (i >= rts) return false;
+  x.rt = rts - 1 - i;
+  x.split = sub - i * a.splits;
+  x.v0 = x.rt * kTRows;
+  x.nv = min(kTRows, x.s.n * a.G - x.v0);
+  return true;
+}
+
+template <int D>
+__device__ __host__ constexpr size_t tall_part() { return (size_t)kTRows * (D + 2); }
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+// Four values of a column of 4 x 16 ones in LDS (this lane reads a quarter of a row).
+__device__ __forceinline__ uint2 lds_read_transposed(uint32_t addr) {
+  typedef __attribute__((address_space(3))) s16x4* Ptr;
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(uintptr_t)addr));
+}
+__device__ __forceinline__ u32x4 lds_read16(uint32_t addr) {
+  typedef const __attribute__((address_space(3))) u32x4* Ptr;
+  return *(Ptr)(uintptr_t)addr;
+}
+
+template <int D, bool OUT_F32>
+__global__ void __launch_bounds__(kTThreads, 2)
+cache_tall_kernel(TallArgs a) {
+  constexpr int KC = D / 16, FB = D / 32, PIECES = kTPieces<OUT_F32>;
+  constexpr int ROW = 2 * D;                        // bytes of a token
+  constexpr int CH = D / 8;                         // chunks of a token
+  constexpr uint32_t kKeys = kTTile * ROW, kBuffer = 2 * kKeys;
+  __shared__ __attribute__((aligned(1024))) uint8_t tile[2 * kBuffer];
+  TallItem it;
+  if (!tall_item(a, blockIdx.x, it)) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int shift = a.cache.shift;
+  const uint32_t lds = lds_addr(tile);
+
+  // this lane's row and how many tokens it sees; the wave's least and most
+  const int wv = it.v0 + 32 * wave;                 // the wave's first virtual row
+  const bool any = wv < it.v0 + it.nv;
+  const int v = min(wv + n, it.v0 + it.nv - 1);
+  const int ri = v / a.G, head = it.hk * a.G + (v - ri * a.G), row = it.s.r0 + ri;
+  const int lim = max(it.s.len - it.s.n + ri + 1, 0);
+  const int least = max(it.s.len - it.s.n + min(wv, it.v0 + it.nv - 1) / a.G + 1, 0);
+  const int most = max(it.s.len - it.s.n + min(wv + 31, it.v0 + it.nv - 1) / a.G + 1, 0);
+  // tokens of the item, tiles of this share
+  const int hi = max(it.s.len - it.s.n + (it.v0 + it.nv - 1) / a.G + 1, 0);
+  const int tiles = (hi + kTTile - 1) / kTTile;
+  const int i0 = (int)((long long)tiles * it.split / a.splits);
+  const int i1 = (int)((long long)tiles * (it.split + 1) / a.splits);
+
+  const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;
+  const bool flat = a.scale_log2 == 0.f;
+  const float sc = flat ? 1.f : fabsf(a.scale_log2);
+  u32x4 qf[KC];
+  {
+    const bf16_t* src = a.q + ((size_t)row * a.H + head) * D + 8 * hh;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      qf[c] = *reinterpret_cast<const u32x4*>(src + 16 * c);
+      if (neg || flat) qf[c] = flat ? u32x4{0u, 0u, 0u, 0u} : qf[c] ^ neg;
+    }
+  }
+
+  // LDS addresses of this lane's operands in the first buffer
+  uint32_t ka[KC], va_[FB];
+#pragma unroll
+  for (int c = 0; c < KC; ++c) ka[c] = lds + n * ROW + 16 * ((2 * c + hh) ^ (n & (CH - 1)));
+  {
+    const int j = lane & 15, fh = (lane >> 4) & 1, r = 4 * hh + (j >> 2);
+#pragma unroll
+    for (int f = 0; f < FB; ++f) {
+      const int c = 4 * f + 2 * fh + ((j & 3) >> 1);
+      va_[f] = lds + kKeys + r * ROW + 16 * (c ^ ((2 * r) & (CH - 1))) + 8 * (j & 1);
+    }
+  }
+
+  // direct loads: the wave takes 16 tokens of each tile, 1 KiB an instruction
+  constexpr int RI = 1024 / ROW, NI = 16 / RI;      // tokens an instruction, instructions
+  uint32_t kg[NI], vg[NI];                          // source offsets from the 16 tokens (bytes)
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int r = RI * i + lane / CH, c = lane % CH;          // (r: of 16)
+    kg[i] = r * ROW + 16 * (c ^ (r & (CH - 1)));
+    vg[i] = r * ROW + 16 * (c ^ ((2 * r) & (CH - 1)));
+  }
+  // pages of 64 tiles at a time: lane i those of tile i's two halves
+  int pa = 0, pb = 0, pages_from = i0;
+  auto load_pages = [&]() {
+    const int t = (pages_from + lane) * kTTile;
+    pa = t < hi ? a.cache.page(it.b, t >> shift) : 0;
+    pb = t + 32 < hi ? a.cache.page(it.b, (t + 32) >> shift) : 0;
+  };
+  // (tokens behind the last one are loaded from where they would lie, and masked)
+  auto fetch = [&](int i, uint32_t buffer) {
+    if (i - pages_from >= 64) {
+      pages_from = i;
+      load_pages();
+    }
+    const int own = wave < 2 ? __builtin_amdgcn_readlane(pa, i - pages_from)
+                             : __builtin_amdgcn_readlane(pb, i - pages_from);
+    const int t = i * kTTile + 16 * wave;
+    const size_t off = a.cache.base<D>(max(own, 0), it.hk) + (size_t)(t & ((1 << shift) - 1)) * D;
+    const uint8_t* ks = reinterpret_cast<const uint8_t*>(a.cache.k + off);
+    const uint8_t* vs = reinterpret_cast<const uint8_t*>(a.cache.v + off);
+    const uint32_t to = lds + buffer + 16 * wave * ROW;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) lds_dma16(ks + kg[j], to + 1024 * j);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) lds_dma16(vs + vg[j], to + kKeys + 1024 * j);
+  };
+
+  f32x16_t acc[FB];
+  float m_run = -INFINITY, l_run = 0.f;
+#pragma unroll
+  for (int f = 0; f < FB; ++f)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[f][i] = 0.f;
+
+  uint32_t buffer = 0;
+  auto compute = [&](bool masked, int t, int miss) {
+    f32x16_t s[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[h][i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+        s[h] = mfma32_bf16(lds_read16(ka[c] + buffer + 32 * h * ROW), qf[c], s[h]);
+    }
+    // the lane's tokens that its row, and that some row of the wave sees (asm holds
+    // what is masked in its branch, and what it is compared with out of registers)
+    int rem[2] = {0, 0}, rem_most[2] = {0, 0};
+    if (masked) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        rem[h] = (miss >> h) & 1 ? 0 : lim - t - 32 * h - 4 * hh;
+        rem_most[h] = (miss >> h) & 1 ? 0 : most - t - 32 * h - 4 * hh;
+        asm volatile("" : "+v"(rem[h]), "+v"(rem_most[h]));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float x = 8 * (i >> 2) + (i & 3) < rem[h] ? s[h][i] : -INFINITY;
+          asm volatile("" : "+v"(x));
+          s[h][i] = x;
+        }
+      }
+    }
+    float lm = s[0][0];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) lm = fmaxf(lm, s[h][i]);
+    if (__any(lm * sc > m_run)) {
+      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(lm), __float_as_uint(lm),
+                                                      false, false);
+      const float mx = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * sc;
+      const bool up = mx > m_run;
+      const float to = up ? mx + kTOver : m_run;
+      const float alpha = !up ? 1.f : m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - to);
+      l_run *= alpha;
+#pragma unroll
+      for (int f = 0; f < FB; ++f) acc[f] *= alpha;
+      m_run = to;
+    }
+    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    unrolled<4>([&](auto step) {
+      constexpr int h = decltype(step)::value >> 1, q = decltype(step)::value & 1;
+      u32x4 pc[PIECES];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        float p0 = __builtin_amdgcn_exp2f(fmaf(s[h][8 * q + 2 * w], sc, -ref));
+        float p1 = __builtin_amdgcn_exp2f(fmaf(s[h][8 * q + 2 * w + 1], sc, -ref));
+        l_run += p0 + p1;
+#pragma unroll
+        for (int c = 0; c + 1 < PIECES; ++c) {
+          const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+          pc[c][w] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+          p0 -= __uint_as_float(b0 & 0xffff0000u);
+          p1 -= __uint_as_float(b1 & 0xffff0000u);
+        }
+        pc[PIECES - 1][w] = pack2_bf16(p0, p1);
+      }
+      u32x4 x[FB];
+#pragma unroll
+      for (int f = 0; f < FB; ++f) {
+        const uint32_t at = va_[f] + buffer + (32 * h + 16 * q) * ROW;
+        const uint2 lo = lds_read_transposed(at), up = lds_read_transposed(at + 8 * ROW);
+        x[f] = u32x4{lo.x, lo.y, up.x, up.y};
+      }
+      if (masked) {
+        // values that no row of the wave sees are left out
+        bool odd = false;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int m = 16 * q + 8 * (w >> 1) + 2 * (w & 1);
+          const uint32_t keep = (m < rem_most[h] ? 0xffffu : 0u) |
+                                (m + 1 < rem_most[h] ? 0xffff0000u : 0u);
+#pragma unroll
+          for (int f = 0; f < FB; ++f) {
+            uint32_t y = x[f][w] & keep;
+            asm volatile("" : "+v"(y));
+            x[f][w] = y;
+            odd |= bf16_odd_pair(y) != 0u;
+          }
+        }
+        // of the others, a weight of 0 must not meet an infinity or NaN: these are left
+        // out, too, and make NaN of the rows that see them (as one product more finds
+        // them, of ones)
+        if (__any(odd)) {
+          u32x4 sees;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int m = 16 * q + 8 * (w >> 1) + 2 * (w & 1);
+            sees[w] = (m < rem[h] ? 0x3f80u : 0u) | (m + 1 < rem[h] ? 0x3f800000u : 0u);
+          }
+#pragma unroll
+          for (int f = 0; f < FB; ++f) {
+            u32x4 ones;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const uint32_t bad = bf16_odd_pair(x[f][w]);
+              x[f][w] &= ~bad;
+              ones[w] = bad & 0x3f803f80u;
+            }
+            f32x16_t found;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) found[i] = 0.f;
+            found = mfma32_bf16(ones, sees, found);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[f][i] += found[i] > 0.f ? NAN : 0.f;
+            __builtin_amdgcn_sched_barrier(0);      // (one product at a time in registers)
+          }
+        }
+      }
+#pragma unroll
+      for (int f = 0; f < FB; ++f)
+#pragma unroll
+        for (int c = 0; c < PIECES; ++c) acc[f] = mfma32_bf16(x[f], pc[c], acc[f]);
+    });
+  };
+
+  if (i0 < i1) {
+    load_pages();
+    fetch(i0, 0);
+  }
+  for (int i = i0; i < i1; ++i) {
+    // this tile's loads have landed, and every wave is through with the last one, whose
+    // place the next one takes
+    wait_vmcnt<0>();
+    barrier_nofence();
+    const int l = i - pages_from;
+    const int miss = (__builtin_amdgcn_readlane(pa, l) < 0 ? 1 : 0) |
+                     (__builtin_amdgcn_readlane(pb, l) < 0 ? 2 : 0);
+    if (i + 1 < i1) fetch(i + 1, buffer ^ kBuffer);
+    const int t = i * kTTile;
+    if (any && t < most) compute(t + kTTile > least || miss, t, miss);
+    buffer ^= kBuffer;
+  }
+
+  if (!any) return;
+  {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run),
+                                                    false, false);
+    l_run = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
+  if (wv + n >= it.v0 + it.nv) return;
+  if (a.splits > 1) {
+    const size_t item = ((size_t)it.b * a.cache.heads_kv + it.hk) * a.row_tiles + it.rt;
+    float* w = a.part + (item * a.splits + it.split) * tall_part<D>();
+    const int col = 32 * wave + n;
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<float4*>(w + (size_t)col * D + 32 * f + 8 * c + 4 * hh) = make_float4(
+            acc[f][4 * c], acc[f][4 * c + 1], acc[f][4 * c + 2], acc[f][4 * c + 3]);
+    if (hh == 0) {
+      w[(size_t)kTRows * D + col] = m_run;
+      w[(size_t)kTRows * D + kTRows + col] = l_run;
+    }
+    return;
+  }
+  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;            // (keeps NaN)
+  const size_t vr = (size_t)row * a.H + head;
+#pragma unroll
+  for (int f = 0; f < FB; ++f)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const size_t at = vr * D + 32 * f + 8 * c + 4 * hh;
+      const float o0 = acc[f][4 * c] * inv, o1 = acc[f][4 * c + 1] * inv;
+      const float o2 = acc[f][4 * c + 2] * inv, o3 = acc[f][4 * c + 3] * inv;
+      if (OUT_F32)
+        *reinterpret_cast<float4*>(static_cast<float*>(a.O) + at) = make_float4(o0, o1, o2, o3);
+      else
+        *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + at) =
+            make_uint2(pack2_bf16(o0, o1), pack2_bf16(o2, o3));
+    }
+  if (a.lse && hh == 0) a.lse[vr] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * kTLn2;
+}
+
+// Joins an item's shares, in the order of the tokens: D / 4 lanes a virtual row.
+template <int D, bool OUT_F32>
+__global__ void __launch_bounds__(256)
+cache_tall_join_kernel(TallArgs a) {
+  constexpr int NC4 = D / 4, VR = 256 / NC4, WG = kTRows / VR;
+  const int item = blockIdx.x / WG;
+  const int rt = item % a.row_tiles, grp = item / a.row_tiles;
+  const int b = grp / a.cache.heads_kv, hk = grp - b * a.cache.heads_kv;
+  const int col = (blockIdx.x - item * WG) * VR + threadIdx.x / NC4, c4 = threadIdx.x % NC4;
+  CacheSeq s;
+  s.load(a.row_offsets, a.lens, b, a.total_rows, a.k_max, a.L_max);
+  const int v = rt * kTRows + col;
+  if (v >= s.n * a.G) return;
+  const float* w = a.part + (size_t)item * a.splits * tall_part<D>();
+  float m = -INFINITY;
+  for (int i = 0; i < a.splits; ++i)
+    m = fmaxf(m, w[i * tall_part<D>() + (size_t)kTRows * D + col]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < a.splits; ++i) {
+    const float* x = w + i * tall_part<D>();
+    const float f = __builtin_amdgcn_exp2f(x[(size_t)kTRows * D + col] - ref);
+    const float4 y = *reinterpret_cast<const float4*>(x + (size_t)col * D + 4 * c4);
+    o = make_float4(fmaf(y.x, f, o.x), fmaf(y.y, f, o.y), fmaf(y.z, f, o.z), fmaf(y.w, f, o.w));
+    l = fmaf(x[(size_t)kTRows * D + kTRows + col], f, l);
+  }
+  const int ri = v / a.G;
+  const size_t vr = (size_t)(s.r0 + ri) * a.H + hk * a.G + (v - ri * a.G);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (OUT_F32)
+    *reinterpret_cast<float4*>(static_cast<float*>(a.O) + vr * D + 4 * c4) =
+        make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  else
+    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + vr * D + 4 * c4) =
+        make_uint2(pack2_bf16(o.x * inv, o.y * inv), pack2_bf16(o.z * inv, o.w * inv));
+  if (a.lse && c4 == 0) a.lse[vr] = l == 0.f ? -INFINITY : (m + log2f(l)) * kTLn2;
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+
+static int tall_row_tiles(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  return (int)(((long long)p.k_max * (p.H / c.heads_kv) + kTRows - 1) / kTRows);
+}
+// Shares of an item: as many as leave some two workgroups a CU where there are few
+// items, of eight tiles at least.
+static int tall_splits(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  const long long items = (long long)p.B * c.heads_kv * tall_row_tiles(p, c);
+  const long long tiles = (p.L_max + kTTile - 1) / kTTile;
+  return (int)std::max<long long>(1, std::min({512 / std::max(items, 1ll), tiles / 8, 16ll}));
+}
+
+bool cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  return (long long)p.k_max * (p.H / c.heads_kv) > 64;
+}
+
+size_t cache_tall_scratch(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  const int splits = tall_splits(p, c);
+  if (splits == 1) return 0;
+  return (size_t)p.B * c.heads_kv * tall_row_tiles(p, c) * splits * kTRows * (p.d_h + 2) *
+         sizeof(float);
+}
+
+template <int D, bool OUT_F32>
+static hipError_t launch_tall(const TallArgs& a, hipStream_t s) {
+  const int groups = a.B * a.cache.heads_kv;
+  const unsigned grid = (unsigned)groups * a.row_tiles * a.splits;
+  cache_tall_kernel<D, OUT_F32><<<dim3(grid), kTThreads, 0, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  constexpr int WG = kTRows / (1024 / D);
+  cache_tall_join_kernel<D, OUT_F32>
+      <<<dim3((unsigned)groups * a.row_tiles * WG), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c, const void* q,
+                             const int32_t* row_offsets, const int32_t* lens, void* O, float* lse,
+                             void* scratch, hipStream_t s) {
+  TallArgs a{cache_view(c), static_cast<const bf16_t*>(q), row_offsets, lens, O, lse,
+             static_cast<float*>(scratch), p.B, p.H, p.H / c.heads_kv, p.total_kept, p.k_max,
+             p.L_max, tall_row_tiles(p, c), tall_splits(p, c), p.B * c.heads_kv % 8 == 0,
+             p.sm_scale * 1.4426950408889634f};
+  if (p.d_h == 64) return p.o_f32 ? launch_tall<64, true>(a, s) : launch_tall<64, false>(a, s);
+  return p.o_f32 ? launch_tall<128, true>(a, s) : launch_tall<128, false>(a, s);
+}
+
+}  // namespace skip

@@ -39,6 +39,12 @@ struct CacheSeq {
   }
 };
 
+// All ones in the halves of a word that hold a bf16 infinity or NaN.
+__device__ __forceinline__ uint32_t bf16_odd_pair(uint32_t x) {
+  return ((x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) |
+         ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+
 // The sequence of a row (every lane the same), or -1: a row behind the last one, or
 // one that a sequence has no place for.
 __device__ __forceinline__ int seq_of_row(const int32_t* row_offsets, const int32_t* lens, int B,

@@ -205,6 +205,12 @@ hipError_t launch_cache_select(const skip_problem_t& p, const skip_kv_cache_t& c
                                const int32_t* row_offsets, const int32_t* lens, int n_sel,
                                int n_first, int n_last, int32_t* pages, void* scratch,
                                hipStream_t s);
+// sequences with many new tokens, each read by itself
+bool cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c);
+size_t cache_tall_scratch(const skip_problem_t& p, const skip_kv_cache_t& c);
+hipError_t launch_cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c, const void* q,
+                             const int32_t* row_offsets, const int32_t* lens, void* O, float* lse,
+                             void* scratch, hipStream_t s);
 // n_sel 0: all tokens; else the listed pages
 bool cache_attn_fits(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel);
 size_t cache_attn_scratch(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel,

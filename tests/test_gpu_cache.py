@@ -329,7 +329,7 @@ def test_shared_prefixes(B, case):
 def test_what_a_row_does_not_see_does_not_reach_it(B, n, ln, o_f32):
     """Infinities and NaN in the keys and values of later new tokens: rows before them
     are as without, rows after them are not finite where they meet them (infinity or
-    NaN: a weight whose second piece is 0 makes NaN of an infinity)."""
+    NaN: what is not finite is found apart from the products)."""
     s = Setup(B, [(n, ln), (n, ln)], H=4, hk=2, D=128, page=64, o_f32=o_f32, seed=9)
     ref = s.reference()
     for b, bad in ((0, n - 3), (1, n // 2)):
