@@ -41,9 +41,8 @@ constexpr float kCLog2e = 1.4426950408889634f;
 constexpr float kCLn2 = 0.6931471805599453f;
 constexpr int kCWaves = 4;
 constexpr int kCThreads = 64 * kCWaves;
-constexpr int kCTile = 32;                 // tokens of a tile
+constexpr int kCTile = kOwnTile;           // tokens of a tile
 constexpr int kCLeast = 8;                 // tiles of a run, at least
-constexpr int kCMeta = 8;                  // ints a sequence in the workspace
 constexpr float kCOver = 8.f;
 
 // bf16 pieces of a softmax weight in the second product: two for bf16 output (2^-16
@@ -51,71 +50,15 @@ constexpr float kCOver = 8.f;
 template <bool OUT_F32> constexpr int kCPieces = OUT_F32 ? 3 : 2;
 
 struct CacheAttnArgs {
+  CacheBatch batch;
   CacheView cache;
+  CacheResults res;                 // (where results are joined)
   const bf16_t* q;
-  const int32_t *row_offsets, *lens, *prefix_ids, *prefix_lens;
   const int32_t* pages;             // listed pages [rows][heads_kv][n_sel], or NULL
   void* O;
   float* lse;
-  int32_t* meta;                    // [B][kCMeta] + the run's tiles, where results are joined
-  float* part;                      // [2 runs] results of parts of items
-  float* whole;                     // [2][rows H] results of whole items, with prefixes
-  int B, H, G, total_rows, k_max, L_max, n_sel, o_f32, runs, direct;
+  int n_sel, o_f32, runs, direct;
   float scale_log2;
-};
-
-// Floats of a partial result: cols rows of D values, references, sums.
-template <int D>
-__device__ __host__ constexpr size_t part_floats(int cols) { return (size_t)cols * (D + 2); }
-
-// 64 sequences, one a lane, and the tiles of their items.
-struct SeqBlock {
-  CacheSeq s;
-  int P, first, run_rows;           // shared prefix; its run's first lane and rows
-  int up, us, incl;                 // tiles of the prefix's items (of the run's first
-                                    // lane) and of the sequence's own; running sums
-  template <int COLS>
-  __device__ __forceinline__ int row_tiles(const CacheAttnArgs& a, int rows) const {
-    return (rows * a.G + COLS - 1) / COLS;
-  }
-  __device__ __forceinline__ static int tiles(int lo, int hi) {
-    return max((hi + kCTile - 1) / kCTile - lo / kCTile, 1);
-  }
-  template <int COLS>
-  __device__ __forceinline__ void load(const CacheAttnArgs& a, int b0) {
-    const int lane = (int)__lane_id(), b = b0 + lane;
-    s = CacheSeq{0, 0, 0};
-    int id = -1, pl = 0;
-    if (b < a.B) {
-      s.load(a.row_offsets, a.lens, b, a.total_rows, a.k_max, a.L_max);
-      if (a.prefix_ids) {
-        id = a.prefix_ids[b];
-        pl = clampi(a.prefix_lens[b], 0, a.L_max);
-      }
-    }
-    P = 0;
-    first = lane;
-    run_rows = 0;
-    up = 0;
-    if (a.prefix_ids) {
-      const int id_b = __shfl_up(id, 1, kWave), pl_b = __shfl_up(pl, 1, kWave);
-      const bool member = lane > 0 && id >= 0 && pl > 0 && id == id_b && pl == pl_b;
-      const uint64_t starts = __ballot(!member);
-      const uint64_t upto = lane == 63 ? ~0ull : (2ull << lane) - 1ull;
-      first = 63 - __builtin_clzll(starts & upto);
-      const uint64_t after = starts & ~upto;
-      const int last = after ? __builtin_ctzll(after) - 1 : 63;    // of the run
-      if (last > first) {
-        P = pl;
-        const int end = s.r0 + s.n;
-        run_rows = __shfl(end, last, kWave) - __shfl(s.r0, first, kWave);
-        if (lane == first && run_rows > 0)
-          up = a.cache.heads_kv * row_tiles<COLS>(a, run_rows) * tiles(0, P);
-      }
-    }
-    us = s.n > 0 ? a.cache.heads_kv * row_tiles<COLS>(a, s.n) * tiles(min(P, s.len), s.len) : 0;
-    incl = (int)wave_incl_scan((uint32_t)(up + us));
-  }
 };
 
 // What a run's part of an item is: tiles t0 .. t1 - 1 of its nt.
@@ -124,13 +67,15 @@ struct CacheItem {
   int r0, v0, nv;                   // first row; virtual rows v0 .. v0 + nv - 1
   int lo, hi, nt, t0, t1;
   int start;                        // tile 0 among all items' tiles
+  int n;                            // the sequence's new tokens
   bool shared;                      // rows with a prefix: results are joined
-  int kind;                         // 0 a prefix, 1 a sequence's own, 2 listed pages
 };
 
 template <int D, int R, bool OUT_F32, bool LISTED>
 __global__ void __launch_bounds__(kCThreads, R > 2 ? 1 : 2)
-cache_attn_kernel(CacheAttnArgs a) {
+cache_attn_kernel(CacheAttnArgs args) {
+  const CacheAttnArgs& a = args;
+  const CacheBatch& bt = a.batch;
   constexpr int COLS = 16 * R, KC = D / 32, NB = D / 16, FPL = D / 16, PIECES = kCPieces<OUT_F32>;
   constexpr int VW = FPL / 2;               // dwords of a lane's features of a token
   constexpr int OS = D + 4;
@@ -150,9 +95,6 @@ cache_attn_kernel(CacheAttnArgs a) {
   const int koff = (8 * (n >> 2) + (n & 3)) * D + 8 * g;
   const int voff = 8 * g * D + FPL * n;
 
-  SeqBlock sb;                               // (of the item's sequences)
-  int sb0 = 0;                               // their first
-
   // One part of an item: every wave its tiles, then the waves' results together.
   auto work = [&](const CacheItem& it) {
     // this lane's columns: rows, how many tokens they see
@@ -162,30 +104,15 @@ cache_attn_kernel(CacheAttnArgs a) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int v = it.v0 + min(16 * r + n, it.nv - 1);
-      const int ri = v / a.G, row = it.r0 + ri;
-      const bf16_t* src = a.q + ((size_t)row * a.H + it.hk * a.G + (v - ri * a.G)) * D + 8 * g;
+      const int ri = v / bt.G, row = it.r0 + ri;
+      const bf16_t* src = a.q + ((size_t)row * bt.H + it.hk * bt.G + (v - ri * bt.G)) * D + 8 * g;
       if (r < nblk)
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
           qf[r][c] = *reinterpret_cast<const u32x4*>(src + 32 * c);
           if (neg || flat) qf[r][c] = flat ? u32x4{0u, 0u, 0u, 0u} : qf[r][c] ^ neg;
         }
-      if constexpr (LISTED) {
-        lim[r] = it.hi;
-      } else if (it.kind == 0) {
-        // the row's sequence: the last of the block that starts at or before it (a
-        // sequence without rows starts where the next one does)
-        int l = 0;
-#pragma unroll
-        for (int st = 32; st >= 1; st >>= 1)
-          if (__shfl(sb.s.r0, l + st, kWave) <= row && sb0 + l + st < a.B) l += st;
-        const int sr0 = __shfl(sb.s.r0, l, kWave), sn = __shfl(sb.s.n, l, kWave);
-        const int sl = __shfl(sb.s.len, l, kWave);
-        lim[r] = row < sr0 + sn ? min(it.hi, sl - sn + (row - sr0) + 1) : 0;
-      } else {
-        const int sn = __builtin_amdgcn_readlane(sb.s.n, it.b - sb0);
-        lim[r] = min(it.hi, it.hi - sn + ri + 1);        // (hi is the sequence's length)
-      }
+      lim[r] = LISTED ? it.hi : min(it.hi, it.hi - it.n + ri + 1);   // (hi: the length)
     }
     int least = lim[0], most = lim[0];
 #pragma unroll
@@ -437,8 +364,8 @@ cache_attn_kernel(CacheAttnArgs a) {
         o.w = fmaf(x.w, f, o.w);
         l = fmaf(pl[w][col], f, l);
       }
-      const int v = it.v0 + col, ri = v / a.G;
-      const size_t vr = (size_t)(it.r0 + ri) * a.H + it.hk * a.G + (v - ri * a.G);
+      const int v = it.v0 + col, ri = v / bt.G;
+      const size_t vr = (size_t)(it.r0 + ri) * bt.H + it.hk * bt.G + (v - ri * bt.G);
       if (all && !it.shared) {
         const float inv = l == 0.f ? 0.f : 1.f / l;            // (keeps NaN)
         if (OUT_F32)
@@ -448,29 +375,33 @@ cache_attn_kernel(CacheAttnArgs a) {
           *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + vr * D + 4 * c4) =
               make_uint2(pack2_bf16(o.x * inv, o.y * inv), pack2_bf16(o.z * inv, o.w * inv));
         if (a.lse && c4 == 0) a.lse[vr] = l == 0.f ? -INFINITY : (m + log2f(l)) * kCLn2;
-      } else if (all) {
-        float* w = a.whole + ((size_t)it.kind * a.total_rows * a.H + vr) * (D + 4);
+      } else {
+        float *w, *ml;
+        int ml_step;
+        if (all) {
+          w = whole_at<D>(a.res, bt, 1, vr);
+          ml = w + D;
+          ml_step = 1;
+        } else {
+          w = a.res.part + (size_t)(2 * run + (it.t0 == 0 ? 1 : 0)) * part_floats<D>(COLS);
+          ml = w + (size_t)COLS * D + col;
+          ml_step = COLS;
+          w += (size_t)col * D;
+        }
         *reinterpret_cast<float4*>(w + 4 * c4) = o;
         if (c4 == 0) {
-          w[D] = m;
-          w[D + 1] = l;
-        }
-      } else {
-        float* w = a.part + (size_t)(2 * run + (it.t0 == 0 ? 1 : 0)) * part_floats<D>(COLS);
-        *reinterpret_cast<float4*>(w + (size_t)col * D + 4 * c4) = o;
-        if (c4 == 0) {
-          w[(size_t)COLS * D + col] = m;
-          w[(size_t)COLS * D + COLS + col] = l;
+          ml[0] = m;
+          ml[ml_step] = l;
         }
       }
     }
   };
 
   if constexpr (LISTED) {
-    const int rows = clampi(a.row_offsets[a.B], 0, a.total_rows);
+    const int rows = clampi(bt.row_offsets[bt.B], 0, bt.total_rows);
     const int nt = a.n_sel << (shift - 5);
     const int W = rows * hkv * nt, per = a.direct ? nt : max((W + a.runs - 1) / a.runs, kCLeast);
-    if (blockIdx.x == 0 && tid == 0) a.meta[(size_t)a.B * kCMeta] = per;
+    if (!a.direct && blockIdx.x == 0 && tid == 0) a.res.meta[(size_t)bt.B * kCacheMeta] = per;
     int u = blockIdx.x * per;
     const int end = min(W - u, per) + u;
     while (u < end) {
@@ -484,99 +415,84 @@ cache_attn_kernel(CacheAttnArgs a) {
       it.t1 = min(nt, end - it.start);
       u = it.start + it.t1;
       CacheSeq s;
-      it.b = seq_of_row(a.row_offsets, a.lens, a.B, a.total_rows, a.k_max, a.L_max, it.r0, s);
+      it.b = seq_of_row(bt.row_offsets, bt.lens, bt.B, bt.total_rows, bt.k_max, bt.L_max, it.r0, s);
       if (it.b < 0) continue;
       it.v0 = 0;
-      it.nv = a.G;
+      it.nv = bt.G;
       it.lo = 0;
       it.hi = max(s.len - s.n + it.r0 - s.r0 + 1, 0);
+      it.n = 1;
       it.shared = false;
-      it.kind = 2;
       work(it);
     }
   } else {
-    auto item = [&](int L, int start, int x, int end) -> CacheItem {
-      // tile x (among all) of the sequence in lane L, whose tiles begin at `start`
-      const int up = __builtin_amdgcn_readlane(sb.up, L);
-      const int n_ = __builtin_amdgcn_readlane(sb.s.n, L), len = __builtin_amdgcn_readlane(sb.s.len, L);
-      const int P = __builtin_amdgcn_readlane(sb.P, L);
-      CacheItem it;
-      it.b = sb0 + L;
-      it.r0 = __builtin_amdgcn_readlane(sb.s.r0, L);
+    SeqWalk<false> walk;
+    walk.cols = COLS;
+    auto own = [&](CacheItem& it, int L) {       // the sequence in lane L
+      it.b = walk.sb0 + L;
+      it.r0 = walk.of_lane(walk.sb.s.r0, L);
+      it.n = walk.of_lane(walk.sb.s.n, L);
+      it.hi = walk.of_lane(walk.sb.s.len, L);
+      const int P = walk.of_lane(walk.sb.P, L);
+      it.lo = min(P, it.hi);
       it.shared = P > 0;
-      const bool pre = x - start < up;
-      it.kind = pre ? 0 : 1;
-      const int rows = pre ? __builtin_amdgcn_readlane(sb.run_rows, L) : n_;
-      const int rt = sb.row_tiles<COLS>(a, rows);
-      it.lo = pre ? 0 : min(P, len);
-      it.hi = pre ? P : len;
-      it.nt = SeqBlock::tiles(it.lo, it.hi);
-      const int s0 = pre ? start : start + up;
-      const int i = (x - s0) / it.nt;
-      it.hk = i / rt;
-      it.v0 = (i - it.hk * rt) * COLS;
-      it.nv = min(COLS, rows * a.G - it.v0);
-      it.start = s0 + i * it.nt;
-      it.t0 = x - it.start;
-      it.t1 = min(it.nt, end - it.start);
-      return it;
+      it.nt = SeqBlock::own_tiles(it.lo, it.hi);
     };
     if (a.direct) {
       // short sequences: an item a workgroup, no parts
-      const int rt = (a.k_max * a.G + COLS - 1) / COLS;
+      const int rt = (bt.k_max * bt.G + COLS - 1) / COLS;
       const int b = blockIdx.x / (hkv * rt), i = blockIdx.x - b * hkv * rt;
-      sb0 = b & ~63;
-      sb.load<COLS>(a, sb0);
+      CacheSeq s;
+      s.load(bt.row_offsets, bt.lens, b, bt.total_rows, bt.k_max, bt.L_max);
       CacheItem it;
       it.b = b;
+      it.r0 = s.r0;
+      it.n = s.n;
       it.hk = i / rt;
       it.v0 = (i - it.hk * rt) * COLS;
-      it.r0 = __builtin_amdgcn_readlane(sb.s.r0, b - sb0);
-      it.nv = min(COLS, __builtin_amdgcn_readlane(sb.s.n, b - sb0) * a.G - it.v0);
+      it.nv = min(COLS, s.n * bt.G - it.v0);
       if (it.nv <= 0) return;
       it.lo = 0;
-      it.hi = __builtin_amdgcn_readlane(sb.s.len, b - sb0);
-      it.nt = SeqBlock::tiles(0, it.hi);
+      it.hi = s.len;
+      it.nt = SeqBlock::own_tiles(0, s.len);
       it.t0 = it.start = 0;
       it.t1 = it.nt;
       it.shared = false;
-      it.kind = 1;
       work(it);
       return;
     }
     // all tiles, and the places of the items for the join
-    int W = 0;
-    for (sb0 = 0; sb0 < a.B; sb0 += 64) {
-      sb.load<COLS>(a, sb0);
-      if (blockIdx.x == 0 && wave == 0) {
-        const int own = W + sb.incl - sb.us;            // of the sequence's own items
-        const int pre = __shfl(W + sb.incl - sb.us - sb.up, sb.first, kWave);
-        const int r_first = __shfl(sb.s.r0, sb.first, kWave);
-        if (sb0 + lane < a.B) {
-          int32_t* w = a.meta + (size_t)(sb0 + lane) * kCMeta;
-          reinterpret_cast<int4*>(w)[0] = make_int4(own, pre, sb.P, r_first);
-          reinterpret_cast<int4*>(w)[1] = make_int4(sb.run_rows, sb.s.r0, sb.s.n, sb.s.len);
-        }
+    int pre_before = 0;
+    const int W = walk.total(bt, [&](int before) {
+      if (blockIdx.x != 0 || wave != 0) return;
+      const SeqBlock& sb = walk.sb;
+      const int pre_incl = (int)wave_incl_scan((uint32_t)sb.pre);
+      const int pre = __shfl(pre_before + pre_incl - sb.pre, sb.first, kWave);
+      const int r_first = __shfl(sb.s.r0, sb.first, kWave);
+      if (walk.sb0 + lane < bt.B) {
+        int32_t* w = a.res.meta + (size_t)(walk.sb0 + lane) * kCacheMeta;
+        reinterpret_cast<int4*>(w)[0] = make_int4(before + walk.incl - sb.own, pre, sb.P, r_first);
+        reinterpret_cast<int4*>(w)[1] = make_int4(sb.run_rows, sb.s.r0, sb.s.n, sb.s.len);
       }
-      W += __builtin_amdgcn_readlane(sb.incl, 63);
-    }
+      pre_before += __builtin_amdgcn_readlane(pre_incl, 63);
+    });
     const int per = max((W + a.runs - 1) / a.runs, kCLeast);
-    if (blockIdx.x == 0 && tid == 0) a.meta[(size_t)a.B * kCMeta] = per;
+    if (blockIdx.x == 0 && tid == 0) a.res.meta[(size_t)bt.B * kCacheMeta] = per;
     int u = blockIdx.x * per;
     if (u >= W) return;
     const int end = min(W - u, per) + u;
-    int base = 0;
-    sb0 = 0;
-    if (a.B > 64) sb.load<COLS>(a, 0);
     while (u < end) {
-      while (u >= base + __builtin_amdgcn_readlane(sb.incl, 63)) {
-        base += __builtin_amdgcn_readlane(sb.incl, 63);
-        sb0 += 64;
-        sb.load<COLS>(a, sb0);
-      }
-      const int L = __popcll(__ballot(base + sb.incl <= u));
-      const int start = base + __builtin_amdgcn_readlane(sb.incl - sb.up - sb.us, L);
-      const CacheItem it = item(L, start, u, end);
+      int first;
+      const int L = walk.seek(bt, u, first);
+      CacheItem it;
+      own(it, L);
+      const int rt = SeqBlock::row_tiles(bt, it.n, COLS), i = (u - first) / it.nt;
+      it.hk = i / rt;
+      it.v0 = (i - it.hk * rt) * COLS;
+      it.nv = min(COLS, it.n * bt.G - it.v0);
+      it.start = first + i * it.nt;
+      it.t0 = u - it.start;
+      it.t1 = min(it.nt, end - it.start);
       u = it.start + it.t1;
       work(it);
     }
@@ -589,17 +505,17 @@ template <int D, int COLS, bool OUT_F32, bool LISTED>
 __global__ void __launch_bounds__(256)
 cache_join_kernel(CacheAttnArgs a) {
   constexpr int NC4 = D / 4, VR = 256 / NC4;       // lanes a virtual row, virtual rows
-  const int hkv = a.cache.heads_kv, shift = a.cache.shift;
-  const int per_row = (a.H + VR - 1) / VR;
+  const CacheBatch& bt = a.batch;
+  const int hkv = bt.heads_kv, shift = a.cache.shift;
+  const int per_row = (bt.H + VR - 1) / VR;
   const int row = blockIdx.x / per_row;
   const int h = (blockIdx.x - row * per_row) * VR + threadIdx.x / NC4;
   const int c4 = threadIdx.x % NC4;
   CacheSeq s;
-  const int b = seq_of_row(a.row_offsets, a.lens, a.B, a.total_rows, a.k_max, a.L_max, row, s);
-  if (b < 0 || h >= a.H) return;
-  const int per = a.meta[(size_t)a.B * kCMeta];
-  const int hk = h / a.G;
-  const size_t vr = (size_t)row * a.H + h;
+  const int b = seq_of_row(bt.row_offsets, bt.lens, bt.B, bt.total_rows, bt.k_max, bt.L_max, row, s);
+  if (b < 0 || h >= bt.H) return;
+  const int hk = h / bt.G, g = h - hk * bt.G;
+  const size_t vr = (size_t)row * bt.H + h;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](float4 x, float xm, float xl) {
@@ -610,53 +526,58 @@ cache_join_kernel(CacheAttnArgs a) {
     l = fmaf(xl, fx, l * f);
     m = to;
   };
-  // results of tiles [start, start + nt) in column col
-  auto parts = [&](int kind, int start, int nt, int col) -> bool {
+  // results of tiles [start, start + nt) in column col of cols
+  auto parts = [&](bool own, const float* part, int cols, int per, int start, int nt, int col) {
     const int c0 = start / per, c1 = (start + nt - 1) / per;
     if (c0 == c1) {
-      if (!a.whole) return false;
-      const float* w = a.whole + ((size_t)kind * a.total_rows * a.H + vr) * (D + 4);
+      const float* w = whole_at<D>(a.res, bt, own, vr);
       add(*reinterpret_cast<const float4*>(w + 4 * c4), w[D], w[D + 1]);
-      return true;
+      return;
     }
-    constexpr int U = 4;                           // parts in flight
+    constexpr int U = 8;                           // parts in flight
     for (int c = c0; c <= c1; c += U) {
       float4 x[U];
       float xm[U], xl[U];
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int k = min(c + i, c1);
-        const float* w = a.part + (size_t)(2 * k + (k == c0 && start >= k * per ? 1 : 0)) *
-                                      part_floats<D>(COLS);
+        const float* w = part + (size_t)(2 * k + (k == c0 && start >= k * per ? 1 : 0)) *
+                                    part_floats<D>(cols);
         x[i] = *reinterpret_cast<const float4*>(w + (size_t)col * D + 4 * c4);
-        xm[i] = w[(size_t)COLS * D + col];
-        xl[i] = w[(size_t)COLS * D + COLS + col];
+        xm[i] = w[(size_t)cols * D + col];
+        xl[i] = w[(size_t)cols * D + cols + col];
       }
 #pragma unroll
       for (int i = 0; i < U; ++i)
         if (c + i <= c1) add(x[i], xm[i], xl[i]);
     }
-    return true;
   };
+  const int32_t* pers = a.res.meta + (size_t)bt.B * kCacheMeta;
+  int start, nt, col;
+  bool alone = true;                               // no prefix
   if constexpr (LISTED) {
-    const int nt = a.n_sel << (shift - 5);
-    if (!parts(1, (row * hkv + hk) * nt, nt, h - hk * a.G)) return;
+    nt = a.n_sel << (shift - 5);
+    start = (row * hkv + hk) * nt;
+    col = g;
   } else {
-    const int4 x = reinterpret_cast<const int4*>(a.meta + (size_t)b * kCMeta)[0];
-    const int4 y = reinterpret_cast<const int4*>(a.meta + (size_t)b * kCMeta)[1];
-    const int own = x.x, pre = x.y, P = x.z;
-    const int g = h - hk * a.G;
-    if (P > 0) {
-      const int v = (row - x.w) * a.G + g, rt = (y.x * a.G + COLS - 1) / COLS;
-      const int nt = SeqBlock::tiles(0, P);
-      parts(0, pre + (hk * rt + v / COLS) * nt, nt, v % COLS);
+    const int4 x = reinterpret_cast<const int4*>(a.res.meta + (size_t)b * kCacheMeta)[0];
+    const int4 y = reinterpret_cast<const int4*>(a.res.meta + (size_t)b * kCacheMeta)[1];
+    const int P = x.z;
+    alone = P == 0;
+    if (!alone) {
+      const int v = (row - x.w) * bt.G + g, n = SeqBlock::prefix_tiles(P);
+      parts(false, a.res.part_pre, a.res.cols_pre, pers[1],
+            x.y + (hk * SeqBlock::row_tiles(bt, y.x, kPrefixRows) + v / kPrefixRows) * n, n,
+            v % kPrefixRows);
     }
-    const int v = (row - s.r0) * a.G + g, rt = (s.n * a.G + COLS - 1) / COLS;
-    const int lo = min(P, s.len), nt = SeqBlock::tiles(lo, s.len);
-    const int start = own + (hk * rt + v / COLS) * nt;
-    if (P == 0 && start / per == (start + nt - 1) / per) return;     // (it is written)
-    parts(1, start, nt, v % COLS);
+    const int v = (row - s.r0) * bt.G + g, lo = min(P, s.len);
+    nt = SeqBlock::own_tiles(lo, s.len);
+    start = x.x + (hk * SeqBlock::row_tiles(bt, s.n, COLS) + v / COLS) * nt;
+    col = v % COLS;
   }
+  const int per = pers[0];
+  if (alone && start / per == (start + nt - 1) / per) return;          // (it is written)
+  parts(true, a.res.part, COLS, per, start, nt, col);
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (OUT_F32)
     *reinterpret_cast<float4*>(static_cast<float*>(a.O) + vr * D + 4 * c4) =
@@ -673,9 +594,9 @@ cache_join_kernel(CacheAttnArgs a) {
 namespace {
 
 struct CachePlan {
-  int R, runs;
+  int R, runs, cols_pre;
   bool direct, prefixes;
-  size_t meta, part, whole;          // bytes
+  size_t meta, part, part_pre, whole;          // bytes
 };
 
 CachePlan cache_plan(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel, bool prefixes) {
@@ -690,17 +611,19 @@ CachePlan cache_plan(const skip_problem_t& p, const skip_kv_cache_t& c, int n_se
     // sequences of up to 512 tokens: an item a workgroup, prefixes with them
     x.direct = p.L_max <= 512;
     x.prefixes = prefixes && !x.direct;
-    const long long rows = (long long)(x.prefixes ? p.total_kept : p.k_max) * G;
-    x.R = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    x.R = p.k_max * G <= 16 ? 1 : 2;
     const int cols = 16 * x.R;
-    x.runs = x.direct ? p.B * c.heads_kv * ((p.k_max * G + cols - 1) / cols)
-                      : x.R > 2 ? 256 : 512;
+    x.runs = x.direct ? p.B * c.heads_kv * ((p.k_max * G + cols - 1) / cols) : 512;
   }
   if (!x.direct) {
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
-    x.meta = up(((size_t)p.B * kCMeta + 1) * sizeof(int32_t));
+    x.meta = up(((size_t)p.B * kCacheMeta + 2) * sizeof(int32_t));
     x.part = up(2 * (size_t)x.runs * 16 * x.R * (p.d_h + 2) * sizeof(float));
-    if (x.prefixes) x.whole = 2 * (size_t)p.total_kept * p.H * (p.d_h + 4) * sizeof(float);
+    if (x.prefixes) {
+      x.cols_pre = (int)std::min<long long>(kPrefixRows, ((long long)p.total_kept * G + 31) / 32 * 32);
+      x.part_pre = up(2 * (size_t)kPrefixRuns * x.cols_pre * (p.d_h + 2) * sizeof(float));
+      x.whole = 2 * (size_t)p.total_kept * p.H * (p.d_h + 4) * sizeof(float);
+    }
   }
   return x;
 }
@@ -710,8 +633,12 @@ hipError_t launch_one(const CacheAttnArgs& a, hipStream_t s) {
   cache_attn_kernel<D, R, OUT_F32, LISTED><<<dim3((unsigned)a.runs), kCThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.direct) return e;
+  if (a.batch.prefix_ids) {
+    e = launch_cache_prefixes(a.batch, a.cache, a.res, a.q, D, a.o_f32, a.scale_log2, s);
+    if (e != hipSuccess) return e;
+  }
   constexpr int VR = 1024 / D;
-  const unsigned grid = (unsigned)a.total_rows * (unsigned)((a.H + VR - 1) / VR);
+  const unsigned grid = (unsigned)a.batch.total_rows * (unsigned)((a.batch.H + VR - 1) / VR);
   cache_join_kernel<D, 16 * R, OUT_F32, LISTED><<<dim3(grid), 256, 0, s>>>(a);
   return hipGetLastError();
 }
@@ -719,11 +646,7 @@ template <int D, bool LISTED>
 hipError_t launch_rows(const CacheAttnArgs& a, int R, hipStream_t s) {
   if (R == 1)
     return a.o_f32 ? launch_one<D, 1, true, LISTED>(a, s) : launch_one<D, 1, false, LISTED>(a, s);
-  if (R == 2)
-    return a.o_f32 ? launch_one<D, 2, true, LISTED>(a, s) : launch_one<D, 2, false, LISTED>(a, s);
-  if constexpr (!LISTED)
-    return a.o_f32 ? launch_one<D, 4, true, false>(a, s) : launch_one<D, 4, false, false>(a, s);
-  return hipErrorInvalidValue;
+  return a.o_f32 ? launch_one<D, 2, true, LISTED>(a, s) : launch_one<D, 2, false, LISTED>(a, s);
 }
 
 }  // namespace
@@ -741,7 +664,7 @@ size_t cache_attn_scratch(const skip_problem_t& p, const skip_kv_cache_t& c, int
                           bool prefixes) {
   if (n_sel == 0 && cache_tall(p, c)) return cache_tall_scratch(p, c);
   const CachePlan x = cache_plan(p, c, n_sel, prefixes);
-  return x.meta + x.part + x.whole;
+  return x.meta + x.part + x.part_pre + x.whole;
 }
 
 hipError_t launch_cache_attn(const skip_problem_t& p, const skip_kv_cache_t& c, const void* q,
@@ -753,12 +676,23 @@ hipError_t launch_cache_attn(const skip_problem_t& p, const skip_kv_cache_t& c, 
     return launch_cache_tall(p, c, q, row_offsets, lens, O, lse, scratch, s);
   const CachePlan x = cache_plan(p, c, n_sel, prefix_ids != nullptr);
   char* w = static_cast<char*>(scratch);
-  CacheAttnArgs a{cache_view(c), static_cast<const bf16_t*>(q), row_offsets, lens,
-                  x.prefixes ? prefix_ids : nullptr, prefix_lens, pages, O, lse,
-                  reinterpret_cast<int32_t*>(w), reinterpret_cast<float*>(w + x.meta),
-                  x.whole ? reinterpret_cast<float*>(w + x.meta + x.part) : nullptr, p.B, p.H,
-                  p.H / c.heads_kv, p.total_kept, p.k_max, p.L_max, n_sel, p.o_f32, x.runs,
-                  x.direct, p.sm_scale * kCLog2e};
+  auto take = [&](size_t bytes) {
+    char* r = w;
+    w += bytes;
+    return reinterpret_cast<float*>(r);
+  };
+  CacheResults res{};
+  if (!x.direct) {
+    res.meta = reinterpret_cast<int32_t*>(take(x.meta));
+    res.part = take(x.part);
+    res.part_pre = take(x.part_pre);
+    res.whole = take(x.whole);
+    res.cols_pre = x.cols_pre;
+  }
+  CacheAttnArgs a{cache_batch(p, c, row_offsets, lens, x.prefixes ? prefix_ids : nullptr,
+                              prefix_lens),
+                  cache_view(c), res, static_cast<const bf16_t*>(q), pages, O, lse, n_sel, p.o_f32,
+                  x.runs, x.direct, p.sm_scale * kCLog2e};
   if (n_sel > 0)
     return p.d_h == 64 ? launch_rows<64, true>(a, x.R, s) : launch_rows<128, true>(a, x.R, s);
   return p.d_h == 64 ? launch_rows<64, false>(a, x.R, s) : launch_rows<128, false>(a, x.R, s);

@@ -29,49 +29,59 @@ constexpr int kTWaves = 4;
 constexpr int kTThreads = 64 * kTWaves;
 constexpr int kTRows = 32 * kTWaves;       // virtual rows of an item
 constexpr int kTTile = 64;                 // tokens of a tile
+constexpr int kTLeast = 4;                 // tiles of a share or run, at least
+static_assert(kTRows == kPrefixRows && kTTile == kPrefixTile, "items of prefixes");
 constexpr float kTLn2 = 0.6931471805599453f;
 constexpr float kTOver = 8.f;
 template <bool OUT_F32> constexpr int kTPieces = OUT_F32 ? 3 : 2;
 
 struct TallArgs {
+  CacheBatch batch;
   CacheView cache;
+  CacheResults res;                 // (prefixes)
   const bf16_t* q;
-  const int32_t *row_offsets, *lens;
   void* O;
   float* lse;
   float* part;                      // [items][splits] results of shares
-  int B, H, G, total_rows, k_max, L_max, row_tiles, splits, grouped;
+  int row_tiles, splits, grouped;
   float scale_log2;
 };
 
-// Which sequence, key head, 128 virtual rows and share a workgroup takes.  Workgroup
-// id L goes to XCD L % 8; where sequences and key heads make whole eights, the items of
-// one of them follow one another on one XCD, whose L2 then holds its keys and values.
-// Row tiles from the last, which see most tokens, to the first.
+// What a workgroup works on: 128 virtual rows, tiles i0 .. i1 - 1 of the nt that hold
+// the tokens before hi.
 struct TallItem {
-  int b, hk, rt, split;
+  int b, hk;                        // the sequence whose pages are read; key head
+  int r0, v0, nv;                   // first row of the set; virtual rows v0 .. v0 + nv - 1
+  int hi, nt, i0, i1;
+  int place;                        // of a share's result; a run's first tile of the item
   CacheSeq s;
-  int v0, nv;
 };
+// Workgroup id L goes to XCD L % 8; where sequences and key heads make whole eights,
+// the items of one of them follow one another on one XCD, whose L2 then holds its keys
+// and values.  Row tiles from the last, which see most tokens, to the first.
 __device__ __forceinline__ bool tall_item(const TallArgs& a, int L, TallItem& x) {
-  const int per = a.row_tiles * a.splits, groups = a.B * a.cache.heads_kv;
+  const CacheBatch& bt = a.batch;
+  const int per = a.row_tiles * a.splits, groups = bt.B * bt.heads_kv;
   const int grp = a.grouped ? (L & 7) + 8 * ((L >> 3) / per) : L / per;
   const int sub = a.grouped ? (L >> 3) % per : L % per;
   if (grp >= groups) return false;
-  x.b = grp / a.cache.heads_kv;
-  x.hk = grp - x.b * a.cache.heads_kv;
-  x.s.load(a.row_offsets, a.lens, x.b, a.total_rows, a.k_max, a.L_max);
-  const int rts = (x.s.n * a.G + kTRows - 1) / kTRows, i = sub / a.splits;
+  x.b = grp / bt.heads_kv;
+  x.hk = grp - x.b * bt.heads_kv;
+  x.s.load(bt.row_offsets, bt.lens, x.b, bt.total_rows, bt.k_max, bt.L_max);
+  const int rts = (x.s.n * bt.G + kTRows - 1) / kTRows, i = sub / a.splits;
   if (i >= rts) return false;
-  x.rt = rts - 1 - i;
-  x.split = sub - i * a.splits;
-  x.v0 = x.rt * kTRows;
-  x.nv = min(kTRows, x.s.n * a.G - x.v0);
+  const int rt = rts - 1 - i, split = sub - i * a.splits;
+  x.r0 = x.s.r0;
+  x.v0 = rt * kTRows;
+  x.nv = min(kTRows, x.s.n * bt.G - x.v0);
+  // the tokens that the last row sees
+  x.hi = max(x.s.len - x.s.n + (x.v0 + x.nv - 1) / bt.G + 1, 0);
+  x.nt = (x.hi + kTTile - 1) / kTTile;
+  x.i0 = (int)((long long)x.nt * split / a.splits);
+  x.i1 = (int)((long long)x.nt * (split + 1) / a.splits);
+  x.place = (grp * a.row_tiles + rt) * a.splits + split;
   return true;
 }
-
-template <int D>
-__device__ __host__ constexpr size_t tall_part() { return (size_t)kTRows * (D + 2); }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 // Four values of a column of 4 x 16 ones in LDS (this lane reads a quarter of a row).
@@ -84,49 +94,27 @@ __device__ __forceinline__ u32x4 lds_read16(uint32_t addr) {
   return *(Ptr)(uintptr_t)addr;
 }
 
-template <int D, bool OUT_F32>
+template <int D, bool OUT_F32, bool PREFIX>
 __global__ void __launch_bounds__(kTThreads, 2)
-cache_tall_kernel(TallArgs a) {
+cache_tall_kernel(TallArgs args) {
+  const TallArgs& a = args;
+  const CacheBatch& bt = a.batch;
   constexpr int KC = D / 16, FB = D / 32, PIECES = kTPieces<OUT_F32>;
   constexpr int ROW = 2 * D;                        // bytes of a token
   constexpr int CH = D / 8;                         // chunks of a token
   constexpr uint32_t kKeys = kTTile * ROW, kBuffer = 2 * kKeys;
   __shared__ __attribute__((aligned(1024))) uint8_t tile[2 * kBuffer];
-  TallItem it;
-  if (!tall_item(a, blockIdx.x, it)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, hh = lane >> 5;
   const int shift = a.cache.shift;
   const uint32_t lds = lds_addr(tile);
-
-  // this lane's row and how many tokens it sees; the wave's least and most
-  const int wv = it.v0 + 32 * wave;                 // the wave's first virtual row
-  const bool any = wv < it.v0 + it.nv;
-  const int v = min(wv + n, it.v0 + it.nv - 1);
-  const int ri = v / a.G, head = it.hk * a.G + (v - ri * a.G), row = it.s.r0 + ri;
-  const int lim = max(it.s.len - it.s.n + ri + 1, 0);
-  const int least = max(it.s.len - it.s.n + min(wv, it.v0 + it.nv - 1) / a.G + 1, 0);
-  const int most = max(it.s.len - it.s.n + min(wv + 31, it.v0 + it.nv - 1) / a.G + 1, 0);
-  // tokens of the item, tiles of this share
-  const int hi = max(it.s.len - it.s.n + (it.v0 + it.nv - 1) / a.G + 1, 0);
-  const int tiles = (hi + kTTile - 1) / kTTile;
-  const int i0 = (int)((long long)tiles * it.split / a.splits);
-  const int i1 = (int)((long long)tiles * (it.split + 1) / a.splits);
+  SeqWalk<true> walk;
+  walk.cols = 16;                                   // (own items are not looked at)
 
   const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;
   const bool flat = a.scale_log2 == 0.f;
   const float sc = flat ? 1.f : fabsf(a.scale_log2);
-  u32x4 qf[KC];
-  {
-    const bf16_t* src = a.q + ((size_t)row * a.H + head) * D + 8 * hh;
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      qf[c] = *reinterpret_cast<const u32x4*>(src + 16 * c);
-      if (neg || flat) qf[c] = flat ? u32x4{0u, 0u, 0u, 0u} : qf[c] ^ neg;
-    }
-  }
-
   // LDS addresses of this lane's operands in the first buffer
   uint32_t ka[KC], va_[FB];
 #pragma unroll
@@ -149,12 +137,52 @@ cache_tall_kernel(TallArgs a) {
     kg[i] = r * ROW + 16 * (c ^ (r & (CH - 1)));
     vg[i] = r * ROW + 16 * (c ^ ((2 * r) & (CH - 1)));
   }
+  auto work = [&](const TallItem& it) {
+  // this lane's row and how many tokens it sees; the wave's least and most
+  const int wv = it.v0 + 32 * wave;                 // the wave's first virtual row
+  const bool any = wv < it.v0 + it.nv;
+  const int v = min(wv + n, it.v0 + it.nv - 1);
+  const int ri = v / bt.G, head = it.hk * bt.G + (v - ri * bt.G), row = it.r0 + ri;
+  int lim, least, most;
+  if constexpr (PREFIX) {
+    // the row's sequence: the last of the block that starts at or before it (a sequence
+    // without rows starts where the next one does)
+    int l = 0;
+#pragma unroll
+    for (int st = 32; st >= 1; st >>= 1)
+      if (__shfl(walk.sb.s.r0, l + st, kWave) <= row && walk.sb0 + l + st < bt.B) l += st;
+    const int sr0 = __shfl(walk.sb.s.r0, l, kWave), sn = __shfl(walk.sb.s.n, l, kWave);
+    const int sl = __shfl(walk.sb.s.len, l, kWave);
+    lim = row < sr0 + sn ? clampi(sl - sn + (row - sr0) + 1, 0, it.hi) : 0;
+    least = most = lim;
+#pragma unroll
+    for (int st = 1; st < 32; st <<= 1) {
+      least = min(least, __shfl_xor(least, st, kWave));
+      most = max(most, __shfl_xor(most, st, kWave));
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    most = __builtin_amdgcn_readfirstlane(most);
+  } else {
+    const int before = it.s.len - it.s.n + 1;
+    lim = max(before + ri, 0);
+    least = max(before + min(wv, it.v0 + it.nv - 1) / bt.G, 0);
+    most = max(before + min(wv + 31, it.v0 + it.nv - 1) / bt.G, 0);
+  }
+  u32x4 qf[KC];
+  {
+    const bf16_t* src = a.q + ((size_t)row * bt.H + head) * D + 8 * hh;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      qf[c] = *reinterpret_cast<const u32x4*>(src + 16 * c);
+      if (neg || flat) qf[c] = flat ? u32x4{0u, 0u, 0u, 0u} : qf[c] ^ neg;
+    }
+  }
   // pages of 64 tiles at a time: lane i those of tile i's two halves
-  int pa = 0, pb = 0, pages_from = i0;
+  int pa = 0, pb = 0, pages_from = it.i0;
   auto load_pages = [&]() {
     const int t = (pages_from + lane) * kTTile;
-    pa = t < hi ? a.cache.page(it.b, t >> shift) : 0;
-    pb = t + 32 < hi ? a.cache.page(it.b, (t + 32) >> shift) : 0;
+    pa = t < it.hi ? a.cache.page(it.b, t >> shift) : 0;
+    pb = t + 32 < it.hi ? a.cache.page(it.b, (t + 32) >> shift) : 0;
   };
   // (tokens behind the last one are loaded from where they would lie, and masked)
   auto fetch = [&](int i, uint32_t buffer) {
@@ -304,11 +332,12 @@ cache_tall_kernel(TallArgs a) {
     });
   };
 
-  if (i0 < i1) {
+  if (it.i0 < it.i1) {
     load_pages();
-    fetch(i0, 0);
+    if constexpr (PREFIX) barrier_nofence();        // (the last item's tiles are read)
+    fetch(it.i0, 0);
   }
-  for (int i = i0; i < i1; ++i) {
+  for (int i = it.i0; i < it.i1; ++i) {
     // this tile's loads have landed, and every wave is through with the last one, whose
     // place the next one takes
     wait_vmcnt<0>();
@@ -316,7 +345,7 @@ cache_tall_kernel(TallArgs a) {
     const int l = i - pages_from;
     const int miss = (__builtin_amdgcn_readlane(pa, l) < 0 ? 1 : 0) |
                      (__builtin_amdgcn_readlane(pb, l) < 0 ? 2 : 0);
-    if (i + 1 < i1) fetch(i + 1, buffer ^ kBuffer);
+    if (i + 1 < it.i1) fetch(i + 1, buffer ^ kBuffer);
     const int t = i * kTTile;
     if (any && t < most) compute(t + kTTile > least || miss, t, miss);
     buffer ^= kBuffer;
@@ -329,24 +358,37 @@ cache_tall_kernel(TallArgs a) {
     l_run = __uint_as_float(x[0]) + __uint_as_float(x[1]);
   }
   if (wv + n >= it.v0 + it.nv) return;
-  if (a.splits > 1) {
-    const size_t item = ((size_t)it.b * a.cache.heads_kv + it.hk) * a.row_tiles + it.rt;
-    float* w = a.part + (item * a.splits + it.split) * tall_part<D>();
+  const size_t vr = (size_t)row * bt.H + head;
+  if (PREFIX || a.splits > 1) {
+    float *w, *ml;
+    int ml_step;
     const int col = 32 * wave + n;
+    if (PREFIX && it.i0 == 0 && it.i1 == it.nt) {
+      w = whole_at<D>(a.res, bt, 0, vr);
+      ml = w + D;
+      ml_step = 1;
+    } else {
+      const int cols = PREFIX ? a.res.cols_pre : kTRows;
+      w = PREFIX ? a.res.part_pre + (size_t)(2 * blockIdx.x + (it.i0 == 0 ? 1 : 0)) *
+                                        part_floats<D>(cols)
+                 : a.part + (size_t)it.place * part_floats<D>(kTRows);
+      ml = w + (size_t)cols * D + col;
+      ml_step = cols;
+      w += (size_t)col * D;
+    }
 #pragma unroll
     for (int f = 0; f < FB; ++f)
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        *reinterpret_cast<float4*>(w + (size_t)col * D + 32 * f + 8 * c + 4 * hh) = make_float4(
+        *reinterpret_cast<float4*>(w + 32 * f + 8 * c + 4 * hh) = make_float4(
             acc[f][4 * c], acc[f][4 * c + 1], acc[f][4 * c + 2], acc[f][4 * c + 3]);
     if (hh == 0) {
-      w[(size_t)kTRows * D + col] = m_run;
-      w[(size_t)kTRows * D + kTRows + col] = l_run;
+      ml[0] = m_run;
+      ml[ml_step] = l_run;
     }
     return;
   }
   const float inv = l_run == 0.f ? 0.f : 1.f / l_run;            // (keeps NaN)
-  const size_t vr = (size_t)row * a.H + head;
 #pragma unroll
   for (int f = 0; f < FB; ++f)
 #pragma unroll
@@ -361,6 +403,38 @@ cache_tall_kernel(TallArgs a) {
             make_uint2(pack2_bf16(o0, o1), pack2_bf16(o2, o3));
     }
   if (a.lse && hh == 0) a.lse[vr] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * kTLn2;
+  };
+
+  if constexpr (!PREFIX) {
+    TallItem it;
+    if (tall_item(a, blockIdx.x, it)) work(it);
+  } else {
+    const int W = walk.total(bt, [](int) {});
+    const int per = max((W + kPrefixRuns - 1) / kPrefixRuns, kTLeast);
+    if (blockIdx.x == 0 && tid == 0) a.res.meta[(size_t)bt.B * kCacheMeta + 1] = per;
+    int u = blockIdx.x * per;
+    if (u >= W) return;
+    const int end = min(W - u, per) + u;
+    while (u < end) {
+      int first;
+      const int L = walk.seek(bt, u, first);
+      TallItem it;
+      it.b = walk.sb0 + L;
+      it.r0 = walk.of_lane(walk.sb.s.r0, L);
+      it.hi = walk.of_lane(walk.sb.P, L);
+      it.nt = SeqBlock::prefix_tiles(it.hi);
+      const int rows = walk.of_lane(walk.sb.run_rows, L);
+      const int rt = SeqBlock::row_tiles(bt, rows, kTRows), i = (u - first) / it.nt;
+      it.hk = i / rt;
+      it.v0 = (i - it.hk * rt) * kTRows;
+      it.nv = min(kTRows, rows * bt.G - it.v0);
+      const int start = first + i * it.nt;
+      it.i0 = u - start;
+      it.i1 = min(it.nt, end - start);
+      u = start + it.i1;
+      work(it);
+    }
+  }
 }
 
 // Joins an item's shares, in the order of the tokens: D / 4 lanes a virtual row.
@@ -368,30 +442,31 @@ template <int D, bool OUT_F32>
 __global__ void __launch_bounds__(256)
 cache_tall_join_kernel(TallArgs a) {
   constexpr int NC4 = D / 4, VR = 256 / NC4, WG = kTRows / VR;
+  const CacheBatch& bt = a.batch;
   const int item = blockIdx.x / WG;
   const int rt = item % a.row_tiles, grp = item / a.row_tiles;
-  const int b = grp / a.cache.heads_kv, hk = grp - b * a.cache.heads_kv;
+  const int b = grp / bt.heads_kv, hk = grp - b * bt.heads_kv;
   const int col = (blockIdx.x - item * WG) * VR + threadIdx.x / NC4, c4 = threadIdx.x % NC4;
   CacheSeq s;
-  s.load(a.row_offsets, a.lens, b, a.total_rows, a.k_max, a.L_max);
+  s.load(bt.row_offsets, bt.lens, b, bt.total_rows, bt.k_max, bt.L_max);
   const int v = rt * kTRows + col;
-  if (v >= s.n * a.G) return;
-  const float* w = a.part + (size_t)item * a.splits * tall_part<D>();
+  if (v >= s.n * bt.G) return;
+  constexpr size_t step = part_floats<D>(kTRows);
+  const float* w = a.part + (size_t)item * a.splits * step;
   float m = -INFINITY;
-  for (int i = 0; i < a.splits; ++i)
-    m = fmaxf(m, w[i * tall_part<D>() + (size_t)kTRows * D + col]);
+  for (int i = 0; i < a.splits; ++i) m = fmaxf(m, w[i * step + (size_t)kTRows * D + col]);
   const float ref = m == -INFINITY ? 0.f : m;
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = 0; i < a.splits; ++i) {
-    const float* x = w + i * tall_part<D>();
+    const float* x = w + i * step;
     const float f = __builtin_amdgcn_exp2f(x[(size_t)kTRows * D + col] - ref);
     const float4 y = *reinterpret_cast<const float4*>(x + (size_t)col * D + 4 * c4);
     o = make_float4(fmaf(y.x, f, o.x), fmaf(y.y, f, o.y), fmaf(y.z, f, o.z), fmaf(y.w, f, o.w));
     l = fmaf(x[(size_t)kTRows * D + kTRows + col], f, l);
   }
-  const int ri = v / a.G;
-  const size_t vr = (size_t)(s.r0 + ri) * a.H + hk * a.G + (v - ri * a.G);
+  const int ri = v / bt.G;
+  const size_t vr = (size_t)(s.r0 + ri) * bt.H + hk * bt.G + (v - ri * bt.G);
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (OUT_F32)
     *reinterpret_cast<float4*>(static_cast<float*>(a.O) + vr * D + 4 * c4) =
@@ -409,15 +484,15 @@ static int tall_row_tiles(const skip_problem_t& p, const skip_kv_cache_t& c) {
   return (int)(((long long)p.k_max * (p.H / c.heads_kv) + kTRows - 1) / kTRows);
 }
 // Shares of an item: as many as leave some two workgroups a CU where there are few
-// items, of eight tiles at least.
+// items, of four tiles at least.
 static int tall_splits(const skip_problem_t& p, const skip_kv_cache_t& c) {
   const long long items = (long long)p.B * c.heads_kv * tall_row_tiles(p, c);
   const long long tiles = (p.L_max + kTTile - 1) / kTTile;
-  return (int)std::max<long long>(1, std::min({512 / std::max(items, 1ll), tiles / 8, 16ll}));
+  return (int)std::max<long long>(1, std::min({512 / std::max(items, 1ll), tiles / kTLeast, 64ll}));
 }
 
 bool cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c) {
-  return (long long)p.k_max * (p.H / c.heads_kv) > 64;
+  return (long long)p.k_max * (p.H / c.heads_kv) > 32;
 }
 
 size_t cache_tall_scratch(const skip_problem_t& p, const skip_kv_cache_t& c) {
@@ -429,9 +504,9 @@ size_t cache_tall_scratch(const skip_problem_t& p, const skip_kv_cache_t& c) {
 
 template <int D, bool OUT_F32>
 static hipError_t launch_tall(const TallArgs& a, hipStream_t s) {
-  const int groups = a.B * a.cache.heads_kv;
+  const int groups = a.batch.B * a.batch.heads_kv;
   const unsigned grid = (unsigned)groups * a.row_tiles * a.splits;
-  cache_tall_kernel<D, OUT_F32><<<dim3(grid), kTThreads, 0, s>>>(a);
+  cache_tall_kernel<D, OUT_F32, false><<<dim3(grid), kTThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   constexpr int WG = kTRows / (1024 / D);
@@ -443,12 +518,27 @@ static hipError_t launch_tall(const TallArgs& a, hipStream_t s) {
 hipError_t launch_cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c, const void* q,
                              const int32_t* row_offsets, const int32_t* lens, void* O, float* lse,
                              void* scratch, hipStream_t s) {
-  TallArgs a{cache_view(c), static_cast<const bf16_t*>(q), row_offsets, lens, O, lse,
-             static_cast<float*>(scratch), p.B, p.H, p.H / c.heads_kv, p.total_kept, p.k_max,
-             p.L_max, tall_row_tiles(p, c), tall_splits(p, c), p.B * c.heads_kv % 8 == 0,
+  TallArgs a{cache_batch(p, c, row_offsets, lens, nullptr, nullptr), cache_view(c), CacheResults{},
+             static_cast<const bf16_t*>(q), O, lse, static_cast<float*>(scratch),
+             tall_row_tiles(p, c), tall_splits(p, c), p.B * c.heads_kv % 8 == 0,
              p.sm_scale * 1.4426950408889634f};
   if (p.d_h == 64) return p.o_f32 ? launch_tall<64, true>(a, s) : launch_tall<64, false>(a, s);
   return p.o_f32 ? launch_tall<128, true>(a, s) : launch_tall<128, false>(a, s);
+}
+
+hipError_t launch_cache_prefixes(const CacheBatch& batch, const CacheView& cache,
+                                 const CacheResults& res, const bf16_t* q, int d_h, int o_f32,
+                                 float scale_log2, hipStream_t s) {
+  TallArgs a{batch, cache, res, q, nullptr, nullptr, nullptr, 0, 1, 0, scale_log2};
+  const dim3 grid(kPrefixRuns);
+  if (d_h == 64) {
+    if (o_f32) cache_tall_kernel<64, true, true><<<grid, kTThreads, 0, s>>>(a);
+    else cache_tall_kernel<64, false, true><<<grid, kTThreads, 0, s>>>(a);
+  } else {
+    if (o_f32) cache_tall_kernel<128, true, true><<<grid, kTThreads, 0, s>>>(a);
+    else cache_tall_kernel<128, false, true><<<grid, kTThreads, 0, s>>>(a);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace skip

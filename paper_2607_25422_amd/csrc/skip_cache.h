@@ -3,6 +3,7 @@
 #pragma once
 
 #include "skip_common.h"
+#include "skip_select.h"
 
 namespace skip {
 
@@ -63,6 +64,131 @@ __device__ __forceinline__ int seq_of_row(const int32_t* row_offsets, const int3
   return row >= s.r0 && row < s.r0 + s.n ? b : -1;
 }
 
+// A batch's rows, tokens and prefixes.
+struct CacheBatch {
+  const int32_t *row_offsets, *lens, *prefix_ids, *prefix_lens;
+  int B, H, G, heads_kv, total_rows, k_max, L_max;
+};
+
+// Items of sequences' own tokens are up to `cols` virtual rows over tiles of 32 tokens,
+// those of prefixes up to kPrefixRows over tiles of kPrefixTile.
+constexpr int kOwnTile = 32;
+constexpr int kPrefixRows = 128, kPrefixTile = 64;
+
+// 64 sequences, one a lane, and the tiles of their items.
+struct SeqBlock {
+  CacheSeq s;
+  int P, first, run_rows;           // shared prefix; its run's first lane and rows
+  int pre, own;                     // tiles of the prefix's items (of the run's first
+                                    // lane) and of the sequence's own
+  __device__ __forceinline__ static int row_tiles(const CacheBatch& a, int rows, int cols) {
+    return (rows * a.G + cols - 1) / cols;
+  }
+  __device__ __forceinline__ static int own_tiles(int lo, int hi) {
+    return max((hi + kOwnTile - 1) / kOwnTile - lo / kOwnTile, 1);
+  }
+  __device__ __forceinline__ static int prefix_tiles(int P) {
+    return (P + kPrefixTile - 1) / kPrefixTile;
+  }
+  __device__ __forceinline__ void load(const CacheBatch& a, int b0, int cols) {
+    const int lane = (int)__lane_id(), b = b0 + lane;
+    s = CacheSeq{0, 0, 0};
+    int id = -1, pl = 0;
+    if (b < a.B) {
+      s.load(a.row_offsets, a.lens, b, a.total_rows, a.k_max, a.L_max);
+      if (a.prefix_ids) {
+        id = a.prefix_ids[b];
+        pl = clampi(a.prefix_lens[b], 0, a.L_max);
+      }
+    }
+    P = 0;
+    first = lane;
+    run_rows = 0;
+    pre = 0;
+    if (a.prefix_ids) {
+      const int id_b = __shfl_up(id, 1, kWave), pl_b = __shfl_up(pl, 1, kWave);
+      const bool member = lane > 0 && id >= 0 && pl > 0 && id == id_b && pl == pl_b;
+      const uint64_t starts = __ballot(!member);
+      const uint64_t upto = lane == 63 ? ~0ull : (2ull << lane) - 1ull;
+      first = 63 - __builtin_clzll(starts & upto);
+      const uint64_t after = starts & ~upto;
+      const int last = after ? __builtin_ctzll(after) - 1 : 63;    // of the run
+      // (every lane takes part in the exchange)
+      const int rows = __shfl(s.r0 + s.n, last, kWave) - __shfl(s.r0, first, kWave);
+      if (last > first) {
+        P = pl;
+        run_rows = rows;
+        if (lane == first && run_rows > 0)
+          pre = a.heads_kv * row_tiles(a, run_rows, kPrefixRows) * prefix_tiles(P);
+      }
+    }
+    own = s.n > 0 ? a.heads_kv * row_tiles(a, s.n, cols) * own_tiles(min(P, s.len), s.len) : 0;
+  }
+};
+
+// The tiles of all items (of prefixes, or of sequences' own tokens) in order, and the
+// sequence that a tile is of.
+template <bool PREFIX>
+struct SeqWalk {
+  SeqBlock sb;                      // sequences sb0 ..
+  int sb0, base, incl;              // tiles before them; running sums of theirs
+  int cols;
+  __device__ __forceinline__ int mine() const { return PREFIX ? sb.pre : sb.own; }
+  __device__ __forceinline__ void block(const CacheBatch& a, int b0) {
+    sb0 = b0;
+    sb.load(a, b0, cols);
+    incl = (int)wave_incl_scan((uint32_t)mine());
+  }
+  __device__ __forceinline__ int block_tiles() const { return __builtin_amdgcn_readlane(incl, 63); }
+  // All tiles; leaves the walk at the first sequences.
+  template <class F>
+  __device__ __forceinline__ int total(const CacheBatch& a, F&& each) {
+    int W = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      block(a, b0);
+      each(W);
+      W += block_tiles();
+    }
+    base = 0;
+    if (a.B > 64) block(a, 0);
+    return W;
+  }
+  // The lane whose sequence tile u is of, and that sequence's first tile.
+  __device__ __forceinline__ int seek(const CacheBatch& a, int u, int& start) {
+    while (u >= base + block_tiles()) {
+      base += block_tiles();
+      block(a, sb0 + 64);
+    }
+    const int L = __popcll(__ballot(base + incl <= u));
+    start = base + __builtin_amdgcn_readlane(incl - mine(), L);
+    return L;
+  }
+  __device__ __forceinline__ int of_lane(int x, int L) const {
+    return __builtin_amdgcn_readlane(x, L);
+  }
+};
+
+// What the kernels of one call leave for the join, in the workspace: kCacheMeta ints
+// a sequence, then the tiles of a run of own items and of prefix items.
+constexpr int kCacheMeta = 8;
+struct CacheResults {
+  int32_t* meta;
+  float* part;                      // [2 runs][cols] parts of own items
+  float* part_pre;                  // [2 runs][cols_pre] parts of prefix items
+  float* whole;                     // [2][rows H] whole prefix items; whole own items
+                                    // of sequences with a prefix
+  int cols_pre;
+};
+// Floats of a partial result of cols rows of D values: values, references, sums.
+template <int D>
+__device__ __host__ constexpr size_t part_floats(int cols) { return (size_t)cols * (D + 2); }
+// Place of a whole result (D values, reference, sum).
+template <int D>
+__device__ __forceinline__ float* whole_at(const CacheResults& r, const CacheBatch& a, int own,
+                                           size_t vr) {
+  return r.whole + ((size_t)own * a.total_rows * a.H + vr) * (D + 4);
+}
+
 // Value of lane l ^ 16 and l ^ 32 joined with the lane's own by op, in every lane.
 template <class F>
 __device__ __forceinline__ float over_groups(float x, F op) {
@@ -74,5 +200,16 @@ __device__ __forceinline__ float over_groups(float x, F op) {
 }
 
 CacheView cache_view(const skip_kv_cache_t& c);
+inline CacheBatch cache_batch(const skip_problem_t& p, const skip_kv_cache_t& c,
+                              const int32_t* row_offsets, const int32_t* lens,
+                              const int32_t* prefix_ids, const int32_t* prefix_lens) {
+  return CacheBatch{row_offsets, lens, prefix_ids, prefix_lens, p.B, p.H, p.H / c.heads_kv,
+                    c.heads_kv, p.total_kept, p.k_max, p.L_max};
+}
+// The items of shared prefixes, their results left for the join.
+constexpr int kPrefixRuns = 512;
+hipError_t launch_cache_prefixes(const CacheBatch& batch, const CacheView& cache,
+                                 const CacheResults& res, const bf16_t* q, int d_h, int o_f32,
+                                 float scale_log2, hipStream_t s);
 
 }  // namespace skip
