@@ -27,7 +27,7 @@
 // are cut into equal runs, one a workgroup, whose four waves take every fourth tile.
 // An item that a run does not hold whole leaves partial results (O, reference, sum),
 // which a second kernel joins in the order of the tokens, so that the result does
-// not depend on which workgroup was faster.
+// not depend on which workgroup was faster.  (More of the split beside kOwnStart.)
 #include <algorithm>
 
 #include "skip_cache.h"
@@ -66,7 +66,6 @@ struct CacheItem {
   int hk, b;                        // key head; the sequence whose pages are read
   int r0, v0, nv;                   // first row; virtual rows v0 .. v0 + nv - 1
   int lo, hi, nt, t0, t1;
-  int start;                        // tile 0 among all items' tiles
   int n;                            // the sequence's new tokens
   bool shared;                      // rows with a prefix: results are joined
 };
@@ -399,21 +398,22 @@ cache_attn_kernel(CacheAttnArgs args) {
 
   if constexpr (LISTED) {
     const int rows = clampi(bt.row_offsets[bt.B], 0, bt.total_rows);
-    const int nt = a.n_sel << (shift - 5);
-    const int W = rows * hkv * nt, per = a.direct ? nt : max((W + a.runs - 1) / a.runs, kCLeast);
+    const int nt = a.n_sel << (shift - 5), step = nt + kOwnStart;
+    const int W = rows * hkv * step;
+    const int per = a.direct ? step : max((W + a.runs - 1) / a.runs, kCLeast);
     if (!a.direct && blockIdx.x == 0 && tid == 0) a.res.meta[(size_t)bt.B * kCacheMeta] = per;
     int u = blockIdx.x * per;
     const int end = min(W - u, per) + u;
     while (u < end) {
-      const int i = u / nt;
+      const int i = u / step, start = i * step;
       CacheItem it;
       it.r0 = i / hkv;
       it.hk = i - it.r0 * hkv;
       it.nt = nt;
-      it.start = i * nt;
-      it.t0 = u - it.start;
-      it.t1 = min(nt, end - it.start);
-      u = it.start + it.t1;
+      it.t0 = tile_at<kOwnStart>(u - start, nt);
+      it.t1 = tile_at<kOwnStart>(end - start, nt);
+      u = start + step;
+      if (it.t0 == it.t1) continue;
       CacheSeq s;
       it.b = seq_of_row(bt.row_offsets, bt.lens, bt.B, bt.total_rows, bt.k_max, bt.L_max, it.r0, s);
       if (it.b < 0) continue;
@@ -455,7 +455,7 @@ cache_attn_kernel(CacheAttnArgs args) {
       it.lo = 0;
       it.hi = s.len;
       it.nt = SeqBlock::own_tiles(0, s.len);
-      it.t0 = it.start = 0;
+      it.t0 = 0;
       it.t1 = it.nt;
       it.shared = false;
       work(it);
@@ -486,15 +486,16 @@ cache_attn_kernel(CacheAttnArgs args) {
       const int L = walk.seek(bt, u, first);
       CacheItem it;
       own(it, L);
-      const int rt = SeqBlock::row_tiles(bt, it.n, COLS), i = (u - first) / it.nt;
+      const int step = it.nt + kOwnStart;
+      const int rt = SeqBlock::row_tiles(bt, it.n, COLS), i = (u - first) / step;
       it.hk = i / rt;
       it.v0 = (i - it.hk * rt) * COLS;
       it.nv = min(COLS, it.n * bt.G - it.v0);
-      it.start = first + i * it.nt;
-      it.t0 = u - it.start;
-      it.t1 = min(it.nt, end - it.start);
-      u = it.start + it.t1;
-      work(it);
+      const int start = first + i * step;
+      it.t0 = tile_at<kOwnStart>(u - start, it.nt);
+      it.t1 = tile_at<kOwnStart>(end - start, it.nt);
+      u = start + step;
+      if (it.t0 < it.t1) work(it);
     }
   }
 }
@@ -526,10 +527,10 @@ cache_join_kernel(CacheAttnArgs a) {
     l = fmaf(xl, fx, l * f);
     m = to;
   };
-  // results of tiles [start, start + nt) in column col of cols
-  auto parts = [&](bool own, const float* part, int cols, int per, int start, int nt, int col) {
-    const int c0 = start / per, c1 = (start + nt - 1) / per;
-    if (c0 == c1) {
+  // results of the tiles at places [first, first + nt), in column col of cols
+  auto parts = [&](bool own, const float* part, int cols, int per, int first, int nt, int col) {
+    const int c0 = first / per, c1 = (first + nt - 1) / per;
+    if (c0 == c1) {                                // (alone: not reached)
       const float* w = whole_at<D>(a.res, bt, own, vr);
       add(*reinterpret_cast<const float4*>(w + 4 * c4), w[D], w[D + 1]);
       return;
@@ -541,7 +542,7 @@ cache_join_kernel(CacheAttnArgs a) {
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int k = min(c + i, c1);
-        const float* w = part + (size_t)(2 * k + (k == c0 && start >= k * per ? 1 : 0)) *
+        const float* w = part + (size_t)(2 * k + (k == c0 ? 1 : 0)) *
                                     part_floats<D>(cols);
         x[i] = *reinterpret_cast<const float4*>(w + (size_t)col * D + 4 * c4);
         xm[i] = w[(size_t)cols * D + col];
@@ -553,11 +554,11 @@ cache_join_kernel(CacheAttnArgs a) {
     }
   };
   const int32_t* pers = a.res.meta + (size_t)bt.B * kCacheMeta;
-  int start, nt, col;
+  int first, nt, col;
   bool alone = true;                               // no prefix
   if constexpr (LISTED) {
     nt = a.n_sel << (shift - 5);
-    start = (row * hkv + hk) * nt;
+    first = (row * hkv + hk) * (nt + kOwnStart) + kOwnStart;
     col = g;
   } else {
     const int4 x = reinterpret_cast<const int4*>(a.res.meta + (size_t)b * kCacheMeta)[0];
@@ -567,17 +568,18 @@ cache_join_kernel(CacheAttnArgs a) {
     if (!alone) {
       const int v = (row - x.w) * bt.G + g, n = SeqBlock::prefix_tiles(P);
       parts(false, a.res.part_pre, a.res.cols_pre, pers[1],
-            x.y + (hk * SeqBlock::row_tiles(bt, y.x, kPrefixRows) + v / kPrefixRows) * n, n,
-            v % kPrefixRows);
+            x.y + kPrefixStart + (hk * SeqBlock::row_tiles(bt, y.x, kPrefixRows) +
+                                  v / kPrefixRows) * (n + kPrefixStart), n, v % kPrefixRows);
     }
     const int v = (row - s.r0) * bt.G + g, lo = min(P, s.len);
     nt = SeqBlock::own_tiles(lo, s.len);
-    start = x.x + (hk * SeqBlock::row_tiles(bt, s.n, COLS) + v / COLS) * nt;
+    first = x.x + kOwnStart +
+            (hk * SeqBlock::row_tiles(bt, s.n, COLS) + v / COLS) * (nt + kOwnStart);
     col = v % COLS;
   }
   const int per = pers[0];
-  if (alone && start / per == (start + nt - 1) / per) return;          // (it is written)
-  parts(true, a.res.part, COLS, per, start, nt, col);
+  if (alone && first / per == (first + nt - 1) / per) return;          // (it is written)
+  parts(true, a.res.part, COLS, per, first, nt, col);
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (OUT_F32)
     *reinterpret_cast<float4*>(static_cast<float*>(a.O) + vr * D + 4 * c4) =
@@ -654,8 +656,8 @@ hipError_t launch_rows(const CacheAttnArgs& a, int R, hipStream_t s) {
 bool cache_attn_fits(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel) {
   const long long G = p.H / c.heads_kv, hkv = c.heads_kv, rows = p.total_kept;
   const long long items = n_sel > 0 ? rows * hkv : (rows * G / 16 + 2ll * p.B) * hkv;
-  const long long tiles = n_sel > 0 ? (long long)n_sel * (c.page_tokens / kCTile)
-                                    : p.L_max / kCTile + 2;
+  const long long tiles = kOwnStart + (n_sel > 0 ? (long long)n_sel * (c.page_tokens / kCTile)
+                                                 : p.L_max / kCTile + 2);
   return items <= INT32_MAX / tiles && rows * p.H < (1ll << 31) &&
          (long long)p.B * hkv * ((p.k_max * G + 15) / 16) < (1ll << 31);
 }

@@ -4,7 +4,7 @@
 // An item is 128 virtual rows of one sequence and key head, over the tokens that its
 // last row sees or an equal share of them.  A workgroup takes one: its four waves
 // hold 32 virtual rows each and share tiles of 64 tokens in LDS, which direct loads
-// fill a tile ahead.  Per tile and wave,
+// fill a tile (d_h 64: three) ahead.  Per tile and wave,
 //   S^T (64 tokens x 32 rows) = K . Q^T,  O^T (D x 32) += V^T . P^T
 // (v_mfma_f32_32x32x16_bf16).  Lane l is n = l % 32, hh = l / 32.  Element i of the
 // first product's half h is token 32 h + 8 (i / 4) + 4 hh + i % 4 of row n, and stays
@@ -103,7 +103,8 @@ cache_tall_kernel(TallArgs args) {
   constexpr int ROW = 2 * D;                        // bytes of a token
   constexpr int CH = D / 8;                         // chunks of a token
   constexpr uint32_t kKeys = kTTile * ROW, kBuffer = 2 * kKeys;
-  __shared__ __attribute__((aligned(1024))) uint8_t tile[2 * kBuffer];
+  constexpr uint32_t kBuffers = D == 64 ? 4 : 2;    // (64 KiB: two workgroups a CU)
+  __shared__ __attribute__((aligned(1024))) uint8_t tile[kBuffers * kBuffer];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, hh = lane >> 5;
@@ -184,14 +185,18 @@ cache_tall_kernel(TallArgs args) {
     pa = t < it.hi ? a.cache.page(it.b, t >> shift) : 0;
     pb = t + 32 < it.hi ? a.cache.page(it.b, (t + 32) >> shift) : 0;
   };
+  uint32_t missing = 0;                             // halves without a page, by buffer
   // (tokens behind the last one are loaded from where they would lie, and masked)
   auto fetch = [&](int i, uint32_t buffer) {
     if (i - pages_from >= 64) {
       pages_from = i;
       load_pages();
     }
-    const int own = wave < 2 ? __builtin_amdgcn_readlane(pa, i - pages_from)
-                             : __builtin_amdgcn_readlane(pb, i - pages_from);
+    const int pa_i = __builtin_amdgcn_readlane(pa, i - pages_from);
+    const int pb_i = __builtin_amdgcn_readlane(pb, i - pages_from);
+    const int own = wave < 2 ? pa_i : pb_i;
+    const int at = 2 * (buffer / kBuffer);
+    missing = (missing & ~(3u << at)) | (((pa_i < 0 ? 1u : 0u) | (pb_i < 0 ? 2u : 0u)) << at);
     const int t = i * kTTile + 16 * wave;
     const size_t off = a.cache.base<D>(max(own, 0), it.hk) + (size_t)(t & ((1 << shift) - 1)) * D;
     const uint8_t* ks = reinterpret_cast<const uint8_t*>(a.cache.k + off);
@@ -335,20 +340,23 @@ cache_tall_kernel(TallArgs args) {
   if (it.i0 < it.i1) {
     load_pages();
     if constexpr (PREFIX) barrier_nofence();        // (the last item's tiles are read)
-    fetch(it.i0, 0);
+#pragma unroll
+    for (uint32_t j = 0; j + 1 < kBuffers; ++j)
+      if (it.i0 + (int)j < it.i1) fetch(it.i0 + j, j * kBuffer);
   }
   for (int i = it.i0; i < it.i1; ++i) {
     // this tile's loads have landed, and every wave is through with the last one, whose
     // place the next one takes
-    wait_vmcnt<0>();
+    constexpr int ahead = kBuffers - 2;
+    if (i + ahead < it.i1) wait_vmcnt<ahead * 2 * NI>();
+    else wait_vmcnt<0>();
     barrier_nofence();
-    const int l = i - pages_from;
-    const int miss = (__builtin_amdgcn_readlane(pa, l) < 0 ? 1 : 0) |
-                     (__builtin_amdgcn_readlane(pb, l) < 0 ? 2 : 0);
-    if (i + 1 < it.i1) fetch(i + 1, buffer ^ kBuffer);
+    const int miss = (missing >> (2 * (buffer / kBuffer))) & 3;
+    if (i + (int)kBuffers - 1 < it.i1)
+      fetch(i + kBuffers - 1, (buffer + (kBuffers - 1) * kBuffer) % (kBuffers * kBuffer));
     const int t = i * kTTile;
     if (any && t < most) compute(t + kTTile > least || miss, t, miss);
-    buffer ^= kBuffer;
+    buffer = (buffer + kBuffer) % (kBuffers * kBuffer);
   }
 
   if (!any) return;
@@ -424,15 +432,16 @@ cache_tall_kernel(TallArgs args) {
       it.hi = walk.of_lane(walk.sb.P, L);
       it.nt = SeqBlock::prefix_tiles(it.hi);
       const int rows = walk.of_lane(walk.sb.run_rows, L);
-      const int rt = SeqBlock::row_tiles(bt, rows, kTRows), i = (u - first) / it.nt;
+      const int step = it.nt + kPrefixStart;
+      const int rt = SeqBlock::row_tiles(bt, rows, kTRows), i = (u - first) / step;
       it.hk = i / rt;
       it.v0 = (i - it.hk * rt) * kTRows;
       it.nv = min(kTRows, rows * bt.G - it.v0);
-      const int start = first + i * it.nt;
-      it.i0 = u - start;
-      it.i1 = min(it.nt, end - start);
-      u = start + it.i1;
-      work(it);
+      const int start = first + i * step;
+      it.i0 = tile_at<kPrefixStart>(u - start, it.nt);
+      it.i1 = tile_at<kPrefixStart>(end - start, it.nt);
+      u = start + step;
+      if (it.i0 < it.i1) work(it);
     }
   }
 }
@@ -483,12 +492,16 @@ cache_tall_join_kernel(TallArgs a) {
 static int tall_row_tiles(const skip_problem_t& p, const skip_kv_cache_t& c) {
   return (int)(((long long)p.k_max * (p.H / c.heads_kv) + kTRows - 1) / kTRows);
 }
-// Shares of an item: as many as leave some two workgroups a CU where there are few
-// items, of four tiles at least.
+// Shares of an item: where there are few items, as many as make some 768 workgroups
+// (three a CU), of four tiles at least.
 static int tall_splits(const skip_problem_t& p, const skip_kv_cache_t& c) {
-  const long long items = (long long)p.B * c.heads_kv * tall_row_tiles(p, c);
+  // row tiles of all sequences: about half of one more than full ones for each
+  const long long G = p.H / c.heads_kv;
+  const long long rts = std::min<long long>((long long)p.B * tall_row_tiles(p, c),
+                                            (p.total_kept * G / kTRows + (p.B + 1) / 2));
+  const long long items = std::max(rts, 1ll) * c.heads_kv;
   const long long tiles = (p.L_max + kTTile - 1) / kTTile;
-  return (int)std::max<long long>(1, std::min({512 / std::max(items, 1ll), tiles / kTLeast, 64ll}));
+  return (int)std::max<long long>(1, std::min({768 / items, tiles / kTLeast, 64ll}));
 }
 
 bool cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c) {
