@@ -4,7 +4,7 @@
 // An item is 128 virtual rows of one sequence and key head, over the tokens that its
 // last row sees or an equal share of them.  A workgroup takes one: its four waves
 // hold 32 virtual rows each and share tiles of 64 tokens in LDS, which direct loads
-// fill a tile (d_h 64: three) ahead.  Per tile and wave,
+// fill a tile (d_h 64: two) ahead.  Per tile and wave,
 //   S^T (64 tokens x 32 rows) = K . Q^T,  O^T (D x 32) += V^T . P^T
 // (v_mfma_f32_32x32x16_bf16).  Lane l is n = l % 32, hh = l / 32.  Element i of the
 // first product's half h is token 32 h + 8 (i / 4) + 4 hh + i % 4 of row n, and stays
@@ -95,7 +95,7 @@ __device__ __forceinline__ u32x4 lds_read16(uint32_t addr) {
 }
 
 template <int D, bool OUT_F32, bool PREFIX>
-__global__ void __launch_bounds__(kTThreads, 2)
+__global__ void __launch_bounds__(kTThreads, D == 64 ? 3 : 2)
 cache_tall_kernel(TallArgs args) {
   const TallArgs& a = args;
   const CacheBatch& bt = a.batch;
@@ -103,8 +103,10 @@ cache_tall_kernel(TallArgs args) {
   constexpr int ROW = 2 * D;                        // bytes of a token
   constexpr int CH = D / 8;                         // chunks of a token
   constexpr uint32_t kKeys = kTTile * ROW, kBuffer = 2 * kKeys;
-  constexpr uint32_t kBuffers = D == 64 ? 4 : 2;    // (64 KiB: two workgroups a CU)
+  constexpr uint32_t kBuffers = D == 64 ? 3 : 2;    // (48 KiB: three workgroups a CU; 64: two)
   __shared__ __attribute__((aligned(1024))) uint8_t tile[kBuffers * kBuffer];
+  __shared__ __attribute__((aligned(16))) uint8_t unseen[kTTile][CH];   // (see clean)
+  __shared__ int flags[kTWaves];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, hh = lane >> 5;
@@ -144,28 +146,37 @@ cache_tall_kernel(TallArgs args) {
   const bool any = wv < it.v0 + it.nv;
   const int v = min(wv + n, it.v0 + it.nv - 1);
   const int ri = v / bt.G, head = it.hk * bt.G + (v - ri * bt.G), row = it.r0 + ri;
-  int lim, least, most;
+  int lim, least, most, least_all;
   if constexpr (PREFIX) {
     // the row's sequence: the last of the block that starts at or before it (a sequence
     // without rows starts where the next one does)
-    int l = 0;
+    auto limit = [&](int r) -> int {
+      int l = 0;
 #pragma unroll
-    for (int st = 32; st >= 1; st >>= 1)
-      if (__shfl(walk.sb.s.r0, l + st, kWave) <= row && walk.sb0 + l + st < bt.B) l += st;
-    const int sr0 = __shfl(walk.sb.s.r0, l, kWave), sn = __shfl(walk.sb.s.n, l, kWave);
-    const int sl = __shfl(walk.sb.s.len, l, kWave);
-    lim = row < sr0 + sn ? clampi(sl - sn + (row - sr0) + 1, 0, it.hi) : 0;
+      for (int st = 32; st >= 1; st >>= 1)
+        if (__shfl(walk.sb.s.r0, l + st, kWave) <= r && walk.sb0 + l + st < bt.B) l += st;
+      const int sr0 = __shfl(walk.sb.s.r0, l, kWave), sn = __shfl(walk.sb.s.n, l, kWave);
+      const int sl = __shfl(walk.sb.s.len, l, kWave);
+      return r < sr0 + sn ? clampi(sl - sn + (r - sr0) + 1, 0, it.hi) : 0;
+    };
+    lim = limit(row);
     least = most = lim;
+    least_all = it.hi;
+    for (int u = lane; u - lane < it.nv; u += kWave)
+      least_all = min(least_all, limit(it.r0 + (it.v0 + min(u, it.nv - 1)) / bt.G));
 #pragma unroll
-    for (int st = 1; st < 32; st <<= 1) {
+    for (int st = 1; st < kWave; st <<= 1) {
       least = min(least, __shfl_xor(least, st, kWave));
       most = max(most, __shfl_xor(most, st, kWave));
+      least_all = min(least_all, __shfl_xor(least_all, st, kWave));
     }
     least = __builtin_amdgcn_readfirstlane(least);
     most = __builtin_amdgcn_readfirstlane(most);
+    least_all = __builtin_amdgcn_readfirstlane(least_all);
   } else {
     const int before = it.s.len - it.s.n + 1;
     lim = max(before + ri, 0);
+    least_all = max(before + it.v0 / bt.G, 0);
     least = max(before + min(wv, it.v0 + it.nv - 1) / bt.G, 0);
     most = max(before + min(wv + 31, it.v0 + it.nv - 1) / bt.G, 0);
   }
@@ -219,25 +230,32 @@ cache_tall_kernel(TallArgs args) {
   auto compute = [&](bool masked, int t, int miss) {
     f32x16_t s[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[h][i] = 0.f;
+    // (the two halves' products in turn: neither waits for its own last one)
 #pragma unroll
-      for (int c = 0; c < KC; ++c)
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
         s[h] = mfma32_bf16(lds_read16(ka[c] + buffer + 32 * h * ROW), qf[c], s[h]);
+    // four pairs of reads ahead of the products
+    __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+      if (c < KC - 4) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
-    // the lane's tokens that its row, and that some row of the wave sees (asm holds
-    // what is masked in its branch, and what it is compared with out of registers)
-    int rem[2] = {0, 0}, rem_most[2] = {0, 0};
     if (masked) {
+      // (asm holds what is masked in its branch, and what it is compared with out of
+      // registers)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        rem[h] = (miss >> h) & 1 ? 0 : lim - t - 32 * h - 4 * hh;
-        rem_most[h] = (miss >> h) & 1 ? 0 : most - t - 32 * h - 4 * hh;
-        asm volatile("" : "+v"(rem[h]), "+v"(rem_most[h]));
+        int rem = (miss >> h) & 1 ? 0 : lim - t - 32 * h - 4 * hh;
+        asm volatile("" : "+v"(rem));
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          float x = 8 * (i >> 2) + (i & 3) < rem[h] ? s[h][i] : -INFINITY;
+          float x = 8 * (i >> 2) + (i & 3) < rem ? s[h][i] : -INFINITY;
           asm volatile("" : "+v"(x));
           s[h][i] = x;
         }
@@ -261,9 +279,9 @@ cache_tall_kernel(TallArgs args) {
       m_run = to;
     }
     const float ref = m_run == -INFINITY ? 0.f : m_run;
-    unrolled<4>([&](auto step) {
+    // weights of step (h, q) as bf16 pieces, and its values
+    auto weigh = [&](auto step, u32x4 (&pc)[PIECES]) {
       constexpr int h = decltype(step)::value >> 1, q = decltype(step)::value & 1;
-      u32x4 pc[PIECES];
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         float p0 = __builtin_amdgcn_exp2f(fmaf(s[h][8 * q + 2 * w], sc, -ref));
@@ -278,63 +296,74 @@ cache_tall_kernel(TallArgs args) {
         }
         pc[PIECES - 1][w] = pack2_bf16(p0, p1);
       }
-      u32x4 x[FB];
+    };
+    auto values = [&](auto step, u32x4 (&x)[FB]) {
+      constexpr int h = decltype(step)::value >> 1, q = decltype(step)::value & 1;
 #pragma unroll
       for (int f = 0; f < FB; ++f) {
         const uint32_t at = va_[f] + buffer + (32 * h + 16 * q) * ROW;
         const uint2 lo = lds_read_transposed(at), up = lds_read_transposed(at + 8 * ROW);
         x[f] = u32x4{lo.x, lo.y, up.x, up.y};
       }
-      if (masked) {
-        // values that no row of the wave sees are left out
-        bool odd = false;
+    };
+    auto product = [&](const u32x4 (&pc)[PIECES], const u32x4 (&x)[FB]) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int m = 16 * q + 8 * (w >> 1) + 2 * (w & 1);
-          const uint32_t keep = (m < rem_most[h] ? 0xffffu : 0u) |
-                                (m + 1 < rem_most[h] ? 0xffff0000u : 0u);
+      for (int c = 0; c < PIECES; ++c)
 #pragma unroll
-          for (int f = 0; f < FB; ++f) {
-            uint32_t y = x[f][w] & keep;
-            asm volatile("" : "+v"(y));
-            x[f][w] = y;
-            odd |= bf16_odd_pair(y) != 0u;
-          }
-        }
-        // of the others, a weight of 0 must not meet an infinity or NaN: these are left
-        // out, too, and make NaN of the rows that see them (as one product more finds
-        // them, of ones)
-        if (__any(odd)) {
-          u32x4 sees;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int m = 16 * q + 8 * (w >> 1) + 2 * (w & 1);
-            sees[w] = (m < rem[h] ? 0x3f80u : 0u) | (m + 1 < rem[h] ? 0x3f800000u : 0u);
-          }
-#pragma unroll
-          for (int f = 0; f < FB; ++f) {
-            u32x4 ones;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const uint32_t bad = bf16_odd_pair(x[f][w]);
-              x[f][w] &= ~bad;
-              ones[w] = bad & 0x3f803f80u;
-            }
-            f32x16_t found;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) found[i] = 0.f;
-            found = mfma32_bf16(ones, sees, found);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[f][i] += found[i] > 0.f ? NAN : 0.f;
-            __builtin_amdgcn_sched_barrier(0);      // (one product at a time in registers)
-          }
-        }
+        for (int f = 0; f < FB; ++f) acc[f] = mfma32_bf16(x[f], pc[c], acc[f]);
+    };
+    // a step's products in turn with the next one's weights, which they hide
+    u32x4 pc[2][PIECES], x[2][FB];
+    weigh(std::integral_constant<int, 0>{}, pc[0]);
+    values(std::integral_constant<int, 0>{}, x[0]);
+    unrolled<4>([&](auto step) {
+      constexpr int k = decltype(step)::value;
+      if constexpr (k < 3) {
+        values(std::integral_constant<int, k + 1>{}, x[(k + 1) & 1]);
+        weigh(std::integral_constant<int, k + 1>{}, pc[(k + 1) & 1]);
       }
-#pragma unroll
-      for (int f = 0; f < FB; ++f)
-#pragma unroll
-        for (int c = 0; c < PIECES; ++c) acc[f] = mfma32_bf16(x[f], pc[c], acc[f]);
+      product(pc[k & 1], x[k & 1]);
     });
+  };
+
+  // Values in a tile that some rows do not see: a weight of 0 must not meet an infinity
+  // or NaN.  Every wave looks through the 16 tokens that it loaded: what no row sees is
+  // zeroed; of the others, what is not finite is zeroed and remembered, a bit a value.
+  auto clean = [&](int t, int miss) {
+    bool found = false;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int r = 16 * wave + RI * j + lane / CH, c = lane % CH;     // token, place
+      const uint32_t at = buffer + kKeys + r * ROW + 16 * c;
+      u32x4 x = *reinterpret_cast<const u32x4*>(tile + at);
+      const bool seen = t + r < it.hi && !((miss >> (r >> 5)) & 1);
+      uint32_t bits = 0;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t bad = seen ? bf16_odd_pair(x[w]) : 0u;
+        x[w] &= seen ? ~bad : 0u;
+        bits |= (bad & 1u) << (2 * w) | (bad >> 31) << (2 * w + 1);
+      }
+      *reinterpret_cast<u32x4*>(tile + at) = x;
+      unseen[r][c ^ ((2 * r) & (CH - 1))] = (uint8_t)bits;
+      found |= bits != 0u;
+    }
+    const bool any_found = __any(found);
+    if (lane == 0) flags[wave] = any_found;
+  };
+  // NaN to the rows that see such a value, in its feature.
+  auto poison = [&](int t) {
+#pragma clang loop unroll(disable)
+    for (int r = 0; r < kTTile; ++r)
+#pragma unroll
+      for (int f = 0; f < FB; ++f) {
+        uint32_t bits = reinterpret_cast<const uint32_t*>(unseen[r])[f] >> (4 * hh);
+        if (t + r >= lim) bits = 0u;
+        if (!__any(bits != 0u)) continue;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if ((bits >> (8 * (i >> 2) + (i & 3))) & 1u) acc[f][i] = NAN;
+      }
   };
 
   if (it.i0 < it.i1) {
@@ -355,7 +384,16 @@ cache_tall_kernel(TallArgs args) {
     if (i + (int)kBuffers - 1 < it.i1)
       fetch(i + kBuffers - 1, (buffer + (kBuffers - 1) * kBuffer) % (kBuffers * kBuffer));
     const int t = i * kTTile;
-    if (any && t < most) compute(t + kTTile > least || miss, t, miss);
+    bool odd = false;
+    if (t + kTTile > least_all || miss) {
+      clean(t, miss);
+      barrier_lds();
+      odd = flags[0] | flags[1] | flags[2] | flags[3];
+    }
+    if (any && t < most) {
+      compute(t + kTTile > least || miss, t, miss);
+      if (odd) poison(t);
+    }
     buffer = (buffer + kBuffer) % (kBuffers * kBuffer);
   }
 
@@ -501,7 +539,7 @@ static int tall_splits(const skip_problem_t& p, const skip_kv_cache_t& c) {
                                             (p.total_kept * G / kTRows + (p.B + 1) / 2));
   const long long items = std::max(rts, 1ll) * c.heads_kv;
   const long long tiles = (p.L_max + kTTile - 1) / kTTile;
-  return (int)std::max<long long>(1, std::min({768 / items, tiles / kTLeast, 64ll}));
+  return (int)std::max<long long>(1, std::min({(p.d_h == 64 ? 768 : 512) / items, tiles / kTLeast, 64ll}));
 }
 
 bool cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c) {
