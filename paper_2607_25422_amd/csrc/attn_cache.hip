@@ -31,6 +31,7 @@
 #include <algorithm>
 
 #include "skip_cache.h"
+#include "skip_cache_join.h"
 #include "skip_common.h"
 #include "skip_internal.h"
 #include "skip_select.h"
@@ -38,7 +39,6 @@
 namespace skip {
 
 constexpr float kCLog2e = 1.4426950408889634f;
-constexpr float kCLn2 = 0.6931471805599453f;
 constexpr int kCWaves = 4;
 constexpr int kCThreads = 64 * kCWaves;
 constexpr int kCTile = kOwnTile;           // tokens of a tile
@@ -373,7 +373,7 @@ cache_attn_kernel(CacheAttnArgs args) {
         else
           *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + vr * D + 4 * c4) =
               make_uint2(pack2_bf16(o.x * inv, o.y * inv), pack2_bf16(o.z * inv, o.w * inv));
-        if (a.lse && c4 == 0) a.lse[vr] = l == 0.f ? -INFINITY : (m + log2f(l)) * kCLn2;
+        if (a.lse && c4 == 0) a.lse[vr] = l == 0.f ? -INFINITY : (m + log2f(l)) * kCacheLn2;
       } else {
         float *w, *ml;
         int ml_step;
@@ -500,96 +500,6 @@ cache_attn_kernel(CacheAttnArgs args) {
   }
 }
 
-// Joins the parts of each virtual row: of its prefix, then of its own tokens, in order.
-// D / 4 lanes a virtual row.
-template <int D, int COLS, bool OUT_F32, bool LISTED>
-__global__ void __launch_bounds__(256)
-cache_join_kernel(CacheAttnArgs a) {
-  constexpr int NC4 = D / 4, VR = 256 / NC4;       // lanes a virtual row, virtual rows
-  const CacheBatch& bt = a.batch;
-  const int hkv = bt.heads_kv, shift = a.cache.shift;
-  const int per_row = (bt.H + VR - 1) / VR;
-  const int row = blockIdx.x / per_row;
-  const int h = (blockIdx.x - row * per_row) * VR + threadIdx.x / NC4;
-  const int c4 = threadIdx.x % NC4;
-  CacheSeq s;
-  const int b = seq_of_row(bt.row_offsets, bt.lens, bt.B, bt.total_rows, bt.k_max, bt.L_max, row, s);
-  if (b < 0 || h >= bt.H) return;
-  const int hk = h / bt.G, g = h - hk * bt.G;
-  const size_t vr = (size_t)row * bt.H + h;
-  float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](float4 x, float xm, float xl) {
-    const float to = fmaxf(m, xm), ref = to == -INFINITY ? 0.f : to;
-    const float f = __builtin_amdgcn_exp2f(m - ref), fx = __builtin_amdgcn_exp2f(xm - ref);
-    o = make_float4(fmaf(x.x, fx, o.x * f), fmaf(x.y, fx, o.y * f), fmaf(x.z, fx, o.z * f),
-                    fmaf(x.w, fx, o.w * f));
-    l = fmaf(xl, fx, l * f);
-    m = to;
-  };
-  // results of the tiles at places [first, first + nt), in column col of cols
-  auto parts = [&](bool own, const float* part, int cols, int per, int first, int nt, int col) {
-    const int c0 = first / per, c1 = (first + nt - 1) / per;
-    if (c0 == c1) {                                // (alone: not reached)
-      const float* w = whole_at<D>(a.res, bt, own, vr);
-      add(*reinterpret_cast<const float4*>(w + 4 * c4), w[D], w[D + 1]);
-      return;
-    }
-    constexpr int U = 8;                           // parts in flight
-    for (int c = c0; c <= c1; c += U) {
-      float4 x[U];
-      float xm[U], xl[U];
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int k = min(c + i, c1);
-        const float* w = part + (size_t)(2 * k + (k == c0 ? 1 : 0)) *
-                                    part_floats<D>(cols);
-        x[i] = *reinterpret_cast<const float4*>(w + (size_t)col * D + 4 * c4);
-        xm[i] = w[(size_t)cols * D + col];
-        xl[i] = w[(size_t)cols * D + cols + col];
-      }
-#pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (c + i <= c1) add(x[i], xm[i], xl[i]);
-    }
-  };
-  const int32_t* pers = a.res.meta + (size_t)bt.B * kCacheMeta;
-  int first, nt, col;
-  bool alone = true;                               // no prefix
-  if constexpr (LISTED) {
-    nt = a.n_sel << (shift - 5);
-    first = (row * hkv + hk) * (nt + kOwnStart) + kOwnStart;
-    col = g;
-  } else {
-    const int4 x = reinterpret_cast<const int4*>(a.res.meta + (size_t)b * kCacheMeta)[0];
-    const int4 y = reinterpret_cast<const int4*>(a.res.meta + (size_t)b * kCacheMeta)[1];
-    const int P = x.z;
-    alone = P == 0;
-    if (!alone) {
-      const int v = (row - x.w) * bt.G + g, n = SeqBlock::prefix_tiles(P);
-      parts(false, a.res.part_pre, a.res.cols_pre, pers[1],
-            x.y + kPrefixStart + (hk * SeqBlock::row_tiles(bt, y.x, kPrefixRows) +
-                                  v / kPrefixRows) * (n + kPrefixStart), n, v % kPrefixRows);
-    }
-    const int v = (row - s.r0) * bt.G + g, lo = min(P, s.len);
-    nt = SeqBlock::own_tiles(lo, s.len);
-    first = x.x + kOwnStart +
-            (hk * SeqBlock::row_tiles(bt, s.n, COLS) + v / COLS) * (nt + kOwnStart);
-    col = v % COLS;
-  }
-  const int per = pers[0];
-  if (alone && first / per == (first + nt - 1) / per) return;          // (it is written)
-  parts(true, a.res.part, COLS, per, first, nt, col);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (OUT_F32)
-    *reinterpret_cast<float4*>(static_cast<float*>(a.O) + vr * D + 4 * c4) =
-        make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  else
-    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + vr * D + 4 * c4) =
-        make_uint2(pack2_bf16(o.x * inv, o.y * inv), pack2_bf16(o.z * inv, o.w * inv));
-  if (a.lse && c4 == 0) a.lse[vr] = l == 0.f ? -INFINITY : (m + log2f(l)) * kCLn2;
-}
-
 // ---------------------------------------------------------------------------
 // Launches
 
@@ -639,10 +549,8 @@ hipError_t launch_one(const CacheAttnArgs& a, hipStream_t s) {
     e = launch_cache_prefixes(a.batch, a.cache, a.res, a.q, D, a.o_f32, a.scale_log2, s);
     if (e != hipSuccess) return e;
   }
-  constexpr int VR = 1024 / D;
-  const unsigned grid = (unsigned)a.batch.total_rows * (unsigned)((a.batch.H + VR - 1) / VR);
-  cache_join_kernel<D, 16 * R, OUT_F32, LISTED><<<dim3(grid), 256, 0, s>>>(a);
-  return hipGetLastError();
+  const JoinArgs j{a.batch, a.res, a.O, a.lse, a.n_sel * (1 << a.cache.shift) / kCTile};
+  return launch_join<D, OUT_F32, LISTED ? kJoinListed : kJoinOwn>(j, s);
 }
 template <int D, bool LISTED>
 hipError_t launch_rows(const CacheAttnArgs& a, int R, hipStream_t s) {
@@ -689,6 +597,7 @@ hipError_t launch_cache_attn(const skip_problem_t& p, const skip_kv_cache_t& c, 
     res.part = take(x.part);
     res.part_pre = take(x.part_pre);
     res.whole = take(x.whole);
+    res.cols_own = 16 * x.R;
     res.cols_pre = x.cols_pre;
   }
   CacheAttnArgs a{cache_batch(p, c, row_offsets, lens, x.prefixes ? prefix_ids : nullptr,

@@ -1,9 +1,9 @@
 // Attention of new tokens over a paged cache, for sequences with many of them (the
 // formulas and the virtual rows are at the top of attn_cache.hip).
 //
-// An item is 128 virtual rows of one sequence and key head, over the tokens that its
-// last row sees or an equal share of them.  A workgroup takes one: its four waves
-// hold 32 virtual rows each and share tiles of 64 tokens in LDS, which direct loads
+// An item is 128 virtual rows of one sequence (or of the sequences that share a prefix)
+// and key head, over the tokens that its last row sees (or the prefix).  A workgroup
+// takes one, or an equal run of all items' tiles: its four waves hold 32 virtual rows each and share tiles of 64 tokens in LDS, which direct loads
 // fill a tile (d_h 64: two) ahead.  Per tile and wave,
 //   S^T (64 tokens x 32 rows) = K . Q^T,  O^T (D x 32) += V^T . P^T
 // (v_mfma_f32_32x32x16_bf16).  Lane l is n = l % 32, hh = l / 32.  Element i of the
@@ -20,6 +20,7 @@
 #include <algorithm>
 
 #include "skip_cache.h"
+#include "skip_cache_join.h"
 #include "skip_common.h"
 #include "skip_internal.h"
 
@@ -31,7 +32,6 @@ constexpr int kTRows = 32 * kTWaves;       // virtual rows of an item
 constexpr int kTTile = 64;                 // tokens of a tile
 constexpr int kTLeast = 4;                 // tiles of a share or run, at least
 static_assert(kTRows == kPrefixRows && kTTile == kPrefixTile, "items of prefixes");
-constexpr float kTLn2 = 0.6931471805599453f;
 constexpr float kTOver = 8.f;
 template <bool OUT_F32> constexpr int kTPieces = OUT_F32 ? 3 : 2;
 
@@ -42,8 +42,7 @@ struct TallArgs {
   const bf16_t* q;
   void* O;
   float* lse;
-  float* part;                      // [items][splits] results of shares
-  int row_tiles, splits, grouped;
+  int row_tiles, runs, grouped;
   float scale_log2;
 };
 
@@ -53,7 +52,6 @@ struct TallItem {
   int b, hk;                        // the sequence whose pages are read; key head
   int r0, v0, nv;                   // first row of the set; virtual rows v0 .. v0 + nv - 1
   int hi, nt, i0, i1;
-  int place;                        // of a share's result; a run's first tile of the item
   CacheSeq s;
 };
 // Workgroup id L goes to XCD L % 8; where sequences and key heads make whole eights,
@@ -61,25 +59,24 @@ struct TallItem {
 // and values.  Row tiles from the last, which see most tokens, to the first.
 __device__ __forceinline__ bool tall_item(const TallArgs& a, int L, TallItem& x) {
   const CacheBatch& bt = a.batch;
-  const int per = a.row_tiles * a.splits, groups = bt.B * bt.heads_kv;
+  const int per = a.row_tiles, groups = bt.B * bt.heads_kv;
   const int grp = a.grouped ? (L & 7) + 8 * ((L >> 3) / per) : L / per;
   const int sub = a.grouped ? (L >> 3) % per : L % per;
   if (grp >= groups) return false;
   x.b = grp / bt.heads_kv;
   x.hk = grp - x.b * bt.heads_kv;
   x.s.load(bt.row_offsets, bt.lens, x.b, bt.total_rows, bt.k_max, bt.L_max);
-  const int rts = (x.s.n * bt.G + kTRows - 1) / kTRows, i = sub / a.splits;
-  if (i >= rts) return false;
-  const int rt = rts - 1 - i, split = sub - i * a.splits;
+  const int rts = SeqBlock::row_tiles(bt, x.s.n, kTRows);
+  if (sub >= rts) return false;
+  const int rt = rts - 1 - sub;
   x.r0 = x.s.r0;
   x.v0 = rt * kTRows;
   x.nv = min(kTRows, x.s.n * bt.G - x.v0);
   // the tokens that the last row sees
   x.hi = max(x.s.len - x.s.n + (x.v0 + x.nv - 1) / bt.G + 1, 0);
   x.nt = (x.hi + kTTile - 1) / kTTile;
-  x.i0 = (int)((long long)x.nt * split / a.splits);
-  x.i1 = (int)((long long)x.nt * (split + 1) / a.splits);
-  x.place = (grp * a.row_tiles + rt) * a.splits + split;
+  x.i0 = 0;
+  x.i1 = x.nt;
   return true;
 }
 
@@ -94,9 +91,13 @@ __device__ __forceinline__ u32x4 lds_read16(uint32_t addr) {
   return *(Ptr)(uintptr_t)addr;
 }
 
-template <int D, bool OUT_F32, bool PREFIX>
+// OF: sequences, an item a workgroup; sequences, in equal runs of tiles; prefixes, in
+// equal runs.
+enum TallOf { kTallItems, kTallRuns, kTallPrefixes };
+template <int D, bool OUT_F32, TallOf OF>
 __global__ void __launch_bounds__(kTThreads, D == 64 ? 3 : 2)
 cache_tall_kernel(TallArgs args) {
+  constexpr bool PREFIX = OF == kTallPrefixes;
   const TallArgs& a = args;
   const CacheBatch& bt = a.batch;
   constexpr int KC = D / 16, FB = D / 32, PIECES = kTPieces<OUT_F32>;
@@ -112,7 +113,9 @@ cache_tall_kernel(TallArgs args) {
   const int n = lane & 31, hh = lane >> 5;
   const int shift = a.cache.shift;
   const uint32_t lds = lds_addr(tile);
-  SeqWalk<true> walk;
+  // (runs that follow one another go to one XCD, whose L2 holds what they share)
+  const int run = OF == kTallItems ? 0 : (blockIdx.x & 7) * (a.runs / 8) + (blockIdx.x >> 3);
+  SeqWalk<PREFIX, OF == kTallRuns> walk;
   walk.cols = 16;                                   // (own items are not looked at)
 
   const uint32_t neg = (a.scale_log2 < 0.f) ? 0x80008000u : 0u;
@@ -368,7 +371,7 @@ cache_tall_kernel(TallArgs args) {
 
   if (it.i0 < it.i1) {
     load_pages();
-    if constexpr (PREFIX) barrier_nofence();        // (the last item's tiles are read)
+    if constexpr (OF != kTallItems) barrier_nofence();   // (the last item's tiles are read)
 #pragma unroll
     for (uint32_t j = 0; j + 1 < kBuffers; ++j)
       if (it.i0 + (int)j < it.i1) fetch(it.i0 + j, j * kBuffer);
@@ -405,19 +408,19 @@ cache_tall_kernel(TallArgs args) {
   }
   if (wv + n >= it.v0 + it.nv) return;
   const size_t vr = (size_t)row * bt.H + head;
-  if (PREFIX || a.splits > 1) {
+  const bool all = it.i0 == 0 && it.i1 == it.nt;
+  if (PREFIX || (OF == kTallRuns && !all)) {
     float *w, *ml;
     int ml_step;
     const int col = 32 * wave + n;
-    if (PREFIX && it.i0 == 0 && it.i1 == it.nt) {
+    if (PREFIX && all) {
       w = whole_at<D>(a.res, bt, 0, vr);
       ml = w + D;
       ml_step = 1;
     } else {
-      const int cols = PREFIX ? a.res.cols_pre : kTRows;
-      w = PREFIX ? a.res.part_pre + (size_t)(2 * blockIdx.x + (it.i0 == 0 ? 1 : 0)) *
-                                        part_floats<D>(cols)
-                 : a.part + (size_t)it.place * part_floats<D>(kTRows);
+      const int cols = PREFIX ? a.res.cols_pre : a.res.cols_own;
+      w = (PREFIX ? a.res.part_pre : a.res.part) +
+          (size_t)(2 * run + (it.i0 == 0 ? 1 : 0)) * part_floats<D>(cols);
       ml = w + (size_t)cols * D + col;
       ml_step = cols;
       w += (size_t)col * D;
@@ -448,17 +451,23 @@ cache_tall_kernel(TallArgs args) {
         *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + at) =
             make_uint2(pack2_bf16(o0, o1), pack2_bf16(o2, o3));
     }
-  if (a.lse && hh == 0) a.lse[vr] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * kTLn2;
+  if (a.lse && hh == 0) a.lse[vr] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * kCacheLn2;
   };
 
-  if constexpr (!PREFIX) {
+  if constexpr (OF == kTallItems) {
     TallItem it;
     if (tall_item(a, blockIdx.x, it)) work(it);
   } else {
-    const int W = walk.total(bt, [](int) {});
-    const int per = max((W + kPrefixRuns - 1) / kPrefixRuns, kTLeast);
-    if (blockIdx.x == 0 && tid == 0) a.res.meta[(size_t)bt.B * kCacheMeta + 1] = per;
-    int u = blockIdx.x * per;
+    const int W = walk.total(bt, [&](int before) {
+      if (PREFIX || blockIdx.x != 0 || wave != 0 || walk.sb0 + lane >= bt.B) return;
+      int32_t* w = a.res.meta + (size_t)(walk.sb0 + lane) * kCacheMeta;
+      *reinterpret_cast<int2*>(w) = make_int2(before + walk.incl - walk.sb.own,
+                                              walk.sb.own / bt.heads_kv);
+    });
+    const int per = max((W + a.runs - 1) / a.runs, kTLeast);
+    if (blockIdx.x == 0 && tid == 0)
+      a.res.meta[(size_t)bt.B * kCacheMeta + (PREFIX ? 1 : 0)] = per;
+    int u = run * per;
     if (u >= W) return;
     const int end = min(W - u, per) + u;
     while (u < end) {
@@ -467,112 +476,105 @@ cache_tall_kernel(TallArgs args) {
       TallItem it;
       it.b = walk.sb0 + L;
       it.r0 = walk.of_lane(walk.sb.s.r0, L);
-      it.hi = walk.of_lane(walk.sb.P, L);
-      it.nt = SeqBlock::prefix_tiles(it.hi);
-      const int rows = walk.of_lane(walk.sb.run_rows, L);
-      const int step = it.nt + kPrefixStart;
-      const int rt = SeqBlock::row_tiles(bt, rows, kTRows), i = (u - first) / step;
-      it.hk = i / rt;
-      it.v0 = (i - it.hk * rt) * kTRows;
+      int rows, rt, start;
+      if constexpr (PREFIX) {
+        it.hi = walk.of_lane(walk.sb.P, L);
+        it.nt = SeqBlock::prefix_tiles(it.hi);
+        rows = walk.of_lane(walk.sb.run_rows, L);
+        const int rts = SeqBlock::row_tiles(bt, rows, kTRows), step = it.nt + kPrefixStart;
+        const int i = (u - first) / step;
+        it.hk = i / rts;
+        rt = i - it.hk * rts;
+        start = first + i * step;
+      } else {
+        it.s = CacheSeq{it.r0, walk.of_lane(walk.sb.s.n, L), walk.of_lane(walk.sb.s.len, L)};
+        rows = it.s.n;
+        const int head = walk.of_lane(walk.sb.own, L) / bt.heads_kv;     // tiles of a key head
+        it.hk = (u - first) / head;
+        start = first + it.hk * head;
+        for (rt = 0;; ++rt) {
+          it.nt = SeqBlock::tall_tiles(bt, it.s.n, it.s.len, rt);
+          if (u < start + it.nt + kPrefixStart) break;
+          start += it.nt + kPrefixStart;
+        }
+        it.hi = max(it.s.len - it.s.n + (min((rt + 1) * kTRows, rows * bt.G) - 1) / bt.G + 1, 0);
+      }
+      it.v0 = rt * kTRows;
       it.nv = min(kTRows, rows * bt.G - it.v0);
-      const int start = first + i * step;
       it.i0 = tile_at<kPrefixStart>(u - start, it.nt);
       it.i1 = tile_at<kPrefixStart>(end - start, it.nt);
-      u = start + step;
+      u = start + it.nt + kPrefixStart;
       if (it.i0 < it.i1) work(it);
     }
   }
 }
 
-// Joins an item's shares, in the order of the tokens: D / 4 lanes a virtual row.
-template <int D, bool OUT_F32>
-__global__ void __launch_bounds__(256)
-cache_tall_join_kernel(TallArgs a) {
-  constexpr int NC4 = D / 4, VR = 256 / NC4, WG = kTRows / VR;
-  const CacheBatch& bt = a.batch;
-  const int item = blockIdx.x / WG;
-  const int rt = item % a.row_tiles, grp = item / a.row_tiles;
-  const int b = grp / bt.heads_kv, hk = grp - b * bt.heads_kv;
-  const int col = (blockIdx.x - item * WG) * VR + threadIdx.x / NC4, c4 = threadIdx.x % NC4;
-  CacheSeq s;
-  s.load(bt.row_offsets, bt.lens, b, bt.total_rows, bt.k_max, bt.L_max);
-  const int v = rt * kTRows + col;
-  if (v >= s.n * bt.G) return;
-  constexpr size_t step = part_floats<D>(kTRows);
-  const float* w = a.part + (size_t)item * a.splits * step;
-  float m = -INFINITY;
-  for (int i = 0; i < a.splits; ++i) m = fmaxf(m, w[i * step + (size_t)kTRows * D + col]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = 0; i < a.splits; ++i) {
-    const float* x = w + i * step;
-    const float f = __builtin_amdgcn_exp2f(x[(size_t)kTRows * D + col] - ref);
-    const float4 y = *reinterpret_cast<const float4*>(x + (size_t)col * D + 4 * c4);
-    o = make_float4(fmaf(y.x, f, o.x), fmaf(y.y, f, o.y), fmaf(y.z, f, o.z), fmaf(y.w, f, o.w));
-    l = fmaf(x[(size_t)kTRows * D + kTRows + col], f, l);
-  }
-  const int ri = v / bt.G;
-  const size_t vr = (size_t)(s.r0 + ri) * bt.H + hk * bt.G + (v - ri * bt.G);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (OUT_F32)
-    *reinterpret_cast<float4*>(static_cast<float*>(a.O) + vr * D + 4 * c4) =
-        make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  else
-    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.O) + vr * D + 4 * c4) =
-        make_uint2(pack2_bf16(o.x * inv, o.y * inv), pack2_bf16(o.z * inv, o.w * inv));
-  if (a.lse && c4 == 0) a.lse[vr] = l == 0.f ? -INFINITY : (m + log2f(l)) * kTLn2;
-}
-
 // ---------------------------------------------------------------------------
 // Launches
 
-static int tall_row_tiles(const skip_problem_t& p, const skip_kv_cache_t& c) {
-  return (int)(((long long)p.k_max * (p.H / c.heads_kv) + kTRows - 1) / kTRows);
-}
-// Shares of an item: where there are few items, as many as make some 768 workgroups
-// (three a CU), of four tiles at least.
-static int tall_splits(const skip_problem_t& p, const skip_kv_cache_t& c) {
-  // row tiles of all sequences: about half of one more than full ones for each
+namespace {
+
+struct TallPlan {
+  int row_tiles, runs, cols;           // runs 0: an item a workgroup
+  size_t meta, part;
+};
+
+TallPlan tall_plan(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  TallPlan x{};
   const long long G = p.H / c.heads_kv;
-  const long long rts = std::min<long long>((long long)p.B * tall_row_tiles(p, c),
-                                            (p.total_kept * G / kTRows + (p.B + 1) / 2));
-  const long long items = std::max(rts, 1ll) * c.heads_kv;
-  const long long tiles = (p.L_max + kTTile - 1) / kTTile;
-  return (int)std::max<long long>(1, std::min({(p.d_h == 64 ? 768 : 512) / items, tiles / kTLeast, 64ll}));
+  x.row_tiles = (int)((p.k_max * G + kTRows - 1) / kTRows);
+  // Few items are cut into equal runs (items as they come leave CUs without work: six
+  // pieces of 97 to 129 rows over 3200 tokens, 16 heads, 49 us in equal shares of each
+  // item); about half a row tile of a sequence's is empty.
+  const long long items = c.heads_kv * std::min<long long>(
+      (long long)p.B * x.row_tiles, p.total_kept * G / kTRows + (p.B + 1) / 2);
+  if (items < 2048 && x.row_tiles <= 64) {
+    auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+    x.runs = p.d_h == 64 ? 768 : 512;
+    x.cols = (int)std::min<long long>(kTRows, (p.k_max * G + 31) / 32 * 32);
+    x.meta = up(((size_t)p.B * kCacheMeta + 2) * sizeof(int32_t));
+    x.part = 2 * (size_t)x.runs * x.cols * (p.d_h + 2) * sizeof(float);
+  }
+  return x;
 }
+
+}  // namespace
 
 bool cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c) {
   return (long long)p.k_max * (p.H / c.heads_kv) > 32;
 }
 
 size_t cache_tall_scratch(const skip_problem_t& p, const skip_kv_cache_t& c) {
-  const int splits = tall_splits(p, c);
-  if (splits == 1) return 0;
-  return (size_t)p.B * c.heads_kv * tall_row_tiles(p, c) * splits * kTRows * (p.d_h + 2) *
-         sizeof(float);
+  const TallPlan x = tall_plan(p, c);
+  return x.meta + x.part;
 }
 
 template <int D, bool OUT_F32>
 static hipError_t launch_tall(const TallArgs& a, hipStream_t s) {
-  const int groups = a.batch.B * a.batch.heads_kv;
-  const unsigned grid = (unsigned)groups * a.row_tiles * a.splits;
-  cache_tall_kernel<D, OUT_F32, false><<<dim3(grid), kTThreads, 0, s>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
-  constexpr int WG = kTRows / (1024 / D);
-  cache_tall_join_kernel<D, OUT_F32>
-      <<<dim3((unsigned)groups * a.row_tiles * WG), 256, 0, s>>>(a);
-  return hipGetLastError();
+  if (a.runs == 0) {
+    const unsigned grid = (unsigned)a.batch.B * a.batch.heads_kv * a.row_tiles;
+    cache_tall_kernel<D, OUT_F32, kTallItems><<<dim3(grid), kTThreads, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  cache_tall_kernel<D, OUT_F32, kTallRuns><<<dim3(a.runs), kTThreads, 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_join<D, OUT_F32, kJoinTall>(JoinArgs{a.batch, a.res, a.O, a.lse, 0}, s);
 }
 
 hipError_t launch_cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c, const void* q,
                              const int32_t* row_offsets, const int32_t* lens, void* O, float* lse,
                              void* scratch, hipStream_t s) {
-  TallArgs a{cache_batch(p, c, row_offsets, lens, nullptr, nullptr), cache_view(c), CacheResults{},
-             static_cast<const bf16_t*>(q), O, lse, static_cast<float*>(scratch),
-             tall_row_tiles(p, c), tall_splits(p, c), p.B * c.heads_kv % 8 == 0,
-             p.sm_scale * 1.4426950408889634f};
+  const TallPlan x = tall_plan(p, c);
+  CacheResults res{};
+  if (x.runs) {
+    res.meta = static_cast<int32_t*>(scratch);
+    res.part = reinterpret_cast<float*>(static_cast<char*>(scratch) + x.meta);
+    res.cols_own = x.cols;
+  }
+  TallArgs a{cache_batch(p, c, row_offsets, lens, nullptr, nullptr), cache_view(c), res,
+             static_cast<const bf16_t*>(q), O, lse, x.row_tiles, x.runs,
+             p.B * c.heads_kv % 8 == 0, p.sm_scale * 1.4426950408889634f};
   if (p.d_h == 64) return p.o_f32 ? launch_tall<64, true>(a, s) : launch_tall<64, false>(a, s);
   return p.o_f32 ? launch_tall<128, true>(a, s) : launch_tall<128, false>(a, s);
 }
@@ -580,14 +582,14 @@ hipError_t launch_cache_tall(const skip_problem_t& p, const skip_kv_cache_t& c, 
 hipError_t launch_cache_prefixes(const CacheBatch& batch, const CacheView& cache,
                                  const CacheResults& res, const bf16_t* q, int d_h, int o_f32,
                                  float scale_log2, hipStream_t s) {
-  TallArgs a{batch, cache, res, q, nullptr, nullptr, nullptr, 0, 1, 0, scale_log2};
+  TallArgs a{batch, cache, res, q, nullptr, nullptr, 0, kPrefixRuns, 0, scale_log2};
   const dim3 grid(kPrefixRuns);
   if (d_h == 64) {
-    if (o_f32) cache_tall_kernel<64, true, true><<<grid, kTThreads, 0, s>>>(a);
-    else cache_tall_kernel<64, false, true><<<grid, kTThreads, 0, s>>>(a);
+    if (o_f32) cache_tall_kernel<64, true, kTallPrefixes><<<grid, kTThreads, 0, s>>>(a);
+    else cache_tall_kernel<64, false, kTallPrefixes><<<grid, kTThreads, 0, s>>>(a);
   } else {
-    if (o_f32) cache_tall_kernel<128, true, true><<<grid, kTThreads, 0, s>>>(a);
-    else cache_tall_kernel<128, false, true><<<grid, kTThreads, 0, s>>>(a);
+    if (o_f32) cache_tall_kernel<128, true, kTallPrefixes><<<grid, kTThreads, 0, s>>>(a);
+    else cache_tall_kernel<128, false, kTallPrefixes><<<grid, kTThreads, 0, s>>>(a);
   }
   return hipGetLastError();
 }

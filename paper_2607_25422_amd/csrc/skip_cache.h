@@ -100,6 +100,19 @@ struct SeqBlock {
   __device__ __forceinline__ static int prefix_tiles(int P) {
     return (P + kPrefixTile - 1) / kPrefixTile;
   }
+  // tiles of kPrefixTile tokens that row tile i of a sequence's rows sees, at least one
+  __device__ __forceinline__ static int tall_tiles(const CacheBatch& a, int n, int len, int i) {
+    const int last = min((i + 1) * kPrefixRows, n * a.G) - 1;     // its last virtual row
+    return max(prefix_tiles(len - n + last / a.G + 1), 1);
+  }
+  // tiles with their starts of the first `count` row tiles of a key head
+  __device__ __forceinline__ static int tall_before(const CacheBatch& a, int n, int len,
+                                                    int count) {
+    int sum = 0;
+    for (int i = 0; i < count; ++i) sum += tall_tiles(a, n, len, i) + kPrefixStart;
+    return sum;
+  }
+  template <bool TALL>
   __device__ __forceinline__ void load(const CacheBatch& a, int b0, int cols) {
     const int lane = (int)__lane_id(), b = b0 + lane;
     s = CacheSeq{0, 0, 0};
@@ -133,6 +146,11 @@ struct SeqBlock {
                 (prefix_tiles(P) + kPrefixStart);
       }
     }
+    if (TALL) {
+      own = s.n > 0 ? a.heads_kv *
+                      tall_before(a, s.n, s.len, row_tiles(a, s.n, kPrefixRows)) : 0;
+      return;
+    }
     own = s.n > 0 ? a.heads_kv * row_tiles(a, s.n, cols) *
                     (own_tiles(min(P, s.len), s.len) + kOwnStart) : 0;
   }
@@ -140,7 +158,7 @@ struct SeqBlock {
 
 // The tiles of all items (of prefixes, or of sequences' own tokens) in order, and the
 // sequence that a tile is of.
-template <bool PREFIX>
+template <bool PREFIX, bool TALL = false>
 struct SeqWalk {
   SeqBlock sb;                      // sequences sb0 ..
   int sb0, base, incl;              // tiles before them; running sums of theirs
@@ -148,7 +166,7 @@ struct SeqWalk {
   __device__ __forceinline__ int mine() const { return PREFIX ? sb.pre : sb.own; }
   __device__ __forceinline__ void block(const CacheBatch& a, int b0) {
     sb0 = b0;
-    sb.load(a, b0, cols);
+    sb.load<TALL>(a, b0, cols);
     incl = (int)wave_incl_scan((uint32_t)mine());
   }
   __device__ __forceinline__ int block_tiles() const { return __builtin_amdgcn_readlane(incl, 63); }
@@ -185,11 +203,11 @@ struct SeqWalk {
 constexpr int kCacheMeta = 8;
 struct CacheResults {
   int32_t* meta;
-  float* part;                      // [2 runs][cols] parts of own items
+  float* part;                      // [2 runs][cols_own] parts of own items
   float* part_pre;                  // [2 runs][cols_pre] parts of prefix items
   float* whole;                     // [2][rows H] whole prefix items; whole own items
                                     // of sequences with a prefix
-  int cols_pre;
+  int cols_own, cols_pre;
 };
 // Floats of a partial result of cols rows of D values: values, references, sums.
 template <int D>
