@@ -783,34 +783,67 @@ def skip_gather_dense(p: SkipProblem, rows, kept_offsets, rows_idx, packed, d_ou
     _check(st, "skip_gather_dense")
 
 
-def _cache_struct(p: SkipProblem, cache: "KvCache") -> SkipKvCache:
-    k, v = cache.k, cache.v
-    n_pages, heads_kv, page, d_h = k.shape
-    if v.shape != k.shape or d_h != p.d_h:
-        raise ValueError(f"cache.k and cache.v must be [pages, heads_kv, page_tokens, {p.d_h}]")
-    t = cache.page_table
-    if t.dim() != 2 or t.shape[0] < p.B:
-        raise ValueError(f"cache.page_table needs {p.B} rows, has {tuple(t.shape)}")
-    bf, n = torch.bfloat16, n_pages * heads_kv * d_h
-    return SkipKvCache(heads_kv, page, t.shape[1], 0, n_pages, _ptr(k, "cache.k", bf),
-                       _ptr(v, "cache.v", bf), _ptr(cache.mean, "cache.mean", bf, n),
-                       _ptr(t, "cache.page_table", torch.int32))
+def _dptr(t, name, dtype, numel, dev) -> Optional[int]:
+    """``_ptr`` of a tensor that has to be on device ``dev`` (one test where all is
+    well: 0.2 us; None and what is refused go the long way)."""
+    if t is None:
+        return None
+    ptr = t.data_ptr()
+    if (t.dtype is dtype and ptr and not ptr & 15 and t.get_device() == dev
+            and t.numel() >= numel and t.is_contiguous()):
+        return ptr
+    ptr = _ptr(t, name, dtype, numel)
+    _on_current_device(t)
+    return ptr
 
 
-def _row_strided(t: torch.Tensor, name: str, dtype, rows: int, heads: int, d_h: int):
+def _raw_stream(stream, dev) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+
+
+def _cache_struct(p: SkipProblem, cache: "KvCache", dev=None) -> SkipKvCache:
+    """The cache's description: its shapes are looked at when its arrays are set, its
+    pointers at every call."""
+    dev = torch.cuda.current_device() if dev is None else dev
+    k, t = cache.k, cache.page_table
+    c = cache.__dict__.get("_struct")
+    if c is None:
+        n_pages, heads_kv, page, _ = k.shape
+        if cache.v.shape != k.shape:
+            raise ValueError("cache.k and cache.v must be [pages, heads_kv, page_tokens, d_h]")
+        if t.dim() != 2:
+            raise ValueError("cache.page_table must be [B, pages_max]")
+        c = SkipKvCache(heads_kv, page, t.shape[1], 0, n_pages)
+        cache.__dict__["_struct"] = c
+    if k.shape[3] != p.d_h:
+        raise ValueError(f"cache.k must be [pages, heads_kv, page_tokens, {p.d_h}]")
+    n = c.n_pages * c.heads_kv * p.d_h
+    bf = torch.bfloat16
+    c.k = _dptr(k, "cache.k", bf, n * c.page_tokens, dev)
+    c.v = _dptr(cache.v, "cache.v", bf, n * c.page_tokens, dev)
+    c.mean = _dptr(cache.mean, "cache.mean", bf, n, dev)
+    c.page_table = _dptr(t, "cache.page_table", torch.int32, p.B * c.pages_max, dev)
+    return c
+
+
+def _row_strided(t: torch.Tensor, name: str, dtype, rows: int, heads: int, d_h: int, dev: int):
     """Pointer and row stride of [rows, heads, d_h] whose rows are contiguous."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != d_h:
-        raise ValueError(f"{name} must be [{rows}, {heads}, {d_h}], is {tuple(t.shape)}")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d_h):
+    if t.get_device() != dev:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        _on_current_device(t)
+    shape = t.shape
+    if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != d_h:
+        raise ValueError(f"{name} must be [{rows}, {heads}, {d_h}], is {tuple(shape)}")
+    step = t.stride()
+    if step[2] != 1 or (heads > 1 and step[1] != d_h):
         raise ValueError(f"{name}: a row's heads must be contiguous")
     ptr = t.data_ptr()
-    if ptr % 16:
+    if ptr & 15:
         raise ValueError(f"{name} must be 16-byte aligned")
-    return ptr, t.stride(0) if t.shape[0] > 1 else heads * d_h
+    return ptr, step[0] if shape[0] > 1 else heads * d_h
 
 
 def workspace_bytes_cache(p: SkipProblem, cache: "KvCache", n_sel: int = 0,
@@ -823,85 +856,88 @@ def _cache_bytes(p, c, n_sel, prefixes) -> int:
     _check(LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), int(n_sel),
                                           int(prefixes), ctypes.byref(n)),
            "skip_workspace_bytes_cache")
-    return int(n.value)
+    return n.value
 
 
 def skip_cache_append(p: SkipProblem, cache: "KvCache", rotation, q, k, v, row_offsets, lens,
                       q_out, positions=None, stream=None):
-    et = _elem_dtype(p)
-    c = _cache_struct(p, cache)
-    _on_current_device(cache.k, cache.v, cache.mean, cache.page_table, q, k, v, row_offsets, lens,
-                       q_out, positions, None if rotation is None else rotation.freq)
+    et, i32 = _elem_dtype(p), torch.int32
+    dev = torch.cuda.current_device()
+    c = _cache_struct(p, cache, dev)
     rot = None
     if rotation is not None:
         f = rotation.freq
-        rot = ctypes.byref(SkipRotation(_ptr(f, "rotation.freq", torch.float32), 2 * f.numel(),
-                                        ROTATIONS[rotation.style]))
-    M = p.total_kept
+        rot = ctypes.byref(SkipRotation(_dptr(f, "rotation.freq", torch.float32, 1, dev),
+                                        2 * f.numel(), ROTATIONS[rotation.style]))
+    M, D = p.total_kept, p.d_h
     qp = kp = vp_ = (None, 0)
     if M:
         if q is not None:
-            qp = _row_strided(q, "q", et, M, p.H, p.d_h)
-        kp = _row_strided(k, "k", et, M, c.heads_kv, p.d_h)
-        vp_ = _row_strided(v, "v", et, M, c.heads_kv, p.d_h)
+            qp = _row_strided(q, "q", et, M, p.H, D, dev)
+        kp = _row_strided(k, "k", et, M, c.heads_kv, D, dev)
+        vp_ = _row_strided(v, "v", et, M, c.heads_kv, D, dev)
     st = LIB.skip_cache_append(
         ctypes.byref(p), ctypes.byref(c), rot, *qp, *kp, *vp_,
-        _ptr(row_offsets, "row_offsets", torch.int32, p.B + 1),
-        _ptr(lens, "lens", torch.int32, p.B), _ptr(positions, "positions", torch.int32, M),
-        _ptr(q_out, "q_out", torch.bfloat16, M * p.d), _stream(stream))
+        _dptr(row_offsets, "row_offsets", i32, p.B + 1, dev), _dptr(lens, "lens", i32, p.B, dev),
+        _dptr(positions, "positions", i32, M, dev),
+        _dptr(q_out, "q_out", torch.bfloat16, M * p.d, dev), _raw_stream(stream, dev))
     _check(st, "skip_cache_append")
 
 
-def _cache_ws(p, c, workspace, n_sel, prefixes, device, stream):
+def _cache_ws(p, c, workspace, n_sel, prefixes, device, stream, dev):
+    """(tensor to keep, pointer, bytes) of a call's workspace: the caller's, or a fresh
+    one where the call needs one."""
     if workspace is None:
-        workspace = _fresh_workspace(_cache_bytes(p, c, n_sel, prefixes), device, stream)
-    return workspace, _ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
+        need = _cache_bytes(p, c, n_sel, prefixes)
+        if not need:
+            return None, None, 0
+        workspace = _fresh_workspace(need, device, stream)
+    return (workspace, _dptr(workspace, "workspace", workspace.dtype, 0, dev),
+            workspace.numel() * workspace.element_size())
 
 
 def skip_cache_attn(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, O, lse=None,
                     prefix_ids=None, prefix_lens=None, workspace=None, stream=None):
-    c = _cache_struct(p, cache)
-    _on_current_device(cache.k, cache.v, cache.page_table, q, row_offsets, lens, O, lse, prefix_ids,
-                       prefix_lens, workspace)
-    M = p.total_kept
-    ws, wp, wn = _cache_ws(p, c, workspace, 0, prefix_ids is not None, cache.k.device, stream)
+    dev, i32 = torch.cuda.current_device(), torch.int32
+    c = _cache_struct(p, cache, dev)
+    B, M, n = p.B, p.total_kept, p.total_kept * p.d
+    ws, wp, wn = _cache_ws(p, c, workspace, 0, prefix_ids is not None, q.device, stream, dev)
     st = LIB.skip_cache_attn(
-        ctypes.byref(p), ctypes.byref(c), _ptr(q, "q", torch.bfloat16, M * p.d),
-        _ptr(row_offsets, "row_offsets", torch.int32, p.B + 1),
-        _ptr(lens, "lens", torch.int32, p.B), _ptr(prefix_ids, "prefix_ids", torch.int32, p.B),
-        _ptr(prefix_lens, "prefix_lens", torch.int32, p.B), _ptr(O, "O", _out_dtype(p), M * p.d),
-        _ptr(lse, "lse", torch.float32, M * p.H), wp, wn, _stream(stream))
+        ctypes.byref(p), ctypes.byref(c), _dptr(q, "q", torch.bfloat16, n, dev),
+        _dptr(row_offsets, "row_offsets", i32, B + 1, dev), _dptr(lens, "lens", i32, B, dev),
+        _dptr(prefix_ids, "prefix_ids", i32, B, dev),
+        _dptr(prefix_lens, "prefix_lens", i32, B, dev), _dptr(O, "O", _out_dtype(p), n, dev),
+        _dptr(lse, "lse", torch.float32, M * p.H, dev), wp, wn, _raw_stream(stream, dev))
     _check(st, "skip_cache_attn")
 
 
 def skip_cache_select(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, n_sel, pages,
                       n_first=1, n_last=1, workspace=None, stream=None):
-    c = _cache_struct(p, cache)
-    _on_current_device(cache.mean, cache.page_table, q, row_offsets, lens, pages, workspace)
-    M = p.total_kept
-    ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, cache.k.device, stream)
+    dev, i32 = torch.cuda.current_device(), torch.int32
+    c = _cache_struct(p, cache, dev)
+    B, M = p.B, p.total_kept
+    ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, q.device, stream, dev)
     st = LIB.skip_cache_select(
-        ctypes.byref(p), ctypes.byref(c), _ptr(q, "q", torch.bfloat16, M * p.d),
-        _ptr(row_offsets, "row_offsets", torch.int32, p.B + 1),
-        _ptr(lens, "lens", torch.int32, p.B), int(n_sel), int(n_first), int(n_last),
-        _ptr(pages, "pages", torch.int32, M * c.heads_kv * int(n_sel)), wp, wn, _stream(stream))
+        ctypes.byref(p), ctypes.byref(c), _dptr(q, "q", torch.bfloat16, M * p.d, dev),
+        _dptr(row_offsets, "row_offsets", i32, B + 1, dev), _dptr(lens, "lens", i32, B, dev),
+        int(n_sel), int(n_first), int(n_last),
+        _dptr(pages, "pages", i32, M * c.heads_kv * int(n_sel), dev), wp, wn,
+        _raw_stream(stream, dev))
     _check(st, "skip_cache_select")
 
 
 def skip_cache_attn_pages(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, pages, n_sel, O,
                           lse=None, workspace=None, stream=None):
-    c = _cache_struct(p, cache)
-    _on_current_device(cache.k, cache.v, cache.page_table, q, row_offsets, lens, pages, O, lse,
-                       workspace)
-    M = p.total_kept
-    ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, cache.k.device, stream)
+    dev, i32 = torch.cuda.current_device(), torch.int32
+    c = _cache_struct(p, cache, dev)
+    B, M, n = p.B, p.total_kept, p.total_kept * p.d
+    ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, q.device, stream, dev)
     st = LIB.skip_cache_attn_pages(
-        ctypes.byref(p), ctypes.byref(c), _ptr(q, "q", torch.bfloat16, M * p.d),
-        _ptr(row_offsets, "row_offsets", torch.int32, p.B + 1),
-        _ptr(lens, "lens", torch.int32, p.B),
-        _ptr(pages, "pages", torch.int32, M * c.heads_kv * int(n_sel)), int(n_sel),
-        _ptr(O, "O", _out_dtype(p), M * p.d), _ptr(lse, "lse", torch.float32, M * p.H), wp, wn,
-        _stream(stream))
+        ctypes.byref(p), ctypes.byref(c), _dptr(q, "q", torch.bfloat16, n, dev),
+        _dptr(row_offsets, "row_offsets", i32, B + 1, dev), _dptr(lens, "lens", i32, B, dev),
+        _dptr(pages, "pages", i32, M * c.heads_kv * int(n_sel), dev), int(n_sel),
+        _dptr(O, "O", _out_dtype(p), n, dev), _dptr(lse, "lse", torch.float32, M * p.H, dev), wp,
+        wn, _raw_stream(stream, dev))
     _check(st, "skip_cache_attn_pages")
 
 
@@ -1368,6 +1404,10 @@ class KvCache:
     mean: Optional[torch.Tensor]
     page_table: torch.Tensor
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_struct", None)        # (see _cache_struct)
+
 
 @dataclass
 class Rotation:
@@ -1393,18 +1433,19 @@ def cache_append(p: SkipProblem, cache: KvCache, q, k, v, row_offsets, lens, rot
     of a multiple of 8 elements.  Returns the rotated queries, bf16 (``out``: a
     preallocated tensor)."""
     if out is None and q is not None:
-        out = torch.empty((p.total_kept, p.H, p.d_h), dtype=torch.bfloat16, device=cache.k.device)
+        out = cache.k.new_empty((p.total_kept, p.H, p.d_h))
         _record(out, stream)
     skip_cache_append(p, cache, rotation, q, k, v, row_offsets, lens, out, positions, stream)
     return out
 
 
-def _cache_out(p, out, device, stream):
+def _cache_out(p, out, like, stream):
     if out is None:
-        out = (torch.empty((p.total_kept, p.H, p.d_h), dtype=_out_dtype(p), device=device),
-               torch.empty((p.total_kept, p.H), dtype=torch.float32, device=device))
-        for t in out:
-            _record(t, stream)
+        out = (like.new_empty((p.total_kept, p.H, p.d_h), dtype=_out_dtype(p)),
+               like.new_empty((p.total_kept, p.H), dtype=torch.float32))
+        if stream is not None:
+            for t in out:
+                _record(t, stream)
     return out
 
 
@@ -1412,7 +1453,7 @@ def cache_attn(p: SkipProblem, cache: KvCache, q, row_offsets, lens, prefix_ids=
                prefix_lens=None, out=None, workspace=None, stream=None) -> Tuple:
     """Causal attention of the new tokens over the cache.  Returns (O, lse);
     ``out`` = the two preallocated (lse None: not written)."""
-    O, lse = out = _cache_out(p, out, cache.k.device, stream)
+    O, lse = out = _cache_out(p, out, q, stream)
     skip_cache_attn(p, cache, q, row_offsets, lens, O, lse, prefix_ids, prefix_lens, workspace,
                     stream)
     return out
@@ -1424,8 +1465,7 @@ def cache_select(p: SkipProblem, cache: KvCache, q, row_offsets, lens, n_sel: in
     """The pages of the largest scores for every new token and key head, [total_kept,
     heads_kv, n_sel] int32 ascending, -1 behind the last."""
     if out is None:
-        out = torch.empty((p.total_kept, cache.k.shape[1], n_sel), dtype=torch.int32,
-                          device=cache.k.device)
+        out = q.new_empty((p.total_kept, cache.k.shape[1], n_sel), dtype=torch.int32)
         _record(out, stream)
     skip_cache_select(p, cache, q, row_offsets, lens, n_sel, out, n_first, n_last, workspace,
                       stream)
@@ -1436,7 +1476,7 @@ def cache_attn_pages(p: SkipProblem, cache: KvCache, q, row_offsets, lens, pages
                      workspace=None, stream=None) -> Tuple:
     """Attention of the new tokens over ``pages`` [total_kept, heads_kv, n_sel] int32.
     Returns (O, lse); ``out`` = the two preallocated (lse None: not written)."""
-    O, lse = out = _cache_out(p, out, cache.k.device, stream)
+    O, lse = out = _cache_out(p, out, q, stream)
     skip_cache_attn_pages(p, cache, q, row_offsets, lens, pages, pages.shape[-1], O, lse,
                           workspace, stream)
     return out

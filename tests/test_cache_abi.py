@@ -157,12 +157,21 @@ def test_binding_checks(b):
     p = problem(b)
     kv = torch.empty(20, 4, 64, 64, dtype=torch.bfloat16)
     t = torch.zeros(2, 8, dtype=torch.int32)
+    build = lambda *a: b._cache_struct(p, b.KvCache(*a), 0)
     with pytest.raises(ValueError, match="page_tokens"):
-        b.workspace_bytes_cache(p, b.KvCache(kv, kv[:3], None, t))
-    with pytest.raises(ValueError, match="rows"):
-        b.workspace_bytes_cache(p, b.KvCache(kv, kv, None, t[:1]))
+        build(kv, kv[:3], None, t)
+    with pytest.raises(ValueError, match="pages_max"):
+        build(kv, kv, None, t[0])
+    with pytest.raises(ValueError, match="64"):
+        build(kv[..., :32], kv[..., :32], None, t)
     with pytest.raises(ValueError, match="device"):
-        b.workspace_bytes_cache(p, b.KvCache(kv, kv, None, t))
+        build(kv, kv, None, t)
+    # a cache whose arrays are set anew is looked at anew
+    c = b.KvCache(kv, kv, None, t)
+    c.__dict__["_struct"] = "of the old arrays"
+    c.page_table = t[0]
+    with pytest.raises(ValueError, match="pages_max"):
+        b._cache_struct(p, c, 0)
 
 
 # ---------------------------------------------------------------------------
