@@ -70,8 +70,9 @@ struct CacheItem {
   bool shared;                      // rows with a prefix: results are joined
 };
 
-template <int D, int R, bool OUT_F32, bool LISTED>
-__global__ void __launch_bounds__(kCThreads, R > 2 ? 1 : 2)
+// SOLO: every wave takes an item of its own (its partial is the whole).
+template <int D, int R, bool OUT_F32, bool LISTED, bool SOLO>
+__global__ void __launch_bounds__(kCThreads, 2)
 cache_attn_kernel(CacheAttnArgs args) {
   const CacheAttnArgs& a = args;
   const CacheBatch& bt = a.batch;
@@ -163,8 +164,9 @@ cache_attn_kernel(CacheAttnArgs args) {
 
     // 64 of the wave's tiles at a time, one a lane: where the tile lies, and its
     // first token
-    for (int u0 = it.t0 + wave; u0 < it.t1; u0 += 64 * kCWaves) {
-      const int u = u0 + kCWaves * lane;
+    constexpr int SIDE = SOLO ? 1 : kCWaves;        // waves side by side
+    for (int u0 = it.t0 + (SOLO ? 0 : wave); u0 < it.t1; u0 += 64 * SIDE) {
+      const int u = u0 + SIDE * lane;
       int at = -1, tok = 0;
       if (u < it.t1) {
         if constexpr (LISTED) {
@@ -322,7 +324,7 @@ cache_attn_kernel(CacheAttnArgs args) {
     }
 
     // the waves' results together, and where they go
-    __syncthreads();                           // (the last item's are read)
+    if (!SOLO) __syncthreads();                // (the last item's are read)
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (r >= nblk) continue;
@@ -341,20 +343,23 @@ cache_attn_kernel(CacheAttnArgs args) {
         pl[wave][col] = l;
       }
     }
-    __syncthreads();
+    if (SOLO) wait_lgkm0();
+    else __syncthreads();
     constexpr int NC4 = D / 4;
     const bool all = it.t0 == 0 && it.t1 == it.nt;
     const int run = blockIdx.x;
-    for (int e = tid; e < it.nv * NC4; e += kCThreads) {
+    const int w0 = SOLO ? wave : 0, w1 = SOLO ? wave + 1 : kCWaves;
+    for (int e = SOLO ? lane : tid; e < it.nv * NC4; e += SOLO ? 64 : kCThreads) {
       const int col = e / NC4, c4 = e % NC4;
-      float m = pm[0][col];
+      float m = pm[w0][col];
+      if (!SOLO)
 #pragma unroll
-      for (int w = 1; w < kCWaves; ++w) m = fmaxf(m, pm[w][col]);
+        for (int w = 1; w < kCWaves; ++w) m = fmaxf(m, pm[w][col]);
       const float ref = m == -INFINITY ? 0.f : m;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
       float l = 0.f;
 #pragma unroll
-      for (int w = 0; w < kCWaves; ++w) {
+      for (int w = w0; w < w1; ++w) {
         const float f = __builtin_amdgcn_exp2f(pm[w][col] - ref);
         const float4 x = *reinterpret_cast<const float4*>(&po[w][col][4 * c4]);
         o.x = fmaf(x.x, f, o.x);
@@ -398,32 +403,55 @@ cache_attn_kernel(CacheAttnArgs args) {
 
   if constexpr (LISTED) {
     const int rows = clampi(bt.row_offsets[bt.B], 0, bt.total_rows);
-    const int nt = a.n_sel << (shift - 5), step = nt + kOwnStart;
-    const int W = rows * hkv * step;
-    const int per = a.direct ? step : max((W + a.runs - 1) / a.runs, kCLeast);
-    if (!a.direct && blockIdx.x == 0 && tid == 0) a.res.meta[(size_t)bt.B * kCacheMeta] = per;
-    int u = blockIdx.x * per;
-    const int end = min(W - u, per) + u;
-    while (u < end) {
-      const int i = u / step, start = i * step;
+    const int nt = a.n_sel << (shift - 5);
+    auto listed = [&](int row, int hk, int t0, int t1) {
       CacheItem it;
-      it.r0 = i / hkv;
-      it.hk = i - it.r0 * hkv;
+      it.r0 = row;
+      it.hk = hk;
       it.nt = nt;
-      it.t0 = tile_at<kOwnStart>(u - start, nt);
-      it.t1 = tile_at<kOwnStart>(end - start, nt);
-      u = start + step;
-      if (it.t0 == it.t1) continue;
+      it.t0 = t0;
+      it.t1 = t1;
       CacheSeq s;
-      it.b = seq_of_row(bt.row_offsets, bt.lens, bt.B, bt.total_rows, bt.k_max, bt.L_max, it.r0, s);
-      if (it.b < 0) continue;
+      it.b = seq_of_row(bt.row_offsets, bt.lens, bt.B, bt.total_rows, bt.k_max, bt.L_max, row, s);
+      if (it.b < 0) return;
       it.v0 = 0;
       it.nv = bt.G;
       it.lo = 0;
-      it.hi = max(s.len - s.n + it.r0 - s.r0 + 1, 0);
+      it.hi = max(s.len - s.n + row - s.r0 + 1, 0);
       it.n = 1;
       it.shared = false;
       work(it);
+    };
+    if (a.direct) {
+      // An item a workgroup (SOLO: a wave).  Workgroup id L goes to XCD L % 8; rows of
+      // one key head stay on one, whose L2 holds the pages that they share (92 rows of
+      // 16 heads over 17 pages each: PENDING us, 43 in order).
+      const int x = blockIdx.x & 7;
+      const int i = SOLO ? (blockIdx.x >> 3) * kCWaves + wave : blockIdx.x >> 3;
+      int row, hk;
+      if (hkv % 8 == 0) {
+        row = i / (hkv / 8);
+        hk = x + 8 * (i - row * (hkv / 8));
+      } else if (8 % hkv == 0) {
+        row = i * (8 / hkv) + x / hkv;
+        hk = x % hkv;
+      } else {
+        row = (8 * i + x) / hkv;
+        hk = 8 * i + x - row * hkv;
+      }
+      if (row < rows) listed(row, hk, 0, nt);
+      return;
+    }
+    const int step = nt + kOwnStart, W = rows * hkv * step;
+    const int per = max((W + a.runs - 1) / a.runs, kCLeast);
+    if (blockIdx.x == 0 && tid == 0) a.res.meta[(size_t)bt.B * kCacheMeta] = per;
+    int u = blockIdx.x * per;
+    const int end = min(W - u, per) + u;
+    while (u < end) {
+      const int i = u / step, start = i * step, row = i / hkv;
+      const int t0 = tile_at<kOwnStart>(u - start, nt), t1 = tile_at<kOwnStart>(end - start, nt);
+      if (t0 < t1) listed(row, i - row * hkv, t0, t1);
+      u = start + step;
     }
   } else {
     SeqWalk<false> walk;
@@ -507,7 +535,7 @@ namespace {
 
 struct CachePlan {
   int R, runs, cols_pre;
-  bool direct, prefixes;
+  bool direct, solo, prefixes;
   size_t meta, part, part_pre, whole;          // bytes
 };
 
@@ -515,10 +543,13 @@ CachePlan cache_plan(const skip_problem_t& p, const skip_kv_cache_t& c, int n_se
   CachePlan x{};
   const int G = p.H / c.heads_kv;
   if (n_sel > 0) {
-    const int nt = n_sel * (c.page_tokens / kCTile);
+    // many short items: a wave each
+    const int nt = n_sel * (c.page_tokens / kCTile), items = p.total_kept * c.heads_kv;
     x.R = G <= 16 ? 1 : 2;
-    x.direct = nt <= 16 || (long long)p.total_kept * c.heads_kv >= 512;
-    x.runs = x.direct ? p.total_kept * c.heads_kv : 512;
+    x.direct = nt <= 16 || items >= 512;
+    x.solo = x.direct && items >= 1024 && nt <= 64;
+    const int side = x.solo ? kCWaves : 1;
+    x.runs = !x.direct ? 512 : 8 * (((items + 7) / 8 + side - 1) / side);
   } else {
     // sequences of up to 512 tokens: an item a workgroup, prefixes with them
     x.direct = p.L_max <= 512;
@@ -541,8 +572,10 @@ CachePlan cache_plan(const skip_problem_t& p, const skip_kv_cache_t& c, int n_se
 }
 
 template <int D, int R, bool OUT_F32, bool LISTED>
-hipError_t launch_one(const CacheAttnArgs& a, hipStream_t s) {
-  cache_attn_kernel<D, R, OUT_F32, LISTED><<<dim3((unsigned)a.runs), kCThreads, 0, s>>>(a);
+hipError_t launch_one(const CacheAttnArgs& a, bool solo, hipStream_t s) {
+  const dim3 grid((unsigned)a.runs);
+  if (LISTED && solo) cache_attn_kernel<D, R, OUT_F32, true, true><<<grid, kCThreads, 0, s>>>(a);
+  else cache_attn_kernel<D, R, OUT_F32, LISTED, false><<<grid, kCThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.direct) return e;
   if (a.batch.prefix_ids) {
@@ -553,10 +586,12 @@ hipError_t launch_one(const CacheAttnArgs& a, hipStream_t s) {
   return launch_join<D, OUT_F32, LISTED ? kJoinListed : kJoinOwn>(j, s);
 }
 template <int D, bool LISTED>
-hipError_t launch_rows(const CacheAttnArgs& a, int R, hipStream_t s) {
-  if (R == 1)
-    return a.o_f32 ? launch_one<D, 1, true, LISTED>(a, s) : launch_one<D, 1, false, LISTED>(a, s);
-  return a.o_f32 ? launch_one<D, 2, true, LISTED>(a, s) : launch_one<D, 2, false, LISTED>(a, s);
+hipError_t launch_rows(const CacheAttnArgs& a, const CachePlan& x, hipStream_t s) {
+  if (x.R == 1)
+    return a.o_f32 ? launch_one<D, 1, true, LISTED>(a, x.solo, s)
+                   : launch_one<D, 1, false, LISTED>(a, x.solo, s);
+  return a.o_f32 ? launch_one<D, 2, true, LISTED>(a, x.solo, s)
+                 : launch_one<D, 2, false, LISTED>(a, x.solo, s);
 }
 
 }  // namespace
@@ -605,8 +640,8 @@ hipError_t launch_cache_attn(const skip_problem_t& p, const skip_kv_cache_t& c, 
                   cache_view(c), res, static_cast<const bf16_t*>(q), pages, O, lse, n_sel, p.o_f32,
                   x.runs, x.direct, p.sm_scale * kCLog2e};
   if (n_sel > 0)
-    return p.d_h == 64 ? launch_rows<64, true>(a, x.R, s) : launch_rows<128, true>(a, x.R, s);
-  return p.d_h == 64 ? launch_rows<64, false>(a, x.R, s) : launch_rows<128, false>(a, x.R, s);
+    return p.d_h == 64 ? launch_rows<64, true>(a, x, s) : launch_rows<128, true>(a, x, s);
+  return p.d_h == 64 ? launch_rows<64, false>(a, x, s) : launch_rows<128, false>(a, x, s);
 }
 
 }  // namespace skip

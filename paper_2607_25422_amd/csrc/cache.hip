@@ -205,56 +205,87 @@ struct SelectArgs {
   int B, H, G, total_rows, k_max, L_max, P, n_sel, n_first, n_last;
 };
 
-constexpr int kScoreThreads = 256;
-constexpr int kScorePages = 256;          // pages of a workgroup
-
-// Scores of kScorePages pages: D / 8 lanes a page, 16 bytes each.
+// Scores of 64 pages by one wave: D / 8 lanes a page, 16 bytes each, all loads in
+// flight at once.  Returns the score of page j0 + `at`.  qs: the lane's eight features
+// of the summed queries.
 template <int D>
-__global__ void __launch_bounds__(kScoreThreads)
+__device__ __forceinline__ double score64(const SelectArgs& a, int b, int hk, int j0, int vis,
+                                          const double (&qs)[8], int& at) {
+  constexpr int C = D / 8, PL = 64 / C, N = C;       // lanes a page, pages at a time, times
+  const int lane = (int)__lane_id(), c = lane % C, pl = lane / C;
+  const int mine = a.cache.page(b, min(j0 + lane, vis - 1));
+  u32x4 x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int pg = max(__shfl(mine, PL * i + pl, kWave), 0);
+    x[i] = *reinterpret_cast<const u32x4*>(
+        a.cache.mean + ((size_t)(uint32_t)pg * a.cache.heads_kv + hk) * D + 8 * c);
+  }
+  double z[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    double y[8];
+    unpack16_f64<bf16_t>(x[i], y);
+    z[i] = 0.0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[i] = fma(qs[e], y[e], z[i]);
+  }
+  // sums over the lanes of a page; lane c keeps those of time c
+#pragma unroll
+  for (int m = N / 2; m >= 1; m >>= 1) {
+    const bool up = (c & m) != 0;
+#pragma unroll
+    for (int i = 0; i < m; ++i) {
+      const double keep = up ? z[i + m] : z[i], give = up ? z[i] : z[i + m];
+      z[i] = keep + __shfl_xor(give, m, kWave);
+    }
+  }
+  at = PL * c + pl;
+  return __shfl(mine, at, kWave) < 0 ? 0.0 : z[0];
+}
+// The lane's features of the sum of a key head's queries.
+template <int D>
+__device__ __forceinline__ void sum_queries(const SelectArgs& a, int row, int hk,
+                                            double (&qs)[8]) {
+  const bf16_t* q = a.q + ((size_t)row * a.H + hk * a.G) * D + 8 * ((int)__lane_id() % (D / 8));
+#pragma unroll
+  for (int e = 0; e < 8; ++e) qs[e] = 0.0;
+#pragma unroll 4
+  for (int g = 0; g < a.G; ++g) {
+    double x[8];
+    unpack16_f64<bf16_t>(*reinterpret_cast<const u32x4*>(q + (size_t)g * D), x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) qs[e] += x[e];
+  }
+}
+
+// Scores of 256 pages a workgroup, for few rows and many pages.
+template <int D>
+__global__ void __launch_bounds__(256)
 cache_score_kernel(SelectArgs a) {
-  constexpr int C = D / 8, PL = kScoreThreads / C;   // lanes a page, pages side by side
-  const int row = blockIdx.z, hk = blockIdx.y, j0 = blockIdx.x * kScorePages;
+  const int row = blockIdx.z, hk = blockIdx.y, j0 = 64 * (4 * blockIdx.x + threadIdx.x / 64);
   CacheSeq s;
   const int b = seq_of_row(a.row_offsets, a.lens, a.B, a.total_rows, a.k_max, a.L_max, row, s);
   if (b < 0) return;
   const int t = s.len - s.n + row - s.r0;
-  const int vis = t < 0 ? 0 : (t >> a.cache.shift) + 1;
+  const int vis = t < 0 ? 0 : min((t >> a.cache.shift) + 1, a.P);
   if (j0 >= vis) return;
-  const int c = threadIdx.x % C, pl = threadIdx.x / C;
-  double qs[8] = {};
-  for (int g = 0; g < a.G; ++g) {
-    double x[8];
-    unpack16_f64<bf16_t>(*reinterpret_cast<const u32x4*>(
-        a.q + ((size_t)row * a.H + hk * a.G + g) * D + 8 * c), x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) qs[e] += x[e];
-  }
-  double* out = a.scores + ((size_t)row * a.cache.heads_kv + hk) * a.P;
-  const int end = min(min(vis, a.P), j0 + kScorePages);
-  for (int j = j0 + pl; j < j0 + kScorePages; j += PL) {
-    if (j - pl >= end) break;                        // (lanes of a page together)
-    const int at = a.cache.page(b, min(j, end - 1));
-    double z = 0.0;
-    if (at >= 0) {
-      double x[8];
-      unpack16_f64<bf16_t>(*reinterpret_cast<const u32x4*>(
-          a.cache.mean + ((size_t)(uint32_t)at * a.cache.heads_kv + hk) * D + 8 * c), x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z = fma(qs[e], x[e], z);
-    }
-#pragma unroll
-    for (int m = 1; m < C; m <<= 1) z += __shfl_xor(z, m, kWave);
-    if (c == 0 && j < end) out[j] = z;
-  }
+  double qs[8];
+  sum_queries<D>(a, row, hk, qs);
+  int at;
+  const double z = score64<D>(a, b, hk, j0, vis, qs, at);
+  if (j0 + at < vis) a.scores[((size_t)row * a.cache.heads_kv + hk) * a.P + j0 + at] = z;
 }
 
-// The selection of one row and key head: the scores' keys in registers, a radix
-// select, and the chosen pages in ascending order, -1 behind them.
-template <int MAXPT, int THREADS>
+// The selection of one row and key head: scores (from the launch before, or made here
+// and kept in LDS), their keys in registers, a radix select, and the chosen pages in
+// ascending order, -1 behind them.
+template <int D, int THREADS, int MAXPT, bool SCORED>
 __global__ void __launch_bounds__(THREADS)
 cache_select_kernel(SelectArgs a) {
   __shared__ SelectShared sh;
   __shared__ uint32_t scan[THREADS / 64 + 1];
+  __shared__ double zs[SCORED ? 1 : THREADS * MAXPT];
   const int row = blockIdx.y, hk = blockIdx.x, tid = threadIdx.x;
   CacheSeq s;
   const int b = seq_of_row(a.row_offsets, a.lens, a.B, a.total_rows, a.k_max, a.L_max, row, s);
@@ -263,13 +294,27 @@ cache_select_kernel(SelectArgs a) {
   const int vis = t < 0 ? 0 : min((t >> a.cache.shift) + 1, a.P);
   const double* z = a.scores + ((size_t)row * a.cache.heads_kv + hk) * a.P;
   int32_t* out = a.pages + ((size_t)row * a.cache.heads_kv + hk) * a.n_sel;
+  if constexpr (!SCORED) {
+    if (vis > a.n_sel) {                             // (else all of them)
+      double qs[8];
+      sum_queries<D>(a, row, hk, qs);
+      for (int j0 = tid & ~63; j0 < vis; j0 += THREADS) {
+        int at;
+        const double x = score64<D>(a, b, hk, j0, vis, qs, at);
+        if (j0 + at < vis) zs[j0 + at] = x;
+      }
+    }
+    __syncthreads();
+    z = zs;
+  }
   const int C = (vis + THREADS - 1) / THREADS, e0 = tid * C, cnt = clampi(vis - e0, 0, C);
   uint64_t keys[MAXPT];
 #pragma unroll
   for (int i = 0; i < MAXPT; ++i) {
     keys[i] = 0;
     const int j = e0 + i;
-    if (i < cnt) keys[i] = j < a.n_first || j >= vis - a.n_last ? ~0ull : order_key(z[j]);
+    if (i < cnt && vis > a.n_sel)
+      keys[i] = j < a.n_first || j >= vis - a.n_last ? ~0ull : order_key(z[j]);
   }
   const int kk = min(a.n_sel, vis);
   SelectMask<MAXPT> flags;
@@ -324,8 +369,34 @@ bool cache_select_fits(const skip_problem_t& p, const skip_kv_cache_t& c) {
   return select_pages(p, c) <= 16384 && p.total_kept <= 65535;
 }
 
+// Whether scores are made by a launch of their own, which takes more workgroups for
+// few rows over many pages (8 rows and key heads of d_h 128: 1024 pages 11.2 us in one
+// launch, 12.1 in two; 2048 pages 16.0 and 12.7; 256 of them over 1024 pages 12.4 and 17.7,
+// 4096 pages 29.7 and 37.1).
+static bool score_apart(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  return select_pages(p, c) > 1536 && (long long)p.total_kept * c.heads_kv < 256;
+}
+
 size_t cache_select_scratch(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  if (!score_apart(p, c)) return 0;
   return (size_t)p.total_kept * c.heads_kv * select_pages(p, c) * sizeof(double);
+}
+
+template <int D>
+static hipError_t launch_select(const SelectArgs& a, bool apart, hipStream_t s) {
+  const dim3 grid((unsigned)a.cache.heads_kv, (unsigned)a.total_rows);
+  if (apart) {
+    const dim3 g((unsigned)((a.P + 255) / 256), (unsigned)a.cache.heads_kv, (unsigned)a.total_rows);
+    cache_score_kernel<D><<<g, 256, 0, s>>>(a);
+    cache_select_kernel<D, 1024, 16, true><<<grid, 1024, 0, s>>>(a);
+  } else if (a.P <= 256) {
+    cache_select_kernel<D, 256, 1, false><<<grid, 256, 0, s>>>(a);
+  } else if (a.P <= 2048) {
+    cache_select_kernel<D, 1024, 2, false><<<grid, 1024, 0, s>>>(a);
+  } else {
+    cache_select_kernel<D, 1024, 16, false><<<grid, 1024, 0, s>>>(a);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_cache_select(const skip_problem_t& p, const skip_kv_cache_t& c, const void* q,
@@ -335,16 +406,8 @@ hipError_t launch_cache_select(const skip_problem_t& p, const skip_kv_cache_t& c
   SelectArgs a{cache_view(c), static_cast<const bf16_t*>(q), row_offsets, lens,
                static_cast<double*>(scratch), pages, p.B, p.H, p.H / c.heads_kv, p.total_kept,
                p.k_max, p.L_max, select_pages(p, c), n_sel, n_first, n_last};
-  if (a.P > 0) {
-    const dim3 grid((unsigned)((a.P + kScorePages - 1) / kScorePages), (unsigned)c.heads_kv,
-                    (unsigned)p.total_kept);
-    if (p.d_h == 64) cache_score_kernel<64><<<grid, kScoreThreads, 0, s>>>(a);
-    else cache_score_kernel<128><<<grid, kScoreThreads, 0, s>>>(a);
-  }
-  const dim3 grid((unsigned)c.heads_kv, (unsigned)p.total_kept);
-  if (a.P <= 1024) cache_select_kernel<4, 256><<<grid, 256, 0, s>>>(a);
-  else cache_select_kernel<16, 1024><<<grid, 1024, 0, s>>>(a);
-  return hipGetLastError();
+  const bool apart = score_apart(p, c);
+  return p.d_h == 64 ? launch_select<64>(a, apart, s) : launch_select<128>(a, apart, s);
 }
 
 }  // namespace skip

@@ -401,6 +401,9 @@ SELECT = [
     dict(seqs=[(1, 3000)], n_sel=200),
     dict(seqs=[(1, 600 + 50 * (i % 5)) for i in range(70)], H=6, hk=3, n_sel=5),
     dict(seqs=[(4, 1500), (1, 900)], H=24, hk=1, D=128, page=128, n_sel=6, o_f32=True),
+    dict(seqs=[(1, 80000), (1, 40)], H=2, hk=1, n_sel=30, n_last=2),        # 2500 pages, few rows
+    dict(seqs=[(130, 66000)], H=2, hk=2, n_sel=3),                          # and many
+    dict(seqs=[(70, 300), (1, 20)], H=32, hk=16, D=128, n_sel=5, o_f32=True),     # a wave each
 ]
 
 
