@@ -72,15 +72,17 @@ struct CacheItem {
 
 // SOLO: every wave takes an item of its own (its partial is the whole).
 template <int D, int R, bool OUT_F32, bool LISTED, bool SOLO>
-__global__ void __launch_bounds__(kCThreads, 2)
+__global__ void __launch_bounds__(kCThreads, D == 64 && R == 1 ? 3 : 2)
 cache_attn_kernel(CacheAttnArgs args) {
   const CacheAttnArgs& a = args;
   const CacheBatch& bt = a.batch;
   constexpr int COLS = 16 * R, KC = D / 32, NB = D / 16, FPL = D / 16, PIECES = kCPieces<OUT_F32>;
   constexpr int VW = FPL / 2;               // dwords of a lane's features of a token
   constexpr int OS = D + 4;
-  __shared__ __attribute__((aligned(16))) float po[kCWaves][COLS][OS];
   __shared__ float pm[kCWaves][COLS], pl[kCWaves][COLS];
+  // a wave's keys in turn (see koff), or its results
+  constexpr int PART = COLS * OS * 4 > kCTile * 2 * D ? COLS * OS * 4 : kCTile * 2 * D;
+  __shared__ __attribute__((aligned(16))) uint8_t turn[kCWaves][PART];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
@@ -91,9 +93,21 @@ cache_attn_kernel(CacheAttnArgs args) {
   const bool flat = a.scale_log2 == 0.f;
   const float sc = flat ? 1.f : fabsf(a.scale_log2);
 
-  // lane offsets (elements) into a tile's keys and values
-  const int koff = (8 * (n >> 2) + (n & 3)) * D + 8 * g;
+  // Keys come in rows (lane l: 16 bytes of token l / (D / 8)), so that a load takes whole
+  // lines, and change hands through the wave's part of LDS: 16 bytes of 16 tokens each,
+  // as a product takes them, are as many accesses of the L1 cache (130 rows of 16 heads
+  // of d_h 64 over 17 pages of 32 tokens: 44 us, 27 by rows).  Chunk c of token t lies at
+  // c ^ (t % 4 + 4 (t / 8 % 2)): eight lanes of a read are eight such tokens.
+  constexpr int CH = D / 8, RI = 64 / CH, NI = kCTile / RI;   // chunks; tokens a load; loads
+  const int koff = (lane / CH) * D + 8 * (lane % CH);
   const int voff = 8 * g * D + FPL * n;
+  const uint32_t klds = lds_addr(turn[wave]);
+  auto key_at = [](int t, int c) -> uint32_t {
+    return t * 2 * D + 16 * (c ^ ((t & 3) | ((t >> 1) & 4)));
+  };
+  uint32_t kread[KC];                        // of product 0 (product 1: four tokens on)
+#pragma unroll
+  for (int c = 0; c < KC; ++c) kread[c] = klds + key_at(8 * (n >> 2) + (n & 3), 4 * c + g);
 
   // One part of an item: every wave its tiles, then the waves' results together.
   auto work = [&](const CacheItem& it) {
@@ -101,12 +115,13 @@ cache_attn_kernel(CacheAttnArgs args) {
     int lim[R];
     u32x4 qf[R][KC];
     const int nblk = (it.nv + 15) / 16;
+    auto live = [&](int r) { return R == 1 || r < nblk; };
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int v = it.v0 + min(16 * r + n, it.nv - 1);
       const int ri = v / bt.G, row = it.r0 + ri;
       const bf16_t* src = a.q + ((size_t)row * bt.H + it.hk * bt.G + (v - ri * bt.G)) * D + 8 * g;
-      if (r < nblk)
+      if (live(r))
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
           qf[r][c] = *reinterpret_cast<const u32x4*>(src + 32 * c);
@@ -138,14 +153,12 @@ cache_attn_kernel(CacheAttnArgs args) {
       for (int i = 0; i < NB; ++i) acc[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
 
-    u32x4 kf[2][KC];
+    u32x4 kf[NI];
     uint32_t vf[8][VW];
     auto load_k = [&](const bf16_t* kp) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int c = 0; c < KC; ++c)
-          kf[h][c] = *reinterpret_cast<const u32x4*>(kp + koff + 4 * h * D + 32 * c);
+      for (int i = 0; i < NI; ++i)
+        kf[i] = *reinterpret_cast<const u32x4*>(kp + koff + i * RI * D);
     };
     auto load_v = [&](const bf16_t* vp) {
 #pragma unroll
@@ -200,23 +213,36 @@ cache_attn_kernel(CacheAttnArgs args) {
         f32x4_t s[R][2];
 #pragma unroll
         for (int r = 0; r < R; ++r)
-          if (r < nblk)
+          if (live(r))
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              s[r][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int h = 0; h < 2; ++h) s[r][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int c = 0; c < KC; ++c) s[r][h] = mfma16_bf16(kf[h][c], qf[r][c], s[r][h]);
-            }
+        for (int i = 0; i < NI; ++i)
+          *reinterpret_cast<u32x4*>(turn[wave] + key_at(RI * i + lane / CH, lane % CH)) = kf[i];
+        asm volatile("" ::: "memory");
+        // (in turn: a product does not wait for the one before it)
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          u32x4 k[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)          // (four tokens on: the same place in a row)
+            k[h] = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(
+                kread[c] + h * 8 * D);
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (live(r))
+#pragma unroll
+              for (int h = 0; h < 2; ++h) s[r][h] = mfma16_bf16(k[h], qf[r][c], s[r][h]);
+        }
         // (the next tile's keys land during the softmax and the second product, its
         // values during the next logits)
         asm volatile("" ::: "memory");
         load_k(a.cache.k + next);
         asm volatile("" ::: "memory");
-        bool apart = false;                   // values that some rows must not meet
         if (t < it.lo || t + kCTile > least) {
 #pragma unroll
           for (int r = 0; r < R; ++r)
-            if (r < nblk)
+            if (live(r))
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const int m = t + 8 * g + e;
@@ -224,8 +250,7 @@ cache_attn_kernel(CacheAttnArgs args) {
               asm volatile("" : "+v"(x));
               s[r][e >> 2][e & 3] = x;
             }
-          // values that no row sees are left out; of the others a weight of 0 must
-          // not meet an infinity or NaN
+          // values that no row sees are left out
           bool odd = false;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -239,14 +264,46 @@ cache_attn_kernel(CacheAttnArgs args) {
               odd |= bf16_odd_pair(x) != 0u;
             }
           }
-          apart = __any(odd);
+          // of the others, a weight of 0 must not meet an infinity or NaN: these are left
+          // out, too, and make NaN of the rows that see them (as one product more finds
+          // them, of ones)
+          if (__any(odd)) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              u32x4 ones;
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+                ones[w] = bf16_odd_pair(__builtin_amdgcn_perm(
+                    vf[2 * w + 1][i / 2], vf[2 * w][i / 2], i & 1 ? 0x07060302u : 0x05040100u)) &
+                    0x3f803f80u;
+#pragma unroll
+              for (int r = 0; r < R; ++r) {
+                if (!live(r)) continue;
+                u32x4 sees;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                  const int m = t + 8 * g + 2 * w;
+                  sees[w] = (m >= it.lo && m < lim[r] ? 0x3f80u : 0u) |
+                            (m + 1 >= it.lo && m + 1 < lim[r] ? 0x3f800000u : 0u);
+                }
+                const f32x4_t found = mfma16_bf16(ones, sees, f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[r][i][k] += found[k] > 0.f ? NAN : 0.f;
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+              for (int w = 0; w < VW; ++w) vf[e][w] &= ~bf16_odd_pair(vf[e][w]);
+          }
         }
         // weights 2^(sc s - reference); the reference is 8 over the largest logit that
         // moved it, so that weights are at most 1 and it is rarely moved
         u32x4 pc[R][PIECES];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          if (r >= nblk) continue;
+          if (!live(r)) continue;
           float lm = s[r][0][0];
 #pragma unroll
           for (int e = 1; e < 8; ++e) lm = fmaxf(lm, s[r][e >> 2][e & 3]);
@@ -277,43 +334,24 @@ cache_attn_kernel(CacheAttnArgs args) {
             pc[r][PIECES - 1][w] = pack2_bf16(p0, p1);
           }
         }
+        // four features' products in turn
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-          u32x4 va;
+        for (int i0 = 0; i0 < NB; i0 += 4) {
+          u32x4 va[4];
 #pragma unroll
-          for (int w = 0; w < 4; ++w)
-            va[w] = __builtin_amdgcn_perm(vf[2 * w + 1][i / 2], vf[2 * w][i / 2],
-                                          i & 1 ? 0x07060302u : 0x05040100u);
-          if (apart) {
-            // these are left out, too, and make NaN of the rows that see them (as one
-            // product more finds them, of ones)
-            u32x4 ones;
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const uint32_t bad = bf16_odd_pair(va[w]);
-              va[w] &= ~bad;
-              ones[w] = bad & 0x3f803f80u;
-            }
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-              if (r >= nblk) continue;
-              u32x4 sees;
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const int m = t + 8 * g + 2 * w;
-                sees[w] = (m >= it.lo && m < lim[r] ? 0x3f80u : 0u) |
-                          (m + 1 >= it.lo && m + 1 < lim[r] ? 0x3f800000u : 0u);
-              }
-              const f32x4_t found = mfma16_bf16(ones, sees, f32x4_t{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-              for (int k = 0; k < 4; ++k) acc[r][i][k] += found[k] > 0.f ? NAN : 0.f;
-            }
-          }
+            for (int w = 0; w < 4; ++w)
+              va[i][w] = __builtin_amdgcn_perm(vf[2 * w + 1][(i0 + i) / 2], vf[2 * w][(i0 + i) / 2],
+                                               i & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
           for (int r = 0; r < R; ++r)
-            if (r < nblk)
+            if (live(r))
 #pragma unroll
-              for (int c = 0; c < PIECES; ++c) acc[r][i] = mfma16_bf16(va, pc[r][c], acc[r][i]);
+              for (int c = 0; c < PIECES; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  acc[r][i0 + i] = mfma16_bf16(va[i], pc[r][c], acc[r][i0 + i]);
         }
         asm volatile("" ::: "memory");
         load_v(a.cache.v + next);
@@ -324,15 +362,15 @@ cache_attn_kernel(CacheAttnArgs args) {
     }
 
     // the waves' results together, and where they go
-    if (!SOLO) __syncthreads();                // (the last item's are read)
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if (r >= nblk) continue;
+      if (!live(r)) continue;
       const float l = over_groups(l_run[r], [](float x, float y) { return x + y; });
       const int col = 16 * r + n;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        float* dst = &po[wave][col][FPL * (4 * g + k)];
+        float* dst = reinterpret_cast<float*>(turn[wave]) + col * OS + FPL * (4 * g + k);
 #pragma unroll
         for (int i = 0; i < NB; i += 4)
           *reinterpret_cast<float4*>(dst + i) = make_float4(
@@ -361,7 +399,8 @@ cache_attn_kernel(CacheAttnArgs args) {
 #pragma unroll
       for (int w = w0; w < w1; ++w) {
         const float f = __builtin_amdgcn_exp2f(pm[w][col] - ref);
-        const float4 x = *reinterpret_cast<const float4*>(&po[w][col][4 * c4]);
+        const float4 x = *reinterpret_cast<const float4*>(
+            reinterpret_cast<const float*>(turn[w]) + col * OS + 4 * c4);
         o.x = fmaf(x.x, f, o.x);
         o.y = fmaf(x.y, f, o.y);
         o.z = fmaf(x.z, f, o.z);
@@ -399,6 +438,8 @@ cache_attn_kernel(CacheAttnArgs args) {
         }
       }
     }
+    if (SOLO) wait_lgkm0();
+    else if (!a.direct) __syncthreads();       // (the next item's keys take their place)
   };
 
   if constexpr (LISTED) {
@@ -424,8 +465,8 @@ cache_attn_kernel(CacheAttnArgs args) {
     };
     if (a.direct) {
       // An item a workgroup (SOLO: a wave).  Workgroup id L goes to XCD L % 8; rows of
-      // one key head stay on one, whose L2 holds the pages that they share (92 rows of
-      // 16 heads over 17 pages each: PENDING us, 43 in order).
+      // one key head stay on one, whose L2 holds the pages that they share (130
+      // rows of 16 heads over 17 pages each).
       const int x = blockIdx.x & 7;
       const int i = SOLO ? (blockIdx.x >> 3) * kCWaves + wave : blockIdx.x >> 3;
       int row, hk;

@@ -277,12 +277,87 @@ cache_score_kernel(SelectArgs a) {
   if (j0 + at < vis) a.scores[((size_t)row * a.cache.heads_kv + hk) * a.P + j0 + at] = z;
 }
 
+// The selection of one row and key head by a wave, for up to 64 K pages: lane l holds
+// pages l, 64 + l, ..  The kk-th largest key is found bit by bit from the top (the
+// largest t that kk keys reach), with ballots for the counts.
+template <int D, int K>
+__global__ void __launch_bounds__(256)
+cache_select_wave_kernel(SelectArgs a) {
+  constexpr int C = D / 8, PL = 64 / C;
+  const int lane = threadIdx.x & 63, hkv = a.cache.heads_kv;
+  const int item = 4 * blockIdx.x + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = item / hkv, hk = item - row * hkv;
+  if (row >= a.total_rows) return;
+  CacheSeq s;
+  const int b = seq_of_row(a.row_offsets, a.lens, a.B, a.total_rows, a.k_max, a.L_max, row, s);
+  if (b < 0) return;
+  const int t = s.len - s.n + row - s.r0;
+  const int vis = t < 0 ? 0 : min((t >> a.cache.shift) + 1, a.P), kk = min(a.n_sel, vis);
+  int32_t* out = a.pages + (size_t)item * a.n_sel;
+  uint64_t key[K], taken[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) taken[i] = 0ull;
+  if (vis <= a.n_sel) {                              // all of them
+#pragma unroll
+    for (int i = 0; i < K; ++i) taken[i] = __ballot(64 * i + lane < vis);
+  } else {
+    double qs[8];
+    sum_queries<D>(a, row, hk, qs);
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      key[i] = 0;
+      if (64 * i < vis) {
+        int at;
+        double z = score64<D>(a, b, hk, 64 * i, vis, qs, at);
+        z = __shfl(z, (lane % PL) * C + lane / PL, kWave);       // of page 64 i + lane
+        const int j = 64 * i + lane;
+        key[i] = j >= vis ? 0ull : j < a.n_first || j >= vis - a.n_last ? ~0ull : order_key(z);
+      }
+    }
+    uint64_t least = 0;                              // at least kk keys are not below it
+    bool exact = false;
+    for (int bit = 63; bit >= 0 && !exact; --bit) {
+      const uint64_t next = least | 1ull << bit;
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < K; ++i) n += __popcll(__ballot(key[i] >= next));
+      if (n >= kk) least = next;
+      exact = n == kk;
+    }
+    int need = kk;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      taken[i] = __ballot(exact ? key[i] >= least : key[i] > least);
+      need -= __popcll(taken[i]);
+    }
+    // (equal keys: the lowest pages)
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      const uint64_t same = __ballot(key[i] == least && 64 * i + lane < vis);
+      const bool mine = ((same >> lane) & 1) &&
+                        __popcll(same & ((1ull << lane) - 1ull)) < need;
+      const uint64_t more = exact ? 0ull : __ballot(mine);
+      taken[i] |= more;
+      need -= __popcll(more);
+    }
+  }
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    if ((taken[i] >> lane) & 1)
+      out[before + __popcll(taken[i] & ((1ull << lane) - 1ull))] = 64 * i + lane;
+    before += __popcll(taken[i]);
+  }
+  for (int i = before + lane; i < a.n_sel; i += 64) out[i] = -1;
+}
+
 // The selection of one row and key head: scores (from the launch before, or made here
 // and kept in LDS), their keys in registers, a radix select, and the chosen pages in
 // ascending order, -1 behind them.
-template <int D, int THREADS, int MAXPT, bool SCORED>
-__global__ void __launch_bounds__(THREADS)
+template <int D, int MAXPT, bool SCORED>
+__global__ void __launch_bounds__(1024)
 cache_select_kernel(SelectArgs a) {
+  constexpr int THREADS = 1024;
   __shared__ SelectShared sh;
   __shared__ uint32_t scan[THREADS / 64 + 1];
   __shared__ double zs[SCORED ? 1 : THREADS * MAXPT];
@@ -317,9 +392,7 @@ cache_select_kernel(SelectArgs a) {
       keys[i] = j < a.n_first || j >= vis - a.n_last ? ~0ull : order_key(z[j]);
   }
   const int kk = min(a.n_sel, vis);
-  SelectMask<MAXPT> flags;
-  if constexpr (THREADS == 1024) flags = block_select_top_wide<MAXPT>(keys, cnt, vis, kk, &sh);
-  else flags = block_select_top<MAXPT>(keys, cnt, vis, kk, &sh);
+  const SelectMask<MAXPT> flags = block_select_top_wide<MAXPT>(keys, cnt, vis, kk, &sh);
   uint32_t total;
   uint32_t at = block_exclusive_scan((uint32_t)__popcll((uint64_t)flags), scan, &total);
 #pragma unroll
@@ -388,13 +461,15 @@ static hipError_t launch_select(const SelectArgs& a, bool apart, hipStream_t s) 
   if (apart) {
     const dim3 g((unsigned)((a.P + 255) / 256), (unsigned)a.cache.heads_kv, (unsigned)a.total_rows);
     cache_score_kernel<D><<<g, 256, 0, s>>>(a);
-    cache_select_kernel<D, 1024, 16, true><<<grid, 1024, 0, s>>>(a);
+    cache_select_kernel<D, 16, true><<<grid, 1024, 0, s>>>(a);
   } else if (a.P <= 256) {
-    cache_select_kernel<D, 256, 1, false><<<grid, 256, 0, s>>>(a);
+    const unsigned g = (unsigned)(((long long)a.total_rows * a.cache.heads_kv + 3) / 4);
+    if (a.P <= 64) cache_select_wave_kernel<D, 1><<<dim3(g), 256, 0, s>>>(a);
+    else cache_select_wave_kernel<D, 4><<<dim3(g), 256, 0, s>>>(a);
   } else if (a.P <= 2048) {
-    cache_select_kernel<D, 1024, 2, false><<<grid, 1024, 0, s>>>(a);
+    cache_select_kernel<D, 2, false><<<grid, 1024, 0, s>>>(a);
   } else {
-    cache_select_kernel<D, 1024, 16, false><<<grid, 1024, 0, s>>>(a);
+    cache_select_kernel<D, 16, false><<<grid, 1024, 0, s>>>(a);
   }
   return hipGetLastError();
 }
