@@ -35,50 +35,67 @@ struct AppendArgs {
   int B, H, G, total_rows, k_max, L_max, half, pairs;
 };
 
-// Eight elements as floats.
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-  x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-}
-__device__ __forceinline__ void load8(const bf16_t* p, float (&x)[8]) {
-  unpack8_bf16(*reinterpret_cast<const u32x4*>(p), x);
-}
 __device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
   return u32x4{pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]),
                pack2_bf16(x[6], x[7])};
 }
 
-// Features 8 c .. + 7 of a row, rotated by the angles of its token (cosine and sine
-// of pair i at cs[i]).
+// Features 8 c .. + 7 of a row, and those that rotation joins them with.
 template <typename T>
-__device__ __forceinline__ u32x4 rotated8(const T* row, int c, int half, int pairs,
-                                          const float2* cs) {
-  float x[8];
-  load8(row + 8 * c, x);
-  if (8 * c < 2 * half) {
-    if (pairs) {
+struct Chunk {
+  typedef typename std::conditional<sizeof(T) == 2, u32x4, float4>::type Half;
+  static constexpr int N = sizeof(T) / 2;          // 16-byte words of eight elements
+  Half x[N], y[N];
+  __device__ __forceinline__ void load(const T* row, int c, int half, int pairs) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 w = cs[4 * c + e];
-        const float a = x[2 * e], b = x[2 * e + 1];
-        x[2 * e] = a * w.x - b * w.y;
-        x[2 * e + 1] = b * w.x + a * w.y;
-      }
+    for (int i = 0; i < N; ++i) x[i] = reinterpret_cast<const Half*>(row + 8 * c)[i];
+    if (!pairs && 8 * c < 2 * half) {
+      const T* other = row + (8 * c < half ? 8 * c + half : 8 * c - half);
+#pragma unroll
+      for (int i = 0; i < N; ++i) y[i] = reinterpret_cast<const Half*>(other)[i];
+    }
+  }
+  static __device__ __forceinline__ void floats(const Half (&h)[N], float (&f)[8]) {
+    if constexpr (N == 1) {
+      unpack8_bf16(h[0], f);
     } else {
-      const bool low = 8 * c < half;
-      const int i = low ? 8 * c : 8 * c - half;
-      float y[8];
-      load8(row + (low ? i + half : i), y);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float2 w = cs[i + e];
-        x[e] = x[e] * w.x + (low ? -y[e] : y[e]) * w.y;
+      for (int i = 0; i < 2; ++i) {
+        f[4 * i] = h[i].x, f[4 * i + 1] = h[i].y;
+        f[4 * i + 2] = h[i].z, f[4 * i + 3] = h[i].w;
       }
     }
   }
-  return pack8(x);
-}
+  // rotated by the angles of its token (cosine and sine of pair i at cs[i])
+  __device__ __forceinline__ u32x4 rotated(int c, int half, int pairs, const float2* cs) const {
+    float a[8];
+    floats(x, a);
+    if (8 * c < 2 * half) {
+      if (pairs) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 w = cs[4 * c + e];
+          const float p = a[2 * e], q = a[2 * e + 1];
+          a[2 * e] = p * w.x - q * w.y;
+          a[2 * e + 1] = q * w.x + p * w.y;
+        }
+      } else {
+        float b[8];
+        floats(y, b);
+        const bool low = 8 * c < half;
+        const float2* w = cs + (low ? 8 * c : 8 * c - half);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = a[e] * w[e].x + (low ? -b[e] : b[e]) * w[e].y;
+      }
+    }
+    return pack8(a);
+  }
+  __device__ __forceinline__ u32x4 rounded() const {
+    float a[8];
+    floats(x, a);
+    return pack8(a);
+  }
+};
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kAppThreads)
@@ -129,7 +146,7 @@ cache_append_kernel(AppendArgs a) {
   if (a.cache.mean && at >= 0)
     for (int t = t0 + tl; t < max(first, t0); t += TL) {
       float x[8];
-      load8(kp + (size_t)(t - t0) * D + 8 * c, x);
+      unpack8_bf16(*reinterpret_cast<const u32x4*>(kp + (size_t)(t - t0) * D + 8 * c), x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] += x[e];
     }
@@ -146,31 +163,44 @@ cache_append_kernel(AppendArgs a) {
       cs[j][f] = make_float2(cospif(2.f * frac), sinpif(2.f * frac));
     }
     __syncthreads();
-    // (rows: the key, the value, then the group's queries, of every token)
+    // a token's key and value; then the group's queries, four rows of loads in flight
     for (int j = tl; j < nt; j += TL) {
       const int t = u + j;
       const size_t r = (size_t)(row0 + t);
-      const u32x4 kx = rotated8(static_cast<const T*>(a.k) + r * a.ks + (size_t)hk * D, c, a.half,
-                                a.pairs, cs[j]);
-      float vx[8];
-      load8(static_cast<const T*>(a.v) + r * a.vs + (size_t)hk * D + 8 * c, vx);
+      Chunk<T> kx, vx;
+      kx.load(static_cast<const T*>(a.k) + r * a.ks + (size_t)hk * D, c, a.half, a.pairs);
+      vx.load(static_cast<const T*>(a.v) + r * a.vs + (size_t)hk * D, c, 0, 0);
+      const u32x4 ko = kx.rotated(c, a.half, a.pairs, cs[j]);
       if (at >= 0) {
-        *reinterpret_cast<u32x4*>(kp + (size_t)(t - t0) * D + 8 * c) = kx;
-        *reinterpret_cast<u32x4*>(vp + (size_t)(t - t0) * D + 8 * c) = pack8(vx);
+        *reinterpret_cast<u32x4*>(kp + (size_t)(t - t0) * D + 8 * c) = ko;
+        *reinterpret_cast<u32x4*>(vp + (size_t)(t - t0) * D + 8 * c) = vx.rounded();
       }
       float x[8];
-      unpack8_bf16(kx, x);
+      unpack8_bf16(ko, x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] += x[e];
     }
-    if (a.q)
-      for (int i = tl; i < nt * a.G; i += TL) {
-        const int j = i / a.G, h = hk * a.G + (i - j * a.G);
-        const size_t r = (size_t)(row0 + u + j);
-        *reinterpret_cast<u32x4*>(a.q_out + (r * a.H + h) * D + 8 * c) =
-            rotated8(static_cast<const T*>(a.q) + r * a.qs + (size_t)h * D, c, a.half, a.pairs,
-                     cs[j]);
+    if (a.q) {
+      constexpr int U = 4;
+      const int n = nt * a.G;
+      for (int i = tl; i < n; i += U * TL) {
+        Chunk<T> x[U];
+        int tok[U], h[U];
+#pragma unroll
+        for (int m = 0; m < U; ++m) {
+          const int k = min(i + m * TL, n - 1);
+          tok[m] = k / a.G;
+          h[m] = hk * a.G + (k - tok[m] * a.G);
+          x[m].load(static_cast<const T*>(a.q) + (size_t)(row0 + u + tok[m]) * a.qs +
+                        (size_t)h[m] * D, c, a.half, a.pairs);
+        }
+#pragma unroll
+        for (int m = 0; m < U; ++m)
+          if (i + m * TL < n)
+            *reinterpret_cast<u32x4*>(a.q_out + ((size_t)(row0 + u + tok[m]) * a.H + h[m]) * D +
+                                      8 * c) = x[m].rotated(c, a.half, a.pairs, cs[tok[m]]);
       }
+    }
     __syncthreads();
   }
   if (!a.cache.mean || at < 0) return;
@@ -465,7 +495,8 @@ static hipError_t launch_select(const SelectArgs& a, bool apart, hipStream_t s) 
   } else if (a.P <= 256) {
     const unsigned g = (unsigned)(((long long)a.total_rows * a.cache.heads_kv + 3) / 4);
     if (a.P <= 64) cache_select_wave_kernel<D, 1><<<dim3(g), 256, 0, s>>>(a);
-    else cache_select_wave_kernel<D, 4><<<dim3(g), 256, 0, s>>>(a);
+    else if (g >= 128) cache_select_wave_kernel<D, 4><<<dim3(g), 256, 0, s>>>(a);
+    else cache_select_kernel<D, 2, false><<<grid, 1024, 0, s>>>(a);
   } else if (a.P <= 2048) {
     cache_select_kernel<D, 2, false><<<grid, 1024, 0, s>>>(a);
   } else {
