@@ -802,27 +802,38 @@ def _raw_stream(stream, dev) -> int:
 
 
 def _cache_struct(p: SkipProblem, cache: "KvCache", dev=None) -> SkipKvCache:
-    """The cache's description: its shapes are looked at when its arrays are set, its
-    pointers at every call."""
+    """The cache's description: its arrays are looked at when they are set, their
+    pointers read at every call."""
     dev = torch.cuda.current_device() if dev is None else dev
-    k, t = cache.k, cache.page_table
-    c = cache.__dict__.get("_struct")
-    if c is None:
-        n_pages, heads_kv, page, _ = k.shape
+    known = cache.__dict__.get("_struct")
+    if known is None:
+        k, t = cache.k, cache.page_table
+        n_pages, heads_kv, page, d_h = k.shape
         if cache.v.shape != k.shape:
             raise ValueError("cache.k and cache.v must be [pages, heads_kv, page_tokens, d_h]")
         if t.dim() != 2:
             raise ValueError("cache.page_table must be [B, pages_max]")
-        c = SkipKvCache(heads_kv, page, t.shape[1], 0, n_pages)
-        cache.__dict__["_struct"] = c
-    if k.shape[3] != p.d_h:
+        n, at = n_pages * heads_kv * d_h, k.get_device()
+        for x, name, dt, m in ((k, "k", torch.bfloat16, n * page),
+                               (cache.v, "v", torch.bfloat16, n * page),
+                               (cache.mean, "mean", torch.bfloat16, n),
+                               (t, "page_table", torch.int32, t.numel())):
+            _ptr(x, "cache." + name, dt, m)
+            if x is not None and x.get_device() != at:
+                raise ValueError(f"cache.{name} is on device {x.get_device()}, cache.k on {at}")
+        known = (SkipKvCache(heads_kv, page, t.shape[1], 0, n_pages), d_h, t.shape[0], at)
+        cache.__dict__["_struct"] = known
+    c, d_h, rows, at = known
+    if d_h != p.d_h:
         raise ValueError(f"cache.k must be [pages, heads_kv, page_tokens, {p.d_h}]")
-    n = c.n_pages * c.heads_kv * p.d_h
-    bf = torch.bfloat16
-    c.k = _dptr(k, "cache.k", bf, n * c.page_tokens, dev)
-    c.v = _dptr(cache.v, "cache.v", bf, n * c.page_tokens, dev)
-    c.mean = _dptr(cache.mean, "cache.mean", bf, n, dev)
-    c.page_table = _dptr(t, "cache.page_table", torch.int32, p.B * c.pages_max, dev)
+    if rows < p.B:
+        raise ValueError(f"cache.page_table needs {p.B} rows, has {rows}")
+    if at != dev:
+        raise ValueError(f"the cache is on device {at}, the current one is {dev}")
+    c.k = cache.k.data_ptr()
+    c.v = cache.v.data_ptr()
+    c.mean = None if cache.mean is None else cache.mean.data_ptr()
+    c.page_table = cache.page_table.data_ptr()
     return c
 
 
@@ -881,7 +892,8 @@ def skip_cache_append(p: SkipProblem, cache: "KvCache", rotation, q, k, v, row_o
         _dptr(row_offsets, "row_offsets", i32, p.B + 1, dev), _dptr(lens, "lens", i32, p.B, dev),
         _dptr(positions, "positions", i32, M, dev),
         _dptr(q_out, "q_out", torch.bfloat16, M * p.d, dev), _raw_stream(stream, dev))
-    _check(st, "skip_cache_append")
+    if st:
+        raise SkipError(st, "skip_cache_append")
 
 
 def _cache_ws(p, c, workspace, n_sel, prefixes, device, stream, dev):
@@ -908,7 +920,8 @@ def skip_cache_attn(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, O, l
         _dptr(prefix_ids, "prefix_ids", i32, B, dev),
         _dptr(prefix_lens, "prefix_lens", i32, B, dev), _dptr(O, "O", _out_dtype(p), n, dev),
         _dptr(lse, "lse", torch.float32, M * p.H, dev), wp, wn, _raw_stream(stream, dev))
-    _check(st, "skip_cache_attn")
+    if st:
+        raise SkipError(st, "skip_cache_attn")
 
 
 def skip_cache_select(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, n_sel, pages,
@@ -923,7 +936,8 @@ def skip_cache_select(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, n_
         int(n_sel), int(n_first), int(n_last),
         _dptr(pages, "pages", i32, M * c.heads_kv * int(n_sel), dev), wp, wn,
         _raw_stream(stream, dev))
-    _check(st, "skip_cache_select")
+    if st:
+        raise SkipError(st, "skip_cache_select")
 
 
 def skip_cache_attn_pages(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, pages, n_sel, O,
@@ -938,7 +952,8 @@ def skip_cache_attn_pages(p: SkipProblem, cache: "KvCache", q, row_offsets, lens
         _dptr(pages, "pages", i32, M * c.heads_kv * int(n_sel), dev), int(n_sel),
         _dptr(O, "O", _out_dtype(p), n, dev), _dptr(lse, "lse", torch.float32, M * p.H, dev), wp,
         wn, _raw_stream(stream, dev))
-    _check(st, "skip_cache_attn_pages")
+    if st:
+        raise SkipError(st, "skip_cache_attn_pages")
 
 
 def skip_route_fused(p: SkipProblem, V, Qtok, q_offsets, w_bias, kept_offsets, Kh, Vh,
@@ -1434,15 +1449,17 @@ def cache_append(p: SkipProblem, cache: KvCache, q, k, v, row_offsets, lens, rot
     preallocated tensor)."""
     if out is None and q is not None:
         out = cache.k.new_empty((p.total_kept, p.H, p.d_h))
-        _record(out, stream)
+        if stream is not None:
+            _record(out, stream)
     skip_cache_append(p, cache, rotation, q, k, v, row_offsets, lens, out, positions, stream)
     return out
 
 
 def _cache_out(p, out, like, stream):
     if out is None:
-        out = (like.new_empty((p.total_kept, p.H, p.d_h), dtype=_out_dtype(p)),
-               like.new_empty((p.total_kept, p.H), dtype=torch.float32))
+        M, H = p.total_kept, p.H
+        out = (like.new_empty((M, H, p.d_h), dtype=_out_dtype(p)),
+               like.new_empty((M, H), dtype=torch.float32))
         if stream is not None:
             for t in out:
                 _record(t, stream)
@@ -1466,7 +1483,8 @@ def cache_select(p: SkipProblem, cache: KvCache, q, row_offsets, lens, n_sel: in
     heads_kv, n_sel] int32 ascending, -1 behind the last."""
     if out is None:
         out = q.new_empty((p.total_kept, cache.k.shape[1], n_sel), dtype=torch.int32)
-        _record(out, stream)
+        if stream is not None:
+            _record(out, stream)
     skip_cache_select(p, cache, q, row_offsets, lens, n_sel, out, n_first, n_last, workspace,
                       stream)
     return out

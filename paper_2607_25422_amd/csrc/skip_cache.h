@@ -78,9 +78,9 @@ constexpr int kPrefixRows = 128, kPrefixTile = 64;
 // Work is cut into equal runs of tiles, one a workgroup.  An item counts for a few
 // tiles more than it has, which stand before its first: its queries, pages and first
 // loads, and the join of its waves, take as long (short items one after the other in
-// one workgroup: 512 items of 4 tiles on average 38 us, 14 with four more).  A run that
+// one workgroup: 512 items of 4 tiles on average 38 us without, 17 with).  A run that
 // ends among them holds nothing of the item.
-constexpr int kOwnStart = 4, kPrefixStart = 2;
+constexpr int kOwnStart = 8, kPrefixStart = 4;
 // Tile of an item of nt at place u of its start + nt.
 template <int START>
 __device__ __forceinline__ int tile_at(int u, int nt) { return clampi(u - START, 0, nt); }

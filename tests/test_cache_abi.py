@@ -112,9 +112,12 @@ def test_attention(b):
         assert call(b, fn, p, c, ws=FAKE + 8) == inv
     for fn in ("attn", "pages"):
         assert call(b, fn, p, c, O=None) == inv and call(b, fn, p, c, O=FAKE + 4) == inv
-    for kw in (dict(ids=FAKE), dict(pls=FAKE), dict(ws=None)):
+    for kw in (dict(ids=FAKE), dict(pls=FAKE)):
         assert call(b, "attn", p, c, **kw) == inv, kw
-    for fn, n_sel, pre in (("attn", 0, 0), ("attn", 0, 1), ("select", 90, 0), ("pages", 90, 0)):
+    long = problem(b, L_max=64 * 2000)                       # (scores in a launch of their own)
+    wide = cache(b, pages_max=2000)
+    for fn, n_sel, pre, p, c in (("attn", 0, 0, p, c), ("attn", 0, 1, p, c),
+                                 ("pages", 90, 0, p, c), ("select", 9, 0, long, wide)):
         need = ctypes.c_size_t(0)
         assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), n_sel, pre,
                                                 ctypes.byref(need)) == b.SKIP_OK
@@ -125,6 +128,8 @@ def test_attention(b):
         if fn != "select":
             assert call(b, fn, p, c, nb=need.value - 1, **kw) == b.SKIP_ERR_WORKSPACE
         assert call(b, fn, p, c, nb=7, **kw) == b.SKIP_ERR_WORKSPACE
+        assert call(b, fn, p, c, ws=None, **kw) == inv
+    p, c = problem(b, L_max=6000), cache(b, pages_max=100)
     # sequences that a workgroup takes whole need none
     assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(problem(b)), ctypes.byref(c), 0, 1,
                                             ctypes.byref(need)) == b.SKIP_OK and need.value == 0
@@ -162,13 +167,20 @@ def test_binding_checks(b):
         build(kv, kv[:3], None, t)
     with pytest.raises(ValueError, match="pages_max"):
         build(kv, kv, None, t[0])
-    with pytest.raises(ValueError, match="64"):
-        build(kv[..., :32], kv[..., :32], None, t)
     with pytest.raises(ValueError, match="device"):
         build(kv, kv, None, t)
-    # a cache whose arrays are set anew is looked at anew
+    # known arrays: the problem's sizes and the device are compared at every call
     c = b.KvCache(kv, kv, None, t)
-    c.__dict__["_struct"] = "of the old arrays"
+    known = (b.SkipKvCache(4, 64, 8, 0, 20), 64, 2, 0)
+    c.__dict__["_struct"] = known
+    assert b._cache_struct(p, c, 0).k == kv.data_ptr()
+    with pytest.raises(ValueError, match="device 0"):
+        b._cache_struct(p, c, 1)
+    with pytest.raises(ValueError, match="128"):
+        b._cache_struct(problem(b, d=2048, d_h=128), c, 0)
+    with pytest.raises(ValueError, match="3 rows"):
+        b._cache_struct(problem(b, B=3, kept_offsets=[0, 1, 2, 3]), c, 0)
+    # arrays that are set anew are looked at anew
     c.page_table = t[0]
     with pytest.raises(ValueError, match="pages_max"):
         b._cache_struct(p, c, 0)
