@@ -585,16 +585,20 @@ CachePlan cache_plan(const skip_problem_t& p, const skip_kv_cache_t& c, int n_se
   const int G = p.H / c.heads_kv;
   if (n_sel > 0) {
     // many short items: a wave each
-    const int nt = n_sel * (c.page_tokens / kCTile), items = p.total_kept * c.heads_kv;
+    const int pages = std::min(n_sel, (p.L_max + c.page_tokens - 1) / c.page_tokens);
+    const int nt = pages * (c.page_tokens / kCTile), items = p.total_kept * c.heads_kv;
     x.R = G <= 16 ? 1 : 2;
     x.direct = nt <= 16 || items >= 512;
     x.solo = x.direct && items >= 1024 && nt <= 64;
     const int side = x.solo ? kCWaves : 1;
     x.runs = !x.direct ? 512 : 8 * (((items + 7) / 8 + side - 1) / side);
   } else {
-    // sequences of up to 512 tokens: an item a workgroup, prefixes with them
+    // sequences of up to 512 tokens: an item a workgroup, prefixes with them.  Prefixes
+    // of their own take a launch more: where all sequences' keys and values are 64 MB
+    // or more (9 sequences of 600 tokens, one key head: 29 us with it, 13 without)
     x.direct = p.L_max <= 512;
-    x.prefixes = prefixes && !x.direct;
+    x.prefixes = prefixes && !x.direct &&
+                 4ll * p.B * c.heads_kv * p.L_max * p.d_h >= (64ll << 20);
     x.R = p.k_max * G <= 16 ? 1 : 2;
     const int cols = 16 * x.R;
     x.runs = x.direct ? p.B * c.heads_kv * ((p.k_max * G + cols - 1) / cols) : 512;

@@ -30,7 +30,10 @@ constexpr int kTWaves = 4;
 constexpr int kTThreads = 64 * kTWaves;
 constexpr int kTRows = 32 * kTWaves;       // virtual rows of an item
 constexpr int kTTile = 64;                 // tokens of a tile
-constexpr int kTLeast = 4;                 // tiles of a share or run, at least
+constexpr int kTLeast = 4;                 // tiles of a run, at least
+// Tokens of a sequence that a workgroup takes whole, rather than in runs with a join
+// (480 rows of 481 tokens, 32 heads over 8: 31 us in runs, 17 whole).
+constexpr int kTShort = 768;
 static_assert(kTRows == kPrefixRows && kTTile == kPrefixTile, "items of prefixes");
 constexpr float kTOver = 8.f;
 template <bool OUT_F32> constexpr int kTPieces = OUT_F32 ? 3 : 2;
@@ -528,7 +531,7 @@ TallPlan tall_plan(const skip_problem_t& p, const skip_kv_cache_t& c) {
   // item); about half a row tile of a sequence's is empty.
   const long long items = c.heads_kv * std::min<long long>(
       (long long)p.B * x.row_tiles, p.total_kept * G / kTRows + (p.B + 1) / 2);
-  if (items < 2048 && x.row_tiles <= 64) {
+  if (items < 2048 && x.row_tiles <= 64 && p.L_max > kTShort) {
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
     x.runs = p.d_h == 64 ? 768 : 512;
     x.cols = (int)std::min<long long>(kTRows, (p.k_max * G + 31) / 32 * 32);

@@ -97,45 +97,96 @@ struct Chunk {
   }
 };
 
-template <typename T, int D>
+// A page that new tokens go to: tokens t0 .. end - 1 of it are held, from `first` on new.
+struct AppendPage {
+  int t0, first, end, row0;                        // row0: the row of token 0
+  int at;                                          // the physical page, or -1
+  // The slot-th such page of the batch (every wave the same): prefix sums of the pages
+  // that each sequence's new tokens go to.
+  __device__ __forceinline__ bool find(const AppendArgs& a, int slot) {
+    const int lane = threadIdx.x & 63, shift = a.cache.shift;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      int pages = 0;
+      CacheSeq s{0, 0, 0};
+      if (b0 + lane < a.B) {
+        s.load(a.row_offsets, a.lens, b0 + lane, a.total_rows, a.k_max, a.L_max);
+        if (s.n > 0 && s.len > 0)
+          pages = ((s.len - 1) >> shift) - (max(s.len - s.n, 0) >> shift) + 1;
+      }
+      const int incl = (int)wave_incl_scan((uint32_t)pages);
+      const int total = __builtin_amdgcn_readlane(incl, 63);
+      if (slot < total) {
+        const int l = __popcll(__ballot(incl <= slot));
+        const int r0 = __builtin_amdgcn_readlane(s.r0, l), n = __builtin_amdgcn_readlane(s.n, l);
+        const int len = __builtin_amdgcn_readlane(s.len, l);
+        const int pg = (max(len - n, 0) >> shift) + slot -
+                       __builtin_amdgcn_readlane(incl - pages, l);
+        t0 = pg << shift;
+        first = max(len - n, t0);
+        end = min(len, t0 + (1 << shift));
+        row0 = r0 + n - len;
+        at = a.cache.page(b0 + l, pg);
+        return true;
+      }
+      slot -= total;
+    }
+    return false;
+  }
+};
+
+// The mean of a page's keys from the sums that TL threads a chunk hold.
+template <int D, int TL>
+__device__ __forceinline__ void store_mean(const AppendArgs& a, const AppendPage& p, int hk,
+                                           const float (&sum)[8], float (*sums)[D]) {
+  const int tid = threadIdx.x, c = tid % (D / 8), tl = tid / (D / 8);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[tl][8 * c + e] = sum[e];
+  __syncthreads();
+  if (tid >= D / 2) return;
+  float x = 0.f, y = 0.f;
+  for (int i = 0; i < TL; ++i) {
+    x += sums[i][2 * tid];
+    y += sums[i][2 * tid + 1];
+  }
+  const float inv = 1.f / (float)(p.end - p.t0);
+  reinterpret_cast<uint32_t*>(a.cache.mean + ((size_t)(uint32_t)p.at * a.cache.heads_kv + hk) *
+                                                 D)[tid] = pack2_bf16(x * inv, y * inv);
+}
+// Sums of the keys of tokens t0 .. t1 - 1 as the page holds them.
+template <int D, int TL>
+__device__ __forceinline__ void sum_keys(const bf16_t* kp, int t0, int t1, float (&sum)[8]) {
+  const int c = threadIdx.x % (D / 8), tl = threadIdx.x / (D / 8);
+#pragma unroll 4
+  for (int t = t0 + tl; t < t1; t += TL) {
+    float x[8];
+    unpack8_bf16(*reinterpret_cast<const u32x4*>(kp + (size_t)(t - t0) * D + 8 * c), x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += x[e];
+  }
+}
+
+// PIECES: a workgroup takes 32 tokens of the page and four of the group's queries, and
+// the mean is left to a launch of its own.
+constexpr int kAppHeads = 4;
+template <typename T, int D, bool PIECES>
 __global__ void __launch_bounds__(kAppThreads)
 cache_append_kernel(AppendArgs a) {
   constexpr int C = D / 8;                         // 16-byte chunks of a row
   constexpr int TL = kAppThreads / C;              // tokens side by side
   __shared__ float2 cs[kAppTokens][kAppMaxHalf];
-  __shared__ float sums[TL][D];
-  const int tid = threadIdx.x, lane = tid & 63, hk = blockIdx.y;
-  const int shift = a.cache.shift, page = 1 << shift;
-
-  // the sequence and page of this slot (every wave the same): prefix sums of the
-  // pages that each sequence's new tokens go to
-  int b = -1, pg = 0, slot = blockIdx.x;
-  CacheSeq q{0, 0, 0};
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    int pages = 0;
-    CacheSeq s{0, 0, 0};
-    if (b0 + lane < a.B) {
-      s.load(a.row_offsets, a.lens, b0 + lane, a.total_rows, a.k_max, a.L_max);
-      if (s.n > 0 && s.len > 0)
-        pages = ((s.len - 1) >> shift) - (max(s.len - s.n, 0) >> shift) + 1;
-    }
-    const int incl = (int)wave_incl_scan((uint32_t)pages);
-    const int total = __builtin_amdgcn_readlane(incl, 63);
-    if (slot < total) {
-      const int l = __popcll(__ballot(incl <= slot));
-      b = b0 + l;
-      q = CacheSeq{__builtin_amdgcn_readlane(s.r0, l), __builtin_amdgcn_readlane(s.n, l),
-                   __builtin_amdgcn_readlane(s.len, l)};
-      pg = (max(q.len - q.n, 0) >> shift) +
-           slot - __builtin_amdgcn_readlane(incl - pages, l);
-      break;
-    }
-    slot -= total;
+  __shared__ float sums[PIECES ? 1 : TL][D];
+  const int tid = threadIdx.x, hk = blockIdx.y, shift = a.cache.shift;
+  AppendPage p;
+  const int pieces = PIECES ? 1 << (shift - 5) : 1;
+  if (!p.find(a, blockIdx.x / pieces)) return;
+  const int t0 = p.t0, row0 = p.row0, at = p.at;
+  int first = p.first, end = p.end;
+  if (PIECES) {
+    const int u = t0 + kAppTokens * (blockIdx.x % pieces);
+    first = max(first, u);
+    end = min(end, u + kAppTokens);
+    if (first >= end) return;
   }
-  if (b < 0) return;
-  const int t0 = pg << shift, first = max(q.len - q.n, t0), end = min(q.len, t0 + page);
-  const int row0 = q.r0 + q.n - q.len;             // row of token 0
-  const int at = a.cache.page(b, pg);
   const size_t base = a.cache.base<D>(max(at, 0), hk);
   bf16_t* const kp = a.cache.k + base;
   bf16_t* const vp = a.cache.v + base;
@@ -143,13 +194,7 @@ cache_append_kernel(AppendArgs a) {
 
   // keys that were there
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (a.cache.mean && at >= 0)
-    for (int t = t0 + tl; t < max(first, t0); t += TL) {
-      float x[8];
-      unpack8_bf16(*reinterpret_cast<const u32x4*>(kp + (size_t)(t - t0) * D + 8 * c), x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += x[e];
-    }
+  if (!PIECES && a.cache.mean && at >= 0) sum_keys<D, TL>(kp, t0, first, sum);
 
   for (int u = max(first, 0); u < end; u += kAppTokens) {
     const int nt = min(end - u, kAppTokens);
@@ -164,7 +209,7 @@ cache_append_kernel(AppendArgs a) {
     }
     __syncthreads();
     // a token's key and value; then the group's queries, four rows of loads in flight
-    for (int j = tl; j < nt; j += TL) {
+    for (int j = PIECES && blockIdx.z > 0 ? nt : tl; j < nt; j += TL) {
       const int t = u + j;
       const size_t r = (size_t)(row0 + t);
       Chunk<T> kx, vx;
@@ -182,15 +227,16 @@ cache_append_kernel(AppendArgs a) {
     }
     if (a.q) {
       constexpr int U = 4;
-      const int n = nt * a.G;
+      const int h0 = PIECES ? kAppHeads * blockIdx.z : 0;
+      const int heads = PIECES ? min(a.G - h0, kAppHeads) : a.G, n = nt * heads;
       for (int i = tl; i < n; i += U * TL) {
         Chunk<T> x[U];
         int tok[U], h[U];
 #pragma unroll
         for (int m = 0; m < U; ++m) {
           const int k = min(i + m * TL, n - 1);
-          tok[m] = k / a.G;
-          h[m] = hk * a.G + (k - tok[m] * a.G);
+          tok[m] = k / heads;
+          h[m] = hk * a.G + h0 + (k - tok[m] * heads);
           x[m].load(static_cast<const T*>(a.q) + (size_t)(row0 + u + tok[m]) * a.qs +
                         (size_t)h[m] * D, c, a.half, a.pairs);
         }
@@ -203,20 +249,20 @@ cache_append_kernel(AppendArgs a) {
     }
     __syncthreads();
   }
-  if (!a.cache.mean || at < 0) return;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) sums[tl][8 * c + e] = sum[e];
-  __syncthreads();
-  if (tid < D / 2) {
-    float x = 0.f, y = 0.f;
-    for (int i = 0; i < TL; ++i) {
-      x += sums[i][2 * tid];
-      y += sums[i][2 * tid + 1];
-    }
-    const float inv = 1.f / (float)(end - t0);
-    reinterpret_cast<uint32_t*>(a.cache.mean + ((size_t)(uint32_t)at * a.cache.heads_kv + hk) *
-                                                   D)[tid] = pack2_bf16(x * inv, y * inv);
-  }
+  if constexpr (!PIECES)
+    if (a.cache.mean && at >= 0) store_mean<D, TL>(a, p, hk, sum, sums);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kAppThreads)
+cache_mean_kernel(AppendArgs a) {
+  constexpr int TL = kAppThreads / (D / 8);
+  __shared__ float sums[TL][D];
+  AppendPage p;
+  if (!p.find(a, blockIdx.x) || p.at < 0) return;
+  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  sum_keys<D, TL>(a.cache.k + a.cache.base<D>(p.at, blockIdx.y), p.t0, p.end, sum);
+  store_mean<D, TL>(a, p, blockIdx.y, sum, sums);
 }
 
 // ---------------------------------------------------------------------------
@@ -442,6 +488,22 @@ CacheView cache_view(const skip_kv_cache_t& c) {
                    c.pages_max, shift};
 }
 
+template <typename T, int D>
+static hipError_t launch_append(const AppendArgs& a, long long slots, bool pieces, hipStream_t s) {
+  const unsigned n = (unsigned)slots, hk = (unsigned)a.cache.heads_kv;
+  if (!pieces) {
+    cache_append_kernel<T, D, false><<<dim3(n, hk), kAppThreads, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  const unsigned z = a.q ? (unsigned)((a.G + kAppHeads - 1) / kAppHeads) : 1u;
+  cache_append_kernel<T, D, true>
+      <<<dim3(n << (a.cache.shift - 5), hk, z), kAppThreads, 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.cache.mean) return e;
+  cache_mean_kernel<D><<<dim3(n, hk), kAppThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
 hipError_t launch_cache_append(const skip_problem_t& p, const skip_kv_cache_t& c,
                                const skip_rotation_t* rot, const void* q, int64_t qs,
                                const void* k, int64_t ks, const void* v, int64_t vs,
@@ -453,15 +515,16 @@ hipError_t launch_cache_append(const skip_problem_t& p, const skip_kv_cache_t& c
   // n tokens of a sequence go to at most n pages, and to n / page + 2
   const long long slots = std::min<long long>(p.total_kept,
                                               p.total_kept / c.page_tokens + 2ll * p.B);
-  const dim3 grid((unsigned)slots, (unsigned)c.heads_kv);
-  if (p.dtype == SKIP_F32) {
-    if (p.d_h == 64) cache_append_kernel<float, 64><<<grid, kAppThreads, 0, s>>>(a);
-    else cache_append_kernel<float, 128><<<grid, kAppThreads, 0, s>>>(a);
-  } else {
-    if (p.d_h == 64) cache_append_kernel<bf16_t, 64><<<grid, kAppThreads, 0, s>>>(a);
-    else cache_append_kernel<bf16_t, 128><<<grid, kAppThreads, 0, s>>>(a);
-  }
-  return hipGetLastError();
+  // Where many tokens make few such pages, 32 tokens and four heads a workgroup and the
+  // means after them (6 prompts of 78 to 210 tokens, 16 heads over one, pages of 256: 70 us
+  // by page, 13.6 so).
+  const bool pieces = p.k_max > kAppTokens && c.page_tokens > kAppTokens &&
+                      slots * c.heads_kv < 512;
+  if (p.dtype == SKIP_F32)
+    return p.d_h == 64 ? launch_append<float, 64>(a, slots, pieces, s)
+                       : launch_append<float, 128>(a, slots, pieces, s);
+  return p.d_h == 64 ? launch_append<bf16_t, 64>(a, slots, pieces, s)
+                     : launch_append<bf16_t, 128>(a, slots, pieces, s);
 }
 
 static int select_pages(const skip_problem_t& p, const skip_kv_cache_t& c) {
