@@ -148,6 +148,7 @@ APPEND = [
     dict(seqs=[(9, 20), (1, 64)], dims=0),
     dict(seqs=[(2, 50), (7, 90)], mean=False, q=False),
     dict(seqs=[(40, 100), (3, 3)], extra_rows=11),
+    dict(seqs=[(50, 80), (34, 40), (0, 3), (1, 64)], H=9, hk=1, page=64, dims=32, dtype="f32"),
 ]
 
 
@@ -270,6 +271,9 @@ ATTN = [
     dict(seqs=[(1, 700), (3, 90)], extra_rows=9),
     dict(seqs=[(200, 200), (300, 777), (129, 1500)], H=8, hk=2, D=128, page=64),
     dict(seqs=[(257, 257), (0, 50), (64, 64), (1, 900)], H=3, hk=1, D=64, o_f32=True),
+    dict(seqs=[(257, 300), (130, 700), (1, 64)], H=3, hk=1, D=128, page=256),     # taken whole
+    dict(seqs=[(40, 41)] * 90, H=32, hk=32, D=64, page=32),                       # 90 items a head
+    dict(seqs=[(9, 2000), (5, 1000)], H=16, hk=2, D=128, page=32, extra_rows=5, o_f32=True),
 ]
 
 
@@ -292,21 +296,28 @@ def test_attention(B, case):
     assert lse2 is None and torch.equal(O2[:M], out[0][:M])
 
 
+# (sequences whose keys and values are 64 MB or more, where prefixes are items of their
+# own, and one batch of fewer)
 SHARED = [
+    dict(seqs=[(1, 2140), (1, 2800), (1, 2101), (1, 2333), (1, 2102), (1, 2164)],
+         shared=[(0, i, 2100) for i in range(1, 6)], ids=[0] * 6, P=[2100] * 6, H=16, hk=8, D=128),
+    dict(seqs=[(2, 2900), (1, 2145), (4, 2200), (1, 40), (1, 2300), (0, 2250)],
+         shared=[(0, 1, 2113), (3, 4, 32), (3, 5, 32)], ids=[5, 5, -1, 2, 2, 2],
+         P=[2113, 2113, 2113, 32, 32, 32], H=16, hk=8, D=128, page=64),
+    # new tokens inside the prefix, a prefix that some sequences have not reached
+    dict(seqs=[(12, 5590), (10, 5585), (3, 5100)], shared=[(0, 1, 5580), (0, 2, 5100)], ids=[1] * 3,
+         P=[5580] * 3, H=16, hk=8, D=128, page=256, o_f32=True),
+    # a run across blocks of 64 sequences and of 128 virtual rows, alone ones between
+    dict(seqs=[(1, 1320 + i % 9) for i in range(100)],
+         shared=[(0, i, 1310) for i in range(1, 70)] + [(72, i, 1280) for i in range(73, 100)],
+         ids=[0] * 70 + [1, 3] + [2] * 28, P=[1310] * 70 + [1310, 1310] + [1280] * 28, H=8, hk=2),
+    # ids equal, lengths not: not shared
+    dict(seqs=[(1, 8300), (1, 8200)], ids=[0, 0], P=[64, 96], shared=[], H=8, hk=8, D=128),
+    # 16 query heads a key head, two tokens: two blocks of 16; float32 output
+    dict(seqs=[(2, 8500 + 300 * i) for i in range(9)], shared=[(0, i, 8400) for i in range(1, 9)],
+         ids=[7] * 9, P=[8400] * 9, H=48, hk=3, D=64, page=128, o_f32=True, extra_rows=2),
     dict(seqs=[(1, 640), (1, 700), (1, 601)], shared=[(0, 1, 600), (0, 2, 600)], ids=[0, 0, 0],
          P=[600, 600, 600]),
-    dict(seqs=[(2, 900), (1, 545), (4, 600), (1, 40), (1, 700), (0, 650)],
-         shared=[(0, 1, 513), (2, 4, 0)], ids=[5, 5, -1, 2, 2, 2], P=[513, 513, 513, 32, 32, 32],
-         H=16, hk=2, D=128, page=64, extra=[(3, 4, 32), (3, 5, 32)]),
-    # new tokens inside the prefix, a prefix that some sequences have not reached
-    dict(seqs=[(50, 620), (40, 610), (3, 605)], shared=[(0, 1, 600), (0, 2, 600)], ids=[1] * 3,
-         P=[600] * 3, H=4, hk=2, o_f32=True),
-    # a run across blocks of 64 sequences, alone ones between
-    dict(seqs=[(1, 530 + i % 9) for i in range(100)],
-         shared=[(0, i, 520) for i in range(1, 70)] + [(72, i, 500) for i in range(73, 100)],
-         ids=[0] * 70 + [1, 3] + [2] * 28, P=[520] * 70 + [520, 520] + [500] * 28, H=4, hk=2),
-    # ids equal, lengths not: not shared
-    dict(seqs=[(1, 640), (1, 700)], ids=[0, 0], P=[64, 96], shared=[]),
 ]
 
 
@@ -314,9 +325,10 @@ SHARED = [
 def test_shared_prefixes(B, case):
     c = dict(SHARED[case])
     ids, P = c.pop("ids"), c.pop("P")
-    c["shared"] = c["shared"] + c.pop("extra", [])
     s = Setup(B, seed=200 + case, **c)
-    say("[shared]", case, c)
+    say("[shared]", case)
+    whole = 4 * len(ids) * s.hk * int(s.lens.max()) * s.D
+    assert (whole >= 64 << 20) == (case != len(SHARED) - 1)
     got = attn(s, B, prefix_ids=dev(ids), prefix_lens=dev(P))
     torch.cuda.synchronize()
     ref = s.reference()
