@@ -713,7 +713,8 @@ skip_status_t skip_workspace_bytes_cache(const skip_problem_t* p, const skip_kv_
  *                speed alone where that is so; results may differ in their last bits
  *   prefix_lens  [B] int32
  *   O, lse       out [total_kept][H][d_h], [total_kept][H] float or NULL
- *   workspace    skip_workspace_bytes_cache bytes (0: it may be NULL)
+ *   workspace    skip_workspace_bytes_cache bytes (0: it may be NULL; 0 wherever L_max
+ *                is at most 512)
  * Calls of 2^31 blocks of 32 tokens and 16 rows and heads or more are refused
  * (SKIP_ERR_UNSUPPORTED).
  */

@@ -900,6 +900,8 @@ def _cache_ws(p, c, workspace, n_sel, prefixes, device, stream, dev):
     """(tensor to keep, pointer, bytes) of a call's workspace: the caller's, or a fresh
     one where the call needs one."""
     if workspace is None:
+        if not n_sel and p.L_max <= 512:          # (skip_cache_attn needs none)
+            return None, None, 0
         need = _cache_bytes(p, c, n_sel, prefixes)
         if not need:
             return None, None, 0
@@ -1458,7 +1460,9 @@ def cache_append(p: SkipProblem, cache: KvCache, q, k, v, row_offsets, lens, rot
 def _cache_out(p, out, like, stream):
     if out is None:
         M, H = p.total_kept, p.H
-        out = (like.new_empty((M, H, p.d_h), dtype=_out_dtype(p)),
+        out = (torch.empty_like(like) if not p.o_f32 and like.shape == (M, H, p.d_h)
+               and like.dtype is torch.bfloat16 and like.is_contiguous()
+               else like.new_empty((M, H, p.d_h), dtype=_out_dtype(p)),
                like.new_empty((M, H), dtype=torch.float32))
         if stream is not None:
             for t in out:

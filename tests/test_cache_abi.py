@@ -130,9 +130,14 @@ def test_attention(b):
         assert call(b, fn, p, c, nb=7, **kw) == b.SKIP_ERR_WORKSPACE
         assert call(b, fn, p, c, ws=None, **kw) == inv
     p, c = problem(b, L_max=6000), cache(b, pages_max=100)
-    # sequences that a workgroup takes whole need none
-    assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(problem(b)), ctypes.byref(c), 0, 1,
-                                            ctypes.byref(need)) == b.SKIP_OK and need.value == 0
+    # up to 512 tokens a sequence: none, whatever the rows
+    for pre in (0, 1):
+        for H, d_h, n in ((16, 64, 1), (16, 64, 9), (32, 128, 500), (64, 64, 2000), (12, 64, 3)):
+            short = problem(b, B=70, H=H, d=H * d_h, d_h=d_h, L_max=512,
+                            kept_offsets=[0] + list(range(n, 70 + n)))
+            assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(short), ctypes.byref(c), 0, pre,
+                                                    ctypes.byref(need)) == b.SKIP_OK
+            assert need.value == 0
     assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), 0, 0, None) == inv
     assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), -1, 0,
                                             ctypes.byref(need)) == inv
