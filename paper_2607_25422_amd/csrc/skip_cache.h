@@ -236,10 +236,6 @@ inline CacheBatch cache_batch(const skip_problem_t& p, const skip_kv_cache_t& c,
   return CacheBatch{row_offsets, lens, prefix_ids, prefix_lens, p.B, p.H, p.H / c.heads_kv,
                     c.heads_kv, p.total_kept, p.k_max, p.L_max};
 }
-// The items of shared prefixes, their results left for the join.
-constexpr int kPrefixRuns = 512;
-hipError_t launch_cache_prefixes(const CacheBatch& batch, const CacheView& cache,
-                                 const CacheResults& res, const bf16_t* q, int d_h, int o_f32,
-                                 float scale_log2, hipStream_t s);
+constexpr int kPrefixRuns = 512;            // workgroups of a call with shared prefixes
 
 }  // namespace skip
