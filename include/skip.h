@@ -709,8 +709,9 @@ skip_status_t skip_workspace_bytes_cache(const skip_problem_t* p, const skip_kv_
  *   prefix_ids   [B] int32, or NULL (then prefix_lens is): consecutive sequences
  *                with the same id >= 0 and the same prefix_lens hold the same keys
  *                and values in their first prefix_lens tokens, which are read once for
- *                all of them (through the table row of one of them).  A hint on
- *                speed alone where that is so; results may differ in their last bits
+ *                all of them (through the table row of one that has rows; a sequence
+ *                of fewer tokens than that reads its own).  A hint on speed alone
+ *                where that is so; results may differ in their last bits
  *   prefix_lens  [B] int32
  *   O, lse       out [total_kept][H][d_h], [total_kept][H] float or NULL
  *   workspace    skip_workspace_bytes_cache bytes (0: it may be NULL; 0 wherever L_max

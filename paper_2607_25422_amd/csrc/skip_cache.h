@@ -89,6 +89,7 @@ __device__ __forceinline__ int tile_at(int u, int nt) { return clampi(u - START,
 struct SeqBlock {
   CacheSeq s;
   int P, first, run_rows;           // shared prefix; its run's first lane and rows
+  int source;                       // the run's first lane with rows, whose pages are read
   int pre, own;                     // tiles (with their starts) of the prefix's items (of the run's first
                                     // lane) and of the sequence's own
   __device__ __forceinline__ static int row_tiles(const CacheBatch& a, int rows, int cols) {
@@ -122,10 +123,12 @@ struct SeqBlock {
       if (a.prefix_ids) {
         id = a.prefix_ids[b];
         pl = clampi(a.prefix_lens[b], 0, a.L_max);
+        if (s.n > 0 && s.len < pl) id = -1;            // (does not hold the prefix)
       }
     }
     P = 0;
     first = lane;
+    source = lane;
     run_rows = 0;
     pre = 0;
     if (a.prefix_ids) {
@@ -138,6 +141,8 @@ struct SeqBlock {
       const int last = after ? __builtin_ctzll(after) - 1 : 63;    // of the run
       // (every lane takes part in the exchange)
       const int rows = __shfl(s.r0 + s.n, last, kWave) - __shfl(s.r0, first, kWave);
+      // (a sequence that is passed over may have no pages left)
+      source = __builtin_ctzll((__ballot(s.n > 0) & (~0ull << first)) | 1ull << 63);
       if (last > first) {
         P = pl;
         run_rows = rows;

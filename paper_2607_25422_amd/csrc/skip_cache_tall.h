@@ -489,6 +489,7 @@ __device__ __forceinline__ void cache_tall_work(const TallArgs& a, TallShared<D>
       it.r0 = walk.of_lane(walk.sb.s.r0, L);
       int rows, rt, start;
       if constexpr (PREFIX) {
+        it.b = walk.sb0 + walk.of_lane(walk.sb.source, L);
         it.hi = walk.of_lane(walk.sb.P, L);
         it.nt = SeqBlock::prefix_tiles(it.hi);
         rows = walk.of_lane(walk.sb.run_rows, L);

@@ -336,6 +336,19 @@ def test_shared_prefixes(B, case):
     s.check(attn(s, B), ref, c.get("o_f32", False))
 
 
+def test_prefixes_of_sequences_that_are_passed_over(B):
+    """A run's sequences without rows, its first one among them, need no pages; one that
+    has fewer tokens than the prefix reads its own."""
+    ids, P = [4] * 8, [2100] * 8
+    s = Setup(B, [(0, 0), (1, 2140), (0, 0), (2, 2800), (1, 2101), (1, 900), (1, 2333), (0, 0)],
+              shared=[(1, i, 2100) for i in (3, 4, 6)], H=16, hk=8, D=128, seed=211)
+    say("[passed over]")
+    assert (s.table[[0, 2, 7]] == -1).all() and 4 * 8 * 8 * 2800 * 128 >= 64 << 20
+    got = attn(s, B, prefix_ids=dev(ids), prefix_lens=dev(P))
+    torch.cuda.synchronize()
+    s.check(got, s.reference(), False)
+
+
 @pytest.mark.parametrize("o_f32", [False, True])
 @pytest.mark.parametrize("n,ln", [(40, 40), (7, 600), (200, 200), (40, 700)])
 def test_what_a_row_does_not_see_does_not_reach_it(B, n, ln, o_f32):
