@@ -382,7 +382,7 @@ __device__ __forceinline__ void cache_tall_work(const TallArgs& a, TallShared<D>
 
   if (it.i0 < it.i1) {
     load_pages();
-    if constexpr (OF != kTallItems) barrier_nofence();   // (the last item's tiles are read)
+    if constexpr (OF != kTallItems) barrier_lds();       // (the last item's tiles are read)
 #pragma unroll
     for (uint32_t j = 0; j + 1 < kBuffers; ++j)
       if (it.i0 + (int)j < it.i1) fetch(it.i0 + j, j * kBuffer);
@@ -393,7 +393,7 @@ __device__ __forceinline__ void cache_tall_work(const TallArgs& a, TallShared<D>
     constexpr int ahead = kBuffers - 2;
     if (i + ahead < it.i1) wait_vmcnt<ahead * 2 * NI>();
     else wait_vmcnt<0>();
-    barrier_nofence();
+    barrier_lds();
     const int miss = (missing >> (2 * (buffer / kBuffer))) & 3;
     if (i + (int)kBuffers - 1 < it.i1)
       fetch(i + kBuffers - 1, (buffer + (kBuffers - 1) * kBuffer) % (kBuffers * kBuffer));
