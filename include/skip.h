@@ -642,7 +642,8 @@ skip_status_t skip_gather_dense(const skip_problem_t* p, const void* rows,
  * Slots behind a sequence's last token, and tokens that a row does not see, may
  * hold anything, infinities and NaN among it; of a value that it sees and that is not
  * finite, infinity or NaN comes out.  Errors as for all entry points; d_h
- * 64 or 128, else SKIP_ERR_UNSUPPORTED.
+ * 64 or 128, at most 65535 key heads, and no more rows or sequences than a launch holds
+ * (2^24 workgroups; 2^27 rows and heads), else SKIP_ERR_UNSUPPORTED.
  */
 typedef struct skip_kv_cache {
   int32_t heads_kv;
@@ -713,10 +714,10 @@ skip_status_t skip_workspace_bytes_cache(const skip_problem_t* p, const skip_kv_
  *                of fewer tokens than that reads its own).  A hint on speed alone
  *                where that is so; results may differ in their last bits
  *   prefix_lens  [B] int32
- *   O, lse       out [total_kept][H][d_h], [total_kept][H] float or NULL
+ *   O, lse       out [total_kept][H][d_h], [total_kept][H] float or NULL; apart from q
  *   workspace    skip_workspace_bytes_cache bytes (0: it may be NULL; 0 wherever L_max
  *                is at most 512)
- * Calls of 2^31 blocks of 32 tokens and 16 rows and heads or more are refused
+ * Calls of more than 2^30 blocks of 32 tokens and 16 rows and heads are refused
  * (SKIP_ERR_UNSUPPORTED).
  */
 skip_status_t skip_cache_attn(const skip_problem_t* p, const skip_kv_cache_t* cache, const void* q,

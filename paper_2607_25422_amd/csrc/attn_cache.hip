@@ -92,13 +92,16 @@ hipError_t launch_rows(const CacheAttnArgs& a, const CachePlan& x, hipStream_t s
 
 }  // namespace
 
+// Tiles are counted in 32 bits (with the workgroups' shares rounded up), and a grid has
+// fewer than 2^32 threads.
 bool cache_attn_fits(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel) {
   const long long G = p.H / c.heads_kv, hkv = c.heads_kv, rows = p.total_kept;
   const long long items = n_sel > 0 ? rows * hkv : (rows * G / 16 + 2ll * p.B) * hkv;
   const long long tiles = kOwnStart + (n_sel > 0 ? (long long)n_sel * (c.page_tokens / kCTile)
                                                  : p.L_max / kCTile + 2);
-  return items <= INT32_MAX / tiles && rows * p.H < (1ll << 31) &&
-         (long long)p.B * hkv * ((p.k_max * G + 15) / 16) < (1ll << 31);
+  const long long cols = n_sel == 0 && cache_tall(p, c) ? kPrefixRows : 16;
+  return items <= (1ll << 30) / tiles && rows * ((p.H + 7) / 8) < kMaxGrid &&
+         (n_sel > 0 ? items : p.B * hkv * ((p.k_max * G + cols - 1) / cols)) < kMaxGrid;
 }
 
 size_t cache_attn_scratch(const skip_problem_t& p, const skip_kv_cache_t& c, int n_sel,

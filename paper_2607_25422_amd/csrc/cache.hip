@@ -504,6 +504,15 @@ static hipError_t launch_append(const AppendArgs& a, long long slots, bool piece
   return hipGetLastError();
 }
 
+// n tokens of a sequence go to at most n pages, and to n / page + 2
+static long long append_slots(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  return std::min<long long>(p.total_kept, p.total_kept / c.page_tokens + 2ll * p.B);
+}
+
+bool cache_append_fits(const skip_problem_t& p, const skip_kv_cache_t& c) {
+  return append_slots(p, c) < kMaxGrid;
+}
+
 hipError_t launch_cache_append(const skip_problem_t& p, const skip_kv_cache_t& c,
                                const skip_rotation_t* rot, const void* q, int64_t qs,
                                const void* k, int64_t ks, const void* v, int64_t vs,
@@ -512,9 +521,7 @@ hipError_t launch_cache_append(const skip_problem_t& p, const skip_kv_cache_t& c
   AppendArgs a{cache_view(c), q, k, v, qs, ks, vs, rot ? rot->freq : nullptr, row_offsets, lens,
                positions, static_cast<bf16_t*>(q_out), p.B, p.H, p.H / c.heads_kv, p.total_kept,
                p.k_max, p.L_max, rot ? rot->dims / 2 : 0, rot ? rot->pairs : 0};
-  // n tokens of a sequence go to at most n pages, and to n / page + 2
-  const long long slots = std::min<long long>(p.total_kept,
-                                              p.total_kept / c.page_tokens + 2ll * p.B);
+  const long long slots = append_slots(p, c);
   // Where many tokens make few such pages, 32 tokens and four heads a workgroup and the
   // means after them (6 prompts of 78 to 210 tokens, 16 heads over one, pages of 256: 70 us
   // by page, 13.6 so).
@@ -532,7 +539,8 @@ static int select_pages(const skip_problem_t& p, const skip_kv_cache_t& c) {
 }
 
 bool cache_select_fits(const skip_problem_t& p, const skip_kv_cache_t& c) {
-  return select_pages(p, c) <= 16384 && p.total_kept <= 65535;
+  return select_pages(p, c) <= 16384 && p.total_kept <= 65535 &&
+         (long long)p.total_kept * c.heads_kv < 4 * kMaxGrid;
 }
 
 // Whether scores are made by a launch of their own, which takes more workgroups for

@@ -741,7 +741,7 @@ static skip_status_t check_cache(const skip_problem_t* p, const skip_kv_cache_t*
   if (p->H < 1 || p->d_h < 1 || (int64_t)p->H * p->d_h != p->d) return SKIP_ERR_INVALID_ARG;
   if (p->d_h != 64 && p->d_h != 128) return SKIP_ERR_UNSUPPORTED;
   if (c->heads_kv < 1 || p->H % c->heads_kv != 0) return SKIP_ERR_INVALID_ARG;
-  if (p->H / c->heads_kv > 32) return SKIP_ERR_UNSUPPORTED;
+  if (p->H / c->heads_kv > 32 || c->heads_kv > 65535) return SKIP_ERR_UNSUPPORTED;
   if (c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128 &&
       c->page_tokens != 256)
     return SKIP_ERR_UNSUPPORTED;
@@ -778,6 +778,7 @@ skip_status_t skip_cache_append(const skip_problem_t* p, const skip_kv_cache_t* 
   if (k_stride < kv || v_stride < kv || k_stride % 8 != 0 || v_stride % 8 != 0)
     return SKIP_ERR_INVALID_ARG;
   if (q && (q_stride < p->d || q_stride % 8 != 0)) return SKIP_ERR_INVALID_ARG;
+  if (!cache_append_fits(*p, *cache)) return SKIP_ERR_UNSUPPORTED;
   SKIP_TRY(launch_cache_append(*p, *cache, rotation, q, q_stride, k, k_stride, v, v_stride,
                                row_offsets, lens, positions, q_out,
                                static_cast<hipStream_t>(stream)));

@@ -241,6 +241,7 @@ inline CacheBatch cache_batch(const skip_problem_t& p, const skip_kv_cache_t& c,
   return CacheBatch{row_offsets, lens, prefix_ids, prefix_lens, p.B, p.H, p.H / c.heads_kv,
                     c.heads_kv, p.total_kept, p.k_max, p.L_max};
 }
+constexpr long long kMaxGrid = 1ll << 24;   // workgroups of up to 256 threads in a row
 constexpr int kPrefixRuns = 512;            // workgroups of a call with shared prefixes
 
 }  // namespace skip

@@ -194,6 +194,7 @@ hipError_t launch_attention_quant(const skip_problem_t& p, const skip_kv_store_t
                                   float* lse, void* scratch, hipStream_t s);
 
 // Paged cache -----------------------------------------------------------------
+bool cache_append_fits(const skip_problem_t& p, const skip_kv_cache_t& c);
 hipError_t launch_cache_append(const skip_problem_t& p, const skip_kv_cache_t& c,
                                const skip_rotation_t* rot, const void* q, int64_t q_stride,
                                const void* k, int64_t k_stride, const void* v, int64_t v_stride,

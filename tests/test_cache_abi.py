@@ -141,9 +141,36 @@ def test_attention(b):
     assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), 0, 0, None) == inv
     assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), -1, 0,
                                             ctypes.byref(need)) == inv
-    # 2^31 blocks of work
+    # more than 2^30 blocks of work
     wide = problem(b, B=4096, kept_offsets=list(range(4097)), L_max=1 << 30)
     assert call(b, "attn", wide, cache(b, pages_max=1 << 30)) == uns
+
+
+def test_more_than_a_launch_holds(b):
+    uns = b.SKIP_ERR_UNSUPPORTED
+
+    def big(B, rows, k_max, **kw):
+        p = problem(b, **kw)
+        p.B, p.total_kept, p.k_max = B, rows, k_max
+        return p
+    one = cache(b, heads_kv=1)
+    kw = dict(H=1, d=64, d_h=64)
+    strides = dict(qs=64, ks=64, vs=64)
+    for B, rows, k_max in ((1 << 24, 1 << 24, 1), (1 << 23, 1 << 30, 1 << 8)):
+        p = big(B, rows, k_max, L_max=500, **kw)
+        assert call(b, "append", p, one, **strides) == uns, (B, rows)
+        assert call(b, "attn", p, one) == uns, (B, rows)
+        assert call(b, "pages", p, one) == uns, (B, rows)
+    many = cache(b, heads_kv=65536)
+    p = problem(b, H=65536, d=65536 * 64, d_h=64)
+    for fn in ALL:
+        assert call(b, fn, p, many, qs=p.d, ks=p.d, vs=p.d) == uns, fn
+    wide = cache(b, heads_kv=16384)
+    p = problem(b, H=16384, d=16384 * 64, d_h=64, B=1, kept_offsets=[0, 4096])
+    assert call(b, "select", p, wide) == uns
+    # the tiles of all blocks just past what is counted
+    p = big(1, 1 << 20, 1 << 20, L_max=32 * 16384, **kw)
+    assert call(b, "attn", p, cache(b, heads_kv=1, pages_max=8192)) == uns
 
 
 def test_selection(b):
