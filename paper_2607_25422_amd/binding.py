@@ -802,38 +802,37 @@ def _raw_stream(stream, dev) -> int:
 
 
 def _cache_struct(p: SkipProblem, cache: "KvCache", dev=None) -> SkipKvCache:
-    """The cache's description: its arrays are looked at when they are set, their
-    pointers read at every call."""
+    """The cache's description.  Its arrays are looked at again where one of them lies
+    elsewhere than when they last were."""
     dev = torch.cuda.current_device() if dev is None else dev
+    mean = cache.mean
+    at = (cache.k.data_ptr(), cache.v.data_ptr(), None if mean is None else mean.data_ptr(),
+          cache.page_table.data_ptr())
     known = cache.__dict__.get("_struct")
-    if known is None:
+    if known is None or known[4] != at:
         k, t = cache.k, cache.page_table
-        n_pages, heads_kv, page, d_h = k.shape
-        if cache.v.shape != k.shape:
+        if k.dim() != 4 or cache.v.shape != k.shape:
             raise ValueError("cache.k and cache.v must be [pages, heads_kv, page_tokens, d_h]")
         if t.dim() != 2:
             raise ValueError("cache.page_table must be [B, pages_max]")
-        n, at = n_pages * heads_kv * d_h, k.get_device()
+        n_pages, heads_kv, page, d_h = k.shape
+        n, on = n_pages * heads_kv * d_h, k.get_device()
         for x, name, dt, m in ((k, "k", torch.bfloat16, n * page),
                                (cache.v, "v", torch.bfloat16, n * page),
-                               (cache.mean, "mean", torch.bfloat16, n),
+                               (mean, "mean", torch.bfloat16, n),
                                (t, "page_table", torch.int32, t.numel())):
             _ptr(x, "cache." + name, dt, m)
-            if x is not None and x.get_device() != at:
-                raise ValueError(f"cache.{name} is on device {x.get_device()}, cache.k on {at}")
-        known = (SkipKvCache(heads_kv, page, t.shape[1], 0, n_pages), d_h, t.shape[0], at)
+            if x is not None and x.get_device() != on:
+                raise ValueError(f"cache.{name} is on device {x.get_device()}, cache.k on {on}")
+        known = (SkipKvCache(heads_kv, page, t.shape[1], 0, n_pages, *at), d_h, t.shape[0], on, at)
         cache.__dict__["_struct"] = known
-    c, d_h, rows, at = known
+    c, d_h, rows, on, _ = known
     if d_h != p.d_h:
         raise ValueError(f"cache.k must be [pages, heads_kv, page_tokens, {p.d_h}]")
     if rows < p.B:
         raise ValueError(f"cache.page_table needs {p.B} rows, has {rows}")
-    if at != dev:
-        raise ValueError(f"the cache is on device {at}, the current one is {dev}")
-    c.k = cache.k.data_ptr()
-    c.v = cache.v.data_ptr()
-    c.mean = None if cache.mean is None else cache.mean.data_ptr()
-    c.page_table = cache.page_table.data_ptr()
+    if on != dev:
+        raise ValueError(f"the cache is on device {on}, the current one is {dev}")
     return c
 
 

@@ -203,8 +203,8 @@ def test_binding_checks(b):
         build(kv, kv, None, t)
     # known arrays: the problem's sizes and the device are compared at every call
     c = b.KvCache(kv, kv, None, t)
-    known = (b.SkipKvCache(4, 64, 8, 0, 20), 64, 2, 0)
-    c.__dict__["_struct"] = known
+    at = (kv.data_ptr(), kv.data_ptr(), None, t.data_ptr())
+    c.__dict__["_struct"] = known = (b.SkipKvCache(4, 64, 8, 0, 20, *at), 64, 2, 0, at)
     assert b._cache_struct(p, c, 0).k == kv.data_ptr()
     with pytest.raises(ValueError, match="device 0"):
         b._cache_struct(p, c, 1)
@@ -214,6 +214,13 @@ def test_binding_checks(b):
         b._cache_struct(problem(b, B=3, kept_offsets=[0, 1, 2, 3]), c, 0)
     # arrays that are set anew are looked at anew
     c.page_table = t[0]
+    with pytest.raises(ValueError, match="pages_max"):
+        b._cache_struct(p, c, 0)
+    # and so are those that were given other memory in place
+    c = b.KvCache(kv, kv, None, t.clone())
+    c.__dict__["_struct"] = known[:4] + (at[:3] + (c.page_table.data_ptr(),),)
+    assert b._cache_struct(p, c, 0) is known[0]
+    c.page_table.set_(torch.zeros(16, dtype=torch.int32))
     with pytest.raises(ValueError, match="pages_max"):
         b._cache_struct(p, c, 0)
 
