@@ -8,11 +8,11 @@
 // A (row, query head of the group) pair is one virtual row: virtual row v of a set of
 // rows is its row v / G and query head v % G, and all of them meet the same keys.  An
 // item is up to 16 R virtual rows of one key head and one range of tokens:
-//   - the tokens of a sequence behind its shared prefix, for its rows;
-//   - a prefix, for the rows of all sequences of a run that shares it;
+//   - the tokens of a sequence behind its shared prefix, for its rows (the prefix, for
+//     the rows of all sequences of a run that shares it, is skip_cache_tall.h's work);
 //   - the listed pages of one row.
 // Its tokens are taken in tiles of 32 (a page holds a multiple of that), and a
-// wave computes a tile alone, with no LDS and no barrier:
+// wave computes a tile alone, with no barrier:
 //   S^T (32 tokens x 16 R rows) = K . Q^T,  O^T (D x 16 R) += V^T . P^T
 // (v_mfma_f32_16x16x32_bf16).  Lane l is n = l % 16, g = l / 16.  Which token a row
 // of the first product stands for is free: row r of product a is token
@@ -28,6 +28,13 @@
 // An item that a run does not hold whole leaves partial results (O, reference, sum),
 // which a second kernel joins in the order of the tokens, so that the result does
 // not depend on which workgroup was faster.  (More of the split beside kOwnStart.)
+//
+// The memory bounds it: a tile's keys and values are read once, for whatever rows
+// there are, and its loads are in flight during the tile before it.  48 sequences of 300
+// to 16384 tokens, 32 heads of 128 over 8: 160 us for 899 MB, 5.6 TB/s, and 5.6 for the
+// join.  32 rows of 32 pages of 64 tokens each, the same heads: 54 us for 268 MB, 5.0
+// TB/s, and 4.7.  (Loads of two tiles in flight: 196 us against 169; more runs, 768 to
+// 4096: 165 to 179 against 162.)
 #pragma once
 
 #include "skip_cache.h"

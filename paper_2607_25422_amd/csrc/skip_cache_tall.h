@@ -3,8 +3,9 @@
 //
 // An item is 128 virtual rows of one sequence (or of the sequences that share a prefix)
 // and key head, over the tokens that its last row sees (or the prefix).  A workgroup
-// takes one, or an equal run of all items' tiles: its four waves hold 32 virtual rows each and share tiles of 64 tokens in LDS, which direct loads
-// fill a tile (d_h 64: two) ahead.  Per tile and wave,
+// takes one, or an equal run of all items' tiles: its four waves hold 32 virtual rows each
+// and share tiles of 64 tokens in LDS, which direct loads fill a tile (d_h 64: two)
+// ahead.  Per tile and wave,
 //   S^T (64 tokens x 32 rows) = K . Q^T,  O^T (D x 32) += V^T . P^T
 // (v_mfma_f32_32x32x16_bf16).  Lane l is n = l % 32, hh = l / 32.  Element i of the
 // first product's half h is token 32 h + 8 (i / 4) + 4 hh + i % 4 of row n, and stays
@@ -17,6 +18,13 @@
 // token: chunk c of token r lies at c ^ (r % 16) (keys: eight lanes of a 16-byte read
 // are eight tokens) and at c ^ 2 (r % 8) (values: 16 lanes of a transposing read are
 // four tokens of 32 bytes).  The direct loads take chunks in that order.
+//
+// Matrix and vector instructions bound it together: four prompts of 1024 to 4096
+// tokens, 32 heads of 128 over 8, take 348 us, 680 TFLOP/s (1020 with the second piece of
+// the weights); the matrix units are busy for 48 % of the SIMDs' cycles, vector
+// instructions are issued in 45 % of them, two waves a SIMD.  Four prefixes of 8217
+// tokens for 16 sequences each, with their own 1 to 500 tokens behind them in one launch:
+// 51 us.  Six pieces of 97 to 131 rows over 3900 tokens, 16 heads of 64, float output: 40.
 #pragma once
 
 #include "skip_cache.h"
