@@ -91,7 +91,7 @@ struct SeqBlock {
   int P, first, run_rows;           // shared prefix; its run's first lane and rows
   int source;                       // the run's first lane with rows, whose pages are read
   int pre, own;                     // tiles (with their starts) of the prefix's items (of the run's first
-                                    // lane) and of the sequence's own
+                                    // lane) and of the sequence's own (TALL: of one key head)
   __device__ __forceinline__ static int row_tiles(const CacheBatch& a, int rows, int cols) {
     return (rows * a.G + cols - 1) / cols;
   }
@@ -152,8 +152,7 @@ struct SeqBlock {
       }
     }
     if (TALL) {
-      own = s.n > 0 ? a.heads_kv *
-                      tall_before(a, s.n, s.len, row_tiles(a, s.n, kPrefixRows)) : 0;
+      own = s.n > 0 ? tall_before(a, s.n, s.len, row_tiles(a, s.n, kPrefixRows)) : 0;
       return;
     }
     own = s.n > 0 ? a.heads_kv * row_tiles(a, s.n, cols) *
@@ -204,7 +203,8 @@ struct SeqWalk {
 };
 
 // What the kernels of one call leave for the join, in the workspace: kCacheMeta ints
-// a sequence, then the tiles of a run of own items and of prefix items.
+// a sequence, then the tiles of a run of own items, and of prefix items (or the tiles of
+// a key head, where items go by key heads).
 constexpr int kCacheMeta = 8;
 struct CacheResults {
   int32_t* meta;

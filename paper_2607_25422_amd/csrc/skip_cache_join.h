@@ -78,10 +78,10 @@ cache_join_kernel(JoinArgs a) {
     first = (row * hkv + hk) * (nt + kOwnStart) + kOwnStart;
     col = g;
   } else if constexpr (OWN == kJoinTall) {
-    const int4 x = reinterpret_cast<const int4*>(a.res.meta + (size_t)b * kCacheMeta)[0];
     const int v = (row - s.r0) * bt.G + g, rt = v / kPrefixRows;
     nt = SeqBlock::tall_tiles(bt, s.n, s.len, rt);
-    first = x.x + hk * x.y + SeqBlock::tall_before(bt, s.n, s.len, rt) + kPrefixStart;
+    first = hk * pers[1] + a.res.meta[(size_t)b * kCacheMeta] +
+            SeqBlock::tall_before(bt, s.n, s.len, rt) + kPrefixStart;
     col = v % kPrefixRows;
   } else {
     const int4 x = reinterpret_cast<const int4*>(a.res.meta + (size_t)b * kCacheMeta)[0];

@@ -477,22 +477,32 @@ __device__ __forceinline__ void cache_tall_work(const TallArgs& a, TallShared<D>
     TallItem it;
     if (tall_item(a, block, it)) work(it);
   } else {
-    const int W = walk.total(bt, [&](int before) {
+    // (sequences by key heads: those that share pages, a prompt's pieces over one context,
+    // meet on one XCD, whose L2 they are in)
+    const int Wh = walk.total(bt, [&](int before) {
       if (PREFIX || block != 0 || wave != 0 || walk.sb0 + lane >= bt.B) return;
-      int32_t* w = a.res.meta + (size_t)(walk.sb0 + lane) * kCacheMeta;
-      *reinterpret_cast<int2*>(w) = make_int2(before + walk.incl - walk.sb.own,
-                                              walk.sb.own / bt.heads_kv);
+      a.res.meta[(size_t)(walk.sb0 + lane) * kCacheMeta] = before + walk.incl - walk.sb.own;
     });
+    const int W = PREFIX ? Wh : Wh * bt.heads_kv;
     const int per = max((W + a.runs - 1) / a.runs, kTLeast);
-    if (block == 0 && tid == 0)
-      a.res.meta[(size_t)bt.B * kCacheMeta + (PREFIX ? 1 : 0)] = per;
+    if (block == 0 && tid == 0) {
+      int32_t* w = a.res.meta + (size_t)bt.B * kCacheMeta;
+      if (!PREFIX) w[0] = per;
+      w[1] = PREFIX ? per : Wh;
+    }
     int u = run * per;
     if (u >= W) return;
     const int end = min(W - u, per) + u;
     while (u < end) {
       int first;
-      const int L = walk.seek(bt, u, first);
       TallItem it;
+      const int at = PREFIX ? 0 : u / Wh * Wh;           // the key head's first tile
+      if (!PREFIX && u - at < walk.base) {
+        walk.base = 0;
+        walk.block(bt, 0);
+      }
+      const int L = walk.seek(bt, u - at, first);
+      first += at;
       it.b = walk.sb0 + L;
       it.r0 = walk.of_lane(walk.sb.s.r0, L);
       int rows, rt, start;
@@ -509,9 +519,8 @@ __device__ __forceinline__ void cache_tall_work(const TallArgs& a, TallShared<D>
       } else {
         it.s = CacheSeq{it.r0, walk.of_lane(walk.sb.s.n, L), walk.of_lane(walk.sb.s.len, L)};
         rows = it.s.n;
-        const int head = walk.of_lane(walk.sb.own, L) / bt.heads_kv;     // tiles of a key head
-        it.hk = (u - first) / head;
-        start = first + it.hk * head;
+        it.hk = u / Wh;
+        start = first;
         for (rt = 0;; ++rt) {
           it.nt = SeqBlock::tall_tiles(bt, it.s.n, it.s.len, rt);
           if (u < start + it.nt + kPrefixStart) break;
