@@ -21,10 +21,11 @@
 //
 // Matrix and vector instructions bound it together: four prompts of 1024 to 4096
 // tokens, 32 heads of 128 over 8, take 348 us, 680 TFLOP/s (1020 with the second piece of
-// the weights); the matrix units are busy for 48 % of the SIMDs' cycles, vector
+// the weights); the matrix units are busy for 49 % of the SIMDs' cycles, vector
 // instructions are issued in 45 % of them, two waves a SIMD.  Four prefixes of 8217
 // tokens for 16 sequences each, with their own 1 to 500 tokens behind them in one launch:
-// 51 us.  Six pieces of 97 to 131 rows over 3900 tokens, 16 heads of 64, float output: 40.
+// 51 us.  Six pieces of 97 to 131 rows over 3900 tokens, 16 heads of 64, float output:
+// 37 (40 with sequences' heads in the order of their memory, see below).
 #pragma once
 
 #include "skip_cache.h"
