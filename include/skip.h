@@ -732,6 +732,7 @@ skip_status_t skip_cache_attn(const skip_problem_t* p, const skip_kv_cache_t* ca
  * (double sums of the bf16 values; ties: the lower page), the n_first first and the
  * n_last last always among them (the last page, whose mean may take in tokens behind
  * t, so needs no score).  Fewer pages: all of them.  A page without a physical one scores 0.
+ *   workspace  as for attention (0, and NULL, wherever L_max is at most 1024 pages)
  *   n_sel    1 .. 1024;  n_first >= 0, n_last >= 1, n_first + n_last <= n_sel
  *   pages    out [total_kept][heads_kv][n_sel] int32 ascending, -1 behind the last
  * cache->mean is required.  At most 65535 rows and 16384 pages a sequence
@@ -746,7 +747,8 @@ skip_status_t skip_cache_select(const skip_problem_t* p, const skip_kv_cache_t* 
  * skip_cache_attn over listed pages: the row of token t and key head h attends to
  * the tokens <= t of the pages that pages[row][h][0 .. n_sel - 1] names (places in
  * the sequence's row of page_table, in any order; entries outside the pages that t
- * sees are passed over; a page named twice counts twice).
+ * sees are passed over; a page named twice counts twice).  No workspace is needed
+ * wherever n_sel pages hold at most 512 tokens.
  */
 skip_status_t skip_cache_attn_pages(const skip_problem_t* p, const skip_kv_cache_t* cache,
                                     const void* q, const int32_t* row_offsets,

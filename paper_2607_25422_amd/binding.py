@@ -783,13 +783,14 @@ def skip_gather_dense(p: SkipProblem, rows, kept_offsets, rows_idx, packed, d_ou
     _check(st, "skip_gather_dense")
 
 
-def _dptr(t, name, dtype, numel, dev) -> Optional[int]:
+def _dptr(t, name, dtype, numel, dev, made=False) -> Optional[int]:
     """``_ptr`` of a tensor that has to be on device ``dev`` (one test where all is
-    well: 0.2 us; None and what is refused go the long way)."""
+    well: 0.3 us; what is refused goes the long way).  ``made``: it was allocated for the
+    call, like one that was looked at."""
     if t is None:
         return None
     ptr = t.data_ptr()
-    if (t.dtype is dtype and ptr and not ptr & 15 and t.get_device() == dev
+    if made or (t.dtype is dtype and ptr and not ptr & 15 and t.get_device() == dev
             and t.numel() >= numel and t.is_contiguous()):
         return ptr
     ptr = _ptr(t, name, dtype, numel)
@@ -803,14 +804,14 @@ def _raw_stream(stream, dev) -> int:
 
 def _cache_struct(p: SkipProblem, cache: "KvCache", dev=None) -> SkipKvCache:
     """The cache's description.  Its arrays are looked at again where one of them lies
-    elsewhere than when they last were."""
+    elsewhere than when they last were, or holds more or fewer."""
     dev = torch.cuda.current_device() if dev is None else dev
-    mean = cache.mean
-    at = (cache.k.data_ptr(), cache.v.data_ptr(), None if mean is None else mean.data_ptr(),
-          cache.page_table.data_ptr())
+    k, t, mean = cache.k, cache.page_table, cache.mean
+    at = (k.data_ptr(), cache.v.data_ptr(), None if mean is None else mean.data_ptr(),
+          t.data_ptr())
+    size = (k.numel(), t.numel())
     known = cache.__dict__.get("_struct")
-    if known is None or known[4] != at:
-        k, t = cache.k, cache.page_table
+    if known is None or known[4] != at or known[5] != size:
         if k.dim() != 4 or cache.v.shape != k.shape:
             raise ValueError("cache.k and cache.v must be [pages, heads_kv, page_tokens, d_h]")
         if t.dim() != 2:
@@ -824,9 +825,10 @@ def _cache_struct(p: SkipProblem, cache: "KvCache", dev=None) -> SkipKvCache:
             _ptr(x, "cache." + name, dt, m)
             if x is not None and x.get_device() != on:
                 raise ValueError(f"cache.{name} is on device {x.get_device()}, cache.k on {on}")
-        known = (SkipKvCache(heads_kv, page, t.shape[1], 0, n_pages, *at), d_h, t.shape[0], on, at)
+        known = (SkipKvCache(heads_kv, page, t.shape[1], 0, n_pages, *at), d_h, t.shape[0], on, at,
+                 size)
         cache.__dict__["_struct"] = known
-    c, d_h, rows, on, _ = known
+    c, d_h, rows, on = known[:4]
     if d_h != p.d_h:
         raise ValueError(f"cache.k must be [pages, heads_kv, page_tokens, {p.d_h}]")
     if rows < p.B:
@@ -834,6 +836,18 @@ def _cache_struct(p: SkipProblem, cache: "KvCache", dev=None) -> SkipKvCache:
     if on != dev:
         raise ValueError(f"the cache is on device {on}, the current one is {dev}")
     return c
+
+
+def _rotation_struct(rotation: "Rotation", dev) -> SkipRotation:
+    """The rotation's description, made again where its frequencies or style are others."""
+    f = rotation.freq
+    key = (f.data_ptr(), f.numel(), rotation.style, dev)
+    known = rotation.__dict__.get("_struct")
+    if known is None or known[0] != key:
+        known = key, SkipRotation(_dptr(f, "rotation.freq", torch.float32, 1, dev), 2 * f.numel(),
+                                  ROTATIONS[rotation.style])
+        rotation.__dict__["_struct"] = known
+    return known[1]
 
 
 def _row_strided(t: torch.Tensor, name: str, dtype, rows: int, heads: int, d_h: int, dev: int):
@@ -870,15 +884,11 @@ def _cache_bytes(p, c, n_sel, prefixes) -> int:
 
 
 def skip_cache_append(p: SkipProblem, cache: "KvCache", rotation, q, k, v, row_offsets, lens,
-                      q_out, positions=None, stream=None):
+                      q_out, positions=None, stream=None, _made=False):
     et, i32 = _elem_dtype(p), torch.int32
     dev = torch.cuda.current_device()
     c = _cache_struct(p, cache, dev)
-    rot = None
-    if rotation is not None:
-        f = rotation.freq
-        rot = ctypes.byref(SkipRotation(_dptr(f, "rotation.freq", torch.float32, 1, dev),
-                                        2 * f.numel(), ROTATIONS[rotation.style]))
+    rot = None if rotation is None else ctypes.byref(_rotation_struct(rotation, dev))
     M, D = p.total_kept, p.d_h
     qp = kp = vp_ = (None, 0)
     if M:
@@ -889,17 +899,17 @@ def skip_cache_append(p: SkipProblem, cache: "KvCache", rotation, q, k, v, row_o
     st = LIB.skip_cache_append(
         ctypes.byref(p), ctypes.byref(c), rot, *qp, *kp, *vp_,
         _dptr(row_offsets, "row_offsets", i32, p.B + 1, dev), _dptr(lens, "lens", i32, p.B, dev),
-        _dptr(positions, "positions", i32, M, dev),
-        _dptr(q_out, "q_out", torch.bfloat16, M * p.d, dev), _raw_stream(stream, dev))
+        None if positions is None else _dptr(positions, "positions", i32, M, dev),
+        _dptr(q_out, "q_out", torch.bfloat16, M * p.d, dev, _made), _raw_stream(stream, dev))
     if st:
         raise SkipError(st, "skip_cache_append")
 
 
-def _cache_ws(p, c, workspace, n_sel, prefixes, device, stream, dev):
+def _cache_ws(p, c, workspace, n_sel, prefixes, none, device, stream, dev):
     """(tensor to keep, pointer, bytes) of a call's workspace: the caller's, or a fresh
-    one where the call needs one."""
+    one where the call needs one (``none``: the sizes say already that it does not)."""
     if workspace is None:
-        if not n_sel and p.L_max <= 512:          # (skip_cache_attn needs none)
+        if none:
             return None, None, 0
         need = _cache_bytes(p, c, n_sel, prefixes)
         if not need:
@@ -910,49 +920,52 @@ def _cache_ws(p, c, workspace, n_sel, prefixes, device, stream, dev):
 
 
 def skip_cache_attn(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, O, lse=None,
-                    prefix_ids=None, prefix_lens=None, workspace=None, stream=None):
+                    prefix_ids=None, prefix_lens=None, workspace=None, stream=None, _made=False):
     dev, i32 = torch.cuda.current_device(), torch.int32
     c = _cache_struct(p, cache, dev)
     B, M, n = p.B, p.total_kept, p.total_kept * p.d
-    ws, wp, wn = _cache_ws(p, c, workspace, 0, prefix_ids is not None, q.device, stream, dev)
+    ws, wp, wn = _cache_ws(p, c, workspace, 0, prefix_ids is not None, p.L_max <= 512, q.device,
+                           stream, dev)
     st = LIB.skip_cache_attn(
         ctypes.byref(p), ctypes.byref(c), _dptr(q, "q", torch.bfloat16, n, dev),
         _dptr(row_offsets, "row_offsets", i32, B + 1, dev), _dptr(lens, "lens", i32, B, dev),
         _dptr(prefix_ids, "prefix_ids", i32, B, dev),
-        _dptr(prefix_lens, "prefix_lens", i32, B, dev), _dptr(O, "O", _out_dtype(p), n, dev),
-        _dptr(lse, "lse", torch.float32, M * p.H, dev), wp, wn, _raw_stream(stream, dev))
+        _dptr(prefix_lens, "prefix_lens", i32, B, dev), _dptr(O, "O", _out_dtype(p), n, dev, _made),
+        _dptr(lse, "lse", torch.float32, M * p.H, dev, _made), wp, wn, _raw_stream(stream, dev))
     if st:
         raise SkipError(st, "skip_cache_attn")
 
 
 def skip_cache_select(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, n_sel, pages,
-                      n_first=1, n_last=1, workspace=None, stream=None):
+                      n_first=1, n_last=1, workspace=None, stream=None, _made=False):
     dev, i32 = torch.cuda.current_device(), torch.int32
     c = _cache_struct(p, cache, dev)
     B, M = p.B, p.total_kept
-    ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, q.device, stream, dev)
+    ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, p.L_max <= 1024 * c.page_tokens,
+                           q.device, stream, dev)
     st = LIB.skip_cache_select(
         ctypes.byref(p), ctypes.byref(c), _dptr(q, "q", torch.bfloat16, M * p.d, dev),
         _dptr(row_offsets, "row_offsets", i32, B + 1, dev), _dptr(lens, "lens", i32, B, dev),
         int(n_sel), int(n_first), int(n_last),
-        _dptr(pages, "pages", i32, M * c.heads_kv * int(n_sel), dev), wp, wn,
+        _dptr(pages, "pages", i32, M * c.heads_kv * int(n_sel), dev, _made), wp, wn,
         _raw_stream(stream, dev))
     if st:
         raise SkipError(st, "skip_cache_select")
 
 
 def skip_cache_attn_pages(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, pages, n_sel, O,
-                          lse=None, workspace=None, stream=None):
+                          lse=None, workspace=None, stream=None, _made=False):
     dev, i32 = torch.cuda.current_device(), torch.int32
     c = _cache_struct(p, cache, dev)
     B, M, n = p.B, p.total_kept, p.total_kept * p.d
-    ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, q.device, stream, dev)
+    ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, n_sel * c.page_tokens <= 512, q.device,
+                           stream, dev)
     st = LIB.skip_cache_attn_pages(
         ctypes.byref(p), ctypes.byref(c), _dptr(q, "q", torch.bfloat16, n, dev),
         _dptr(row_offsets, "row_offsets", i32, B + 1, dev), _dptr(lens, "lens", i32, B, dev),
         _dptr(pages, "pages", i32, M * c.heads_kv * int(n_sel), dev), int(n_sel),
-        _dptr(O, "O", _out_dtype(p), n, dev), _dptr(lse, "lse", torch.float32, M * p.H, dev), wp,
-        wn, _raw_stream(stream, dev))
+        _dptr(O, "O", _out_dtype(p), n, dev, _made),
+        _dptr(lse, "lse", torch.float32, M * p.H, dev, _made), wp, wn, _raw_stream(stream, dev))
     if st:
         raise SkipError(st, "skip_cache_attn_pages")
 
@@ -1432,6 +1445,10 @@ class Rotation:
     freq: torch.Tensor
     style: str = "halves"
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_struct", None)        # (see _rotation_struct)
+
 
 def new_kv_cache(n_pages: int, heads_kv: int, page_tokens: int, d_h: int, page_table,
                  mean: bool = True, device="cuda") -> KvCache:
@@ -1448,35 +1465,39 @@ def cache_append(p: SkipProblem, cache: KvCache, q, k, v, row_offsets, lens, rot
     [total_kept, heads_kv, d_h] in the problem's element type, rows at any stride
     of a multiple of 8 elements.  Returns the rotated queries, bf16 (``out``: a
     preallocated tensor)."""
-    if out is None and q is not None:
-        out = cache.k.new_empty((p.total_kept, p.H, p.d_h))
+    made = out is None and q is not None
+    if made:
+        # (the fastest of torch's ways to one)
+        out = (torch.empty_like(q) if q.dtype is torch.bfloat16 and q.is_contiguous()
+               and q.shape == (p.total_kept, p.H, p.d_h)
+               else cache.k.new_empty((p.total_kept, p.H, p.d_h)))
         if stream is not None:
             _record(out, stream)
-    skip_cache_append(p, cache, rotation, q, k, v, row_offsets, lens, out, positions, stream)
+    skip_cache_append(p, cache, rotation, q, k, v, row_offsets, lens, out, positions, stream, made)
     return out
 
 
-def _cache_out(p, out, like, stream):
-    if out is None:
-        M, H = p.total_kept, p.H
-        out = (torch.empty_like(like) if not p.o_f32 and like.shape == (M, H, p.d_h)
-               and like.dtype is torch.bfloat16 and like.is_contiguous()
-               else like.new_empty((M, H, p.d_h), dtype=_out_dtype(p)),
-               like.new_empty((M, H), dtype=torch.float32))
-        if stream is not None:
-            for t in out:
-                _record(t, stream)
-    return out
+def _cache_out(p, like, stream):
+    """O and lse of an attention call whose queries ``like`` are."""
+    M, H = p.total_kept, p.H
+    O = (torch.empty_like(like) if not p.o_f32 and like.shape == (M, H, p.d_h)
+         and like.dtype is torch.bfloat16 and like.is_contiguous()
+         else like.new_empty((M, H, p.d_h), dtype=_out_dtype(p)))
+    lse = torch.empty_strided((M, H), (H, 1), dtype=torch.float32, device=like.device)
+    if stream is not None:
+        _record(O, stream)
+        _record(lse, stream)
+    return O, lse
 
 
 def cache_attn(p: SkipProblem, cache: KvCache, q, row_offsets, lens, prefix_ids=None,
                prefix_lens=None, out=None, workspace=None, stream=None) -> Tuple:
     """Causal attention of the new tokens over the cache.  Returns (O, lse);
     ``out`` = the two preallocated (lse None: not written)."""
-    O, lse = out = _cache_out(p, out, q, stream)
+    O, lse = made = _cache_out(p, q, stream) if out is None else out
     skip_cache_attn(p, cache, q, row_offsets, lens, O, lse, prefix_ids, prefix_lens, workspace,
-                    stream)
-    return out
+                    stream, out is None)
+    return made
 
 
 def cache_select(p: SkipProblem, cache: KvCache, q, row_offsets, lens, n_sel: int,
@@ -1484,12 +1505,13 @@ def cache_select(p: SkipProblem, cache: KvCache, q, row_offsets, lens, n_sel: in
                  stream=None) -> torch.Tensor:
     """The pages of the largest scores for every new token and key head, [total_kept,
     heads_kv, n_sel] int32 ascending, -1 behind the last."""
-    if out is None:
+    made = out is None
+    if made:
         out = q.new_empty((p.total_kept, cache.k.shape[1], n_sel), dtype=torch.int32)
         if stream is not None:
             _record(out, stream)
     skip_cache_select(p, cache, q, row_offsets, lens, n_sel, out, n_first, n_last, workspace,
-                      stream)
+                      stream, made)
     return out
 
 
@@ -1497,7 +1519,7 @@ def cache_attn_pages(p: SkipProblem, cache: KvCache, q, row_offsets, lens, pages
                      workspace=None, stream=None) -> Tuple:
     """Attention of the new tokens over ``pages`` [total_kept, heads_kv, n_sel] int32.
     Returns (O, lse); ``out`` = the two preallocated (lse None: not written)."""
-    O, lse = out = _cache_out(p, out, q, stream)
+    O, lse = made = _cache_out(p, q, stream) if out is None else out
     skip_cache_attn_pages(p, cache, q, row_offsets, lens, pages, pages.shape[-1], O, lse,
-                          workspace, stream)
-    return out
+                          workspace, stream, out is None)
+    return made

@@ -25,7 +25,7 @@
 // instructions are issued in 45 % of them, two waves a SIMD.  Four prefixes of 8217
 // tokens for 16 sequences each, with their own 1 to 500 tokens behind them in one launch:
 // 51 us.  Six pieces of 97 to 131 rows over 3900 tokens, 16 heads of 64, float output:
-// 37 (40 with sequences' heads in the order of their memory, see below).
+// 37 (40 with items sequence by sequence, see the end of the work).
 #pragma once
 
 #include "skip_cache.h"

@@ -138,6 +138,17 @@ def test_attention(b):
             assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(short), ctypes.byref(c), 0, pre,
                                                     ctypes.byref(need)) == b.SKIP_OK
             assert need.value == 0
+    # listed pages of up to 512 tokens, selection of up to 1024 pages: none
+    for page in (32, 64, 128, 256):
+        wide = cache(b, page_tokens=page, pages_max=1024)
+        for n in (1, 40, 3000):
+            for L in (5, 1024 * page):
+                short = problem(b, kept_offsets=[0, 1, n + 1], L_max=L)
+                assert b.LIB.skip_workspace_bytes_cache(
+                    ctypes.byref(short), ctypes.byref(wide), 512 // page, 0,
+                    ctypes.byref(need)) == b.SKIP_OK
+                assert need.value == 0
+    p, c = problem(b, L_max=6000), cache(b, pages_max=100)
     assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), 0, 0, None) == inv
     assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), -1, 0,
                                             ctypes.byref(need)) == inv
@@ -204,7 +215,8 @@ def test_binding_checks(b):
     # known arrays: the problem's sizes and the device are compared at every call
     c = b.KvCache(kv, kv, None, t)
     at = (kv.data_ptr(), kv.data_ptr(), None, t.data_ptr())
-    c.__dict__["_struct"] = known = (b.SkipKvCache(4, 64, 8, 0, 20, *at), 64, 2, 0, at)
+    c.__dict__["_struct"] = known = (b.SkipKvCache(4, 64, 8, 0, 20, *at), 64, 2, 0, at,
+                                       (kv.numel(), t.numel()))
     assert b._cache_struct(p, c, 0).k == kv.data_ptr()
     with pytest.raises(ValueError, match="device 0"):
         b._cache_struct(p, c, 1)
@@ -218,11 +230,34 @@ def test_binding_checks(b):
         b._cache_struct(p, c, 0)
     # and so are those that were given other memory in place
     c = b.KvCache(kv, kv, None, t.clone())
-    c.__dict__["_struct"] = known[:4] + (at[:3] + (c.page_table.data_ptr(),),)
+    c.__dict__["_struct"] = known[:4] + (at[:3] + (c.page_table.data_ptr(),), known[5])
+    assert b._cache_struct(p, c, 0) is known[0]
+    c.page_table.resize_(1, 8)
+    with pytest.raises(ValueError, match="device"):          # (looked at, and not on one)
+        b._cache_struct(p, c, 0)
+    c.page_table.resize_(2, 8)
     assert b._cache_struct(p, c, 0) is known[0]
     c.page_table.set_(torch.zeros(16, dtype=torch.int32))
     with pytest.raises(ValueError, match="pages_max"):
         b._cache_struct(p, c, 0)
+
+
+def test_binding_looks_at_a_changed_rotation(b):
+    import torch
+    r = b.Rotation(torch.ones(16))
+    key = (r.freq.data_ptr(), 16, "halves", 0)
+    r.__dict__["_struct"] = known = (key, b.SkipRotation(r.freq.data_ptr(), 32, 0))
+    assert b._rotation_struct(r, 0) is known[1]
+    r.freq.resize_(8)
+    with pytest.raises(ValueError, match="device"):          # (looked at, and not on one)
+        b._rotation_struct(r, 0)
+    r.freq.resize_(16)
+    assert b._rotation_struct(r, 0) is known[1]
+    for change in (lambda: setattr(r, "style", "pairs"), lambda: setattr(r, "freq", torch.ones(24))):
+        r.__dict__["_struct"] = known
+        change()
+        with pytest.raises(ValueError, match="device"):
+            b._rotation_struct(r, 0)
 
 
 # ---------------------------------------------------------------------------
