@@ -274,6 +274,9 @@ ATTN = [
     dict(seqs=[(257, 300), (130, 700), (1, 64)], H=3, hk=1, D=128, page=256),     # taken whole
     dict(seqs=[(40, 41)] * 90, H=32, hk=32, D=64, page=32),                       # 90 items a head
     dict(seqs=[(9, 2000), (5, 1000)], H=16, hk=2, D=128, page=32, extra_rows=5, o_f32=True),
+    # runs over more than 64 sequences, key head by key head
+    dict(seqs=[(33 + 3 * (i % 40), 300 + 61 * (i % 13)) for i in range(70)], H=3, hk=3, D=64),
+    dict(seqs=[(20 * (i % 3), 790 + i) for i in range(131)], H=6, hk=2, D=128, page=64, o_f32=True),
 ]
 
 
@@ -429,6 +432,8 @@ SELECT = [
     dict(seqs=[(1, 80000), (1, 40)], H=2, hk=1, n_sel=30, n_last=2),        # 2500 pages, few rows
     dict(seqs=[(130, 66000)], H=2, hk=2, n_sel=3),                          # and many
     dict(seqs=[(70, 300), (1, 20)], H=32, hk=16, D=128, n_sel=5, o_f32=True),     # a wave each
+    dict(seqs=[(200, 300), (150, 260)], H=6, hk=3, n_sel=5),                      # likewise
+    dict(seqs=[(530, 600)], H=4, hk=2, D=128, n_sel=4, extra_rows=2),
 ]
 
 
