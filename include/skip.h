@@ -706,6 +706,7 @@ skip_status_t skip_workspace_bytes_cache(const skip_problem_t* p, const skip_kv_
  * O = 0 and LSE = -inf where it sees none.  bf16 rows (SKIP_ERR_UNSUPPORTED otherwise); O
  * bf16, or float with o_f32.  Logits and sums are float32; softmax weights enter the
  * product with V as pairs of bf16 values (2^-16 relative), for float output as three.
+ * The weights are at most 1, so that values of up to 2^127 / tokens have finite sums.
  *   q            [total_kept][H][d_h] (as skip_cache_append writes them)
  *   prefix_ids   [B] int32, or NULL (then prefix_lens is): consecutive sequences
  *                with the same id >= 0 and the same prefix_lens hold the same keys

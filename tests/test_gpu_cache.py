@@ -375,6 +375,85 @@ def test_what_a_row_does_not_see_does_not_reach_it(B, n, ln, o_f32):
         assert torch.isfinite(after[:, :2, :5]).all() and torch.isfinite(after[:, :2, 6:]).all()
 
 
+def plant(s, tokens):
+    """An infinity and NaN in the values, NaN in the keys, of one token of some
+    sequences."""
+    for b, t in tokens:
+        pg, at = int(s.table[b, t // s.page]), t % s.page
+        s.cache.v[pg, 0, at, 5] = float("inf")
+        s.cache.v[pg, 1, at, s.D - 3] = float("nan")
+        s.cache.k[pg, 1, at, 3] = float("nan")
+
+
+def check_planted(s, got, ref, o_f32, b, t):
+    """The sequence's rows before token t are as without; the others are not finite
+    where they meet it."""
+    r0, n, ln, G = int(s.ro[b]), *s.seqs[b], s.H // s.hk
+    first = r0 + min(max(t - (ln - n), 0), n)
+    s.check(got, ref, o_f32, rows=slice(r0, first))
+    after = got[0][first:r0 + n].float()
+    assert not torch.isfinite(after[:, :G, 5]).any() and torch.isnan(after[:, G:2 * G]).all()
+    assert torch.isfinite(after[:, :G, :5]).all() and torch.isfinite(after[:, :G, 6:]).all()
+    assert torch.isfinite(after[:, 2 * G:]).all()
+
+
+@pytest.mark.parametrize("n,ln,page,D,o_f32", [
+    (130, 1500, 32, 64, True), (130, 1500, 64, 128, False), (300, 300, 256, 64, False),
+    (5, 400, 32, 64, True), (9, 1800, 128, 128, False)])
+def test_every_form_keeps_unseen_values_out(B, n, ln, page, D, o_f32):
+    """Rows in runs and whole, both head sizes, few and many new tokens."""
+    s = Setup(B, [(n, ln), (n, ln), (1, ln)], H=6, hk=3, D=D, page=page, o_f32=o_f32, seed=10)
+    ref = s.reference()
+    at = [(0, ln - 2), (1, ln - n // 2 - 1)]
+    plant(s, at)
+    got = attn(s, B)
+    torch.cuda.synchronize()
+    for b, t in at:
+        check_planted(s, got, ref, o_f32, b, t)
+    s.check(got, ref, o_f32, rows=slice(2 * n, 2 * n + 1))
+
+
+def test_unseen_values_inside_a_shared_prefix(B):
+    """New tokens inside the prefix, which not all rows of the run see."""
+    s = Setup(B, [(12, 5606), (10, 5601), (16, 5616)], shared=[(0, 1, 5600), (0, 2, 5600)], H=16,
+              hk=8, D=128, page=32, seed=12)
+    assert 4 * 3 * 8 * 5616 * 128 >= 64 << 20
+    ref = s.reference()
+    plant(s, [(0, 5597)])
+    got = attn(s, B, prefix_ids=dev([0] * 3), prefix_lens=dev([5600] * 3))
+    torch.cuda.synchronize()
+    for b in range(3):
+        check_planted(s, got, ref, False, b, 5597)
+
+
+@pytest.mark.parametrize("n,ln,page,D", [(2, 300, 32, 64), (70, 600, 32, 128), (70, 600, 64, 64),
+                                         (70, 1700, 32, 64), (70, 1700, 128, 128)])
+def test_missing_pages_in_every_form(B, n, ln, page, D):
+    s = Setup(B, [(n, ln), (n, ln - 90)], H=4, hk=2, D=D, page=page, seed=13)
+    last = (ln - 1) // page
+    s.table[0, 1], s.table[0, last], s.table[1, 0] = -1, -9, 1 << 30
+    s.cache.page_table.copy_(dev(s.table))
+    got = attn(s, B)
+    torch.cuda.synchronize()
+    s.check(got, s.reference(), False)
+    listed = np.tile(np.arange(min(last + 1, 12), dtype=np.int32), (2 * n, 2, 1))
+    got = B.cache_attn_pages(s.p, s.cache, s.q, s.row_offsets, s.dlens, dev(listed))
+    torch.cuda.synchronize()
+    s.check(got, s.reference(listed), False)
+
+
+def test_pages_that_a_whole_run_misses(B):
+    """A prefix's page that is in none of its sequences' tables."""
+    s = Setup(B, [(1, 2900), (2, 2700), (1, 2600)] * 2, H=16, hk=8, D=128, page=32, seed=14,
+              shared=[(0, i, 2500) for i in range(1, 6)])
+    assert 4 * 6 * 8 * 2900 * 128 >= 64 << 20
+    s.table[:, 3] = s.table[:, 40] = -1
+    s.cache.page_table.copy_(dev(s.table))
+    got = attn(s, B, prefix_ids=dev([0] * 6), prefix_lens=dev([2500] * 6))
+    torch.cuda.synchronize()
+    s.check(got, s.reference(), False)
+
+
 def test_large_values_and_logits(B):
     """Values near the largest bfloat16 keep their sums finite; logits far apart."""
     s = Setup(B, [(1, 3000), (2, 70)], H=4, hk=2, seed=3, scale=40.0, o_f32=True)
