@@ -122,7 +122,7 @@ struct SeqBlock {
       s.load(a.row_offsets, a.lens, b, a.total_rows, a.k_max, a.L_max);
       if (a.prefix_ids) {
         id = a.prefix_ids[b];
-        pl = clampi(a.prefix_lens[b], 0, a.L_max);
+        pl = a.prefix_lens[b];                         // (as it is: L_max makes no two alike)
         if (s.n > 0 && s.len < pl) id = -1;            // (does not hold the prefix)
       }
     }
@@ -146,7 +146,7 @@ struct SeqBlock {
       if (last > first) {
         P = pl;
         run_rows = rows;
-        if (lane == first && run_rows > 0)
+        if (lane == first && run_rows > 0 && source <= last)     // (one holds all of it)
           pre = a.heads_kv * row_tiles(a, run_rows, kPrefixRows) *
                 (prefix_tiles(P) + kPrefixStart);
       }

@@ -352,6 +352,17 @@ def test_prefixes_of_sequences_that_are_passed_over(B):
     s.check(got, s.reference(), False)
 
 
+def test_prefixes_longer_than_any_sequence(B):
+    """prefix_lens past L_max: no sequence holds such a prefix, all read their own."""
+    s = Setup(B, [(1, 5600), (2, 5600), (1, 5590), (1, 5600)], H=16, hk=8, D=128, page=32, seed=15)
+    assert 4 * 4 * 8 * 5600 * 128 >= 64 << 20
+    ref = s.reference()
+    for P in ([6000, 6000, 6000, 6000], [6000, 7000, 7000, 9000], [2 ** 31 - 1] * 4):
+        got = attn(s, B, prefix_ids=dev([0] * 4), prefix_lens=dev(P))
+        torch.cuda.synchronize()
+        s.check(got, ref, False)
+
+
 @pytest.mark.parametrize("o_f32", [False, True])
 @pytest.mark.parametrize("n,ln", [(40, 40), (7, 600), (200, 200), (40, 700)])
 def test_what_a_row_does_not_see_does_not_reach_it(B, n, ln, o_f32):
