@@ -707,6 +707,8 @@ skip_status_t skip_workspace_bytes_cache(const skip_problem_t* p, const skip_kv_
  * bf16, or float with o_f32.  Logits and sums are float32; softmax weights enter the
  * product with V as pairs of bf16 values (2^-16 relative), for float output as three.
  * The weights are at most 1, so that values of up to 2^127 / tokens have finite sums.
+ * A logit below float32's range weighs nothing, one above it makes NaN of its row;
+ * sm_scale is at most 2^127.
  *   q            [total_kept][H][d_h] (as skip_cache_append writes them)
  *   prefix_ids   [B] int32, or NULL (then prefix_lens is): consecutive sequences
  *                with the same id >= 0 and the same prefix_lens hold the same keys

@@ -810,6 +810,7 @@ static skip_status_t cache_attn_impl(const skip_problem_t* p, const skip_kv_cach
                                      int32_t n_sel, void* O, float* lse, void* workspace,
                                      size_t workspace_bytes, void* stream) {
   if (p->dtype != SKIP_BF16) return SKIP_ERR_UNSUPPORTED;
+  if (!std::isfinite(p->sm_scale * 1.4426950408889634f)) return SKIP_ERR_INVALID_ARG;
   if (p->total_kept == 0) return SKIP_OK;
   if (!q || !O || !al16(q) || !al16(O) || !al16(workspace)) return SKIP_ERR_INVALID_ARG;
   if (!cache_attn_fits(*p, *cache, n_sel)) return SKIP_ERR_UNSUPPORTED;

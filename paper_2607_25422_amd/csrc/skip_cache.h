@@ -2,6 +2,8 @@
 // skip.h).
 #pragma once
 
+#include <cfloat>
+
 #include "skip_common.h"
 #include "skip_select.h"
 
@@ -232,6 +234,30 @@ __device__ __forceinline__ float over_groups(float x, F op) {
   const uint32_t w = __float_as_uint(op(__uint_as_float(a[0]), __uint_as_float(a[1])));
   const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
   return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// The reference of weights 2^(logit - reference) once mx is the largest logit: 8 over it,
+// so that it is rarely moved.  It stays finite: a logit past float32 then has an infinite
+// weight, which makes its row NaN (an infinite reference would make all weights 0).
+constexpr float kCacheOver = 8.f;
+__device__ __forceinline__ float cache_reference(float mx) {
+  return fminf(mx, FLT_MAX) + kCacheOver;
+}
+// A weight's exponent is s sc - reference in one multiply-add, whose product is exact, while
+// the reference is a rounded one: half a step apart, which is 1 at 2^24 and past any
+// exponent from 2^32 on.  Rows whose reference is farther than kCacheFar take their logits
+// rounded as well, less the reference (over sc, so that the multiply-add serves both).
+// (Prompts: 0.8 % slower with it; 1.1 where a wave looks for them at every tile and not
+// where references move.)
+constexpr float kCacheFar = 16777216.f;
+__device__ __forceinline__ float finite_reference(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ bool cache_far(float m) {
+  return fabsf(finite_reference(m)) > kCacheFar;
+}
+__device__ __forceinline__ float far_logit(float s, float sc, float ref, float back) {
+  float z = s * sc;
+  asm volatile("" : "+v"(z));                       // (not joined with the subtraction)
+  return (z - ref) * back;
 }
 
 CacheView cache_view(const skip_kv_cache_t& c);

@@ -47,7 +47,6 @@ constexpr int kCWaves = 4;
 constexpr int kCThreads = 64 * kCWaves;
 constexpr int kCTile = kOwnTile;           // tokens of a tile
 constexpr int kCLeast = 8;                 // tiles of a run, at least
-constexpr float kCOver = 8.f;
 
 // bf16 pieces of a softmax weight in the second product: two for bf16 output (2^-16
 // relative, as in the attention over passages), three for float output (2^-24).
@@ -157,8 +156,10 @@ __device__ __forceinline__ void cache_rows(const CacheAttnArgs& a, RowsShared<D,
 
     f32x4_t acc[R][NB];
     float m_run[R], l_run[R];
+    bool any_far[R];                         // a row's reference is far (see kCacheFar)
 #pragma unroll
     for (int r = 0; r < R; ++r) {
+      any_far[r] = false;
       m_run[r] = -INFINITY;
       l_run[r] = 0.f;
 #pragma unroll
@@ -310,8 +311,8 @@ __device__ __forceinline__ void cache_rows(const CacheAttnArgs& a, RowsShared<D,
               for (int w = 0; w < VW; ++w) vf[e][w] &= ~bf16_odd_pair(vf[e][w]);
           }
         }
-        // weights 2^(sc s - reference); the reference is 8 over the largest logit that
-        // moved it, so that weights are at most 1 and it is rarely moved
+        // weights 2^(sc s - reference); the reference is over the largest logit that moved
+        // it, so that weights are at most 1
         u32x4 pc[R][PIECES];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -322,15 +323,26 @@ __device__ __forceinline__ void cache_rows(const CacheAttnArgs& a, RowsShared<D,
           if (__any(lm * sc > m_run[r])) {
             const float mx = over_groups(lm, [](float x, float y) { return fmaxf(x, y); }) * sc;
             const bool up = mx > m_run[r];
-            const float to = up ? mx + kCOver : m_run[r];
+            const float to = up ? cache_reference(mx) : m_run[r];
             const float alpha = !up ? 1.f : m_run[r] == -INFINITY ? 0.f
                                             : __builtin_amdgcn_exp2f(m_run[r] - to);
             l_run[r] *= alpha;
 #pragma unroll
             for (int i = 0; i < NB; ++i) acc[r][i] *= alpha;
             m_run[r] = to;
+            any_far[r] = __any(cache_far(to));
           }
-          const float ref = m_run[r] == -INFINITY ? 0.f : m_run[r];
+          float ref = finite_reference(m_run[r]);
+          if (any_far[r]) {
+            const bool far = cache_far(ref);
+            const float back = 1.f / sc;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float x = s[r][e >> 2][e & 3];
+              s[r][e >> 2][e & 3] = far ? far_logit(x, sc, ref, back) : x;
+            }
+            ref = far ? 0.f : ref;
+          }
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             float p0 = __builtin_amdgcn_exp2f(fmaf(s[r][w >> 1][2 * (w & 1)], sc, -ref));

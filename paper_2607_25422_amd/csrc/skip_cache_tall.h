@@ -42,7 +42,6 @@ constexpr int kTLeast = 4;                 // tiles of a run, at least
 // (480 rows of 481 tokens, 32 heads over 8: 31 us in runs, 17 whole).
 constexpr int kTShort = 768;
 static_assert(kTRows == kPrefixRows && kTTile == kPrefixTile, "items of prefixes");
-constexpr float kTOver = 8.f;
 template <bool OUT_F32> constexpr int kTPieces = OUT_F32 ? 3 : 2;
 
 struct TallArgs {
@@ -244,6 +243,7 @@ __device__ __forceinline__ void cache_tall_work(const TallArgs& a, TallShared<D>
 
   f32x16_t acc[FB];
   float m_run = -INFINITY, l_run = 0.f;
+  bool any_far = false;                             // a row's reference is far (see kCacheFar)
 #pragma unroll
   for (int f = 0; f < FB; ++f)
 #pragma unroll
@@ -294,14 +294,27 @@ __device__ __forceinline__ void cache_tall_work(const TallArgs& a, TallShared<D>
                                                       false, false);
       const float mx = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * sc;
       const bool up = mx > m_run;
-      const float to = up ? mx + kTOver : m_run;
+      const float to = up ? cache_reference(mx) : m_run;
       const float alpha = !up ? 1.f : m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - to);
       l_run *= alpha;
 #pragma unroll
       for (int f = 0; f < FB; ++f) acc[f] *= alpha;
       m_run = to;
+      any_far = __any(cache_far(to));
     }
-    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    float ref = finite_reference(m_run);
+    if (any_far) {
+      const bool far = cache_far(ref);
+      const float back = 1.f / sc;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = s[h][i];
+          s[h][i] = far ? far_logit(x, sc, ref, back) : x;
+        }
+      ref = far ? 0.f : ref;
+    }
     // weights of step (h, q) as bf16 pieces, and its values
     auto weigh = [&](auto step, u32x4 (&pc)[PIECES]) {
       constexpr int h = decltype(step)::value >> 1, q = decltype(step)::value & 1;

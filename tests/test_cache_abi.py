@@ -157,6 +157,16 @@ def test_attention(b):
     assert call(b, "attn", wide, cache(b, pages_max=1 << 30)) == uns
 
 
+def test_scales_past_float32(b):
+    """The scale enters in base 2: one whose product with log2 e is infinite is refused by
+    the calls that use it."""
+    c = cache(b)
+    for scale in (2.5e38, -3.4e38):
+        p = problem(b, sm_scale=scale)
+        for fn in ("attn", "pages"):
+            assert call(b, fn, p, c) == b.SKIP_ERR_INVALID_ARG, (fn, scale)
+
+
 def test_more_than_a_launch_holds(b):
     uns = b.SKIP_ERR_UNSUPPORTED
 

@@ -474,6 +474,34 @@ def test_large_values_and_logits(B):
     s.check(got, s.reference(), True)
 
 
+@pytest.mark.parametrize("n,ln,page,D,o_f32", [
+    (1, 200, 32, 64, False), (3, 1300, 64, 128, False), (40, 300, 32, 64, True),
+    (130, 1500, 64, 128, False), (1, 4000, 32, 64, True)])
+def test_logits_past_float32(B, n, ln, page, D, o_f32):
+    """A finite product whose scaled value is not: below float32 it weighs nothing, above
+    it the row is not finite (a row of zeros would be one that sees no token).  The rows
+    looked at have logits of 2^63 and more otherwise, so that the largest alone has a
+    weight: their results are its value."""
+    s = Setup(B, [(n, ln), (n, ln)], H=4, hk=2, D=D, page=page, o_f32=o_f32, scale=8.0, seed=16)
+    big = 2.0 ** 60
+    for b in range(2):
+        s.cache.k[int(s.table[b, 0]), :, 5] = big          # (times the query: 2^126 or 2^127)
+        s.q[(b + 1) * n - 1] = big if b == 0 else -big
+    k = np.abs(f64(s.cache.k))
+    tol = (D + 4) * U * s.scale * big * np.where(k < big, k, 0.0).sum(-1).max()
+    got = attn(s, B)
+    listed = np.tile(np.arange(12, dtype=np.int32), (2 * n, 2, 1))
+    by = B.cache_attn_pages(s.p, s.cache, s.q, s.row_offsets, s.dlens, dev(listed))
+    torch.cuda.synchronize()
+    for (O, lse), ref in ((got, s.reference()), (by, s.reference(listed))):
+        assert not torch.isfinite(O[n - 1].float()).any() and not torch.isfinite(lse[n - 1]).any()
+        assert (f64(O)[2 * n - 1] == ref[0][2 * n - 1]).all()
+        want = ref[1][2 * n - 1]
+        assert (np.abs(f64(lse)[2 * n - 1] - want) <= tol + 4 * U * np.abs(want)).all()
+        others = [r for r in range(2 * n) if r not in (n - 1, 2 * n - 1)]
+        assert torch.isfinite(O[others].float()).all() and torch.isfinite(lse[others]).all()
+
+
 def test_missing_pages_are_passed_over(B):
     s = Setup(B, [(1, 700), (3, 90)], seed=4)
     s.table[0, 3], s.table[0, 20], s.table[1, 0] = -1, 1 << 29, -5
