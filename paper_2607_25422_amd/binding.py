@@ -388,31 +388,36 @@ def _torch_stream(stream):
     return torch.cuda.ExternalStream(int(stream))
 
 
-def _record(t: torch.Tensor, stream) -> None:
-    """Records a call's stream on a tensor allocated for it, unless it is the
-    current one (None is)."""
+def _alloc(make, stream, returned=True):
+    """What ``make`` allocates for a call on ``stream``.  The caching allocator orders
+    the uses of a block along the stream that it was allocated on, so on another stream
+    than the current one it is allocated as that stream's: a block of the current one's
+    may be in use there still (a workspace is released when its call returns, while the
+    kernels may run on).  What is ``returned`` to the caller, whose stream is the current
+    one, is recorded there."""
     if stream is None:
-        return
-    s = _torch_stream(stream)
-    if s != torch.cuda.current_stream():
-        t.record_stream(s)
+        return make()
+    s, here = _torch_stream(stream), torch.cuda.current_stream()
+    if s == here:
+        return make()
+    with torch.cuda.stream(s):
+        t = make()
+    if returned:
+        for x in t if isinstance(t, tuple) else (t,):
+            x.record_stream(here)
+    return t
 
 
 def _fresh_workspace(nbytes: int, device, stream=None) -> torch.Tensor:
-    """A workspace allocated for one call on ``stream`` (see _ws)."""
-    ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
-    _record(ws, stream)
-    return ws
+    """A workspace allocated for one call on ``stream``."""
+    return _alloc(lambda: torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device),
+                  stream, returned=False)
 
 
 def _ws(p, workspace, stream=None):
-    """The workspace of a call: the caller's, or a fresh one.  A fresh one is
-    released when the call returns, while the kernels may still run on
-    ``stream``; recording that stream on it keeps the caching allocator from
-    handing the memory to other work before they finish."""
+    """The workspace of a call: the caller's, or a fresh one."""
     if workspace is None:
-        workspace = new_workspace(p)
-        _record(workspace, stream)
+        workspace = _alloc(lambda: new_workspace(p), stream, returned=False)
     return workspace, workspace.data_ptr(), workspace.numel()
 
 
@@ -1351,9 +1356,8 @@ def quantize_passages(p: SkipProblem, store: KvStore, Kh, Vh, passage_offsets, p
     [total_passages, H * d_h] float32 with ``want_keys``, else None."""
     keys = None
     if want_keys:
-        keys = torch.empty((max(p.total_passages, 1), p.d), dtype=torch.float32,
-                           device=store.data.device)
-        _record(keys, stream)
+        keys = _alloc(lambda: torch.empty((max(p.total_passages, 1), p.d), dtype=torch.float32,
+                                          device=store.data.device), stream)
     skip_quantize_passages(p, store, Kh, Vh, passage_offsets, passage_blocks, keys, stream)
     return None if keys is None else keys[:p.total_passages]
 
@@ -1468,26 +1472,22 @@ def cache_append(p: SkipProblem, cache: KvCache, q, k, v, row_offsets, lens, rot
     made = out is None and q is not None
     if made:
         # (the fastest of torch's ways to one)
-        out = (torch.empty_like(q) if q.dtype is torch.bfloat16 and q.is_contiguous()
-               and q.shape == (p.total_kept, p.H, p.d_h)
-               else cache.k.new_empty((p.total_kept, p.H, p.d_h)))
-        if stream is not None:
-            _record(out, stream)
+        out = _alloc(lambda: (torch.empty_like(q) if q.dtype is torch.bfloat16
+                              and q.is_contiguous() and q.shape == (p.total_kept, p.H, p.d_h)
+                              else cache.k.new_empty((p.total_kept, p.H, p.d_h))), stream)
     skip_cache_append(p, cache, rotation, q, k, v, row_offsets, lens, out, positions, stream, made)
     return out
 
 
 def _cache_out(p, like, stream):
     """O and lse of an attention call whose queries ``like`` are."""
+    if stream is not None:
+        return _alloc(lambda: _cache_out(p, like, None), stream)
     M, H = p.total_kept, p.H
     O = (torch.empty_like(like) if not p.o_f32 and like.shape == (M, H, p.d_h)
          and like.dtype is torch.bfloat16 and like.is_contiguous()
          else like.new_empty((M, H, p.d_h), dtype=_out_dtype(p)))
-    lse = torch.empty_strided((M, H), (H, 1), dtype=torch.float32, device=like.device)
-    if stream is not None:
-        _record(O, stream)
-        _record(lse, stream)
-    return O, lse
+    return O, torch.empty_strided((M, H), (H, 1), dtype=torch.float32, device=like.device)
 
 
 def cache_attn(p: SkipProblem, cache: KvCache, q, row_offsets, lens, prefix_ids=None,
@@ -1507,9 +1507,8 @@ def cache_select(p: SkipProblem, cache: KvCache, q, row_offsets, lens, n_sel: in
     heads_kv, n_sel] int32 ascending, -1 behind the last."""
     made = out is None
     if made:
-        out = q.new_empty((p.total_kept, cache.k.shape[1], n_sel), dtype=torch.int32)
-        if stream is not None:
-            _record(out, stream)
+        out = _alloc(lambda: q.new_empty((p.total_kept, cache.k.shape[1], n_sel),
+                                         dtype=torch.int32), stream)
     skip_cache_select(p, cache, q, row_offsets, lens, n_sel, out, n_first, n_last, workspace,
                       stream, made)
     return out

@@ -680,6 +680,34 @@ def test_two_streams_at_once(B):
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+def test_memory_of_a_call_on_another_stream(B):
+    """Workspaces and outputs that calls on two streams make in turn: never a block that
+    the other stream may still use, and the same results."""
+    s = Setup(B, [(1, 3000), (2, 1500)], H=16, hk=2, seed=18)
+    want = attn(s, B)
+    sel = B.cache_select(s.p, s.cache, s.q, s.row_offsets, s.dlens, 40)
+    by = B.cache_attn_pages(s.p, s.cache, s.q, s.row_offsets, s.dlens, sel)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    n = 1 << 20
+    here = B._fresh_workspace(n, "cuda").data_ptr()          # (released: the current stream's)
+    other = B._fresh_workspace(n, "cuda", side).data_ptr()
+    assert other != here and B._fresh_workspace(n, "cuda").data_ptr() == here
+    got = []
+    for turn in range(8):
+        for stream in (None, side):
+            args = (s.p, s.cache, s.q, s.row_offsets, s.dlens)
+            got.append((B.cache_attn(*args, stream=stream),
+                        B.cache_attn_pages(*args, sel, stream=stream),
+                        B.cache_select(*args, 40, stream=stream)))
+        if turn % 2:
+            got = got[-3:]                                   # (the others' memory is free again)
+    torch.cuda.synchronize()
+    for a, b, c in got:
+        for x, y in zip((*a, *b, c), (*want, *by, sel)):
+            assert torch.equal(x, y)
+
+
 def test_from_the_route_to_an_answer(B):
     """The calls in the order of a program: kept tokens routed to their passages, the
     layer that makes their queries, keys and values, a cache that takes them in, and
