@@ -12,6 +12,7 @@ tensors (which the kernels read).  ``Offsets.to_device`` makes the pair.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from dataclasses import dataclass
@@ -98,6 +99,10 @@ class SkipKvCache(ctypes.Structure):
         ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("mean", ctypes.c_void_p),
         ("page_table", ctypes.c_void_p),
     ]
+
+    @functools.cached_property
+    def pool(self) -> Tuple[int, int, int]:
+        return self.n_pages, self.heads_kv, self.page_tokens
 
 
 class SkipRotation(ctypes.Structure):
@@ -807,31 +812,44 @@ def _raw_stream(stream, dev) -> int:
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
 
-def _cache_struct(p: SkipProblem, cache: "KvCache", dev=None) -> SkipKvCache:
-    """The cache's description.  Its arrays are looked at again where one of them lies
-    elsewhere than when they last were, or holds more or fewer."""
+def _as_described(known, cache: "KvCache", mean: bool) -> bool:
+    """Whether a cache's arrays (``mean``: its mean keys with them) are what its kept
+    description says."""
+    c, d_h, rows, _, (kp, vp, mp, tp), size = known
+    k, v, t, m = cache.k, cache.v, cache.page_table, cache.mean
+    bf16, pool, shape = torch.bfloat16, c.pool, k.shape
+    return (k.data_ptr() == kp and v.data_ptr() == vp and t.data_ptr() == tp
+            and shape == (*pool, d_h) and v.shape == shape and t.shape == (rows, c.pages_max)
+            and k.dtype is bf16 and v.dtype is bf16 and t.dtype is torch.int32
+            and k.is_contiguous() and v.is_contiguous() and t.is_contiguous()
+            and (not mean or (mp is None if m is None else
+                              m.data_ptr() == mp and m.numel() * pool[2] >= size[0]
+                              and m.dtype is bf16 and m.is_contiguous())))
+
+
+def _cache_struct(p: SkipProblem, cache: "KvCache", dev=None, mean=True) -> SkipKvCache:
+    """The cache's description, made again where its arrays are no longer what it says
+    (1.1 to 1.4 us to compare them, 3.1 to 3.5 to make it).  ``mean``: the call uses the mean keys."""
     dev = torch.cuda.current_device() if dev is None else dev
-    k, t, mean = cache.k, cache.page_table, cache.mean
-    at = (k.data_ptr(), cache.v.data_ptr(), None if mean is None else mean.data_ptr(),
-          t.data_ptr())
-    size = (k.numel(), t.numel())
     known = cache.__dict__.get("_struct")
-    if known is None or known[4] != at or known[5] != size:
-        if k.dim() != 4 or cache.v.shape != k.shape:
+    if known is None or not _as_described(known, cache, mean):
+        k, v, t, means = cache.k, cache.v, cache.page_table, cache.mean
+        if k.dim() != 4 or v.shape != k.shape:
             raise ValueError("cache.k and cache.v must be [pages, heads_kv, page_tokens, d_h]")
         if t.dim() != 2:
             raise ValueError("cache.page_table must be [B, pages_max]")
         n_pages, heads_kv, page, d_h = k.shape
         n, on = n_pages * heads_kv * d_h, k.get_device()
         for x, name, dt, m in ((k, "k", torch.bfloat16, n * page),
-                               (cache.v, "v", torch.bfloat16, n * page),
-                               (mean, "mean", torch.bfloat16, n),
+                               (v, "v", torch.bfloat16, n * page),
+                               (means, "mean", torch.bfloat16, n),
                                (t, "page_table", torch.int32, t.numel())):
             _ptr(x, "cache." + name, dt, m)
             if x is not None and x.get_device() != on:
                 raise ValueError(f"cache.{name} is on device {x.get_device()}, cache.k on {on}")
+        at = (k.data_ptr(), v.data_ptr(), None if means is None else means.data_ptr(), t.data_ptr())
         known = (SkipKvCache(heads_kv, page, t.shape[1], 0, n_pages, *at), d_h, t.shape[0], on, at,
-                 size)
+                 (k.numel(), t.numel()))
         cache.__dict__["_struct"] = known
     c, d_h, rows, on = known[:4]
     if d_h != p.d_h:
@@ -848,7 +866,8 @@ def _rotation_struct(rotation: "Rotation", dev) -> SkipRotation:
     f = rotation.freq
     key = (f.data_ptr(), f.numel(), rotation.style, dev)
     known = rotation.__dict__.get("_struct")
-    if known is None or known[0] != key:
+    if (known is None or known[0] != key or f.dtype is not torch.float32
+            or not f.is_contiguous()):
         known = key, SkipRotation(_dptr(f, "rotation.freq", torch.float32, 1, dev), 2 * f.numel(),
                                   ROTATIONS[rotation.style])
         rotation.__dict__["_struct"] = known
@@ -927,7 +946,7 @@ def _cache_ws(p, c, workspace, n_sel, prefixes, none, device, stream, dev):
 def skip_cache_attn(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, O, lse=None,
                     prefix_ids=None, prefix_lens=None, workspace=None, stream=None, _made=False):
     dev, i32 = torch.cuda.current_device(), torch.int32
-    c = _cache_struct(p, cache, dev)
+    c = _cache_struct(p, cache, dev, False)
     B, M, n = p.B, p.total_kept, p.total_kept * p.d
     ws, wp, wn = _cache_ws(p, c, workspace, 0, prefix_ids is not None, p.L_max <= 512, q.device,
                            stream, dev)
@@ -961,7 +980,7 @@ def skip_cache_select(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, n_
 def skip_cache_attn_pages(p: SkipProblem, cache: "KvCache", q, row_offsets, lens, pages, n_sel, O,
                           lse=None, workspace=None, stream=None, _made=False):
     dev, i32 = torch.cuda.current_device(), torch.int32
-    c = _cache_struct(p, cache, dev)
+    c = _cache_struct(p, cache, dev, False)
     B, M, n = p.B, p.total_kept, p.total_kept * p.d
     ws, wp, wn = _cache_ws(p, c, workspace, n_sel, False, n_sel * c.page_tokens <= 512, q.device,
                            stream, dev)
@@ -1426,8 +1445,20 @@ def gather_dense(p: SkipProblem, rows, packed, d_out: int, kept_offsets=None, ro
 # ---------------------------------------------------------------------------
 # The paged cache
 
+class _Described:
+    """Keeps the description that the calls make of its arrays (``_struct``) with it: not
+    in copies and pickles, and not beyond a change of its attributes."""
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_struct", None)
+
+    def __getstate__(self):
+        return {k: x for k, x in self.__dict__.items() if k != "_struct"}
+
+
 @dataclass
-class KvCache:
+class KvCache(_Described):
     """A paged cache: ``k`` and ``v`` [pages, heads_kv, page_tokens, d_h] bf16, the
     pages' mean keys ``mean`` [pages, heads_kv, d_h] bf16 (None where pages are not
     selected) and ``page_table`` [B, pages_max] int32, the page of each
@@ -1437,21 +1468,13 @@ class KvCache:
     mean: Optional[torch.Tensor]
     page_table: torch.Tensor
 
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        self.__dict__.pop("_struct", None)        # (see _cache_struct)
-
 
 @dataclass
-class Rotation:
+class Rotation(_Described):
     """Rotation by the position: ``freq`` [dims / 2] float32 on the device, pairs of
     features i and i + dims / 2 ("halves") or 2 i and 2 i + 1 ("pairs")."""
     freq: torch.Tensor
     style: str = "halves"
-
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        self.__dict__.pop("_struct", None)        # (see _rotation_struct)
 
 
 def new_kv_cache(n_pages: int, heads_kv: int, page_tokens: int, d_h: int, page_table,
@@ -1463,6 +1486,16 @@ def new_kv_cache(n_pages: int, heads_kv: int, page_tokens: int, d_h: int, page_t
     return KvCache(k, v, m, page_table)
 
 
+def _append_out(p, cache, q, stream):
+    """The rotated queries of an append."""
+    if stream is not None:
+        return _alloc(lambda: _append_out(p, cache, q, None), stream)
+    # (the fastest of torch's ways to one)
+    return (torch.empty_like(q) if q.dtype is torch.bfloat16 and q.is_contiguous()
+            and q.shape == (p.total_kept, p.H, p.d_h)
+            else cache.k.new_empty((p.total_kept, p.H, p.d_h)))
+
+
 def cache_append(p: SkipProblem, cache: KvCache, q, k, v, row_offsets, lens, rotation=None,
                  positions=None, out=None, stream=None) -> Optional[torch.Tensor]:
     """Appends the new tokens: ``q`` [total_kept, H, d_h] (or None), ``k`` and ``v``
@@ -1471,10 +1504,7 @@ def cache_append(p: SkipProblem, cache: KvCache, q, k, v, row_offsets, lens, rot
     preallocated tensor)."""
     made = out is None and q is not None
     if made:
-        # (the fastest of torch's ways to one)
-        out = _alloc(lambda: (torch.empty_like(q) if q.dtype is torch.bfloat16
-                              and q.is_contiguous() and q.shape == (p.total_kept, p.H, p.d_h)
-                              else cache.k.new_empty((p.total_kept, p.H, p.d_h))), stream)
+        out = _append_out(p, cache, q, stream)
     skip_cache_append(p, cache, rotation, q, k, v, row_offsets, lens, out, positions, stream, made)
     return out
 
@@ -1507,8 +1537,9 @@ def cache_select(p: SkipProblem, cache: KvCache, q, row_offsets, lens, n_sel: in
     heads_kv, n_sel] int32 ascending, -1 behind the last."""
     made = out is None
     if made:
-        out = _alloc(lambda: q.new_empty((p.total_kept, cache.k.shape[1], n_sel),
-                                         dtype=torch.int32), stream)
+        shape = p.total_kept, cache.k.shape[1], n_sel
+        out = (q.new_empty(shape, dtype=torch.int32) if stream is None else
+               _alloc(lambda: q.new_empty(shape, dtype=torch.int32), stream))
     skip_cache_select(p, cache, q, row_offsets, lens, n_sel, out, n_first, n_last, workspace,
                       stream, made)
     return out

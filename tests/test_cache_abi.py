@@ -270,6 +270,75 @@ def test_binding_looks_at_a_changed_rotation(b):
             b._rotation_struct(r, 0)
 
 
+def test_binding_looks_at_arrays_changed_in_place(b):
+    """What keeps an array's address and may keep its count of elements: other sizes, an
+    exchange of dimensions, another type."""
+    import torch
+    p = problem(b)
+
+    def known(mean=False, B=2, pages_max=8):
+        k = torch.empty(20, 4, 64, 64, dtype=torch.bfloat16)
+        v, t = torch.empty_like(k), torch.zeros(B, pages_max, dtype=torch.int32)
+        m = torch.empty(20, 4, 64, dtype=torch.bfloat16) if mean else None
+        c = b.KvCache(k, v, m, t)
+        at = (k.data_ptr(), v.data_ptr(), m.data_ptr() if mean else None, t.data_ptr())
+        s = (b.SkipKvCache(4, 64, pages_max, 0, 20, *at), 64, B, 0, at, (k.numel(), t.numel()))
+        c.__dict__["_struct"] = s
+        assert b._cache_struct(p, c, 0) is s[0]
+        return c
+
+    def set_data(x, dtype):
+        x.data = x.view(dtype)
+    for change in (lambda c: c.page_table.resize_(4, 4), lambda c: c.k.resize_(20, 8, 32, 64),
+                   lambda c: c.k.resize_(40, 4, 32, 64), lambda c: c.v.resize_(10, 4, 64, 64),
+                   lambda c: c.k.transpose_(2, 3), lambda c: c.v.transpose_(2, 3),
+                   lambda c: set_data(c.k, torch.float16), lambda c: set_data(c.v, torch.int16),
+                   lambda c: set_data(c.page_table, torch.float32)):
+        c = known()
+        change(c)
+        with pytest.raises(ValueError):                      # (looked at, and not on a device)
+            b._cache_struct(p, c, 0)
+    c = known(B=8)
+    c.page_table.t_()
+    with pytest.raises(ValueError):
+        b._cache_struct(p, c, 0)
+    for change in (lambda m: m.resize_(10, 4, 64), lambda m: m.resize_(0),
+                   lambda m: m.transpose_(0, 1), lambda m: set_data(m, torch.float16)):
+        c = known(mean=True)
+        change(c.mean)
+        with pytest.raises(ValueError):
+            b._cache_struct(p, c, 0)
+    r = b.Rotation(torch.ones(16))
+    r.__dict__["_struct"] = ((r.freq.data_ptr(), 16, "halves", 0),
+                             b.SkipRotation(r.freq.data_ptr(), 32, 0))
+    b._rotation_struct(r, 0)
+    r.freq.data = r.freq.view(torch.int32)
+    with pytest.raises(ValueError):
+        b._rotation_struct(r, 0)
+    r.freq.data = torch.as_strided(torch.ones(32), (16,), (2,))
+    with pytest.raises(ValueError):
+        b._rotation_struct(r, 0)
+
+
+def test_caches_and_rotations_are_copied_and_pickled(b):
+    """The kept description, whose pointers are this process's, stays behind."""
+    import copy
+    import pickle
+    import torch
+    c = b.KvCache(torch.ones(2, 1, 32, 64), torch.zeros(2, 1, 32, 64), None, torch.zeros(1, 2))
+    r = b.Rotation(torch.ones(16), "pairs")
+    c.__dict__["_struct"] = (b.SkipKvCache(1, 32, 2, 0, 2, 4096, 4096, None, 4096),)
+    r.__dict__["_struct"] = (None, b.SkipRotation(4096, 32, 1))
+    for x in (c, r):
+        for y in (copy.copy(x), copy.deepcopy(x), pickle.loads(pickle.dumps(x))):
+            assert "_struct" not in y.__dict__ and type(y) is type(x)
+            for name in ("k", "v", "mean", "page_table") if x is c else ("freq",):
+                a, z = getattr(x, name), getattr(y, name)
+                assert (a is z is None) or torch.equal(a, z)
+        assert "_struct" in x.__dict__
+    assert copy.copy(r).style == "pairs" and copy.copy(c).k is c.k
+
+
 # ---------------------------------------------------------------------------
 # The oracle
 
