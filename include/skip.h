@@ -694,8 +694,9 @@ skip_status_t skip_cache_append(const skip_problem_t* p, const skip_kv_cache_t* 
                                 const int32_t* positions, void* q_out, void* stream);
 
 /* Workspace of the cache's attention (n_sel 0), of skip_cache_select and of
- * skip_cache_attn_pages (n_sel pages a row; the larger of the two) (host-only).
- * `prefixes`: whether prefix_ids will be given. */
+ * skip_cache_attn_pages (n_sel pages a row; the larger of the two, or that of the one
+ * whose limits the sizes are within) (host-only).  `prefixes`: whether prefix_ids will be
+ * given. */
 skip_status_t skip_workspace_bytes_cache(const skip_problem_t* p, const skip_kv_cache_t* cache,
                                          int32_t n_sel, int32_t prefixes, size_t* bytes);
 

@@ -792,14 +792,13 @@ skip_status_t skip_workspace_bytes_cache(const skip_problem_t* p, const skip_kv_
   skip_status_t st = check_cache(p, cache, &given, &given);
   if (st == SKIP_OK && n_sel > 0) st = check_listed(n_sel);
   if (st != SKIP_OK) return st;
-  if (!cache_attn_fits(*p, *cache, n_sel)) return SKIP_ERR_UNSUPPORTED;
-  size_t need = cache_attn_scratch(*p, *cache, n_sel, prefixes != 0);
-  if (n_sel > 0) {
-    if (!cache_select_fits(*p, *cache)) return SKIP_ERR_UNSUPPORTED;
-    const size_t sel = cache_select_scratch(*p, *cache);
-    need = sel > need ? sel : need;
-  }
-  *bytes = need;
+  // (the limits of selection and attention are not each other's)
+  const bool attn = cache_attn_fits(*p, *cache, n_sel);
+  const bool select = n_sel > 0 && cache_select_fits(*p, *cache);
+  if (!attn && !select) return SKIP_ERR_UNSUPPORTED;
+  const size_t of_attn = attn ? cache_attn_scratch(*p, *cache, n_sel, prefixes != 0) : 0;
+  const size_t of_select = select ? cache_select_scratch(*p, *cache) : 0;
+  *bytes = of_attn > of_select ? of_attn : of_select;
   return SKIP_OK;
 }
 

@@ -167,6 +167,32 @@ def test_scales_past_float32(b):
             assert call(b, fn, p, c) == b.SKIP_ERR_INVALID_ARG, (fn, scale)
 
 
+def test_workspace_where_only_one_of_the_two_calls_is_possible(b):
+    """Rows and pages past the selection's limits: the attention's need.  More tiles of
+    listed pages than are counted: the selection's.  Neither: refused."""
+    def need(p, c, n_sel):
+        n = ctypes.c_size_t(77)
+        return b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), n_sel, 0,
+                                                ctypes.byref(n)), n.value
+    ok, uns = b.SKIP_OK, b.SKIP_ERR_UNSUPPORTED
+    # 512 items and more, taken whole: none
+    many = problem(b, B=1, kept_offsets=[0, 70000], L_max=6400)
+    assert need(many, cache(b, pages_max=100), 32) == (ok, 0)
+    # 16385 pages a sequence: parts of 512 runs of 16 rows and 66 floats, and 10 counts
+    long = problem(b, L_max=64 * 16384 + 1)
+    wide = cache(b, pages_max=16385)
+    assert need(long, wide, 32) == (ok, 2 * 512 * 16 * 66 * 4 + 256)
+    assert call(b, "pages", long, wide, n_sel=32, nb=7) == b.SKIP_ERR_WORKSPACE
+    assert call(b, "select", long, wide, n_sel=32) == uns
+    assert call(b, "select", many, cache(b, pages_max=100), n_sel=32) == uns
+    # 2^17 rows and key heads times 8200 tiles; 3000 pages, scores in LDS
+    deep = problem(b, B=1, H=16, kept_offsets=[0, 1 << 13], L_max=256 * 3000)
+    c = cache(b, heads_kv=16, page_tokens=256, pages_max=3000)
+    assert call(b, "pages", deep, c, n_sel=1024) == uns and need(deep, c, 1024) == (ok, 0)
+    far = problem(b, B=1, H=16, kept_offsets=[0, 1 << 13], L_max=256 * 16385)
+    assert need(far, cache(b, heads_kv=16, page_tokens=256, pages_max=16385), 1024)[0] == uns
+
+
 def test_more_than_a_launch_holds(b):
     uns = b.SKIP_ERR_UNSUPPORTED
 

@@ -593,6 +593,24 @@ def test_listed_pages_as_they_are_given(B):
     s.check(got, s.reference(listed), False)
 
 
+@pytest.mark.parametrize("seqs,n_sel", [([(40, 40)] * 1650, 17), ([(1, 32 * 16384 + 9), (2, 70)], 30)])
+def test_listed_pages_past_the_selections_limits(B, seqs, n_sel):
+    """More than 65535 rows, more than 16384 pages a sequence; the call's own workspace."""
+    s = Setup(B, seqs, H=1, hk=1, seed=19)
+    rows = s.p.total_kept
+    assert rows > 65535 or s.p.L_max > 32 * 16384
+    listed = np.full((rows, 1, n_sel), -1, dtype=np.int32)
+    top = max(-(-int(s.lens.max()) // 32), n_sel)
+    listed[:, 0, ::3] = s.rng.integers(0, top, (rows, len(range(0, n_sel, 3))))
+    listed[:, 0, 0] = 0
+    listed[0, 0, -1] = (seqs[0][1] - 1) // 32
+    got = B.cache_attn_pages(s.p, s.cache, s.q, s.row_offsets, s.dlens, dev(listed))
+    torch.cuda.synchronize()
+    s.check(got, s.reference(listed), False)
+    with pytest.raises(B.SkipError):
+        B.cache_select(s.p, s.cache, s.q, s.row_offsets, s.dlens, n_sel)
+
+
 # ---------------------------------------------------------------------------
 # Use
 
