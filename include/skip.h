@@ -643,7 +643,8 @@ skip_status_t skip_gather_dense(const skip_problem_t* p, const void* rows,
  * hold anything, infinities and NaN among it; of a value that it sees and that is not
  * finite, infinity or NaN comes out.  Errors as for all entry points; d_h
  * 64 or 128, at most 65535 key heads, and no more rows or sequences than a launch holds
- * (2^24 workgroups; 2^27 rows and heads), else SKIP_ERR_UNSUPPORTED.
+ * (2^24 workgroups; 2^27 rows and heads), else SKIP_ERR_UNSUPPORTED.  (d may be past the
+ * 8192 of the other calls.)
  */
 typedef struct skip_kv_cache {
   int32_t heads_kv;

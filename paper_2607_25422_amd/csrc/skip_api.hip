@@ -21,14 +21,14 @@ size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 enum Need { kPrune = 1, kGraph = 2 };
 
-skip_status_t check_common(const skip_problem_t* p) {
+skip_status_t check_common(const skip_problem_t* p, int max_d = kMaxD) {
   if (!p) return SKIP_ERR_INVALID_ARG;
   if (p->o_f32 != 0 && p->o_f32 != 1) return SKIP_ERR_INVALID_ARG;
   if (p->dtype != SKIP_F32 && p->dtype != SKIP_BF16) return SKIP_ERR_INVALID_ARG;
   if (p->B < 1 || p->d < 1 || p->k_max < 0 || p->total_kept < 0) return SKIP_ERR_INVALID_ARG;
   if ((int64_t)p->total_kept > (int64_t)p->B * p->k_max) return SKIP_ERR_INVALID_ARG;
   if (p->total_kept < p->k_max) return SKIP_ERR_INVALID_ARG;
-  if (p->d % 8 != 0 || p->d > kMaxD) return SKIP_ERR_UNSUPPORTED;
+  if (p->d % 8 != 0 || p->d > max_d) return SKIP_ERR_UNSUPPORTED;
   return SKIP_OK;
 }
 
@@ -735,7 +735,7 @@ skip_status_t skip_gather_dense(const skip_problem_t* p, const void* rows,
 // Problem and cache of the paged cache's calls.
 static skip_status_t check_cache(const skip_problem_t* p, const skip_kv_cache_t* c,
                                  const int32_t* row_offsets, const int32_t* lens) {
-  skip_status_t st = check_common(p);
+  skip_status_t st = check_common(p, INT32_MAX);       // (a head is the widest that a kernel holds)
   if (st != SKIP_OK) return st;
   if (!c || c->reserved != 0 || !row_offsets || !lens) return SKIP_ERR_INVALID_ARG;
   if (p->H < 1 || p->d_h < 1 || (int64_t)p->H * p->d_h != p->d) return SKIP_ERR_INVALID_ARG;

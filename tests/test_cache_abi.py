@@ -193,6 +193,23 @@ def test_workspace_where_only_one_of_the_two_calls_is_possible(b):
     assert need(far, cache(b, heads_kv=16, page_tokens=256, pages_max=16385), 1024)[0] == uns
 
 
+@pytest.mark.parametrize("H,hk,d_h", [(96, 8, 128), (129, 129, 64), (2048, 64, 128),
+                                      (65535, 65535, 128)])
+def test_wide_rows(b, H, hk, d_h):
+    """Rows wider than the routes take: no limit of the cache's calls but its own ones."""
+    p = problem(b, H=H, d=H * d_h, d_h=d_h, L_max=500)
+    c = cache(b, heads_kv=hk)
+    need = ctypes.c_size_t(0)
+    for n_sel in (0, 4):
+        assert b.LIB.skip_workspace_bytes_cache(ctypes.byref(p), ctypes.byref(c), n_sel, 0,
+                                                ctypes.byref(need)) == b.SKIP_OK
+    none = problem(b, H=H, d=H * d_h, d_h=d_h, kept_offsets=[0, 0, 0])
+    for fn in ALL:
+        assert call(b, fn, none, c) == b.SKIP_OK
+        assert call(b, fn, p, c, q=None, k=None, pages=None) == b.SKIP_ERR_INVALID_ARG
+    assert call(b, "append", p, c, qs=H * d_h - 8, ks=hk * d_h, vs=hk * d_h) == b.SKIP_ERR_INVALID_ARG
+
+
 def test_more_than_a_launch_holds(b):
     uns = b.SKIP_ERR_UNSUPPORTED
 

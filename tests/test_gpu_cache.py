@@ -611,6 +611,37 @@ def test_listed_pages_past_the_selections_limits(B, seqs, n_sel):
         B.cache_select(s.p, s.cache, s.q, s.row_offsets, s.dlens, n_sel)
 
 
+@pytest.mark.parametrize("H,hk,D,seqs", [
+    (96, 8, 128, [(1, 700), (2, 40), (0, 9)]), (130, 130, 64, [(1, 70), (3, 900)]),
+    (160, 8, 128, [(20, 800), (1, 33)]), (640, 20, 64, [(2, 100), (40, 60)])])
+def test_wide_rows(B, H, hk, D, seqs):
+    """Rows of more than 8192 features through all four calls."""
+    s = Setup(B, seqs, H=H, hk=hk, D=D, page=64, seed=21, stale=0.0)
+    assert H * D > 8192
+    q, k, v = s.new_rows(True)
+    rot = B.Rotation(torch.from_numpy(FREQ(D // 2)).cuda())
+    s.q = B.cache_append(s.p, s.cache, q, k, v, s.row_offsets, s.dlens, rotation=rot)
+    tok = np.concatenate([co.tokens(s.ro, s.lens, b) for b in range(len(seqs))])
+    for x, got in ((q, s.q), (k, None)):
+        want = co.rotate(f64(x), tok, FREQ(D // 2).astype(np.float64), "halves")
+        if got is None:
+            seq = np.concatenate([[b] * n for b, (n, _) in enumerate(seqs)]).astype(int)
+            pg = torch.from_numpy(s.table[seq, tok // s.page].astype(np.int64)).cuda()
+            slot = torch.from_numpy(tok % s.page).cuda()
+            got = s.cache.k[pg, :, slot]
+            assert torch.equal(s.cache.v[pg, :, slot], v)
+        part = np.abs(f64(x)) + np.abs(np.roll(f64(x), D // 2, axis=-1))
+        assert (np.abs(f64(got) - want) <= BF * np.abs(want) + (1 + BF) * 8 * U * part).all()
+    got = attn(s, B)
+    sel = B.cache_select(s.p, s.cache, s.q, s.row_offsets, s.dlens, 3)
+    by = B.cache_attn_pages(s.p, s.cache, s.q, s.row_offsets, s.dlens, sel)
+    torch.cuda.synchronize()
+    s.check(got, s.reference(), False)
+    want = co.select(f64(s.q), f64(s.cache.mean), s.table, s.page, s.ro, s.lens, 3, 1, 1)
+    assert (sel.cpu().numpy() == want).all()
+    s.check(by, s.reference(want), False)
+
+
 # ---------------------------------------------------------------------------
 # Use
 
