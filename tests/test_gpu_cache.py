@@ -593,6 +593,21 @@ def test_listed_pages_as_they_are_given(B):
     s.check(got, s.reference(listed), False)
 
 
+@pytest.mark.parametrize("G,hk,n,D,page,o_f32", [
+    (17, 2, 530, 64, 32, False), (32, 2, 520, 128, 64, False), (20, 16, 70, 64, 32, True),
+    (25, 3, 350, 128, 32, True)])
+def test_a_wave_an_item_of_two_row_blocks(B, G, hk, n, D, page, o_f32):
+    """1024 rows and key heads or more, 17 to 32 query heads on one, listed pages that end
+    inside the row's own, and none."""
+    s = Setup(B, [(n, n + 5)], H=G * hk, hk=hk, D=D, page=page, o_f32=o_f32, seed=20)
+    assert n * hk >= 1024 and 16 < G <= 32
+    listed = s.rng.integers(-1, -(-(n + 5) // page) + 1, (n, hk, 3)).astype(np.int32)
+    listed[n // 2, 0] = -1
+    got = B.cache_attn_pages(s.p, s.cache, s.q, s.row_offsets, s.dlens, dev(listed))
+    torch.cuda.synchronize()
+    s.check(got, s.reference(listed), o_f32)
+
+
 @pytest.mark.parametrize("seqs,n_sel", [([(40, 40)] * 1650, 17), ([(1, 32 * 16384 + 9), (2, 70)], 30)])
 def test_listed_pages_past_the_selections_limits(B, seqs, n_sel):
     """More than 65535 rows, more than 16384 pages a sequence; the call's own workspace."""
