@@ -727,6 +727,50 @@ def test_a_step_captured_and_replayed(B):
         assert all((o[M:] == 5).all() for o in flat(out))
 
 
+@pytest.mark.parametrize("tall", [False, True])
+def test_prefixes_and_runs_captured_and_replayed(B, tall):
+    """Shared prefixes, and many new tokens in runs: a captured call replayed while rows,
+    lengths and prefixes change under it, with eager work between; its own workspace."""
+    n = 40 if tall else 2
+    s = Setup(B, [(n, 2500), (n, 2300), (n, 2200), (n, 2400)], H=16, hk=8, D=128, page=64, seed=22,
+              shared=[(0, i, 2100) for i in (1, 2, 3)])
+    s.table = np.concatenate([s.table, np.full((4, 40), -1, np.int32)], 1)
+    s.cache.page_table = dev(s.table)
+    s.p.L_max = 4300                                  # (64 MB and more: prefixes are items)
+    assert 4 * 4 * 8 * s.p.L_max * 128 >= 64 << 20
+    ids, P = dev([0] * 4), dev([2100] * 4)
+    call = lambda out: attn(s, B, prefix_ids=ids, prefix_lens=P, out=out)
+    new = lambda: (torch.empty_like(s.q), torch.empty(s.p.total_kept, s.H, device="cuda"))
+    out, ref = new(), new()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(out)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for ro, lens, i, pl in (([0, n, 2 * n, 3 * n, 4 * n], [2500, 2300, 2200, 2400], 0, 2100),
+                            ([0, 0, n, n, 2 * n], [9, 2250, 0, 2150], 3, 2048),
+                            ([0, 1, 2, 3, 4], [2100, 2120, 2200, 700], 0, 2100),
+                            ([0] * 5, [0] * 4, 0, 2100),
+                            ([0, n, n + 1, n + 2, 2 * n], [2400, 2200, 33, 2300], -1, 2100)):
+        for x, y in ((s.row_offsets, ro), (s.dlens, lens), (ids, [i] * 4), (P, [pl] * 4)):
+            x.copy_(dev(y))
+        s.q.normal_()
+        for x in (*out, *ref):
+            x.fill_(5)
+        graph.replay()
+        torch.cuda.synchronize()
+        call(ref)
+        torch.cuda.synchronize()
+        for x, y in zip(out, ref):
+            assert torch.equal(x, y), (ro, lens)
+        s.ro, s.lens = np.array(ro, np.int32), np.array(lens, np.int32)
+        s.check(out, s.reference(), False)
+        assert (out[0][ro[-1]:] == 5).all()
+
+
 def test_two_streams_at_once(B):
     """Two sequences' steps on streams of their own, workspaces and outputs made by the
     calls."""
