@@ -333,14 +333,12 @@ __device__ __forceinline__ void cache_rows(const CacheAttnArgs& a, RowsShared<D,
             any_far[r] = __any(cache_far(to));
           }
           float ref = finite_reference(m_run[r]);
-          if (any_far[r]) {
+          if (__builtin_expect(any_far[r], 0)) {
             const bool far = cache_far(ref);
-            const float back = 1.f / sc;
+            const float back = far_back(sc);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float x = s[r][e >> 2][e & 3];
-              s[r][e >> 2][e & 3] = far ? far_logit(x, sc, ref, back) : x;
-            }
+            for (int e = 0; e < 8; ++e)
+              s[r][e >> 2][e & 3] = far_logit(s[r][e >> 2][e & 3], sc, ref, back, far);
             ref = far ? 0.f : ref;
           }
 #pragma unroll

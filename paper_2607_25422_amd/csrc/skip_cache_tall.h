@@ -303,16 +303,13 @@ __device__ __forceinline__ void cache_tall_work(const TallArgs& a, TallShared<D>
       any_far = __any(cache_far(to));
     }
     float ref = finite_reference(m_run);
-    if (any_far) {
+    if (__builtin_expect(any_far, 0)) {
       const bool far = cache_far(ref);
-      const float back = 1.f / sc;
+      const float back = far_back(sc);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = s[h][i];
-          s[h][i] = far ? far_logit(x, sc, ref, back) : x;
-        }
+        for (int i = 0; i < 16; ++i) s[h][i] = far_logit(s[h][i], sc, ref, back, far);
       ref = far ? 0.f : ref;
     }
     // weights of step (h, q) as bf16 pieces, and its values
