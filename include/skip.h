@@ -685,7 +685,9 @@ typedef struct skip_rotation {
  *              the row's (q, k and v may be columns of one projection's output)
  *   positions  [total_kept] int32 positions to rotate by, or NULL: each token's
  *              place in its sequence
- *   q_out      out [total_kept][H][d_h] bf16, contiguous; apart from q
+ *   q_out      out [total_kept][H][d_h] bf16, contiguous; apart from q (a row that
+ *              lies before its sequence's first token, where there are more rows than
+ *              tokens, is left as it was, and goes to no page)
  * Arrays are 16-byte aligned.
  */
 skip_status_t skip_cache_append(const skip_problem_t* p, const skip_kv_cache_t* cache,
@@ -714,10 +716,13 @@ skip_status_t skip_workspace_bytes_cache(const skip_problem_t* p, const skip_kv_
  *   q            [total_kept][H][d_h] (as skip_cache_append writes them)
  *   prefix_ids   [B] int32, or NULL (then prefix_lens is): consecutive sequences
  *                with the same id >= 0 and the same prefix_lens hold the same keys
- *                and values in their first prefix_lens tokens, which are read once for
+ *                and values in their first prefix_lens tokens.  These are read once for
  *                all of them (through the table row of one that has rows; a sequence
- *                of fewer tokens than that reads its own).  A hint on speed alone
- *                where that is so; results may differ in their last bits
+ *                of fewer tokens than that reads its own) where k_max * (H / heads_kv)
+ *                is at most 32, L_max is past 512 and 4 B heads_kv L_max d_h, the bytes
+ *                of keys and values that B sequences of L_max tokens hold, is 64 MB or
+ *                more; elsewhere each sequence reads its own.  A hint on speed alone;
+ *                results may differ in their last bits
  *   prefix_lens  [B] int32
  *   O, lse       out [total_kept][H][d_h], [total_kept][H] float or NULL; apart from q
  *   workspace    skip_workspace_bytes_cache bytes (0: it may be NULL; 0 wherever L_max
@@ -736,7 +741,8 @@ skip_status_t skip_cache_attn(const skip_problem_t* p, const skip_kv_cache_t* ca
  *   s_j = <sum of the queries of the key head's group, mean key of page j>
  * (double sums of the bf16 values; ties: the lower page), the n_first first and the
  * n_last last always among them (the last page, whose mean may take in tokens behind
- * t, so needs no score).  Fewer pages: all of them.  A page without a physical one scores 0.
+ * t, so needs no score).  Fewer pages: all of them.  A page without a physical one scores 0;
+ * a score that is NaN is placed by its bits, above or below all others.
  *   workspace  as for attention (0, and NULL, wherever L_max is at most 1024 pages)
  *   n_sel    1 .. 1024;  n_first >= 0, n_last >= 1, n_first + n_last <= n_sel
  *   pages    out [total_kept][heads_kv][n_sel] int32 ascending, -1 behind the last

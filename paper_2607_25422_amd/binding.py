@@ -1446,7 +1446,8 @@ def gather_dense(p: SkipProblem, rows, packed, d_out: int, kept_offsets=None, ro
 
 
 # ---------------------------------------------------------------------------
-# The paged cache
+# The paged cache.  ``p.L_max`` is the limit of every sequence's length, the caller's to
+# set (``make_problem`` does not): lengths past it are clamped to it.
 
 class _Described:
     """Keeps the description that the calls make of its arrays (``_struct``) with it: not

@@ -252,6 +252,32 @@ def test_append_without_a_page(B):
     assert torch.equal(cache.v[int(table[1, 0]), :, 1:3].transpose(0, 1), v[40:42])
 
 
+@pytest.mark.parametrize("page,n", [(32, 9), (64, 50), (256, 300)])
+def test_append_of_more_rows_than_tokens(B, page, n):
+    """Rows before their sequence's first token: their queries are left, nothing of them
+    is written; the others as if they were alone."""
+    s = Setup(B, [(n, n), (n, n), (2, 2)], page=page, D=64, seed=23)
+    lens = np.array([n - 5, 0, 2], np.int32)
+    q, k, v = s.new_rows(True)
+    rot = B.Rotation(torch.from_numpy(FREQ(32)).cuda())
+    out = torch.full((s.p.total_kept, s.H, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    one = [x.clone() for x in (s.cache.k, s.cache.v, s.cache.mean)]
+    B.cache_append(s.p, s.cache, q, k, v, s.row_offsets, dev(lens), rotation=rot, out=out)
+    torch.cuda.synchronize()
+    lost = [*range(5), *range(n, 2 * n)]
+    held = [*range(5, n), 2 * n, 2 * n + 1]
+    assert (out[lost] == 7).all()
+    p = B.make_problem("bf16", B=3, d=s.H * 64, H=s.H, d_h=64, kept_offsets=[0, n - 5, n - 5, n - 3])
+    p.L_max = n
+    cache = B.KvCache(*one, s.cache.page_table)
+    want = B.cache_append(p, cache, *(x[held].contiguous() for x in (q, k, v)),
+                          dev([0, n - 5, n - 5, n - 3]), dev(lens), rotation=rot)
+    torch.cuda.synchronize()
+    assert torch.equal(out[held], want)
+    for a, b in zip((s.cache.k, s.cache.v, s.cache.mean), one):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
 # ---------------------------------------------------------------------------
 # Attention
 
