@@ -34,7 +34,7 @@ TallPlan tall_plan(const skip_problem_t& p, const skip_kv_cache_t& c) {
   const long long G = p.H / c.heads_kv;
   x.row_tiles = (int)((p.k_max * G + kTRows - 1) / kTRows);
   // Few items are cut into equal runs (items as they come leave CUs without work: six
-  // pieces of 97 to 129 rows over 3200 tokens, 16 heads, 49 us in equal shares of each
+  // pieces of 98 to 129 rows over 3102 to 3362 tokens, 16 heads, 49 us in equal shares of each
   // item); about half a row tile of a sequence's is empty.
   const long long items = c.heads_kv * std::min<long long>(
       (long long)p.B * x.row_tiles, p.total_kept * G / kTRows + (p.B + 1) / 2);

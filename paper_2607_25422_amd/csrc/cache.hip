@@ -20,7 +20,9 @@ namespace skip {
 // values and the group's queries of those tokens, and the page's mean, for which it
 // reads the keys that were there (so that the mean is the keys', whatever was
 // appended, cut off or written again before).  Memory bounds it: a new token's rows
-// are read once and written once.
+// are read once and written once (16 prompts of 230 to 544 tokens, 32 heads of 128 over
+// 8: 43 us for 168 MB, 3.9 TB/s where a copy reaches 6.2; the angles, which stand before the
+// first loads, are made again by each key head's workgroup).
 constexpr int kAppThreads = 256;
 constexpr int kAppTokens = 32;             // tokens whose angles are in LDS at a time
 constexpr int kAppMaxHalf = 64;            // rotated pairs of a row

@@ -20,11 +20,11 @@
 // four tokens of 32 bytes).  The direct loads take chunks in that order.
 //
 // Matrix and vector instructions bound it together: four prompts of 1024 to 4096
-// tokens, 32 heads of 128 over 8, take 348 us, 680 TFLOP/s (1020 with the second piece of
+// tokens, 32 heads of 128 over 8, take 340 us, 694 TFLOP/s (1040 with the second piece of
 // the weights); the matrix units are busy for 49 % of the SIMDs' cycles, vector
 // instructions are issued in 45 % of them, two waves a SIMD.  Four prefixes of 8217
 // tokens for 16 sequences each, with their own 1 to 500 tokens behind them in one launch:
-// 51 us.  Six pieces of 97 to 131 rows over 3900 tokens, 16 heads of 64, float output:
+// 51 us.  Six pieces of 98 to 129 rows over 3102 to 3362 tokens, 16 heads of 64, float output:
 // 37 (40 with items sequence by sequence, see the end of the work).
 #pragma once
 
