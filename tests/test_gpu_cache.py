@@ -502,7 +502,8 @@ def test_large_values_and_logits(B):
 
 @pytest.mark.parametrize("n,ln,page,D,o_f32", [
     (1, 200, 32, 64, False), (3, 1300, 64, 128, False), (40, 300, 32, 64, True),
-    (130, 1500, 64, 128, False), (1, 4000, 32, 64, True)])
+    (130, 1500, 64, 128, False), (1, 4000, 32, 64, True), (10, 900, 32, 128, False),
+    (12, 300, 64, 64, True)])
 def test_logits_past_float32(B, n, ln, page, D, o_f32):
     """A finite product whose scaled value is not: below float32 it weighs nothing, above
     it the row is not finite (a row of zeros would be one that sees no token).  The rows
@@ -526,6 +527,27 @@ def test_logits_past_float32(B, n, ln, page, D, o_f32):
         assert (np.abs(f64(lse)[2 * n - 1] - want) <= tol + 4 * U * np.abs(want)).all()
         others = [r for r in range(2 * n) if r not in (n - 1, 2 * n - 1)]
         assert torch.isfinite(O[others].float()).all() and torch.isfinite(lse[others]).all()
+
+
+def test_logits_past_float32_in_a_shared_prefix(B):
+    """As above, for rows of one prefix item: the rows of the first sequence are not
+    finite, those of the second have one weight, those of the third are as ever."""
+    s = Setup(B, [(2, 5610), (1, 5620), (1, 5605)], shared=[(0, 1, 5600), (0, 2, 5600)], H=16,
+              hk=8, D=128, page=64, scale=8.0, seed=24)
+    assert 4 * 3 * 8 * 5620 * 128 >= 64 << 20
+    big = 2.0 ** 60
+    s.cache.k[int(s.table[0, 43]), :, 11] = big
+    s.q[:2], s.q[2] = big, -big
+    s.q[3] = s.q[3].abs() * -0.5                    # (its logit of that token: far below the others)
+    ref = s.reference()
+    O, lse = attn(s, B, prefix_ids=dev([0] * 3), prefix_lens=dev([5600] * 3))
+    torch.cuda.synchronize()
+    assert not torch.isfinite(O[:2].float()).any() and not torch.isfinite(lse[:2]).any()
+    assert (f64(O)[2] == ref[0][2]).all()
+    k = f64(s.cache.k)
+    delta = (128 + 4) * U * 8 * np.abs(f64(s.q[3])).sum(-1).max() * np.nanmax(np.where(k < big, np.abs(k), 0))
+    rel = 2 * delta + 2.0 ** -16 + (2 * 5620 + 16) * U
+    assert (np.abs(f64(O)[3] - ref[0][3]) <= rel * ref[2][3] + BF * np.abs(ref[0][3])).all()
 
 
 def test_missing_pages_are_passed_over(B):
